@@ -321,6 +321,126 @@ track_status track_op_rmsnorm_rope_qk(int32_t dtype, int64_t rows, int32_t heads
                                       int64_t ld, int64_t col0, const void* g_q, const void* g_k, const int32_t* grid,
                                       float* rope_ws, void* stream);
 
+/* Rotary positions of any axes, layout and length, for streaming and long
+ * sequences (the denoiser's own are track_op_rmsnorm_rope's, on a dense grid).
+ * Of each head's head_dim channels the first rot_dim are rotated in pairs, the
+ * rest copied.  Layout: pair i is channels (2i, 2i+1), or (i, rot_dim/2 + i).
+ * The rot_dim/2 pairs are shared out over the axes, section[a] = n_a to axis a
+ * (frames, rows, columns; one axis for plain sequences), and pair i of its
+ * section turns by theta = pos_a f_i, f_i = base^(-i / n_a), changed for
+ * sequences longer than the orig_len the model was made for by:
+ *   LINEAR  f_i / factor (positions squeezed);
+ *   NTK     base' = base factor^(n_a / (n_a - 1)) (n_a > 1): the fastest pair
+ *           kept, the slowest squeezed by factor;
+ *   YARN    (1 - r) f_i + r f_i / factor, r the ramp from 0 at
+ *           max(floor(c(beta_fast)), 0) to 1 at min(ceil(c(beta_slow)), n_a - 1)
+ *           over i, c(t) = n_a ln(orig_len / (2 pi t)) / ln(base) the pair that
+ *           makes t turns over orig_len; amplitude A = 1 + 0.1 ln(factor).
+ * rotated pair (a, b) -> A (a cos - b sin, a sin + b cos). */
+#define TRACK_ROPE_INTERLEAVED 0
+#define TRACK_ROPE_HALF        1
+#define TRACK_ROPE_PLAIN  0
+#define TRACK_ROPE_LINEAR 1
+#define TRACK_ROPE_NTK    2
+#define TRACK_ROPE_YARN   3
+typedef struct track_rope_config {
+  int32_t head_dim;    /* even, 2..256 */
+  int32_t rot_dim;     /* even, 2..head_dim */
+  int32_t layout;      /* TRACK_ROPE_INTERLEAVED or TRACK_ROPE_HALF */
+  int32_t axes;        /* 1..3 */
+  int32_t section[3];  /* pairs of each axis, >= 0, rot_dim/2 in all */
+  int32_t scaling;     /* TRACK_ROPE_PLAIN .. TRACK_ROPE_YARN */
+  double  base;        /* > 1 */
+  double  factor;      /* >= 1 (ignored by PLAIN, as what follows by all but YARN) */
+  double  orig_len;    /* > 0 */
+  double  beta_fast, beta_slow;  /* > 0, usually 32 and 1 */
+} track_rope_config;
+
+/* The frequencies f_i in radians a position (host [rot_dim/2], float64) and the
+ * amplitude A (host).  The caller copies the frequencies to the device once
+ * and gives them to the calls below.  Host only, synchronous. */
+track_status track_rope_freqs(const track_rope_config* cfg, double* freqs, float* amplitude);
+
+/* Rows of heads: row (b, i) of B sequences of L tokens begins at x[b*sx + i*ldx]
+ * and holds `heads` heads of head_dim channels beside each other (elements;
+ * ldx >= heads*head_dim, no negative stride).  The result goes to y, which is x
+ * with the same strides (in place) or rows that overlap none of the inputs. */
+typedef struct track_head_rows {
+  const void* x;
+  int64_t ldx, sx;
+  void* y;
+  int64_t ldy, sy;
+  int32_t heads;       /* >= 1 */
+} track_head_rows;
+
+/* The rotation of queries and keys in one launch.  k may be NULL.  pos: device
+ * int32 [axes][B*L], any values (a key moved from position p to r takes r - p);
+ * freqs: device float64 [rot_dim/2]; angles are formed in float64 and reduced
+ * there, so far positions lose nothing.  inverse != 0 rotates by -theta, A the
+ * same (the transpose: it is also the gradient).  Positions and frequencies are
+ * read when the call runs on the stream, so a captured call follows positions
+ * that change.  Each output is rounded once from float32.  B*L == 0 is a no-op.
+ * Asynchronous, no workspace. */
+track_status track_op_rope(int32_t dtype, const track_rope_config* cfg, int64_t B, int64_t L, const track_head_rows* q,
+                           const track_head_rows* k, const int32_t* pos, const double* freqs, float amplitude,
+                           int32_t inverse, void* stream);
+
+/* The same behind the RMSNorm of each head: x / sqrt(mean over the head of x^2
+ * + eps) * g with gains g_q, g_k [head_dim] (dtype, shared by all heads), then
+ * the rotation; q is multiplied by q_scale inside its one rounding (1, or
+ * log2(e) / sqrt(head_dim) for attention on log2 queries).  eps > 0. */
+track_status track_op_headnorm_rope(int32_t dtype, const track_rope_config* cfg, int64_t B, int64_t L,
+                                    const track_head_rows* q, const track_head_rows* k, const void* g_q,
+                                    const void* g_k, float eps, float q_scale, const int32_t* pos, const double* freqs,
+                                    float amplitude, void* stream);
+
+/* Attention with a sliding window and first tokens that stay visible, for
+ * streaming: softmax(scale q k^T) v over the keys that a query sees.  Tokens
+ * come in groups (frames; group = 1: tokens).  Sequence b has q_len[b] queries
+ * and k_len[b] keys; its query i sits at position p = q_start[b] + i among the
+ * keys' places and sees key j iff j < k_len[b],
+ *   right < 0 or floor(j/group) <= floor(p/group) + right, and
+ *   left < 0 or floor(j/group) >= floor(p/group) - left or j < sink.
+ * A query that sees nothing gets zeros (lse -inf), also where every logit it
+ * sees is -inf.  What K and V hold in places that a query does not see does not
+ * reach it, NaN and infinities included. */
+typedef struct track_window {
+  int64_t left, right;  /* groups before and after the query's own; -1: no limit */
+  int64_t sink;         /* first tokens that stay visible, >= 0 */
+  int64_t group;        /* tokens of a group, >= 1 */
+  double  scale;        /* of the logits; 0: 1 / sqrt(head_dim).  ln 2 takes log2 queries (as track_op_attention_log2q) */
+} track_window;
+
+/* Workspace of the call below in bytes, 0 where it needs none, -1 for what it
+ * refuses.  The size belongs to this build of the library and to the current
+ * device. */
+int64_t track_attention_window_workspace_bytes(int32_t dtype, const track_window* window, int32_t B, int32_t H,
+                                               int32_t Hk, int32_t head_dim, int64_t Lq, int64_t Lk);
+
+/* H query heads over Hk key heads (H % Hk == 0; head h reads key head
+ * h / (H/Hk)).  Row i of q for sequence b is q[b*sq + i*ldq + h*head_dim + c],
+ * likewise k with Hk heads, ldk, sk, and out; v is given transposed,
+ * vt[b*sv + (h*head_dim + c)*ldv + key] (a cache that track_op_linear_vt
+ * appends to), ldv >= Lk.  sk = sv = 0: keys that all sequences share.
+ * Lq, Lk: the most queries and keys of a sequence.  q_len, k_len (device int32
+ * [B], cut to [0, Lq] and [0, Lk]; NULL: all) and q_start (device int32 [B];
+ * NULL: k_len - q_len, the queries are the newest tokens) are read when the
+ * call runs on the stream, so a captured call follows lengths that change.
+ * Rows of out and lse behind q_len[b] are left as they were.  lse: float32
+ * [B][H][Lq], log of the sum of exp of the seen logits (natural), or NULL.
+ * bfloat16: head_dim 128, 16-byte aligned rows (bases, and strides in multiples
+ * of 8); probabilities are rounded to bfloat16 for the product with V, their
+ * sum is that of the rounded ones.  float32: head_dim 32, 64, 128.
+ * ldk, ldv <= 2^23; lengths, window limits <= 2^30.  workspace: 256-byte
+ * aligned; calls that may overlap on the GPU need one each.  B == 0 or Lq == 0
+ * is a no-op; Lk == 0 gives zeros.  Asynchronous. */
+track_status track_op_attention_window(int32_t dtype, const track_window* window, int32_t B, int32_t H, int32_t Hk,
+                                       int32_t head_dim, int64_t Lq, int64_t Lk, const void* q, int64_t ldq, int64_t sq,
+                                       const void* k, int64_t ldk, int64_t sk, const void* vt, int64_t ldv, int64_t sv,
+                                       void* out, int64_t ldo, int64_t so, float* lse, const int32_t* q_len,
+                                       const int32_t* k_len, const int32_t* q_start, void* workspace,
+                                       size_t workspace_bytes, void* stream);
+
 /* Step kernels on token-layout velocities vel [B, n] float32 (B = 2: cond
  * then uncond; B = 1: no guidance).  Guided p = u + w (c - u) (Eq. 1).
  * Sample mode: x[n] += dsigma * p.  Calibration mode also takes the small

@@ -822,6 +822,124 @@ track_status track_op_rmsnorm_rope_qk(int32_t dtype, int64_t rows, int32_t heads
   return op_rmsnorm_rope(dtype, rows, heads, head_dim, buf, ld, col0, g_q, g_k, grid, rope_ws, stream);
 }
 
+static track_status check_rope(const track_rope_config* c) {
+  if (!c) return fail(TRACK_E_INVALID, "rope: null config");
+  if (c->head_dim < 2 || c->head_dim > ROPE_MAX_DIM || c->head_dim % 2 || c->rot_dim < 2 || c->rot_dim > c->head_dim ||
+      c->rot_dim % 2)
+    return fail(TRACK_E_SHAPE, "rope: %d of %d channels (even, at most %d)", c->rot_dim, c->head_dim, ROPE_MAX_DIM);
+  if (c->layout != TRACK_ROPE_INTERLEAVED && c->layout != TRACK_ROPE_HALF)
+    return fail(TRACK_E_INVALID, "rope: bad layout %d", c->layout);
+  if (c->axes < 1 || c->axes > 3) return fail(TRACK_E_INVALID, "rope: %d axes", c->axes);
+  int64_t pairs = 0;
+  for (int i = 0; i < c->axes; ++i) {
+    if (c->section[i] < 0) return fail(TRACK_E_SHAPE, "rope: section %d of %d pairs", i, c->section[i]);
+    pairs += c->section[i];
+  }
+  if (pairs != c->rot_dim / 2)
+    return fail(TRACK_E_SHAPE, "rope: sections of %lld pairs for %d channels", (long long)pairs, c->rot_dim);
+  if (c->scaling < TRACK_ROPE_PLAIN || c->scaling > TRACK_ROPE_YARN)
+    return fail(TRACK_E_INVALID, "rope: bad scaling %d", c->scaling);
+  if (!(c->base > 1.0) || !std::isfinite(c->base)) return fail(TRACK_E_INVALID, "rope: base %g", c->base);
+  if (c->scaling != TRACK_ROPE_PLAIN && (!(c->factor >= 1.0) || !std::isfinite(c->factor)))
+    return fail(TRACK_E_INVALID, "rope: factor %g", c->factor);
+  if (c->scaling == TRACK_ROPE_YARN) {
+    const double v[3] = {c->orig_len, c->beta_fast, c->beta_slow};
+    for (double x : v)
+      if (!(x > 0.0) || !std::isfinite(x)) return fail(TRACK_E_INVALID, "rope: YaRN length and turns must be positive");
+  }
+  return TRACK_OK;
+}
+
+track_status track_rope_freqs(const track_rope_config* c, double* freqs, float* amplitude) {
+  TRY(check_rope(c));
+  if (!freqs || !amplitude) return fail(TRACK_E_INVALID, "rope_freqs: null output");
+  int at = 0;
+  for (int a = 0; a < c->axes; ++a) {
+    const int n = c->section[a];
+    const double base = c->scaling == TRACK_ROPE_NTK && n > 1 ? c->base * std::pow(c->factor, (double)n / (n - 1)) : c->base;
+    double lo = 0.0, hi = 0.0;
+    if (c->scaling == TRACK_ROPE_YARN) {
+      auto pair = [&](double turns) { return n * std::log(c->orig_len / (2.0 * M_PI * turns)) / std::log(c->base); };
+      lo = std::max(std::floor(pair(c->beta_fast)), 0.0);
+      hi = std::min(std::ceil(pair(c->beta_slow)), n - 1.0);
+    }
+    for (int i = 0; i < n; ++i) {
+      double f = std::pow(base, -(double)i / n);
+      if (c->scaling == TRACK_ROPE_LINEAR) f /= c->factor;
+      if (c->scaling == TRACK_ROPE_YARN) {
+        const double r = std::min(std::max((i - lo) / std::max(hi - lo, 0.001), 0.0), 1.0);
+        f = (1.0 - r) * f + r * f / c->factor;
+      }
+      freqs[at++] = f;
+    }
+  }
+  *amplitude = c->scaling == TRACK_ROPE_YARN ? (float)(1.0 + 0.1 * std::log(c->factor)) : 1.0f;
+  return TRACK_OK;
+}
+
+static track_status op_rope(const char* what, int32_t dtype, const track_rope_config* cfg, int64_t B, int64_t L,
+                            const track_head_rows* q, const track_head_rows* k, bool norm, const void* g_q,
+                            const void* g_k, float eps, float q_scale, const int32_t* pos, const double* freqs,
+                            float amplitude, bool inverse, hipStream_t s) {
+  TRY(check_rope(cfg));
+  if (dtype != TRACK_DTYPE_F32 && dtype != TRACK_DTYPE_BF16) return fail(TRACK_E_INVALID, "%s: bad dtype", what);
+  if (!q) return fail(TRACK_E_INVALID, "%s: null rows", what);
+  if (B < 0 || L < 0 || (L > 0 && B > INT32_MAX / L))
+    return fail(TRACK_E_SHAPE, "%s: %lld x %lld tokens", what, (long long)B, (long long)L);
+  if (norm && (!(eps > 0.0f) || !std::isfinite(eps))) return fail(TRACK_E_INVALID, "%s: eps %g", what, eps);
+  if (!std::isfinite(q_scale) || !std::isfinite(amplitude)) return fail(TRACK_E_INVALID, "%s: scale is not finite", what);
+  const uintptr_t mask = dtype == TRACK_DTYPE_BF16 ? 1 : 3;
+  for (const track_head_rows* r : {q, k}) {
+    if (!r) continue;
+    const int64_t width = (int64_t)r->heads * cfg->head_dim;
+    if (r->heads < 1 || r->ldx < width || r->ldy < width || r->sx < 0 || r->sy < 0)
+      return fail(TRACK_E_SHAPE, "%s: rows of %lld and %lld elements for %d heads of %d", what, (long long)r->ldx,
+                  (long long)r->ldy, r->heads, cfg->head_dim);
+    if (B > 1 && L > 0 && r->sy < width) return fail(TRACK_E_SHAPE, "%s: sequences overlap in the output", what);
+    if (B * L == 0) continue;
+    if (!r->x || !r->y) return fail(TRACK_E_INVALID, "%s: null pointer", what);
+    if (((uintptr_t)r->x | (uintptr_t)r->y) & mask) return fail(TRACK_E_INVALID, "%s: rows are not aligned to their elements", what);
+    if (r->x == r->y && ((L > 1 && r->ldx != r->ldy) || (B > 1 && r->sx != r->sy)))
+      return fail(TRACK_E_INVALID, "%s: in place needs the same strides", what);
+  }
+  if (B * L == 0) return TRACK_OK;
+  if (!pos || !freqs || (norm && (!g_q || (k && !g_k)))) return fail(TRACK_E_INVALID, "%s: null pointer", what);
+  if (((uintptr_t)pos & 3) || ((uintptr_t)freqs & 7) || (norm && (((uintptr_t)g_q | (k ? (uintptr_t)g_k : 0)) & mask)))
+    return fail(TRACK_E_INVALID, "%s: positions, frequencies or gains are not aligned to their elements", what);
+  return rope_heads(dtype, *cfg, B, L, *q, k, norm ? g_q : nullptr, norm && k ? g_k : nullptr, eps, q_scale, pos, freqs,
+                    amplitude, inverse, s);
+}
+
+track_status track_op_rope(int32_t dtype, const track_rope_config* cfg, int64_t B, int64_t L, const track_head_rows* q,
+                           const track_head_rows* k, const int32_t* pos, const double* freqs, float amplitude,
+                           int32_t inverse, void* stream) {
+  return op_rope("rope", dtype, cfg, B, L, q, k, false, nullptr, nullptr, 0.0f, 1.0f, pos, freqs, amplitude,
+                 inverse != 0, (hipStream_t)stream);
+}
+
+track_status track_op_headnorm_rope(int32_t dtype, const track_rope_config* cfg, int64_t B, int64_t L,
+                                    const track_head_rows* q, const track_head_rows* k, const void* g_q,
+                                    const void* g_k, float eps, float q_scale, const int32_t* pos, const double* freqs,
+                                    float amplitude, void* stream) {
+  return op_rope("headnorm_rope", dtype, cfg, B, L, q, k, true, g_q, g_k, eps, q_scale, pos, freqs, amplitude, false,
+                 (hipStream_t)stream);
+}
+
+int64_t track_attention_window_workspace_bytes(int32_t dtype, const track_window* window, int32_t B, int32_t H,
+                                               int32_t Hk, int32_t head_dim, int64_t Lq, int64_t Lk) {
+  return attention_window_bytes(dtype, window, B, H, Hk, head_dim, Lq, Lk);
+}
+
+track_status track_op_attention_window(int32_t dtype, const track_window* window, int32_t B, int32_t H, int32_t Hk,
+                                       int32_t head_dim, int64_t Lq, int64_t Lk, const void* q, int64_t ldq, int64_t sq,
+                                       const void* k, int64_t ldk, int64_t sk, const void* vt, int64_t ldv, int64_t sv,
+                                       void* out, int64_t ldo, int64_t so, float* lse, const int32_t* q_len,
+                                       const int32_t* k_len, const int32_t* q_start, void* workspace,
+                                       size_t workspace_bytes, void* stream) {
+  return attention_window(dtype, window, B, H, Hk, head_dim, Lq, Lk, q, ldq, sq, k, ldk, sk, vt, ldv, sv, out, ldo, so,
+                          lse, q_len, k_len, q_start, workspace, workspace_bytes, (hipStream_t)stream);
+}
+
 int64_t track_step_partial_count(int64_t n) { return step_partial_count(n); }
 
 track_status track_op_step(int64_t n, int32_t B, float guidance, float dsigma, const float* vel_L, const float* vel_S,

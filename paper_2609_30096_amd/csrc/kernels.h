@@ -49,6 +49,22 @@ track_status attention_f32_vrows(int B, int H, int head_dim, int64_t Lq, int64_t
 // The softmax scale in log2 units, log2(e) / sqrt(head_dim).
 float attn_log2_scale(int head_dim);
 
+// window.hip (track_op_attention_window)
+constexpr int64_t WIN_MAX = (int64_t)1 << 30;  // largest length and window limit
+// Workspace of attention_window, -1 for what it refuses.
+int64_t attention_window_bytes(int dtype, const track_window* w, int B, int H, int Hk, int D, int64_t Lq, int64_t Lk);
+track_status attention_window(int dtype, const track_window* w, int B, int H, int Hk, int D, int64_t Lq, int64_t Lk,
+                              const void* q, int64_t ldq, int64_t sq, const void* k, int64_t ldk, int64_t sk,
+                              const void* vt, int64_t ldv, int64_t sv, void* out, int64_t ldo, int64_t so, float* lse,
+                              const int32_t* q_len, const int32_t* k_len, const int32_t* q_start, void* ws,
+                              size_t ws_bytes, hipStream_t s);
+
+// rope.hip (track_op_rope; with gains track_op_headnorm_rope).  k may be null.
+constexpr int ROPE_MAX_DIM = 256;  // channels of a head
+track_status rope_heads(int dtype, const track_rope_config& c, int64_t B, int64_t L, const track_head_rows& q,
+                        const track_head_rows* k, const void* g_q, const void* g_k, float eps, float q_scale,
+                        const int32_t* pos, const double* freqs, float amplitude, bool inverse, hipStream_t s);
+
 // elementwise.hip
 struct Grid3 {
   int f, h, w;

@@ -1,0 +1,997 @@
+// Attention with a sliding window of groups (tokens or whole frames) and first tokens that
+// stay visible: o = softmax(scale q k^T over the keys a row sees) v.  The query at position
+// p, of group g = floor(p / G), sees the keys [lo, hi] and those below `sink` up to hi, with
+// lo = (g - left) G and hi = (g + right + 1) G - 1, both cut to the sequence's keys.
+//
+// The query heads that share a key head are rows of one problem: row r = i n + e is query i
+// of head e of n, so a K or V^T tile is read once for all of them.  Both limits grow with
+// the position, so a block of rows sees two ranges of 64-key tiles (the first tokens and the
+// window), and all but the tiles at the ranges' edges are seen whole by every row.  Those
+// take the tile body without a mask; the edge tiles come first, in a loop of their own.
+//
+// Masked places: a hidden key's logit is replaced, whatever K holds there, and its weight is
+// zero.  V^T is cleared in LDS behind a sequence's last key.  An infinity or NaN in a V row
+// that some rows of the block see and others do not would still reach the others through
+// 0 x inf in the matrix product; the edge tiles are the only place where that can happen, so
+// their sums are looked at once, and only where one is not finite the edge tiles are taken
+// again with the keys weighed one by one.
+#include <math.h>
+
+#include <algorithm>
+
+#include "attention_tile.h"
+#include "common.h"
+#include "kernels.h"
+
+namespace track {
+
+// One call's arguments as the kernels take them.
+struct WinArgs {
+  const void *q, *k, *vt;
+  void* out;
+  int64_t ldq, sq, ldk, sk, ldv, sv, ldo, so;
+  float* lse;
+  const int32_t *q_len, *k_len, *q_start;
+  int64_t left, right;  // groups; negative: no limit
+  uint32_t group;
+  int sink;
+  int B, Hk, n;  // sequences, key heads, query heads of each
+  int Lq, Lk;
+  int nrb, nsplit;  // row blocks, shares of the keys
+  float scale_log2;
+  float* po;   // [nsplit][B][Hk][Lq n][D]: a share's sums
+  float2* pml;  // [nsplit][B][Hk][Lq n]: its reference (log2 units) and its denominator
+};
+
+// One sequence of the batch, in wave-uniform registers.
+struct WinSeq {
+  int b, qlen, klen, sink;
+  int64_t start;  // position of its first query
+};
+
+__device__ __forceinline__ WinSeq win_seq(const WinArgs& a, int b) {
+  WinSeq s;
+  s.b = b;
+  // lengths from device memory are cut to the buffers
+  s.qlen = a.q_len ? __builtin_amdgcn_readfirstlane(max(0, min(a.q_len[b], a.Lq))) : a.Lq;
+  s.klen = a.k_len ? __builtin_amdgcn_readfirstlane(max(0, min(a.k_len[b], a.Lk))) : a.Lk;
+  s.start = a.q_start ? __builtin_amdgcn_readfirstlane(a.q_start[b]) : s.klen - s.qlen;
+  s.sink = min(a.sink, s.klen);
+  return s;
+}
+
+// The window [lo, hi] of query i, cut to [0, klen) (lo = klen or hi = -1: nothing left).
+__device__ __forceinline__ void win_range(const WinArgs& a, const WinSeq& s, int i, int& lo, int& hi) {
+  const int64_t p = s.start + i, G = a.group;
+  int64_t g = p;
+  if (a.group != 1)  // floor; |p| < 2^32
+    g = p >= 0 ? (int64_t)((uint32_t)p / a.group) : -(int64_t)(((uint64_t)-p + G - 1) / G);
+  hi = a.right < 0 ? s.klen - 1 : (int)max((int64_t)-1, min((g + a.right + 1) * G - 1, (int64_t)s.klen - 1));
+  lo = a.left < 0 ? 0 : (int)max((int64_t)0, min((g - a.left) * G, (int64_t)s.klen));
+}
+
+// The tiles of TK keys that rows with windows from [lo0, hi0] (the first row's) to [lo1, hi1]
+// (the last's) see between them, in the order they are taken: those seen in part by some
+// row, then those seen whole by all.
+struct WinTiles {
+  int sink;          // first tokens, 0 where the window covers them
+  int ns, w0;        // tiles of first tokens, first tile of the window
+  int n, fs, fa, fb;  // all tiles; seen whole: [0, fs) and [fa, fb)
+  int edge;          // tiles seen in part
+  template <int TK>
+  __device__ __forceinline__ void init(const WinSeq& s, int lo0, int hi0, int lo1, int hi1) {
+    sink = s.sink;
+    if (sink >= lo1) sink = lo0 = lo1 = 0;  // every row sees all from key 0 to its hi
+    ns = (min(sink, hi1 + 1) + TK - 1) / TK;
+    w0 = max(lo0 / TK, ns);
+    n = ns + max(0, hi1 / TK + (hi1 >= 0) - w0);
+    fs = min(sink, hi0 + 1) / TK;
+    const int t0 = max((lo1 + TK - 1) / TK, w0), t1 = min((hi0 + 1) / TK, w0 + n - ns);
+    fa = ns + t0 - w0;
+    fb = ns + t1 - w0;
+    if (t1 <= t0) fa = fb = n;
+    edge = n - fs - (fb - fa);
+  }
+  // first key of the tile at place idx of the order
+  template <int TK>
+  __device__ __forceinline__ int key(int idx) const {
+    int m;
+    if (idx < edge) {
+      m = fs + idx;
+      if (m >= fa) m += fb - fa;
+    } else {
+      m = idx - edge;
+      if (m >= fs) m += fa - fs;
+    }
+    return (m < ns ? m : m - ns + w0) * TK;
+  }
+};
+
+// A row of the output: the joined sums, or a share's.
+__device__ __forceinline__ float win_inverse(float l) { return l == 0.0f ? 0.0f : 1.0f / l; }  // nothing seen: zeros
+__device__ __forceinline__ float win_lse(float m, float l) {
+  return l == 0.0f ? -INFINITY : 0.69314718056f * (m + log2f(l));
+}
+
+// The keys of a tile that a lane's queries do not see.  A lane holds two runs of 8 keys of a
+// tile, 32 apart; a bit for each that is hidden, and a hidden logit's bits replaced by those of
+// -inf: two instructions an element and no branch (as comparisons with && and || the same
+// was compiled to branches around single accumulator elements, and with two query blocks to
+// moves that lost one of them).
+template <bool WEIGHED_>
+struct WinMask {
+  static constexpr bool ACTIVE = true, BITS = true, WEIGHED = WEIGHED_;
+  int lo[ATT_QB], hi[ATT_QB];
+  int sink, key0;
+  uint32_t bits[ATT_QB];
+  static __device__ __forceinline__ uint32_t below(int n) { return (1u << min(max(n, 0), 8)) - 1u; }
+  __device__ __forceinline__ void begin() {
+    key0 += 8 * (att_lane() >> 4);
+#pragma unroll
+    for (int b = 0; b < ATT_QB; ++b) {
+      bits[b] = 0;
+#pragma unroll
+      for (int run = 0; run < 2; ++run) {
+        const int k = key0 + 32 * run;
+        bits[b] |= ((below(lo[b] - k) & ~below(sink - k)) | (below(hi[b] + 1 - k) ^ 0xffu)) << (8 * run);
+      }
+    }
+  }
+  __device__ __forceinline__ float apply(int b, int c, float s) const {
+    const int at = (c & 7) + (c >> 5) * 8;
+    const uint32_t t = (uint32_t)((int32_t)(bits[b] << (31 - at)) >> 31);
+    return __uint_as_float((t & 0xff800000u) | (~t & __float_as_uint(s)));
+  }
+};
+
+// Row block, share, key head and sequence of a workgroup; the last rows of a sequence, which
+// see most keys under a causal mask, start first.
+__device__ __forceinline__ void win_place(const WinArgs& a, int& rb, int& sp, int& h, int& b) {
+  uint32_t id = blockIdx.x;
+  uint32_t t = id / (uint32_t)a.nrb;
+  rb = a.nrb - 1 - (int)(id - t * a.nrb);
+  id = t;
+  t = id / (uint32_t)a.nsplit;
+  sp = (int)(id - t * a.nsplit);
+  b = (int)(t / (uint32_t)a.Hk);
+  h = (int)(t - b * a.Hk);
+  rb = __builtin_amdgcn_readfirstlane(rb);
+  sp = __builtin_amdgcn_readfirstlane(sp);
+  h = __builtin_amdgcn_readfirstlane(h);
+  b = __builtin_amdgcn_readfirstlane(b);
+}
+
+// ---------------------------------------------------------------- many rows, bfloat16
+// 256 rows a workgroup, 32 a wave; K and V^T tiles by DMA into a ring of two slots, and the
+// tile body of the plain attention.
+template <bool QLOG2, bool SPLIT>
+__global__ __launch_bounds__(512) void window_blocks_kernel(WinArgs a) {
+  constexpr int BKV = ATT_BKV, D = ATT_D, SLOT = ATT_SLOT;
+  __shared__ __attribute__((aligned(1024))) uint8_t smem[2 * SLOT];
+  __shared__ int not_finite;
+  const int tid = threadIdx.x;
+  const int lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int jq = lane & 15, g = lane >> 4;
+  int rb, sp, h, b;
+  win_place(a, rb, sp, h, b);
+  const WinSeq seq = win_seq(a, b);
+  const int rows = seq.qlen * a.n;
+  const int r0 = rb * ATT_BQ;
+  if (r0 >= rows) return;  // the whole workgroup
+  if (tid == 0) not_finite = 0;
+
+  // windows of the block's first and last row, and of the wave's
+  auto range_of = [&](int r, int& lo, int& hi) {
+    win_range(a, seq, (int)((uint32_t)min(r, rows - 1) / (uint32_t)a.n), lo, hi);
+    lo = __builtin_amdgcn_readfirstlane(lo);
+    hi = __builtin_amdgcn_readfirstlane(hi);
+  };
+  int lo0, hi0, lo1, hi1;
+  range_of(r0, lo0, hi0);
+  range_of(r0 + ATT_BQ - 1, lo1, hi1);
+  WinTiles tiles;
+  tiles.init<BKV>(seq, lo0, hi0, lo1, hi1);
+  const int wr0 = r0 + 32 * wave;
+  int wlo, whi, unused;
+  range_of(wr0, wlo, unused);
+  range_of(wr0 + 31, unused, whi);
+  if (tiles.sink == 0 && seq.sink >= lo1) wlo = 0;
+  const bool live = wr0 < rows;
+
+  const bf16_t* const kbase = (const bf16_t*)a.k + b * a.sk + (int64_t)h * D;
+  const bf16_t* const vbase = (const bf16_t*)a.vt + b * a.sv + (int64_t)h * D * a.ldv;
+  bf16x8 qf[D / 32][ATT_QB];
+  WinMask<false> mask;
+  mask.sink = tiles.sink;
+#pragma unroll
+  for (int i = 0; i < ATT_QB; ++i) {
+    const uint32_t r = (uint32_t)min(wr0 + 16 * i + jq, rows - 1), qi = r / (uint32_t)a.n;
+    win_range(a, seq, (int)qi, mask.lo[i], mask.hi[i]);
+    if (tiles.sink == 0 && seq.sink >= lo1) mask.lo[i] = 0;
+    const bf16_t* qp = (const bf16_t*)a.q + b * a.sq + (int64_t)qi * a.ldq + (int64_t)(h * a.n + (r - qi * a.n)) * D + g * 8;
+#pragma unroll
+    for (int kc = 0; kc < D / 32; ++kc) qf[kc][i] = __builtin_bit_cast(bf16x8, *(const u32x4*)(qp + kc * 32));
+  }
+  uint32_t koffg[2], voffg[2];
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const int row = 8 * wave + 4 * i + (lane >> 4);
+    koffg[i] = (uint32_t)((att_perm(row) * a.ldk + ((lane & 15) ^ (row & 15)) * 8) * 2);
+    const int vr = 16 * wave + 8 * i + (lane >> 3);
+    voffg[i] = (uint32_t)((att_perm(vr) * a.ldv + ((lane & 7) ^ att_vswz(vr)) * 8) * 2);
+  }
+  // the tile at key0 into the slot at byte `slot`: K rows past the last key read as zero,
+  // V^T columns past the row's end as the next row's (cleared below) or zero
+  auto issue = [&](int key0, int slot) {
+    const __amdgpu_buffer_rsrc_t rsK = __builtin_amdgcn_make_buffer_rsrc(
+        (void*)(kbase + key0 * a.ldk), (short)0, (int)(uint32_t)(min(BKV, seq.klen - key0) * a.ldk * 2), 0x00020000);
+    const __amdgpu_buffer_rsrc_t rsV = __builtin_amdgcn_make_buffer_rsrc(
+        (void*)(vbase + key0), (short)0, (int)(uint32_t)((D * a.ldv - key0) * 2), 0x00020000);
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rsK, (att_lds_ptr_t)(smem + slot + wave * 2048 + i * 1024), 16, koffg[i], 0, 0, 0);
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rsV, (att_lds_ptr_t)(smem + slot + ATT_K_BYTES + wave * 2048 + i * 1024), 16,
+                                               voffg[i], 0, 0, 0);
+  };
+  auto barrier = [&]() {
+    att_wait_vmcnt<0>();
+    __builtin_amdgcn_s_waitcnt((15 << 0) | (3 << 14) | (7 << 4) | (0 << 8));  // lgkmcnt(0)
+    __builtin_amdgcn_s_barrier();
+  };
+  // V^T of keys at or past the last one cleared in the tile just copied (it may be anything
+  // there, and a weight of zero does not remove it): 16-byte units of 8 keys, two a thread
+  auto clear_past_end = [&](int key0, int slot) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int unit = tid + 512 * i, row = unit >> 3, c = (unit & 7) ^ att_vswz(row);
+      u32x4* p = (u32x4*)(smem + slot + ATT_K_BYTES + unit * 16);
+      const int left = seq.klen - key0 - 8 * c;  // keys of the unit to keep
+      if (left < 8) {
+        u32x4 v = *p;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) v[w] &= left > 2 * w + 1 ? 0xffffffffu : (left > 2 * w ? 0xffffu : 0u);
+        *p = v;
+      }
+    }
+    __syncthreads();
+  };
+
+  uint32_t ko = jq * 256 + ((g ^ jq) << 4), vo = jq * ATT_VROW + ((g ^ att_vswz(jq)) << 4);
+  int slot = 0;  // byte offset of the slot computed on
+  AttState st;
+  st.reset();
+
+  const int i0 = SPLIT ? (int)((int64_t)tiles.n * sp / a.nsplit) : 0;
+  const int i1 = SPLIT ? (int)((int64_t)tiles.n * (sp + 1) / a.nsplit) : tiles.n;
+  const int ie = max(i0, min(i1, tiles.edge));  // edge tiles of the share: [i0, ie)
+  auto next = [&]() {
+    ko ^= SLOT;
+    vo ^= SLOT;
+    slot ^= SLOT;
+    barrier();
+  };
+  if (i0 < i1) {
+    issue(tiles.key<BKV>(i0), 0);
+    barrier();
+    if (i0 < ie) {
+      for (int idx = i0; idx < ie; ++idx) {
+        const int key0 = tiles.key<BKV>(idx);
+        issue(tiles.key<BKV>(min(idx + 1, i1 - 1)), slot ^ SLOT);
+        if (key0 + BKV > seq.klen) clear_past_end(key0, slot);
+        if (live && key0 <= whi && (key0 + BKV > wlo || key0 < tiles.sink)) {
+          mask.key0 = key0;
+          att_tile_masked<WinMask<false>, QLOG2, 4, true, false>(smem, qf, ko, vo, st, mask, a.scale_log2);
+        }
+        next();
+      }
+      float z = 0.0f;
+#pragma unroll
+      for (int f = 0; f < D / 16; ++f)
+#pragma unroll
+        for (int i = 0; i < ATT_QB; ++i)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) z = fmaf(st.o[f][i][r], 0.0f, z);
+      if (__ballot(z != 0.0f) && lane == 0) not_finite = 1;
+      __syncthreads();
+      if (not_finite) {  // the whole workgroup
+        st.reset();
+        WinMask<true> weigh;
+#pragma unroll
+        for (int i = 0; i < ATT_QB; ++i) weigh.lo[i] = mask.lo[i], weigh.hi[i] = mask.hi[i];
+        weigh.sink = mask.sink;
+        for (int idx = i0; idx < ie; ++idx) {
+          const int key0 = tiles.key<BKV>(idx);
+          issue(key0, slot);
+          barrier();
+          if (key0 + BKV > seq.klen) clear_past_end(key0, slot);
+          weigh.key0 = key0;
+          att_tile_masked<WinMask<true>, QLOG2, 4, true, false>(smem, qf, ko, vo, st, weigh, a.scale_log2);
+          __syncthreads();
+        }
+        issue(tiles.key<BKV>(min(ie, i1 - 1)), slot);
+        barrier();
+      }
+    }
+    for (int idx = ie; idx < i1; ++idx) {
+      issue(tiles.key<BKV>(min(idx + 1, i1 - 1)), slot ^ SLOT);
+      att_tile_masked<AttAll, QLOG2, 4, true, false>(smem, qf, ko, vo, st, AttAll{}, a.scale_log2);
+      next();
+    }
+  }
+
+  // lane: query jq of each block, channels 32 p + 8 g .. + 7
+#pragma unroll
+  for (int i = 0; i < ATT_QB; ++i) {
+    const int r = wr0 + 16 * i + jq;
+    const float m = att_of_block(st.ms, i, lane), l = st.lsum[i][0];
+    if (r >= rows) continue;
+    if constexpr (SPLIT) {
+      const int64_t pr = ((((int64_t)sp * a.B + b) * a.Hk + h) * a.Lq) * a.n + r;
+      float* o = a.po + pr * D + 8 * g;
+#pragma unroll
+      for (int p = 0; p < D / 32; ++p) {
+        *(f32x4*)(o + 32 * p) = st.o[2 * p][i];
+        *(f32x4*)(o + 32 * p + 4) = st.o[2 * p + 1][i];
+      }
+      if (g == 0) a.pml[pr] = float2{m, l};
+    } else {
+      const int qi = (int)((uint32_t)r / (uint32_t)a.n), head = h * a.n + (r - qi * a.n);
+      const float inv = win_inverse(l);
+      bf16_t* o = (bf16_t*)a.out + b * a.so + (int64_t)qi * a.ldo + (int64_t)head * D + 8 * g;
+#pragma unroll
+      for (int p = 0; p < D / 32; ++p) {
+        const f32x4 &x = st.o[2 * p][i], &y = st.o[2 * p + 1][i];
+        const u32x4 pk = {pack_bf2(x[0] * inv, x[1] * inv), pack_bf2(x[2] * inv, x[3] * inv),
+                          pack_bf2(y[0] * inv, y[1] * inv), pack_bf2(y[2] * inv, y[3] * inv)};
+        *(u32x4*)(o + 32 * p) = pk;
+      }
+      if (a.lse && g == 0) a.lse[((int64_t)b * a.Hk * a.n + head) * a.Lq + qi] = win_lse(m, l);
+    }
+  }
+}
+
+// ---------------------------------------------------------------- few rows, bfloat16
+// One block of 16 QB rows a workgroup of four waves, which take every fourth 64-key tile of
+// the block's share straight from memory into the matrix cores' operands: K rows are the "A"
+// operand as they are stored, and so are V^T rows.  No key is used twice, so LDS would only
+// add a stop; the waves' sums meet there at the end.  What bounds it: reading K and V^T.
+template <int QB, bool SPLIT>
+__global__ __launch_bounds__(256) void window_rows_kernel(WinArgs a) {
+  constexpr int BKV = ATT_BKV, D = ATT_D, F = D / 16;
+  typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+  __shared__ f32x4 so[4][F][QB][64];
+  __shared__ float sm[4][16 * QB], sl[4][16 * QB];
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+  const int jq = lane & 15, g = lane >> 4;
+  int rb, sp, h, b;
+  win_place(a, rb, sp, h, b);
+  const WinSeq seq = win_seq(a, b);
+  const int rows = seq.qlen * a.n;
+  const int r0 = rb * 16 * QB;
+  if (r0 >= rows) return;  // the whole workgroup
+
+  int lo0, hi0, lo1, hi1;
+  win_range(a, seq, (int)((uint32_t)r0 / (uint32_t)a.n), lo0, hi0);
+  win_range(a, seq, (int)((uint32_t)min(r0 + 16 * QB - 1, rows - 1) / (uint32_t)a.n), lo1, hi1);
+  WinTiles tiles;
+  tiles.init<BKV>(seq, __builtin_amdgcn_readfirstlane(lo0), __builtin_amdgcn_readfirstlane(hi0),
+                  __builtin_amdgcn_readfirstlane(lo1), __builtin_amdgcn_readfirstlane(hi1));
+  const int i0 = SPLIT ? (int)((int64_t)tiles.n * sp / a.nsplit) : 0;
+  const int i1 = SPLIT ? (int)((int64_t)tiles.n * (sp + 1) / a.nsplit) : tiles.n;
+
+  bf16x8 qf[D / 32][QB];
+  WinMask<false> mask;
+  mask.sink = tiles.sink;
+#pragma unroll
+  for (int i = 0; i < QB; ++i) {
+    const uint32_t r = (uint32_t)min(r0 + 16 * i + jq, rows - 1), qi = r / (uint32_t)a.n;
+    win_range(a, seq, (int)qi, mask.lo[i], mask.hi[i]);
+    if (tiles.sink == 0 && seq.sink >= lo1) mask.lo[i] = 0;
+    const bf16_t* qp = (const bf16_t*)a.q + b * a.sq + (int64_t)qi * a.ldq + (int64_t)(h * a.n + (r - qi * a.n)) * D + g * 8;
+#pragma unroll
+    for (int kc = 0; kc < D / 32; ++kc) qf[kc][i] = __builtin_bit_cast(bf16x8, *(const u32x4*)(qp + kc * 32));
+  }
+  const uint8_t* const kbase = (const uint8_t*)((const bf16_t*)a.k + b * a.sk + (int64_t)h * D);
+  const uint8_t* const vbase = (const uint8_t*)((const bf16_t*)a.vt + b * a.sv + (int64_t)h * D * a.ldv);
+  const uint32_t krow = (uint32_t)a.ldk * 2;
+  uint32_t voff[F];  // the lane's V^T rows
+#pragma unroll
+  for (int f = 0; f < F; ++f) voff[f] = (uint32_t)(att_perm(16 * f + jq) * a.ldv * 2);
+
+  f32x4 o[F][QB];
+  float m[QB], l[QB];  // reference (log2 units), the lane's part of the denominator
+#pragma unroll
+  for (int i = 0; i < QB; ++i) {
+    m[i] = -INFINITY;
+    l[i] = 0.0f;
+#pragma unroll
+    for (int f = 0; f < F; ++f) o[f][i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+  }
+
+  for (int idx = i0 + wave; idx < i1; idx += 4) {
+    const int key0 = tiles.key<BKV>(idx);
+    const bool edge = idx < tiles.edge;
+    const int last = seq.klen - 1 - key0;  // the last key's place in the tile (or past it)
+    const uint8_t* const kt = kbase + (int64_t)key0 * krow;
+    const uint8_t* const vt = vbase + (int64_t)key0 * 2;
+    u32x4 kf[BKV / 16][D / 32], vf[F][BKV / 32];
+    // addresses past the last key go to the last key's row, or the unit of 8 keys that holds it
+#pragma unroll
+    for (int i = 0; i < BKV / 16; ++i) {
+      const uint32_t off = (uint32_t)min(att_perm(16 * i + jq), last) * krow + 16 * g;
+#pragma unroll
+      for (int kc = 0; kc < D / 32; ++kc) kf[i][kc] = *(const u32x4*)(kt + off + 64 * kc);
+    }
+#pragma unroll
+    for (int c = 0; c < BKV / 32; ++c) {
+      const uint32_t off = (uint32_t)min(32 * c + 8 * g, last & ~7) * 2;
+#pragma unroll
+      for (int f = 0; f < F; ++f) vf[f][c] = *(const u32x4*)(vt + voff[f] + off);
+    }
+    f32x4 s[BKV / 16][QB];
+#pragma unroll
+    for (int i = 0; i < BKV / 16; ++i)
+#pragma unroll
+      for (int q = 0; q < QB; ++q) {
+        s[i][q] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int kc = 0; kc < D / 32; ++kc)
+          s[i][q] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kf[i][kc]), qf[kc][q], s[i][q], 0, 0, 0);
+      }
+    if (edge) {
+      WinMask<false> mk = mask;
+      mk.key0 = key0;
+      mk.begin();
+#pragma unroll
+      for (int i = 0; i < BKV / 16; ++i)
+#pragma unroll
+        for (int q = 0; q < QB; ++q)
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+            s[i][q][r] = mk.apply(q, 32 * (i >> 1) + 4 * (i & 1) + r, s[i][q][r]);
+    }
+    bf16x8 pf[BKV / 32][QB];
+#pragma unroll
+    for (int q = 0; q < QB; ++q) {
+      float t = -INFINITY;
+#pragma unroll
+      for (int i = 0; i < BKV / 16; ++i)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) t = fmaxf(t, s[i][q][r]);
+      const float mn = fmaxf(m[q], group_max2(t, t) * a.scale_log2);
+      if (__ballot(mn > m[q])) {
+        const float alpha = mn == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m[q] - mn);
+        l[q] *= alpha;
+#pragma unroll
+        for (int f = 0; f < F; ++f)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) o[f][q][r] *= alpha;
+        m[q] = mn;
+      }
+      const float nm = m[q] == -INFINITY ? 0.0f : -m[q];
+#pragma unroll
+      for (int c = 0; c < BKV / 32; ++c) {
+        u32x4 w;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const f32x4 x = s[2 * c + (e >> 1)][q];
+          const float p0 = __builtin_amdgcn_exp2f(fmaf(x[2 * (e & 1)], a.scale_log2, nm));
+          const float p1 = __builtin_amdgcn_exp2f(fmaf(x[2 * (e & 1) + 1], a.scale_log2, nm));
+          w[e] = pack_bf2(p0, p1);
+          // the denominator adds the weights as rounded for the product with V
+          l[q] += __uint_as_float(w[e] << 16) + __uint_as_float(w[e] & 0xffff0000u);
+        }
+        pf[c][q] = __builtin_bit_cast(bf16x8, w);
+      }
+    }
+    if (edge) {
+      // V^T past the last key is cleared, and what else is not finite and may be hidden from
+      // some row is weighed key by key
+      u16x2 top = {0, 0};
+#pragma unroll
+      for (int c = 0; c < BKV / 32; ++c)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int left = last + 1 - (32 * c + 8 * g + 2 * e);
+          const uint32_t keep = left > 1 ? 0xffffffffu : (left > 0 ? 0xffffu : 0u);
+#pragma unroll
+          for (int f = 0; f < F; ++f) {
+            vf[f][c][e] &= keep;
+            top = __builtin_elementwise_max(top, __builtin_bit_cast(u16x2, vf[f][c][e] & 0x7f807f80u));
+          }
+        }
+      if (__ballot(top[0] == 0x7f80 || top[1] == 0x7f80)) {
+#pragma unroll 1
+        for (int key = 0; key < min(BKV, last + 1); ++key) {
+          float p[QB];
+#pragma unroll
+          for (int q = 0; q < QB; ++q) {
+            const u32x4 own = __builtin_bit_cast(u32x4, key < 32 ? pf[0][q] : pf[1][q]);
+            const int e = (key >> 1) & 3;
+            const uint32_t w = e == 0 ? own[0] : (e == 1 ? own[1] : (e == 2 ? own[2] : own[3]));
+            const uint32_t got = __builtin_amdgcn_ds_bpermute((jq + 16 * ((key >> 3) & 3)) << 2, (int)w);
+            p[q] = __uint_as_float(key & 1 ? got & 0xffff0000u : got << 16);
+          }
+#pragma unroll
+          for (int f = 0; f < F; ++f)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+              const float v = bf2f(*(const bf16_t*)(vt + (uint32_t)(att_perm(16 * f + 4 * g + r) * a.ldv * 2) + 2 * key));
+#pragma unroll
+              for (int q = 0; q < QB; ++q) o[f][q][r] = p[q] != 0.0f ? fmaf(p[q], v, o[f][q][r]) : o[f][q][r];
+            }
+        }
+        continue;
+      }
+    }
+#pragma unroll
+    for (int c = 0; c < BKV / 32; ++c)
+#pragma unroll
+      for (int f = 0; f < F; ++f)
+#pragma unroll
+        for (int q = 0; q < QB; ++q)
+          o[f][q] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, vf[f][c]), pf[c][q], o[f][q], 0, 0, 0);
+  }
+
+  // join the four waves: each takes two of the eight 16-channel blocks
+#pragma unroll
+  for (int q = 0; q < QB; ++q) {
+    l[q] += __shfl_xor(l[q], 16);
+    l[q] += __shfl_xor(l[q], 32);
+#pragma unroll
+    for (int f = 0; f < F; ++f) so[wave][f][q][lane] = o[f][q];
+    if (g == 0) {
+      sm[wave][16 * q + jq] = m[q];
+      sl[wave][16 * q + jq] = l[q];
+    }
+  }
+  __syncthreads();
+#pragma unroll
+  for (int q = 0; q < QB; ++q) {
+    const int r = r0 + 16 * q + jq;
+    float mx = -INFINITY, sum = 0.0f, wt[4];
+#pragma unroll
+    for (int w = 0; w < 4; ++w) mx = fmaxf(mx, sm[w][16 * q + jq]);
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      const float mi = sm[w][16 * q + jq];
+      wt[w] = mi == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(mi - mx);  // a wave without keys
+      sum = fmaf(wt[w], sl[w][16 * q + jq], sum);
+    }
+    if (r >= rows) continue;
+    const int qi = (int)((uint32_t)r / (uint32_t)a.n), head = h * a.n + (r - qi * a.n);
+    const int64_t pr = ((((int64_t)sp * a.B + b) * a.Hk + h) * a.Lq) * a.n + r;
+    const float inv = win_inverse(sum);
+#pragma unroll
+    for (int fi = 0; fi < 2; ++fi) {
+      const int f = 2 * wave + fi, ch = att_perm(16 * f + 4 * g);
+      f32x4 v = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        const f32x4 u = so[w][f][q][lane];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = fmaf(wt[w], u[e], v[e]);
+      }
+      if constexpr (SPLIT)
+        *(f32x4*)(a.po + pr * D + ch) = v;
+      else
+        *(u32x2*)((bf16_t*)a.out + b * a.so + (int64_t)qi * a.ldo + (int64_t)head * D + ch) =
+            u32x2{pack_bf2(v[0] * inv, v[1] * inv), pack_bf2(v[2] * inv, v[3] * inv)};
+    }
+    if (wave == 0 && g == 0) {
+      if constexpr (SPLIT) a.pml[pr] = float2{mx, sum};
+      else if (a.lse) a.lse[((int64_t)b * a.Hk * a.n + head) * a.Lq + qi] = win_lse(mx, sum);
+    }
+  }
+}
+
+// ---------------------------------------------------------------- float32
+// v_mfma_f32_16x16x4_f32 (float32 products and sums) on 16 rows a wave and 16 keys a step,
+// as the plain float32 attention: K and V^T go from memory to registers, the next step's
+// while this one's are multiplied.  With KS = 4 the workgroup's waves share one row block and
+// take a fourth of its keys each, with KS = 1 they take four row blocks.
+template <int D, int KS, bool VEC, bool SPLIT>
+__global__ __launch_bounds__(256) void window_f32_kernel(WinArgs a) {
+  static_assert(KS == 4 || !SPLIT, "shares of the keys");
+  constexpr int C = D / 16, BKV = 16;
+  __shared__ f32x4 so[KS == 4 ? 4 : 1][KS == 4 ? C : 1][64];
+  __shared__ float sm[4][16], sl[4][16];
+  auto load4 = [](const float* p) {
+    if constexpr (VEC) return *(const f32x4*)p;
+    else return f32x4{p[0], p[1], p[2], p[3]};
+  };
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+  const int jq = lane & 15, g = lane >> 4;
+  int rb, sp, h, b;
+  win_place(a, rb, sp, h, b);
+  const WinSeq seq = win_seq(a, b);
+  const int rows = seq.qlen * a.n;
+  const int r0 = KS == 4 ? rb * 16 : (rb * 4 + wave) * 16;
+  if (r0 >= rows) return;  // the whole workgroup (KS = 4), or a wave that no barrier waits for
+
+  int lo0, hi0, lo1, hi1;
+  win_range(a, seq, (int)((uint32_t)r0 / (uint32_t)a.n), lo0, hi0);
+  win_range(a, seq, (int)((uint32_t)min(r0 + 15, rows - 1) / (uint32_t)a.n), lo1, hi1);
+  WinTiles tiles;
+  tiles.init<BKV>(seq, __builtin_amdgcn_readfirstlane(lo0), __builtin_amdgcn_readfirstlane(hi0),
+                  __builtin_amdgcn_readfirstlane(lo1), __builtin_amdgcn_readfirstlane(hi1));
+  const int64_t shares = KS * (SPLIT ? a.nsplit : 1);
+  const int share = KS == 4 ? (SPLIT ? sp * 4 : 0) + wave : 0;
+  const int i0 = (int)(tiles.n * (int64_t)share / shares), i1 = (int)(tiles.n * (int64_t)(share + 1) / shares);
+
+  const int r = r0 + jq;
+  const uint32_t rr = (uint32_t)min(r, rows - 1), qi = rr / (uint32_t)a.n;
+  const int head = h * a.n + (int)(rr - qi * a.n);
+  int lo, hi;
+  win_range(a, seq, (int)qi, lo, hi);
+  if (tiles.sink == 0 && seq.sink >= lo1) lo = 0;
+  const float* qp = (const float*)a.q + b * a.sq + (int64_t)qi * a.ldq + (int64_t)head * D + 4 * g;
+  const float* kb = (const float*)a.k + b * a.sk + (int64_t)h * D + 4 * g;
+  const float* vb = (const float*)a.vt + b * a.sv + ((int64_t)h * D + jq) * a.ldv + 4 * g;
+  f32x4 qf[C], kf[C], vf[C], o[C];
+  // K row key0 + jq (the last key again past the end) and the V^T columns key0 + 4 g + 0..3,
+  // zero past the end
+  auto load_k = [&](int key0, f32x4 (&d)[C]) {
+    const float* p = kb + min(key0 + jq, seq.klen - 1) * a.ldk;
+#pragma unroll
+    for (int c = 0; c < C; ++c) d[c] = load4(p + 16 * c);
+  };
+  auto load_v = [&](int key0, f32x4 (&d)[C]) {
+    if (key0 + BKV <= seq.klen) {
+#pragma unroll
+      for (int c = 0; c < C; ++c) d[c] = load4(vb + 16 * c * a.ldv + key0);
+    } else {
+#pragma unroll
+      for (int c = 0; c < C; ++c)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) d[c][j] = key0 + 4 * g + j < seq.klen ? vb[16 * c * a.ldv + key0 + j] : 0.0f;
+    }
+  };
+#pragma unroll
+  for (int c = 0; c < C; ++c) {
+    qf[c] = load4(qp + 16 * c);
+    o[c] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+  }
+  float m = -INFINITY, l = 0.0f;  // reference (log2 units), the lane's part of the denominator
+  if (i0 < i1) {
+    load_k(tiles.key<BKV>(i0), kf);
+    load_v(tiles.key<BKV>(i0), vf);
+  }
+  for (int idx = i0; idx < i1; ++idx) {
+    const int key0 = tiles.key<BKV>(idx);
+    const bool edge = idx < tiles.edge;
+    f32x4 kn[C], vn[C];
+    const bool more = idx + 1 < i1;
+    if (more) {
+      const int k1 = tiles.key<BKV>(idx + 1);
+      load_k(k1, kn);
+      load_v(k1, vn);
+    }
+    f32x4 s0 = {0.0f, 0.0f, 0.0f, 0.0f}, s1 = s0;
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+#pragma unroll
+      for (int i = 0; i < 4; i += 2) {
+        s0 = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[c][i], qf[c][i], s0, 0, 0, 0);
+        s1 = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[c][i + 1], qf[c][i + 1], s1, 0, 0, 0);
+      }
+    }
+    float x[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) x[e] = s0[e] + s1[e];
+    if (edge) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int key = key0 + 4 * g + e;
+        x[e] = (key > hi) | ((key < lo) & (key >= tiles.sink)) ? -INFINITY : x[e];
+      }
+    }
+    const float t = fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3]));
+    const float mn = fmaxf(m, group_max2(t, t) * a.scale_log2);
+    if (__ballot(mn > m)) {
+      const float alpha = mn == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m - mn);
+      l *= alpha;
+#pragma unroll
+      for (int c = 0; c < C; ++c)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[c][e] *= alpha;
+      m = mn;
+    }
+    const float nm = m == -INFINITY ? 0.0f : -m;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) x[e] = __builtin_amdgcn_exp2f(fmaf(x[e], a.scale_log2, nm));
+    l += (x[0] + x[1]) + (x[2] + x[3]);
+    bool weigh = false;  // key by key where V is not finite and may be hidden from some row
+    if (edge) {
+      float z = 0.0f;
+#pragma unroll
+      for (int c = 0; c < C; ++c)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) z = fmaf(vf[c][e], 0.0f, z);
+      weigh = __ballot(z != 0.0f) != 0;
+    }
+    if (weigh) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        for (int gg = 0; gg < 4; ++gg) {
+          const float p = __shfl(x[e], jq + 16 * gg);
+#pragma unroll
+          for (int c = 0; c < C; ++c)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const float v = __shfl(vf[c][e], 4 * g + i + 16 * gg);
+              o[c][i] = p != 0.0f ? fmaf(p, v, o[c][i]) : o[c][i];
+            }
+        }
+    } else {
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+#pragma unroll
+        for (int c = 0; c < C; ++c) o[c] = __builtin_amdgcn_mfma_f32_16x16x4f32(vf[c][e], x[e], o[c], 0, 0, 0);
+    }
+    if (more) {
+#pragma unroll
+      for (int c = 0; c < C; ++c) {
+        kf[c] = kn[c];
+        vf[c] = vn[c];
+      }
+    }
+  }
+  l += __shfl_xor(l, 16);
+  l += __shfl_xor(l, 32);
+  float* op = (float*)a.out + b * a.so + (int64_t)qi * a.ldo + (int64_t)head * D + 4 * g;
+  auto store = [&](int c, const f32x4& v) {
+    if (r >= rows) return;
+    if constexpr (VEC) {
+      *(f32x4*)(op + 16 * c) = v;
+    } else {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) op[16 * c + e] = v[e];
+    }
+  };
+  float* const lse = a.lse && g == 0 && r < rows ? a.lse + ((int64_t)b * a.Hk * a.n + head) * a.Lq + qi : nullptr;
+  if constexpr (KS == 1) {
+    const float inv = win_inverse(l);
+#pragma unroll
+    for (int c = 0; c < C; ++c) store(c, f32x4{o[c][0] * inv, o[c][1] * inv, o[c][2] * inv, o[c][3] * inv});
+    if (lse) *lse = win_lse(m, l);
+  } else {
+#pragma unroll
+    for (int c = 0; c < C; ++c) so[wave][c][lane] = o[c];
+    if (g == 0) {
+      sm[wave][jq] = m;
+      sl[wave][jq] = l;
+    }
+    __syncthreads();
+    const float mx = fmaxf(fmaxf(sm[0][jq], sm[1][jq]), fmaxf(sm[2][jq], sm[3][jq]));
+    float wt[4], sum = 0.0f;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      wt[w] = sm[w][jq] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(sm[w][jq] - mx);  // a wave without keys
+      sum = fmaf(wt[w], sl[w][jq], sum);
+    }
+    const float inv = win_inverse(sum);
+    const int64_t pr = ((((int64_t)sp * a.B + b) * a.Hk + h) * a.Lq) * a.n + r;
+    for (int c = wave; c < C; c += 4) {
+      f32x4 v = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        const f32x4 u = so[w][c][lane];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = fmaf(wt[w], u[e], v[e]);
+      }
+      if constexpr (SPLIT) {
+        if (r < rows) *(f32x4*)(a.po + pr * D + 16 * c + 4 * g) = v;
+      } else {
+        store(c, f32x4{v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv});
+      }
+    }
+    if (wave == 0 && g == 0 && r < rows) {
+      if constexpr (SPLIT) a.pml[pr] = float2{mx, sum};
+      else if (lse) *lse = win_lse(mx, sum);
+    }
+  }
+}
+
+// The shares of each row joined: D / 4 threads a row, four channels a thread.
+template <typename T>
+__global__ __launch_bounds__(256) void window_join_kernel(WinArgs a, int D) {
+  const int per = D / 4, c = (int)threadIdx.x % per * 4;
+  const int64_t all = (int64_t)a.B * a.Hk * a.Lq * a.n;
+  const int64_t pr = (int64_t)blockIdx.x * (256 / per) + (int)threadIdx.x / per;
+  if (pr >= all) return;
+  const uint32_t per_head = (uint32_t)(a.Lq * a.n);  // < 2^31
+  const uint32_t bh = (uint32_t)(pr / per_head), r = (uint32_t)(pr - (int64_t)bh * per_head);
+  const int b = (int)(bh / (uint32_t)a.Hk), h = (int)(bh - b * a.Hk);
+  const int qi = (int)(r / (uint32_t)a.n), head = h * a.n + (int)(r - qi * a.n);
+  if (a.q_len && qi >= min(a.q_len[b], a.Lq)) return;
+  float mx = -INFINITY, sum = 0.0f;
+  for (int s = 0; s < a.nsplit; ++s) mx = fmaxf(mx, a.pml[s * all + pr].x);
+  f32x4 v = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 4
+  for (int s = 0; s < a.nsplit; ++s) {
+    const float2 ml = a.pml[s * all + pr];
+    const f32x4 u = *(const f32x4*)(a.po + (s * all + pr) * D + c);
+    const float wt = ml.x == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(ml.x - mx);  // a share without keys
+    sum = fmaf(wt, ml.y, sum);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = fmaf(wt, u[e], v[e]);
+  }
+  const float inv = win_inverse(sum);
+  T* o = (T*)a.out + b * a.so + (int64_t)qi * a.ldo + (int64_t)head * D + c;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) stf(o + e, v[e] * inv);
+  if (a.lse && c == 0) a.lse[((int64_t)b * a.Hk * a.n + head) * a.Lq + qi] = win_lse(mx, sum);
+}
+
+// ---------------------------------------------------------------- host
+struct WinPlan {
+  enum Form { BLOCKS, ROWS16, ROWS32, F32_SHARED, F32_APART } form;
+  int64_t nrb;
+  int nsplit;
+};
+
+// Keys that a block of `rows` rows sees at most.
+static int64_t win_span(const track_window& w, int64_t rows, int n, int64_t Lk) {
+  if (w.left < 0 || w.right < 0) return Lk;
+  const int64_t groups = w.left + w.right + 2 + (rows + n - 1) / n / w.group;
+  return std::min(Lk, groups * w.group + w.sink);
+}
+
+static WinPlan win_plan(int dtype, const track_window& w, int64_t B, int Hk, int n, int64_t Lq, int64_t Lk) {
+  const int64_t rows = Lq * n, cus = device_cus();
+  WinPlan p;
+  if (dtype == TRACK_DTYPE_F32) {
+    p.nrb = (rows + 15) / 16;
+    if (p.nrb * Hk * B >= 4 * cus) {
+      p.form = WinPlan::F32_APART;
+      p.nrb = (p.nrb + 3) / 4;
+      p.nsplit = 1;
+      return p;
+    }
+    p.form = WinPlan::F32_SHARED;
+    const int64_t steps = (win_span(w, 16, n, Lk) + 15) / 16;
+    p.nsplit = (int)std::max<int64_t>(1, std::min<int64_t>(2 * cus / (p.nrb * Hk * B), steps / 32));
+    return p;
+  }
+  if (rows <= 64) {
+    p.form = rows <= 16 ? WinPlan::ROWS16 : WinPlan::ROWS32;
+    const int per = rows <= 16 ? 16 : 32;
+    p.nrb = (rows + per - 1) / per;
+    const int64_t tiles = (win_span(w, per, n, Lk) + 63) / 64;
+    p.nsplit = (int)std::max<int64_t>(1, std::min<int64_t>(2 * cus / (p.nrb * Hk * B), tiles / 8));
+    return p;
+  }
+  p.form = WinPlan::BLOCKS;
+  p.nrb = (rows + ATT_BQ - 1) / ATT_BQ;
+  const int64_t tiles = (win_span(w, ATT_BQ, n, Lk) + 63) / 64, wgs = p.nrb * Hk * B;
+  p.nsplit = (int)std::max<int64_t>(1, std::min<int64_t>(cus / wgs, tiles / 8));
+  return p;
+}
+
+static size_t win_bytes(const WinPlan& p, int64_t B, int Hk, int n, int D, int64_t Lq) {
+  if (p.nsplit == 1) return 0;
+  return (size_t)(p.nsplit * B * Hk * Lq * n) * (size_t)(4 * D + 8);
+}
+
+static track_status win_check(int dtype, const track_window* w, int B, int H, int Hk, int D, int64_t Lq, int64_t Lk) {
+  if (!w) return fail(TRACK_E_INVALID, "attention_window: null window");
+  if (dtype != TRACK_DTYPE_F32 && dtype != TRACK_DTYPE_BF16)
+    return fail(TRACK_E_INVALID, "attention_window: bad dtype %d", dtype);
+  if (w->group < 1 || w->sink < 0 || w->left < -1 || w->right < -1 || !(w->scale >= 0.0) || !(w->scale < 1e30))
+    return fail(TRACK_E_INVALID, "attention_window: window of %lld / %lld groups of %lld, %lld first tokens, scale %g",
+                (long long)w->left, (long long)w->right, (long long)w->group, (long long)w->sink, w->scale);
+  if (w->left > WIN_MAX || w->right > WIN_MAX || w->group > WIN_MAX || w->sink > WIN_MAX)
+    return fail(TRACK_E_SHAPE, "attention_window: window limits are at most 2^30");
+  if (B < 0 || H < 1 || Hk < 1 || Lq < 0 || Lk < 0)
+    return fail(TRACK_E_SHAPE, "attention_window: bad sizes B=%d H=%d Hk=%d Lq=%lld Lk=%lld", B, H, Hk, (long long)Lq, (long long)Lk);
+  if (H % Hk) return fail(TRACK_E_SHAPE, "attention_window: %d query heads over %d key heads", H, Hk);
+  if (dtype == TRACK_DTYPE_BF16 ? D != ATT_D : (D != 32 && D != 64 && D != 128))
+    return fail(TRACK_E_UNSUPPORTED, "attention_window: head_dim %d (bfloat16: 128; float32: 32, 64, 128)", D);
+  if (Lk > WIN_MAX || Lq > WIN_MAX / (H / Hk)) return fail(TRACK_E_SHAPE, "attention_window: sequence too long");
+  return TRACK_OK;
+}
+
+int64_t attention_window_bytes(int dtype, const track_window* w, int B, int H, int Hk, int D, int64_t Lq, int64_t Lk) {
+  if (win_check(dtype, w, B, H, Hk, D, Lq, Lk) != TRACK_OK) return -1;
+  if (B == 0 || Lq == 0) return 0;
+  return (int64_t)win_bytes(win_plan(dtype, *w, B, Hk, H / Hk, Lq, Lk), B, Hk, H / Hk, D, Lq);
+}
+
+track_status attention_window(int dtype, const track_window* w, int B, int H, int Hk, int D, int64_t Lq, int64_t Lk,
+                              const void* q, int64_t ldq, int64_t sq, const void* k, int64_t ldk, int64_t sk,
+                              const void* vt, int64_t ldv, int64_t sv, void* out, int64_t ldo, int64_t so, float* lse,
+                              const int32_t* q_len, const int32_t* k_len, const int32_t* q_start, void* ws,
+                              size_t ws_bytes, hipStream_t s) {
+  const track_status st = win_check(dtype, w, B, H, Hk, D, Lq, Lk);
+  if (st != TRACK_OK) return st;
+  if (B == 0 || Lq == 0) return TRACK_OK;
+  if (!q || !out || (Lk > 0 && (!k || !vt))) return fail(TRACK_E_INVALID, "attention_window: null pointer");
+  const int n = H / Hk;
+  if (ldq < (int64_t)H * D || ldo < (int64_t)H * D || ldk < (int64_t)Hk * D || ldv < Lk)
+    return fail(TRACK_E_SHAPE, "attention_window: leading dimension too small");
+  if (sq < 0 || sk < 0 || sv < 0 || so < 0 || (B > 1 && so < (Lq - 1) * ldo + (int64_t)H * D))
+    return fail(TRACK_E_SHAPE, "attention_window: sequences overlap in out, or a negative stride");
+  if (((uintptr_t)lse | (uintptr_t)q_len | (uintptr_t)k_len | (uintptr_t)q_start) & 3)
+    return fail(TRACK_E_INVALID, "attention_window: lse and lengths need 4-byte alignment");
+  if (ldk > ((int64_t)1 << 23) || ldv > ((int64_t)1 << 23))
+    return fail(TRACK_E_SHAPE, "attention_window: ldk and ldv are at most 2^23");
+  const uintptr_t ptrs = (uintptr_t)q | (uintptr_t)k | (uintptr_t)vt | (uintptr_t)out;
+  const int64_t strides = ldq | ldk | ldv | ldo | (B > 1 ? sq | sk | sv | so : 0);
+  bool vec = true;
+  if (dtype == TRACK_DTYPE_BF16) {
+    if (ptrs & 15 || strides & 7) return fail(TRACK_E_INVALID, "attention_window: bf16 path needs 16-byte aligned rows");
+  } else {
+    if (ptrs & 3) return fail(TRACK_E_INVALID, "attention_window: float32 path needs 4-byte aligned rows");
+    vec = !(ptrs & 15) && !(strides & 3);
+  }
+  const WinPlan p = win_plan(dtype, *w, B, Hk, n, Lq, Lk);
+  const size_t need = win_bytes(p, B, Hk, n, D, Lq);
+  if (need && (!ws || ws_bytes < need)) return fail(TRACK_E_NOMEM, "attention_window: workspace of %zu bytes needed", need);
+  if (need && ((uintptr_t)ws & 255)) return fail(TRACK_E_INVALID, "attention_window: workspace must be 256-byte aligned");
+  const int64_t grid = p.nrb * p.nsplit * Hk * B, joined = (int64_t)B * H * Lq;
+  if (grid >= ((int64_t)1 << 23) || (need && joined >= ((int64_t)1 << 25)))
+    return fail(TRACK_E_SHAPE, "attention_window: too many row blocks");
+  WinArgs a = {};
+  a.q = q, a.k = k, a.vt = vt, a.out = out;
+  a.ldq = ldq, a.sq = sq, a.ldk = ldk, a.sk = sk, a.ldv = ldv, a.sv = sv, a.ldo = ldo, a.so = so;
+  a.lse = lse, a.q_len = q_len, a.k_len = k_len, a.q_start = q_start;
+  a.left = w->left, a.right = w->right, a.group = (uint32_t)w->group, a.sink = (int)w->sink;
+  a.B = B, a.Hk = Hk, a.n = n, a.Lq = (int)Lq, a.Lk = (int)Lk;
+  a.nrb = (int)p.nrb, a.nsplit = p.nsplit;
+  a.scale_log2 = w->scale > 0.0 ? (float)(w->scale * 1.4426950408889634) : attn_log2_scale(D);
+  a.po = (float*)ws;
+  a.pml = need ? (float2*)(a.po + (int64_t)p.nsplit * joined * D) : nullptr;
+  const bool split = p.nsplit > 1, log2q = a.scale_log2 == 1.0f;
+  ProfScope prof(TRACK_PROF_ATTN_SELF, s);
+  const unsigned gr = (unsigned)grid;
+#define TRACK_WIN_F32_K(DH, KS, SPLIT)                                             \
+  do {                                                                             \
+    if (vec) window_f32_kernel<DH, KS, true, SPLIT><<<gr, 256, 0, s>>>(a);         \
+    else window_f32_kernel<DH, KS, false, SPLIT><<<gr, 256, 0, s>>>(a);            \
+  } while (0)
+#define TRACK_WIN_F32(DH)                                                          \
+  do {                                                                             \
+    if (p.form == WinPlan::F32_APART) TRACK_WIN_F32_K(DH, 1, false);               \
+    else if (split) TRACK_WIN_F32_K(DH, 4, true);                                  \
+    else TRACK_WIN_F32_K(DH, 4, false);                                            \
+  } while (0)
+  switch (p.form) {
+    case WinPlan::BLOCKS:
+      if (log2q && split) window_blocks_kernel<true, true><<<gr, 512, 0, s>>>(a);
+      else if (log2q) window_blocks_kernel<true, false><<<gr, 512, 0, s>>>(a);
+      else if (split) window_blocks_kernel<false, true><<<gr, 512, 0, s>>>(a);
+      else window_blocks_kernel<false, false><<<gr, 512, 0, s>>>(a);
+      break;
+    case WinPlan::ROWS16:
+      if (split) window_rows_kernel<1, true><<<gr, 256, 0, s>>>(a);
+      else window_rows_kernel<1, false><<<gr, 256, 0, s>>>(a);
+      break;
+    case WinPlan::ROWS32:
+      if (split) window_rows_kernel<2, true><<<gr, 256, 0, s>>>(a);
+      else window_rows_kernel<2, false><<<gr, 256, 0, s>>>(a);
+      break;
+    default:
+      if (D == 32) TRACK_WIN_F32(32);
+      else if (D == 64) TRACK_WIN_F32(64);
+      else TRACK_WIN_F32(128);
+  }
+#undef TRACK_WIN_F32
+#undef TRACK_WIN_F32_K
+  TRACK_LAUNCH_CHECK();
+  if (split) {
+    const int per = D / 4, rows_wg = 256 / per;
+    const unsigned jg = (unsigned)((joined + rows_wg - 1) / rows_wg);
+    if (dtype == TRACK_DTYPE_BF16) window_join_kernel<bf16_t><<<jg, 256, 0, s>>>(a, D);
+    else window_join_kernel<float><<<jg, 256, 0, s>>>(a, D);
+    TRACK_LAUNCH_CHECK();
+  }
+  return TRACK_OK;
+}
+
+}  // namespace track

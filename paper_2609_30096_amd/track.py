@@ -8,6 +8,7 @@ or ``python -m paper_2609_30096_amd.build``); without it every call raises.
 from __future__ import annotations
 
 import ctypes
+import dataclasses
 import os
 from typing import Dict, List, Optional, Sequence, Tuple
 
@@ -31,6 +32,8 @@ EXPORTS = [
     "track_op_linear", "track_op_linear_vt", "track_op_attention", "track_op_attention_log2q",
     "track_op_layernorm", "track_rope_table_len", "track_op_rmsnorm_rope", "track_op_rmsnorm_rope_qk", "track_step_partial_count",
     "track_op_step", "track_op_step_noalloc", "track_hbm_stream", "track_mfma_stream", "track_unipc_coefficients", "track_op_unipc_step", "track_profile_enable", "track_profile_reset", "track_profile_read", "track_set_progress",
+    "track_rope_freqs", "track_op_rope", "track_op_headnorm_rope", "track_attention_window_workspace_bytes",
+    "track_op_attention_window",
 ]
 
 
@@ -56,7 +59,24 @@ class SamplerConfigC(ctypes.Structure):
                 ("order", ctypes.c_int32)]
 
 
+class RopeConfigC(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_int32) for n in ("head_dim", "rot_dim", "layout", "axes")] +
+                [("section", ctypes.c_int32 * 3), ("scaling", ctypes.c_int32)] +
+                [(n, ctypes.c_double) for n in ("base", "factor", "orig_len", "beta_fast", "beta_slow")])
+
+
+class HeadRowsC(ctypes.Structure):
+    _fields_ = [("x", ctypes.c_void_p), ("ldx", ctypes.c_int64), ("sx", ctypes.c_int64),
+                ("y", ctypes.c_void_p), ("ldy", ctypes.c_int64), ("sy", ctypes.c_int64), ("heads", ctypes.c_int32)]
+
+
+class WindowC(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int64) for n in ("left", "right", "sink", "group")] + [("scale", ctypes.c_double)]
+
+
 SOLVERS = {"euler": 0, "unipc": 1}
+ROPE_LAYOUTS = {"interleaved": 0, "half": 1}
+ROPE_SCALINGS = {"none": 0, "linear": 1, "ntk": 2, "yarn": 3}
 
 
 _vp, _i32, _i64, _f32, _f64, _sz = (ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_float,
@@ -99,6 +119,14 @@ def _declare(L):
         "track_rope_table_len": (_i64, [_i32, P(_i32)]),
         "track_op_rmsnorm_rope": (_i32, [_i32, _i64, _i32, _i32, _vp, _i64, _i64, _vp, P(_i32), _vp, _vp]),
         "track_op_rmsnorm_rope_qk": (_i32, [_i32, _i64, _i32, _i32, _vp, _i64, _i64, _vp, _vp, P(_i32), _vp, _vp]),
+        "track_rope_freqs": (_i32, [P(RopeConfigC), P(_f64), P(_f32)]),
+        "track_op_rope": (_i32, [_i32, P(RopeConfigC), _i64, _i64, P(HeadRowsC), P(HeadRowsC), _vp, _vp, _f32, _i32,
+                                 _vp]),
+        "track_op_headnorm_rope": (_i32, [_i32, P(RopeConfigC), _i64, _i64, P(HeadRowsC), P(HeadRowsC), _vp, _vp, _f32,
+                                          _f32, _vp, _vp, _f32, _vp]),
+        "track_attention_window_workspace_bytes": (_i64, [_i32, P(WindowC), _i32, _i32, _i32, _i32, _i64, _i64]),
+        "track_op_attention_window": (_i32, [_i32, P(WindowC), _i32, _i32, _i32, _i32, _i64, _i64] +
+                                      [_vp, _i64, _i64] * 4 + [_vp] * 5 + [_sz, _vp]),
         "track_step_partial_count": (_i64, [_i64]),
         "track_op_step": (_i32, [_i64, _i32, _f32, _f32, _vp, _vp, _vp, _vp, _f64, _vp, _vp]),
         "track_op_step_noalloc": (_i32, [_i64, _i32, _f32, _f32, _vp, _vp, _vp, _f64, _vp, _vp]),
@@ -436,6 +464,206 @@ def op_rmsnorm_rope_qk(dtype: int, buf, heads: int, head_dim: int, g_q, g_k, col
         ws = torch.empty(2 * n, dtype=torch.float32, device=buf.device)
     _check(lib().track_op_rmsnorm_rope_qk(dtype, rows, heads, head_dim, _ptr(buf), ld, col0, _ptr(g_q), _ptr(g_k), gp,
                                           _ptr(ws), _stream()))
+
+
+@dataclasses.dataclass(frozen=True)
+class RopeConfig:
+    """Rotary positions (track_rope_config): sections are the rotated pairs of each axis."""
+    head_dim: int
+    rot_dim: Optional[int] = None            # head_dim
+    layout: str = "interleaved"              # or "half"
+    sections: Optional[Tuple[int, ...]] = None  # one axis
+    base: float = 10000.0
+    scaling: str = "none"                    # "linear", "ntk", "yarn"
+    factor: float = 1.0
+    orig_len: float = 4096.0
+    beta_fast: float = 32.0
+    beta_slow: float = 1.0
+
+    def c(self) -> RopeConfigC:
+        rot = self.head_dim if self.rot_dim is None else self.rot_dim
+        sec = (rot // 2,) if self.sections is None else tuple(self.sections)
+        if len(sec) > 3:
+            raise ValueError("rotary positions have at most 3 axes")
+        return RopeConfigC(self.head_dim, rot, ROPE_LAYOUTS[self.layout], len(sec),
+                           (ctypes.c_int32 * 3)(*sec), ROPE_SCALINGS[self.scaling], self.base, self.factor,
+                           self.orig_len, self.beta_fast, self.beta_slow)
+
+
+def rope_freqs(cfg: RopeConfig) -> Tuple[np.ndarray, float]:
+    """Radians a position of every rotated pair (float64), and the amplitude."""
+    c = cfg.c()
+    out = np.zeros(max(c.rot_dim // 2, 1), dtype=np.float64)
+    amp = ctypes.c_float(0.0)
+    _check(lib().track_rope_freqs(ctypes.byref(c), out.ctypes.data_as(ctypes.POINTER(_f64)), ctypes.byref(amp)))
+    return out, float(amp.value)
+
+
+class Rope:
+    """A configuration with its frequencies on the device (made once, used by every call)."""
+
+    def __init__(self, cfg: RopeConfig, device="cuda"):
+        freqs, self.amplitude = rope_freqs(cfg)
+        self.cfg = cfg
+        self.c = cfg.c()
+        self.axes = self.c.axes
+        self.freqs = _torch().from_numpy(freqs).to(device)
+
+
+def _float_dtype(t) -> int:
+    torch = _torch()
+    if t.dtype == torch.bfloat16:
+        return DTYPE_BF16
+    if t.dtype == torch.float32:
+        return DTYPE_F32
+    raise TypeError(f"float32 or bfloat16 tensor expected, got {t.dtype}")
+
+
+def _like(t, other, what):
+    if t.dtype != other.dtype or t.device != other.device:
+        raise TypeError(f"{what}: {t.dtype} on {t.device} beside {other.dtype} on {other.device}")
+
+
+def _ints(t, shape, ref, what):
+    """An int32 tensor of the given shape, contiguous, on ref's device (None passes)."""
+    if t is None:
+        return
+    torch = _torch()
+    if t.dtype != torch.int32 or tuple(t.shape) != tuple(shape) or not t.is_contiguous() or t.device != ref.device:
+        raise ValueError(f"{what}: contiguous int32 {tuple(shape)} on {ref.device} expected")
+
+
+def _seq_heads(t, what):
+    """[sequences, tokens, heads, channels] with heads side by side: (row stride, sequence stride)."""
+    if t.dim() != 4:
+        raise ValueError(f"{what}: [sequences, tokens, heads, channels] expected, got {tuple(t.shape)}")
+    B, L, H, D = t.shape
+    if t.numel() and ((D > 1 and t.stride(3) != 1) or (H > 1 and t.stride(2) != D)):
+        raise ValueError(f"{what}: heads of a token must lie side by side")
+    ld = t.stride(1) if L > 1 else H * D
+    return ld, t.stride(0) if B > 1 else ld * L
+
+
+def _head_rows(x, y, what) -> HeadRowsC:
+    if tuple(x.shape) != tuple(y.shape):
+        raise ValueError(f"{what}: output of shape {tuple(y.shape)} for {tuple(x.shape)}")
+    _like(y, x, what)
+    ldx, sx = _seq_heads(x, what)
+    ldy, sy = _seq_heads(y, what)
+    return HeadRowsC(x.data_ptr(), ldx, sx, y.data_ptr(), ldy, sy, x.shape[2])
+
+
+def _rope_call(rope, q, k, pos, q_out, k_out):
+    B, L = q.shape[:2]
+    q_out = q if q_out is None else q_out
+    rq, rk = _head_rows(q, q_out, "q"), None
+    if q.shape[3] != rope.c.head_dim:
+        raise ValueError(f"q: heads of {q.shape[3]} channels, {rope.c.head_dim} configured")
+    if k is not None:
+        if tuple(k.shape[:2]) != (B, L) or k.shape[3] != q.shape[3]:
+            raise ValueError(f"k of shape {tuple(k.shape)} beside q of {tuple(q.shape)}")
+        _like(k, q, "k")
+        k_out = k if k_out is None else k_out
+        rk = _head_rows(k, k_out, "k")
+    elif k_out is not None:
+        raise ValueError("k_out without k")
+    _ints(pos, (rope.axes, B, L), q, "pos")
+    if rope.freqs.device != q.device:
+        raise ValueError(f"rope on {rope.freqs.device}, q on {q.device}")
+    return B, L, rq, rk, q_out, k_out
+
+
+def op_rope(rope: Rope, q, k, pos, q_out=None, k_out=None, inverse: bool = False):
+    """Rotates q [B, L, H, D] and k [B, L, Hk, D] (or None) by positions pos (int32 [axes, B, L]), in place or
+    into q_out and k_out; returns the outputs.  Strides of tokens and sequences are free."""
+    B, L, rq, rk, q_out, k_out = _rope_call(rope, q, k, pos, q_out, k_out)
+    with _torch().cuda.device(q.device):
+        _check(lib().track_op_rope(_float_dtype(q), ctypes.byref(rope.c), B, L, ctypes.byref(rq),
+                                   None if rk is None else ctypes.byref(rk), _ptr(pos), _ptr(rope.freqs),
+                                   rope.amplitude, 1 if inverse else 0, _stream()))
+    return q_out, k_out
+
+
+def op_headnorm_rope(rope: Rope, q, k, g_q, g_k, pos, q_out=None, k_out=None, eps: float = 1e-6,
+                     q_scale: float = 1.0):
+    """op_rope behind the RMSNorm of every head, with gains g_q and g_k [D]; q times q_scale."""
+    B, L, rq, rk, q_out, k_out = _rope_call(rope, q, k, pos, q_out, k_out)
+    for g, what in ((g_q, "g_q"),) + (((g_k, "g_k"),) if k is not None else ()):
+        if tuple(g.shape) != (q.shape[3],) or not g.is_contiguous():
+            raise ValueError(f"{what}: [{q.shape[3]}] expected")
+        _like(g, q, what)
+    with _torch().cuda.device(q.device):
+        _check(lib().track_op_headnorm_rope(_float_dtype(q), ctypes.byref(rope.c), B, L, ctypes.byref(rq),
+                                            None if rk is None else ctypes.byref(rk), _ptr(g_q),
+                                            _ptr(g_k if k is not None else None), float(eps), float(q_scale),
+                                            _ptr(pos), _ptr(rope.freqs), rope.amplitude, _stream()))
+    return q_out, k_out
+
+
+@dataclasses.dataclass(frozen=True)
+class Window:
+    """What a query sees (track_window): groups before and after its own (-1: all), and the first tokens."""
+    left: int = -1
+    right: int = 0
+    sink: int = 0
+    group: int = 1
+    scale: Optional[float] = None  # 1 / sqrt(head_dim)
+
+    def c(self) -> WindowC:
+        return WindowC(self.left, self.right, self.sink, self.group, 0.0 if self.scale is None else self.scale)
+
+
+def attention_window_workspace_bytes(window: Window, dtype: int, B: int, H: int, Hk: int, head_dim: int, Lq: int,
+                                     Lk: int) -> int:
+    n = lib().track_attention_window_workspace_bytes(dtype, ctypes.byref(window.c()), B, H, Hk, head_dim, Lq, Lk)
+    if n < 0:
+        raise TrackError(E_INVALID, lib().track_last_error().decode())
+    return n
+
+
+def attention_window_workspace(window: Window, q, k):
+    """The workspace of op_attention_window on tensors of these shapes (None where it needs none)."""
+    with _torch().cuda.device(q.device):
+        n = attention_window_workspace_bytes(window, _float_dtype(q), q.shape[0], q.shape[2], k.shape[2], q.shape[3],
+                                             q.shape[1], k.shape[1])
+    return _torch().empty(n, dtype=_torch().uint8, device=q.device) if n else None
+
+
+def op_attention_window(window: Window, q, k, vt, out, lse=None, q_len=None, k_len=None, q_start=None,
+                        workspace=None):
+    """Window attention of q [B, Lq, H, D] on k [B, Lk, Hk, D] and vt [B, Hk, D, >= Lk] into out (like q); returns
+    out.  k may be a view into a longer cache; a sequence stride of 0 in k and vt shares them.  lse: float32
+    [B, H, Lq]; q_len, k_len, q_start: int32 [B]."""
+    B, Lq, H, D = q.shape
+    if tuple(out.shape) != tuple(q.shape) or k.dim() != 4 or k.shape[0] != B or k.shape[3] != D:
+        raise ValueError(f"q {tuple(q.shape)}, k {tuple(k.shape)}, out {tuple(out.shape)} do not match")
+    Lk, Hk = k.shape[1], k.shape[2]
+    for t, what in ((k, "k"), (vt, "vt"), (out, "out")):
+        _like(t, q, what)
+    if vt.dim() != 4 or tuple(vt.shape[:3]) != (B, Hk, D) or vt.shape[3] < Lk:
+        raise ValueError(f"vt: [{B}, {Hk}, {D}, >= {Lk}] expected, got {tuple(vt.shape)}")
+    ldv = vt.stride(2)
+    if vt.numel() and (vt.stride(3) != 1 or (Hk > 1 and vt.stride(1) != D * ldv)):
+        raise ValueError("vt: rows of keys, D of them a head, heads one after another")
+    ldq, sq = _seq_heads(q, "q")
+    ldk, sk = _seq_heads(k, "k")
+    ldo, so = _seq_heads(out, "out")
+    sv = vt.stride(0) if B > 1 else Hk * D * ldv
+    _ints(q_len, (B,), q, "q_len")
+    _ints(k_len, (B,), q, "k_len")
+    _ints(q_start, (B,), q, "q_start")
+    if lse is not None and (lse.dtype != _torch().float32 or tuple(lse.shape) != (B, H, Lq) or
+                            not lse.is_contiguous() or lse.device != q.device):
+        raise ValueError(f"lse: contiguous float32 [{B}, {H}, {Lq}] on {q.device} expected")
+    if workspace is not None and workspace.device != q.device:
+        raise ValueError(f"workspace on {workspace.device}, q on {q.device}")
+    nbytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    with _torch().cuda.device(q.device):
+        _check(lib().track_op_attention_window(
+            _float_dtype(q), ctypes.byref(window.c()), B, H, Hk, D, Lq, Lk, _ptr(q), ldq, sq, _ptr(k), ldk, sk,
+            _ptr(vt), ldv, sv, _ptr(out), ldo, so, _ptr(lse), _ptr(q_len), _ptr(k_len), _ptr(q_start),
+            _ptr(workspace), nbytes, _stream()))
+    return out
 
 
 def step_partial_count(n: int) -> int:
