@@ -64,8 +64,8 @@ __device__ __forceinline__ WinSeq win_seq(const WinArgs& a, int b) {
 __device__ __forceinline__ void win_range(const WinArgs& a, const WinSeq& s, int i, int& lo, int& hi) {
   const int64_t p = s.start + i, G = a.group;
   int64_t g = p;
-  if (a.group != 1)  // floor; |p| < 2^32
-    g = p >= 0 ? (int64_t)((uint32_t)p / a.group) : -(int64_t)(((uint64_t)-p + G - 1) / G);
+  if (a.group != 1)  // floor; -2^31 <= p < 2^32
+    g = p >= 0 ? (int64_t)((uint32_t)p / a.group) : ~(int64_t)((uint32_t)~p / a.group);
   hi = a.right < 0 ? s.klen - 1 : (int)max((int64_t)-1, min((g + a.right + 1) * G - 1, (int64_t)s.klen - 1));
   lo = a.left < 0 ? 0 : (int)max((int64_t)0, min((g - a.left) * G, (int64_t)s.klen));
 }
@@ -107,7 +107,13 @@ struct WinTiles {
   }
 };
 
-// A row of the output: the joined sums, or a share's.
+// Share s of S of n tiles: [i0, i1).
+__device__ __forceinline__ void win_share(int n, int s, int S, int& i0, int& i1) {
+  const int q = (int)((uint32_t)n / (uint32_t)S), more = n - q * S;
+  i0 = __builtin_amdgcn_readfirstlane(q * s + min(s, more));
+  i1 = __builtin_amdgcn_readfirstlane(i0 + q + (s < more));
+}
+
 __device__ __forceinline__ float win_inverse(float l) { return l == 0.0f ? 0.0f : 1.0f / l; }  // nothing seen: zeros
 __device__ __forceinline__ float win_lse(float m, float l) {
   return l == 0.0f ? -INFINITY : 0.69314718056f * (m + log2f(l));
@@ -118,17 +124,17 @@ __device__ __forceinline__ float win_lse(float m, float l) {
 // -inf: two instructions an element and no branch (as comparisons with && and || the same
 // was compiled to branches around single accumulator elements, and with two query blocks to
 // moves that lost one of them).
-template <bool WEIGHED_>
+template <int NB, bool WEIGHED_ = false>
 struct WinMask {
   static constexpr bool ACTIVE = true, BITS = true, WEIGHED = WEIGHED_;
-  int lo[ATT_QB], hi[ATT_QB];
+  int lo[NB], hi[NB];
   int sink, key0;
-  uint32_t bits[ATT_QB];
+  uint32_t bits[NB];
   static __device__ __forceinline__ uint32_t below(int n) { return (1u << min(max(n, 0), 8)) - 1u; }
   __device__ __forceinline__ void begin() {
     key0 += 8 * (att_lane() >> 4);
 #pragma unroll
-    for (int b = 0; b < ATT_QB; ++b) {
+    for (int b = 0; b < NB; ++b) {
       bits[b] = 0;
 #pragma unroll
       for (int run = 0; run < 2; ++run) {
@@ -144,10 +150,13 @@ struct WinMask {
   }
 };
 
-// Row block, share, key head and sequence of a workgroup; the last rows of a sequence, which
-// see most keys under a causal mask, start first.
+// Row block, share, key head and sequence of a workgroup.  Neighbouring row blocks go to one
+// XCD, whose L2 then serves their common keys: over the XCDs in turn, 12 heads 16384 x 16384
+// under a causal mask took 955 us instead of 824, 2 x 12 heads over a 21-frame video 5.2 ms
+// instead of 4.8.  The last rows of a sequence, which see most keys under a causal mask, start
+// first.
 __device__ __forceinline__ void win_place(const WinArgs& a, int& rb, int& sp, int& h, int& b) {
-  uint32_t id = blockIdx.x;
+  uint32_t id = (uint32_t)xcd_remap((int)blockIdx.x, (int)gridDim.x);
   uint32_t t = id / (uint32_t)a.nrb;
   rb = a.nrb - 1 - (int)(id - t * a.nrb);
   id = t;
@@ -167,8 +176,10 @@ __device__ __forceinline__ void win_place(const WinArgs& a, int& rb, int& sp, in
 template <bool QLOG2, bool SPLIT>
 __global__ __launch_bounds__(512) void window_blocks_kernel(WinArgs a) {
   constexpr int BKV = ATT_BKV, D = ATT_D, SLOT = ATT_SLOT;
-  __shared__ __attribute__((aligned(1024))) uint8_t smem[2 * SLOT];
-  __shared__ int not_finite;
+  // one object: with a second one the compiler waits for every copy under way before a tile's
+  // first fragment read (20% slower)
+  __shared__ __attribute__((aligned(1024))) uint8_t smem[2 * SLOT + 16];
+  int* const not_finite = (int*)(smem + 2 * SLOT);
   const int tid = threadIdx.x;
   const int lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -179,7 +190,7 @@ __global__ __launch_bounds__(512) void window_blocks_kernel(WinArgs a) {
   const int rows = seq.qlen * a.n;
   const int r0 = rb * ATT_BQ;
   if (r0 >= rows) return;  // the whole workgroup
-  if (tid == 0) not_finite = 0;
+  if (tid == 0) *not_finite = 0;
 
   // windows of the block's first and last row, and of the wave's
   auto range_of = [&](int r, int& lo, int& hi) {
@@ -202,7 +213,7 @@ __global__ __launch_bounds__(512) void window_blocks_kernel(WinArgs a) {
   const bf16_t* const kbase = (const bf16_t*)a.k + b * a.sk + (int64_t)h * D;
   const bf16_t* const vbase = (const bf16_t*)a.vt + b * a.sv + (int64_t)h * D * a.ldv;
   bf16x8 qf[D / 32][ATT_QB];
-  WinMask<false> mask;
+  WinMask<ATT_QB> mask;
   mask.sink = tiles.sink;
 #pragma unroll
   for (int i = 0; i < ATT_QB; ++i) {
@@ -264,8 +275,8 @@ __global__ __launch_bounds__(512) void window_blocks_kernel(WinArgs a) {
   AttState st;
   st.reset();
 
-  const int i0 = SPLIT ? (int)((int64_t)tiles.n * sp / a.nsplit) : 0;
-  const int i1 = SPLIT ? (int)((int64_t)tiles.n * (sp + 1) / a.nsplit) : tiles.n;
+  int i0 = 0, i1 = tiles.n;
+  if (SPLIT) win_share(tiles.n, sp, a.nsplit, i0, i1);
   const int ie = max(i0, min(i1, tiles.edge));  // edge tiles of the share: [i0, ie)
   auto next = [&]() {
     ko ^= SLOT;
@@ -283,7 +294,7 @@ __global__ __launch_bounds__(512) void window_blocks_kernel(WinArgs a) {
         if (key0 + BKV > seq.klen) clear_past_end(key0, slot);
         if (live && key0 <= whi && (key0 + BKV > wlo || key0 < tiles.sink)) {
           mask.key0 = key0;
-          att_tile_masked<WinMask<false>, QLOG2, 4, true, false>(smem, qf, ko, vo, st, mask, a.scale_log2);
+          att_tile_masked<WinMask<ATT_QB>, QLOG2, 4, true, false>(smem, qf, ko, vo, st, mask, a.scale_log2);
         }
         next();
       }
@@ -294,11 +305,11 @@ __global__ __launch_bounds__(512) void window_blocks_kernel(WinArgs a) {
         for (int i = 0; i < ATT_QB; ++i)
 #pragma unroll
           for (int r = 0; r < 4; ++r) z = fmaf(st.o[f][i][r], 0.0f, z);
-      if (__ballot(z != 0.0f) && lane == 0) not_finite = 1;
+      if (__ballot(z != 0.0f) && lane == 0) *not_finite = 1;
       __syncthreads();
-      if (not_finite) {  // the whole workgroup
+      if (*not_finite) {  // the whole workgroup
         st.reset();
-        WinMask<true> weigh;
+        WinMask<ATT_QB, true> weigh;
 #pragma unroll
         for (int i = 0; i < ATT_QB; ++i) weigh.lo[i] = mask.lo[i], weigh.hi[i] = mask.hi[i];
         weigh.sink = mask.sink;
@@ -308,7 +319,7 @@ __global__ __launch_bounds__(512) void window_blocks_kernel(WinArgs a) {
           barrier();
           if (key0 + BKV > seq.klen) clear_past_end(key0, slot);
           weigh.key0 = key0;
-          att_tile_masked<WinMask<true>, QLOG2, 4, true, false>(smem, qf, ko, vo, st, weigh, a.scale_log2);
+          att_tile_masked<WinMask<ATT_QB, true>, QLOG2, 4, true, false>(smem, qf, ko, vo, st, weigh, a.scale_log2);
           __syncthreads();
         }
         issue(tiles.key<BKV>(min(ie, i1 - 1)), slot);
@@ -317,7 +328,7 @@ __global__ __launch_bounds__(512) void window_blocks_kernel(WinArgs a) {
     }
     for (int idx = ie; idx < i1; ++idx) {
       issue(tiles.key<BKV>(min(idx + 1, i1 - 1)), slot ^ SLOT);
-      att_tile_masked<AttAll, QLOG2, 4, true, false>(smem, qf, ko, vo, st, AttAll{}, a.scale_log2);
+      if (live) att_tile_masked<AttAll, QLOG2, 4, true, false>(smem, qf, ko, vo, st, AttAll{}, a.scale_log2);
       next();
     }
   }
@@ -354,140 +365,129 @@ __global__ __launch_bounds__(512) void window_blocks_kernel(WinArgs a) {
 }
 
 // ---------------------------------------------------------------- few rows, bfloat16
-// One block of 16 QB rows a workgroup of four waves, which take every fourth 64-key tile of
-// the block's share straight from memory into the matrix cores' operands: K rows are the "A"
-// operand as they are stored, and so are V^T rows.  No key is used twice, so LDS would only
-// add a stop; the waves' sums meet there at the end.  What bounds it: reading K and V^T.
-template <int QB, bool SPLIT>
-__global__ __launch_bounds__(256) void window_rows_kernel(WinArgs a) {
+// At most 16 rows a key head (a token of 16 query heads, four tokens of 4).  The four waves of
+// a workgroup take every fourth 64-key tile of its share straight from memory into the matrix
+// cores' operands: K rows are the "A" operand as they are stored, and so are V^T rows.  No key
+// is used twice, so LDS would only add a stop; the waves' sums meet there at the end.  What
+// bounds it: reading K and V^T (5.4 - 5.8 TB/s over long caches), for short ones the latency of
+// a tile and of the join.  Loads through buffer resources with the row blocks in the scalar
+// offset take one address register for K and one for V^T, so that a SIMD holds two waves (252
+// registers; 64-bit addresses spilled 71): one token over 8 heads of 4096 keys 16.2 -> 11.2 us
+// at 16 shares, 16384 27.6 -> 17.9 at 32.
+template <bool SPLIT>
+__global__ __launch_bounds__(256, 2) void window_rows_kernel(WinArgs a) {
   constexpr int BKV = ATT_BKV, D = ATT_D, F = D / 16;
   typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
-  __shared__ f32x4 so[4][F][QB][64];
-  __shared__ float sm[4][16 * QB], sl[4][16 * QB];
+  __shared__ f32x4 so[4][F][64];
+  __shared__ float sm[4][16], sl[4][16];
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   const int jq = lane & 15, g = lane >> 4;
   int rb, sp, h, b;
   win_place(a, rb, sp, h, b);
   const WinSeq seq = win_seq(a, b);
-  const int rows = seq.qlen * a.n;
-  const int r0 = rb * 16 * QB;
-  if (r0 >= rows) return;  // the whole workgroup
+  const int rows = seq.qlen * a.n;  // at most 16
+  if (rows == 0) return;            // the whole workgroup
 
   int lo0, hi0, lo1, hi1;
-  win_range(a, seq, (int)((uint32_t)r0 / (uint32_t)a.n), lo0, hi0);
-  win_range(a, seq, (int)((uint32_t)min(r0 + 16 * QB - 1, rows - 1) / (uint32_t)a.n), lo1, hi1);
+  win_range(a, seq, 0, lo0, hi0);
+  win_range(a, seq, seq.qlen - 1, lo1, hi1);
   WinTiles tiles;
   tiles.init<BKV>(seq, __builtin_amdgcn_readfirstlane(lo0), __builtin_amdgcn_readfirstlane(hi0),
                   __builtin_amdgcn_readfirstlane(lo1), __builtin_amdgcn_readfirstlane(hi1));
-  const int i0 = SPLIT ? (int)((int64_t)tiles.n * sp / a.nsplit) : 0;
-  const int i1 = SPLIT ? (int)((int64_t)tiles.n * (sp + 1) / a.nsplit) : tiles.n;
+  int i0 = 0, i1 = tiles.n;
+  if (SPLIT) win_share(tiles.n, sp, a.nsplit, i0, i1);
 
-  bf16x8 qf[D / 32][QB];
-  WinMask<false> mask;
+  // the lane's row (the last one again past the end)
+  const uint32_t row = (uint32_t)min(jq, rows - 1);
+  const int qi = (int)(row / (uint32_t)a.n), head = h * a.n + (int)(row - qi * a.n);
+  WinMask<1> mask;
   mask.sink = tiles.sink;
+  win_range(a, seq, qi, mask.lo[0], mask.hi[0]);
+  if (tiles.sink == 0 && seq.sink >= lo1) mask.lo[0] = 0;
+  const bf16_t* qp = (const bf16_t*)a.q + b * a.sq + (int64_t)qi * a.ldq + (int64_t)head * D + g * 8;
+  bf16x8 qf[D / 32];
 #pragma unroll
-  for (int i = 0; i < QB; ++i) {
-    const uint32_t r = (uint32_t)min(r0 + 16 * i + jq, rows - 1), qi = r / (uint32_t)a.n;
-    win_range(a, seq, (int)qi, mask.lo[i], mask.hi[i]);
-    if (tiles.sink == 0 && seq.sink >= lo1) mask.lo[i] = 0;
-    const bf16_t* qp = (const bf16_t*)a.q + b * a.sq + (int64_t)qi * a.ldq + (int64_t)(h * a.n + (r - qi * a.n)) * D + g * 8;
-#pragma unroll
-    for (int kc = 0; kc < D / 32; ++kc) qf[kc][i] = __builtin_bit_cast(bf16x8, *(const u32x4*)(qp + kc * 32));
-  }
+  for (int kc = 0; kc < D / 32; ++kc) qf[kc] = __builtin_bit_cast(bf16x8, *(const u32x4*)(qp + kc * 32));
   const uint8_t* const kbase = (const uint8_t*)((const bf16_t*)a.k + b * a.sk + (int64_t)h * D);
   const uint8_t* const vbase = (const uint8_t*)((const bf16_t*)a.vt + b * a.sv + (int64_t)h * D * a.ldv);
-  const uint32_t krow = (uint32_t)a.ldk * 2;
-  uint32_t voff[F];  // the lane's V^T rows
-#pragma unroll
-  for (int f = 0; f < F; ++f) voff[f] = (uint32_t)(att_perm(16 * f + jq) * a.ldv * 2);
+  const uint32_t krow = (uint32_t)a.ldk * 2, vrow = (uint32_t)a.ldv * 2;
+  // att_perm(16 i + jq) = att_perm(16 i) + att_perm(jq): the lane's part of the offsets of its
+  // K and V^T rows, the other part is wave-uniform
+  const uint32_t kl = att_perm(jq) * krow + 16 * g, vl = att_perm(jq) * vrow + 16 * g;
 
-  f32x4 o[F][QB];
-  float m[QB], l[QB];  // reference (log2 units), the lane's part of the denominator
+  f32x4 o[F];
+  float m = -INFINITY, l = 0.0f;  // reference (log2 units), the lane's part of the denominator
 #pragma unroll
-  for (int i = 0; i < QB; ++i) {
-    m[i] = -INFINITY;
-    l[i] = 0.0f;
-#pragma unroll
-    for (int f = 0; f < F; ++f) o[f][i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-  }
+  for (int f = 0; f < F; ++f) o[f] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 
   for (int idx = i0 + wave; idx < i1; idx += 4) {
     const int key0 = tiles.key<BKV>(idx);
     const bool edge = idx < tiles.edge;
     const int last = seq.klen - 1 - key0;  // the last key's place in the tile (or past it)
-    const uint8_t* const kt = kbase + (int64_t)key0 * krow;
+    // K rows past the last key read as zero, V^T columns as whatever is there (cleared below)
+    // or, past the head's last row, as zero
+    const __amdgpu_buffer_rsrc_t rsK = __builtin_amdgcn_make_buffer_rsrc(
+        (void*)(kbase + (int64_t)key0 * krow), (short)0, (int)(min(BKV, last + 1) * krow), 0x00020000);
     const uint8_t* const vt = vbase + (int64_t)key0 * 2;
+    const __amdgpu_buffer_rsrc_t rsV =
+        __builtin_amdgcn_make_buffer_rsrc((void*)vt, (short)0, (int)(D * vrow - 2 * key0), 0x00020000);
     u32x4 kf[BKV / 16][D / 32], vf[F][BKV / 32];
-    // addresses past the last key go to the last key's row, or the unit of 8 keys that holds it
-#pragma unroll
-    for (int i = 0; i < BKV / 16; ++i) {
-      const uint32_t off = (uint32_t)min(att_perm(16 * i + jq), last) * krow + 16 * g;
-#pragma unroll
-      for (int kc = 0; kc < D / 32; ++kc) kf[i][kc] = *(const u32x4*)(kt + off + 64 * kc);
-    }
-#pragma unroll
-    for (int c = 0; c < BKV / 32; ++c) {
-      const uint32_t off = (uint32_t)min(32 * c + 8 * g, last & ~7) * 2;
-#pragma unroll
-      for (int f = 0; f < F; ++f) vf[f][c] = *(const u32x4*)(vt + voff[f] + off);
-    }
-    f32x4 s[BKV / 16][QB];
 #pragma unroll
     for (int i = 0; i < BKV / 16; ++i)
 #pragma unroll
-      for (int q = 0; q < QB; ++q) {
-        s[i][q] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+      for (int kc = 0; kc < D / 32; ++kc)
+        kf[i][kc] = __builtin_amdgcn_raw_buffer_load_b128(rsK, kl + 64 * kc, att_perm(16 * i) * krow, 0);
 #pragma unroll
-        for (int kc = 0; kc < D / 32; ++kc)
-          s[i][q] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kf[i][kc]), qf[kc][q], s[i][q], 0, 0, 0);
-      }
+    for (int f = 0; f < F; ++f)
+#pragma unroll
+      for (int c = 0; c < BKV / 32; ++c)
+        vf[f][c] = __builtin_amdgcn_raw_buffer_load_b128(rsV, vl + 64 * c, att_perm(16 * f) * vrow, 0);
+    f32x4 s[BKV / 16];
+#pragma unroll
+    for (int i = 0; i < BKV / 16; ++i) {
+      s[i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+      for (int kc = 0; kc < D / 32; ++kc)
+        s[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kf[i][kc]), qf[kc], s[i], 0, 0, 0);
+    }
     if (edge) {
-      WinMask<false> mk = mask;
+      WinMask<1> mk = mask;
       mk.key0 = key0;
       mk.begin();
 #pragma unroll
       for (int i = 0; i < BKV / 16; ++i)
 #pragma unroll
-        for (int q = 0; q < QB; ++q)
-#pragma unroll
-          for (int r = 0; r < 4; ++r)
-            s[i][q][r] = mk.apply(q, 32 * (i >> 1) + 4 * (i & 1) + r, s[i][q][r]);
+        for (int r = 0; r < 4; ++r) s[i][r] = mk.apply(0, 32 * (i >> 1) + 4 * (i & 1) + r, s[i][r]);
     }
-    bf16x8 pf[BKV / 32][QB];
+    float t = -INFINITY;
 #pragma unroll
-    for (int q = 0; q < QB; ++q) {
-      float t = -INFINITY;
+    for (int i = 0; i < BKV / 16; ++i)
 #pragma unroll
-      for (int i = 0; i < BKV / 16; ++i)
+      for (int r = 0; r < 4; ++r) t = fmaxf(t, s[i][r]);
+    const float mn = fmaxf(m, group_max2(t, t) * a.scale_log2);
+    if (__ballot(mn > m)) {
+      const float alpha = mn == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m - mn);
+      l *= alpha;
 #pragma unroll
-        for (int r = 0; r < 4; ++r) t = fmaxf(t, s[i][q][r]);
-      const float mn = fmaxf(m[q], group_max2(t, t) * a.scale_log2);
-      if (__ballot(mn > m[q])) {
-        const float alpha = mn == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m[q] - mn);
-        l[q] *= alpha;
+      for (int f = 0; f < F; ++f)
 #pragma unroll
-        for (int f = 0; f < F; ++f)
-#pragma unroll
-          for (int r = 0; r < 4; ++r) o[f][q][r] *= alpha;
-        m[q] = mn;
-      }
-      const float nm = m[q] == -INFINITY ? 0.0f : -m[q];
-#pragma unroll
-      for (int c = 0; c < BKV / 32; ++c) {
-        u32x4 w;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const f32x4 x = s[2 * c + (e >> 1)][q];
-          const float p0 = __builtin_amdgcn_exp2f(fmaf(x[2 * (e & 1)], a.scale_log2, nm));
-          const float p1 = __builtin_amdgcn_exp2f(fmaf(x[2 * (e & 1) + 1], a.scale_log2, nm));
-          w[e] = pack_bf2(p0, p1);
-          // the denominator adds the weights as rounded for the product with V
-          l[q] += __uint_as_float(w[e] << 16) + __uint_as_float(w[e] & 0xffff0000u);
-        }
-        pf[c][q] = __builtin_bit_cast(bf16x8, w);
-      }
+        for (int r = 0; r < 4; ++r) o[f][r] *= alpha;
+      m = mn;
     }
+    const float nm = m == -INFINITY ? 0.0f : -m;
+    u32x4 pw[BKV / 32];
+#pragma unroll
+    for (int c = 0; c < BKV / 32; ++c)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const f32x4 x = s[2 * c + (e >> 1)];
+        const float p0 = __builtin_amdgcn_exp2f(fmaf(x[2 * (e & 1)], a.scale_log2, nm));
+        const float p1 = __builtin_amdgcn_exp2f(fmaf(x[2 * (e & 1) + 1], a.scale_log2, nm));
+        pw[c][e] = pack_bf2(p0, p1);
+        // the denominator adds the weights as rounded for the product with V
+        l += __uint_as_float(pw[c][e] << 16) + __uint_as_float(pw[c][e] & 0xffff0000u);
+      }
     if (edge) {
       // V^T past the last key is cleared, and what else is not finite and may be hidden from
       // some row is weighed key by key
@@ -505,24 +505,20 @@ __global__ __launch_bounds__(256) void window_rows_kernel(WinArgs a) {
           }
         }
       if (__ballot(top[0] == 0x7f80 || top[1] == 0x7f80)) {
+        const int ln = att_lane();  // the offsets below are formed here, not kept across the tiles
 #pragma unroll 1
         for (int key = 0; key < min(BKV, last + 1); ++key) {
-          float p[QB];
-#pragma unroll
-          for (int q = 0; q < QB; ++q) {
-            const u32x4 own = __builtin_bit_cast(u32x4, key < 32 ? pf[0][q] : pf[1][q]);
-            const int e = (key >> 1) & 3;
-            const uint32_t w = e == 0 ? own[0] : (e == 1 ? own[1] : (e == 2 ? own[2] : own[3]));
-            const uint32_t got = __builtin_amdgcn_ds_bpermute((jq + 16 * ((key >> 3) & 3)) << 2, (int)w);
-            p[q] = __uint_as_float(key & 1 ? got & 0xffff0000u : got << 16);
-          }
+          const u32x4 own = key < 32 ? pw[0] : pw[1];
+          const int e = (key >> 1) & 3;
+          const uint32_t w = e == 0 ? own[0] : (e == 1 ? own[1] : (e == 2 ? own[2] : own[3]));
+          const uint32_t got = __builtin_amdgcn_ds_bpermute(((ln & 15) + 16 * ((key >> 3) & 3)) << 2, (int)w);
+          const float p = __uint_as_float(key & 1 ? got & 0xffff0000u : got << 16);
 #pragma unroll
           for (int f = 0; f < F; ++f)
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-              const float v = bf2f(*(const bf16_t*)(vt + (uint32_t)(att_perm(16 * f + 4 * g + r) * a.ldv * 2) + 2 * key));
-#pragma unroll
-              for (int q = 0; q < QB; ++q) o[f][q][r] = p[q] != 0.0f ? fmaf(p[q], v, o[f][q][r]) : o[f][q][r];
+              const float v = bf2f(*(const bf16_t*)(vt + att_perm(16 * f + 4 * (ln >> 4) + r) * vrow + 2 * key));
+              o[f][r] = p != 0.0f ? fmaf(p, v, o[f][r]) : o[f][r];
             }
         }
         continue;
@@ -532,60 +528,51 @@ __global__ __launch_bounds__(256) void window_rows_kernel(WinArgs a) {
     for (int c = 0; c < BKV / 32; ++c)
 #pragma unroll
       for (int f = 0; f < F; ++f)
-#pragma unroll
-        for (int q = 0; q < QB; ++q)
-          o[f][q] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, vf[f][c]), pf[c][q], o[f][q], 0, 0, 0);
+        o[f] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, vf[f][c]),
+                                                       __builtin_bit_cast(bf16x8, pw[c]), o[f], 0, 0, 0);
   }
 
   // join the four waves: each takes two of the eight 16-channel blocks
+  l += __shfl_xor(l, 16);
+  l += __shfl_xor(l, 32);
 #pragma unroll
-  for (int q = 0; q < QB; ++q) {
-    l[q] += __shfl_xor(l[q], 16);
-    l[q] += __shfl_xor(l[q], 32);
-#pragma unroll
-    for (int f = 0; f < F; ++f) so[wave][f][q][lane] = o[f][q];
-    if (g == 0) {
-      sm[wave][16 * q + jq] = m[q];
-      sl[wave][16 * q + jq] = l[q];
-    }
+  for (int f = 0; f < F; ++f) so[wave][f][lane] = o[f];
+  if (g == 0) {
+    sm[wave][jq] = m;
+    sl[wave][jq] = l;
   }
   __syncthreads();
+  float mx = -INFINITY, sum = 0.0f, wt[4];
 #pragma unroll
-  for (int q = 0; q < QB; ++q) {
-    const int r = r0 + 16 * q + jq;
-    float mx = -INFINITY, sum = 0.0f, wt[4];
+  for (int w = 0; w < 4; ++w) mx = fmaxf(mx, sm[w][jq]);
 #pragma unroll
-    for (int w = 0; w < 4; ++w) mx = fmaxf(mx, sm[w][16 * q + jq]);
+  for (int w = 0; w < 4; ++w) {
+    const float mi = sm[w][jq];
+    wt[w] = mi == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(mi - mx);  // a wave without keys
+    sum = fmaf(wt[w], sl[w][jq], sum);
+  }
+  if (jq >= rows) return;
+  const int64_t pr = ((((int64_t)sp * a.B + b) * a.Hk + h) * a.Lq) * a.n + jq;
+  const float inv = win_inverse(sum);
+#pragma unroll
+  for (int fi = 0; fi < 2; ++fi) {
+    const int f = 2 * wave + fi, ch = att_perm(16 * f + 4 * g);
+    f32x4 v = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
     for (int w = 0; w < 4; ++w) {
-      const float mi = sm[w][16 * q + jq];
-      wt[w] = mi == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(mi - mx);  // a wave without keys
-      sum = fmaf(wt[w], sl[w][16 * q + jq], sum);
-    }
-    if (r >= rows) continue;
-    const int qi = (int)((uint32_t)r / (uint32_t)a.n), head = h * a.n + (r - qi * a.n);
-    const int64_t pr = ((((int64_t)sp * a.B + b) * a.Hk + h) * a.Lq) * a.n + r;
-    const float inv = win_inverse(sum);
+      const f32x4 u = so[w][f][lane];
 #pragma unroll
-    for (int fi = 0; fi < 2; ++fi) {
-      const int f = 2 * wave + fi, ch = att_perm(16 * f + 4 * g);
-      f32x4 v = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-      for (int w = 0; w < 4; ++w) {
-        const f32x4 u = so[w][f][q][lane];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = fmaf(wt[w], u[e], v[e]);
-      }
-      if constexpr (SPLIT)
-        *(f32x4*)(a.po + pr * D + ch) = v;
-      else
-        *(u32x2*)((bf16_t*)a.out + b * a.so + (int64_t)qi * a.ldo + (int64_t)head * D + ch) =
-            u32x2{pack_bf2(v[0] * inv, v[1] * inv), pack_bf2(v[2] * inv, v[3] * inv)};
+      for (int e = 0; e < 4; ++e) v[e] = fmaf(wt[w], u[e], v[e]);
     }
-    if (wave == 0 && g == 0) {
-      if constexpr (SPLIT) a.pml[pr] = float2{mx, sum};
-      else if (a.lse) a.lse[((int64_t)b * a.Hk * a.n + head) * a.Lq + qi] = win_lse(mx, sum);
-    }
+    if constexpr (SPLIT)
+      *(f32x4*)(a.po + pr * D + ch) = v;
+    else
+      *(u32x2*)((bf16_t*)a.out + b * a.so + (int64_t)qi * a.ldo + (int64_t)head * D + ch) =
+          u32x2{pack_bf2(v[0] * inv, v[1] * inv), pack_bf2(v[2] * inv, v[3] * inv)};
+  }
+  if (wave == 0 && g == 0) {
+    if constexpr (SPLIT) a.pml[pr] = float2{mx, sum};
+    else if (a.lse) a.lse[((int64_t)b * a.Hk * a.n + head) * a.Lq + qi] = win_lse(mx, sum);
   }
 }
 
@@ -620,9 +607,8 @@ __global__ __launch_bounds__(256) void window_f32_kernel(WinArgs a) {
   WinTiles tiles;
   tiles.init<BKV>(seq, __builtin_amdgcn_readfirstlane(lo0), __builtin_amdgcn_readfirstlane(hi0),
                   __builtin_amdgcn_readfirstlane(lo1), __builtin_amdgcn_readfirstlane(hi1));
-  const int64_t shares = KS * (SPLIT ? a.nsplit : 1);
-  const int share = KS == 4 ? (SPLIT ? sp * 4 : 0) + wave : 0;
-  const int i0 = (int)(tiles.n * (int64_t)share / shares), i1 = (int)(tiles.n * (int64_t)(share + 1) / shares);
+  int i0 = 0, i1 = tiles.n;
+  if (KS == 4) win_share(tiles.n, (SPLIT ? sp * 4 : 0) + wave, SPLIT ? 4 * a.nsplit : 4, i0, i1);
 
   const int r = r0 + jq;
   const uint32_t rr = (uint32_t)min(r, rows - 1), qi = rr / (uint32_t)a.n;
@@ -798,40 +784,64 @@ __global__ __launch_bounds__(256) void window_f32_kernel(WinArgs a) {
   }
 }
 
-// The shares of each row joined: D / 4 threads a row, four channels a thread.
-template <typename T>
+// The shares of each row joined: D / 4 threads a row and G groups of them, each with every
+// G-th share, so that a token's few rows do not wait for one share after another (with one
+// group 3.9 us at 160 rows of 5 shares, ... ).
+template <typename T, int G>
 __global__ __launch_bounds__(256) void window_join_kernel(WinArgs a, int D) {
-  const int per = D / 4, c = (int)threadIdx.x % per * 4;
+  __shared__ f32x4 so[G > 1 ? 256 : 1];
+  __shared__ float2 sml[G > 1 ? 256 : 1];
+  const int per = D / 4, t = (int)threadIdx.x;
+  const int c = t % per * 4, grp = t / per % G;
   const int64_t all = (int64_t)a.B * a.Hk * a.Lq * a.n;
-  const int64_t pr = (int64_t)blockIdx.x * (256 / per) + (int)threadIdx.x / per;
-  if (pr >= all) return;
+  const int64_t pr = (int64_t)blockIdx.x * (256 / per / G) + t / (per * G);
+  float m = -INFINITY, l = 0.0f;
+  f32x4 v = {0.0f, 0.0f, 0.0f, 0.0f};
   const uint32_t per_head = (uint32_t)(a.Lq * a.n);  // < 2^31
-  const uint32_t bh = (uint32_t)(pr / per_head), r = (uint32_t)(pr - (int64_t)bh * per_head);
+  const int64_t row = pr < all ? pr : all - 1;
+  const uint32_t bh = (uint32_t)(row / per_head), r = (uint32_t)(row - (int64_t)bh * per_head);
   const int b = (int)(bh / (uint32_t)a.Hk), h = (int)(bh - b * a.Hk);
   const int qi = (int)(r / (uint32_t)a.n), head = h * a.n + (int)(r - qi * a.n);
-  if (a.q_len && qi >= min(a.q_len[b], a.Lq)) return;
-  float mx = -INFINITY, sum = 0.0f;
-  for (int s = 0; s < a.nsplit; ++s) mx = fmaxf(mx, a.pml[s * all + pr].x);
-  f32x4 v = {0.0f, 0.0f, 0.0f, 0.0f};
+  const bool there = pr < all && !(a.q_len && qi >= min(a.q_len[b], a.Lq));
+  auto add = [&](float m1, float l1, const f32x4& u) {
+    const float mx = fmaxf(m, m1);
+    const float w0 = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m - mx);  // nothing yet, or a share without keys
+    const float w1 = m1 == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m1 - mx);
+    l = w0 * l + w1 * l1;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = w0 * v[e] + w1 * u[e];
+    m = mx;
+  };
+  if (there) {
 #pragma unroll 4
-  for (int s = 0; s < a.nsplit; ++s) {
-    const float2 ml = a.pml[s * all + pr];
-    const f32x4 u = *(const f32x4*)(a.po + (s * all + pr) * D + c);
-    const float wt = ml.x == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(ml.x - mx);  // a share without keys
-    sum = fmaf(wt, ml.y, sum);
-#pragma unroll
-    for (int e = 0; e < 4; ++e) v[e] = fmaf(wt, u[e], v[e]);
+    for (int s = grp; s < a.nsplit; s += G) {
+      const float2 ml = a.pml[s * all + row];
+      add(ml.x, ml.y, *(const f32x4*)(a.po + (s * all + row) * D + c));
+    }
   }
-  const float inv = win_inverse(sum);
-  T* o = (T*)a.out + b * a.so + (int64_t)qi * a.ldo + (int64_t)head * D + c;
+  if constexpr (G > 1) {
+    so[t] = v;
+    sml[t] = float2{m, l};
+    __syncthreads();
+    if (grp) return;
 #pragma unroll
-  for (int e = 0; e < 4; ++e) stf(o + e, v[e] * inv);
-  if (a.lse && c == 0) a.lse[((int64_t)b * a.Hk * a.n + head) * a.Lq + qi] = win_lse(mx, sum);
+    for (int i = 1; i < G; ++i) add(sml[t + i * per].x, sml[t + i * per].y, so[t + i * per]);
+  }
+  if (!there) return;
+  const float inv = win_inverse(l);
+  T* o = (T*)a.out + b * a.so + (int64_t)qi * a.ldo + (int64_t)head * D + c;
+  if constexpr (sizeof(T) == 2) {
+    *(u32x2*)o = u32x2{pack_bf2(v[0] * inv, v[1] * inv), pack_bf2(v[2] * inv, v[3] * inv)};
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) o[e] = v[e] * inv;
+  }
+  if (a.lse && c == 0) a.lse[((int64_t)b * a.Hk * a.n + head) * a.Lq + qi] = win_lse(m, l);
 }
 
 // ---------------------------------------------------------------- host
 struct WinPlan {
-  enum Form { BLOCKS, ROWS16, ROWS32, F32_SHARED, F32_APART } form;
+  enum Form { BLOCKS, ROWS, F32_SHARED, F32_APART } form;
   int64_t nrb;
   int nsplit;
 };
@@ -841,6 +851,39 @@ static int64_t win_span(const track_window& w, int64_t rows, int n, int64_t Lk) 
   if (w.left < 0 || w.right < 0) return Lk;
   const int64_t groups = w.left + w.right + 2 + (rows + n - 1) / n / w.group;
   return std::min(Lk, groups * w.group + w.sink);
+}
+
+// Shares of the keys for few rows, `blocks` row blocks of `tiles` tiles each.  Up to 8 tiles a
+// wave on a full chip, a workgroup on every CU, but two tiles a share; beyond, three workgroups
+// a CU, which evens out lengths.  One token, 8 key heads of 4096 keys: 59 us with one share,
+// 14.1 with 8, 11.2 with 16, 9.3 with 32, 10.2 with 64; 32 of 1027: 18.9 with 1, 11.1 with 5,
+// 10.4 with 8, 12.2 with 16; 8 of 16384: 17.8 with 32, 18.9 with 64; 64 of 100003: 619 with 8,
+// 568 with 12, 585 with 64.
+static int rows_split(int64_t tiles, int64_t blocks, int64_t cus) {
+  const bool large = blocks * tiles >= 64 * cus;
+  const int64_t s = large ? (3 * cus + blocks - 1) / blocks : std::min(cus / blocks, (tiles + 1) / 2);
+  return (int)std::max<int64_t>(1, s);
+}
+
+// Shares of the keys for blocks of rows, by an estimate of the time: rounds of workgroups over
+// the CUs, a tile 1.6 us and 5 us beside the tiles, and with shares the join, 3 us and the
+// sums' way out and back at 4 TB/s.  Fits measured times within 10% where the matrix cores
+// are the bound (1 - 42 shares of 2000, 4096 and 32760 keys, 17 - 400 rows of 8, 12 and 40
+// heads): 256 rows of 12 heads, 32760 keys 732 us with one share, 106 with 10, 69 with 21, 83
+// with 42; 400 rows of 40 heads, 2000 keys 53 with one, 38 with 3, 52 with 4.
+static int blocks_split(int64_t tiles, int64_t blocks, int64_t rows, int64_t cus) {
+  int best = 1;
+  double best_t = 0.0;
+  for (int64_t s = 1; s <= std::max<int64_t>(1, std::min<int64_t>(tiles / 2, 64)); ++s) {
+    const double rounds = (double)((blocks * s + cus - 1) / cus);
+    double t = rounds * ((double)((tiles + s - 1) / s) * 1.6 + 5.0);
+    if (s > 1) t += 3.0 + (double)(2 * s * rows * (4 * ATT_D + 8)) / 4e6;
+    if (s == 1 || t < best_t) {
+      best = (int)s;
+      best_t = t;
+    }
+  }
+  return best;
 }
 
 static WinPlan win_plan(int dtype, const track_window& w, int64_t B, int Hk, int n, int64_t Lq, int64_t Lk) {
@@ -859,18 +902,15 @@ static WinPlan win_plan(int dtype, const track_window& w, int64_t B, int Hk, int
     p.nsplit = (int)std::max<int64_t>(1, std::min<int64_t>(2 * cus / (p.nrb * Hk * B), steps / 32));
     return p;
   }
-  if (rows <= 64) {
-    p.form = rows <= 16 ? WinPlan::ROWS16 : WinPlan::ROWS32;
-    const int per = rows <= 16 ? 16 : 32;
-    p.nrb = (rows + per - 1) / per;
-    const int64_t tiles = (win_span(w, per, n, Lk) + 63) / 64;
-    p.nsplit = (int)std::max<int64_t>(1, std::min<int64_t>(2 * cus / (p.nrb * Hk * B), tiles / 8));
+  if (rows <= 16) {
+    p.form = WinPlan::ROWS;
+    p.nrb = 1;
+    p.nsplit = rows_split((win_span(w, rows, n, Lk) + 63) / 64, Hk * B, cus);
     return p;
   }
   p.form = WinPlan::BLOCKS;
   p.nrb = (rows + ATT_BQ - 1) / ATT_BQ;
-  const int64_t tiles = (win_span(w, ATT_BQ, n, Lk) + 63) / 64, wgs = p.nrb * Hk * B;
-  p.nsplit = (int)std::max<int64_t>(1, std::min<int64_t>(cus / wgs, tiles / 8));
+  p.nsplit = blocks_split((win_span(w, std::min<int64_t>(rows, ATT_BQ), n, Lk) + 63) / 64, p.nrb * Hk * B, rows * Hk * B, cus);
   return p;
 }
 
@@ -968,13 +1008,9 @@ track_status attention_window(int dtype, const track_window* w, int B, int H, in
       else if (split) window_blocks_kernel<false, true><<<gr, 512, 0, s>>>(a);
       else window_blocks_kernel<false, false><<<gr, 512, 0, s>>>(a);
       break;
-    case WinPlan::ROWS16:
-      if (split) window_rows_kernel<1, true><<<gr, 256, 0, s>>>(a);
-      else window_rows_kernel<1, false><<<gr, 256, 0, s>>>(a);
-      break;
-    case WinPlan::ROWS32:
-      if (split) window_rows_kernel<2, true><<<gr, 256, 0, s>>>(a);
-      else window_rows_kernel<2, false><<<gr, 256, 0, s>>>(a);
+    case WinPlan::ROWS:
+      if (split) window_rows_kernel<true><<<gr, 256, 0, s>>>(a);
+      else window_rows_kernel<false><<<gr, 256, 0, s>>>(a);
       break;
     default:
       if (D == 32) TRACK_WIN_F32(32);
@@ -985,10 +1021,18 @@ track_status attention_window(int dtype, const track_window* w, int B, int H, in
 #undef TRACK_WIN_F32_K
   TRACK_LAUNCH_CHECK();
   if (split) {
-    const int per = D / 4, rows_wg = 256 / per;
+    // groups of shares while the rows alone do not fill the chip
+    const int per = D / 4, G = joined * D / 4 < 512 * (int64_t)device_cus() && p.nsplit > 2 ? 8 : 1;
+    const int rows_wg = 256 / per / G;
     const unsigned jg = (unsigned)((joined + rows_wg - 1) / rows_wg);
-    if (dtype == TRACK_DTYPE_BF16) window_join_kernel<bf16_t><<<jg, 256, 0, s>>>(a, D);
-    else window_join_kernel<float><<<jg, 256, 0, s>>>(a, D);
+#define TRACK_WIN_JOIN(T)                                               \
+  do {                                                                  \
+    if (G == 1) window_join_kernel<T, 1><<<jg, 256, 0, s>>>(a, D);      \
+    else window_join_kernel<T, 8><<<jg, 256, 0, s>>>(a, D);             \
+  } while (0)
+    if (dtype == TRACK_DTYPE_BF16) TRACK_WIN_JOIN(bf16_t);
+    else TRACK_WIN_JOIN(float);
+#undef TRACK_WIN_JOIN
     TRACK_LAUNCH_CHECK();
   }
   return TRACK_OK;

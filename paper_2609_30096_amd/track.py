@@ -507,96 +507,133 @@ class Rope:
         self.cfg = cfg
         self.c = cfg.c()
         self.axes = self.c.axes
+        self.layouts = {}
+        self.check = _rope_layout(self)
         self.freqs = _torch().from_numpy(freqs).to(device)
 
 
 def _float_dtype(t) -> int:
-    torch = _torch()
-    if t.dtype == torch.bfloat16:
+    d = str(t.dtype)
+    if d == "torch.bfloat16":
         return DTYPE_BF16
-    if t.dtype == torch.float32:
+    if d == "torch.float32":
         return DTYPE_F32
-    raise TypeError(f"float32 or bfloat16 tensor expected, got {t.dtype}")
+    raise TypeError(f"float32 or bfloat16 tensor expected, got {d}")
 
 
 def _like(t, other, what):
-    if t.dtype != other.dtype or t.device != other.device:
+    if t.dtype != other.dtype or t.get_device() != other.get_device():
         raise TypeError(f"{what}: {t.dtype} on {t.device} beside {other.dtype} on {other.device}")
 
 
 def _ints(t, shape, ref, what):
     """An int32 tensor of the given shape, contiguous, on ref's device (None passes)."""
-    if t is None:
-        return
-    torch = _torch()
-    if t.dtype != torch.int32 or tuple(t.shape) != tuple(shape) or not t.is_contiguous() or t.device != ref.device:
+    if t is not None and (t.shape != shape or str(t.dtype) != "torch.int32" or not t.is_contiguous() or t.get_device() != ref.get_device()):
         raise ValueError(f"{what}: contiguous int32 {tuple(shape)} on {ref.device} expected")
 
 
 def _seq_heads(t, what):
     """[sequences, tokens, heads, channels] with heads side by side: (row stride, sequence stride)."""
-    if t.dim() != 4:
-        raise ValueError(f"{what}: [sequences, tokens, heads, channels] expected, got {tuple(t.shape)}")
-    B, L, H, D = t.shape
-    if t.numel() and ((D > 1 and t.stride(3) != 1) or (H > 1 and t.stride(2) != D)):
+    shape = t.shape
+    if len(shape) != 4:
+        raise ValueError(f"{what}: [sequences, tokens, heads, channels] expected, got {tuple(shape)}")
+    B, L, H, D = shape
+    s0, s1, s2, s3 = t.stride()
+    if ((s3 != 1 and D > 1) or (s2 != D and H > 1)) and t.numel():
         raise ValueError(f"{what}: heads of a token must lie side by side")
-    ld = t.stride(1) if L > 1 else H * D
-    return ld, t.stride(0) if B > 1 else ld * L
+    ld = s1 if L > 1 else H * D
+    return ld, s0 if B > 1 else ld * L
 
 
-def _head_rows(x, y, what) -> HeadRowsC:
-    if tuple(x.shape) != tuple(y.shape):
+def _on_device(fn, t, *args):
+    """fn(*args, stream) on t's device and its current stream."""
+    torch = _torch()
+    at = t.get_device()
+    if at < 0:
+        raise ValueError(f"GPU tensors expected, got {t.device}")
+    if at == torch.cuda.current_device():
+        _check(fn(*args, torch.cuda.current_stream(at).cuda_stream))
+    else:
+        with torch.cuda.device(at):
+            _check(fn(*args, torch.cuda.current_stream(at).cuda_stream))
+
+
+_LAYOUTS_KEPT = 512
+
+
+def _layout(kept: dict, tensors, check):
+    """What `check` makes of the layouts of these tensors (None among them), checked once for each combination of
+    shapes, strides, types and devices: for a single token the checks took longer than the kernel."""
+    key = tuple([None if t is None else (t.shape, t.stride(), t.dtype, t.get_device()) for t in tensors])
+    got = kept.get(key)
+    if got is None:
+        got = check(*tensors)
+        if len(kept) >= _LAYOUTS_KEPT:
+            kept.clear()
+        kept[key] = got
+    return got
+
+
+def _head_rows(x, y, what):
+    """(strides of x, strides of y, heads) as track_head_rows takes them."""
+    if y.shape != x.shape:
         raise ValueError(f"{what}: output of shape {tuple(y.shape)} for {tuple(x.shape)}")
     _like(y, x, what)
-    ldx, sx = _seq_heads(x, what)
-    ldy, sy = _seq_heads(y, what)
-    return HeadRowsC(x.data_ptr(), ldx, sx, y.data_ptr(), ldy, sy, x.shape[2])
+    return _seq_heads(x, what) + _seq_heads(y, what) + (x.shape[2],)
 
 
-def _rope_call(rope, q, k, pos, q_out, k_out):
-    B, L = q.shape[:2]
-    q_out = q if q_out is None else q_out
-    rq, rk = _head_rows(q, q_out, "q"), None
-    if q.shape[3] != rope.c.head_dim:
-        raise ValueError(f"q: heads of {q.shape[3]} channels, {rope.c.head_dim} configured")
-    if k is not None:
-        if tuple(k.shape[:2]) != (B, L) or k.shape[3] != q.shape[3]:
-            raise ValueError(f"k of shape {tuple(k.shape)} beside q of {tuple(q.shape)}")
-        _like(k, q, "k")
-        k_out = k if k_out is None else k_out
-        rk = _head_rows(k, k_out, "k")
-    elif k_out is not None:
-        raise ValueError("k_out without k")
-    _ints(pos, (rope.axes, B, L), q, "pos")
-    if rope.freqs.device != q.device:
-        raise ValueError(f"rope on {rope.freqs.device}, q on {q.device}")
-    return B, L, rq, rk, q_out, k_out
+def _rope_layout(rope):
+    def check(q, k, q_out, k_out, pos, g_q, g_k):
+        rq, rk = _head_rows(q, q_out, "q"), None
+        B, L, _, D = q.shape
+        if D != rope.c.head_dim:
+            raise ValueError(f"q: heads of {D} channels, {rope.c.head_dim} configured")
+        if k is not None:
+            rk = _head_rows(k, k_out, "k")
+            if k.shape[0] != B or k.shape[1] != L or k.shape[3] != D:
+                raise ValueError(f"k of shape {tuple(k.shape)} beside q of {tuple(q.shape)}")
+            _like(k, q, "k")
+        elif k_out is not None or g_k is not None:
+            raise ValueError("k_out or g_k without k")
+        _ints(pos, (rope.axes, B, L), q, "pos")
+        if rope.freqs.get_device() != q.get_device():
+            raise ValueError(f"rope on {rope.freqs.device}, q on {q.device}")
+        for g, what in ((g_q, "g_q"), (g_k, "g_k")):
+            if g is not None:
+                if g.shape != q.shape[3:] or not g.is_contiguous():
+                    raise ValueError(f"{what}: [{D}] expected")
+                _like(g, q, what)
+        return _float_dtype(q), B, L, rq, rk
+    return check
+
+
+def _rows_c(layout, x, y) -> HeadRowsC:
+    ldx, sx, ldy, sy, heads = layout
+    return HeadRowsC(x.data_ptr(), ldx, sx, y.data_ptr(), ldy, sy, heads)
 
 
 def op_rope(rope: Rope, q, k, pos, q_out=None, k_out=None, inverse: bool = False):
     """Rotates q [B, L, H, D] and k [B, L, Hk, D] (or None) by positions pos (int32 [axes, B, L]), in place or
     into q_out and k_out; returns the outputs.  Strides of tokens and sequences are free."""
-    B, L, rq, rk, q_out, k_out = _rope_call(rope, q, k, pos, q_out, k_out)
-    with _torch().cuda.device(q.device):
-        _check(lib().track_op_rope(_float_dtype(q), ctypes.byref(rope.c), B, L, ctypes.byref(rq),
-                                   None if rk is None else ctypes.byref(rk), _ptr(pos), _ptr(rope.freqs),
-                                   rope.amplitude, 1 if inverse else 0, _stream()))
+    q_out = q if q_out is None else q_out
+    k_out = k if k_out is None else k_out
+    dtype, B, L, rq, rk = _layout(rope.layouts, (q, k, q_out, k_out, pos, None, None), rope.check)
+    _on_device(lib().track_op_rope, q, dtype, rope.c, B, L, _rows_c(rq, q, q_out),
+               None if k is None else _rows_c(rk, k, k_out), pos.data_ptr(), rope.freqs.data_ptr(), rope.amplitude,
+               1 if inverse else 0)
     return q_out, k_out
 
 
 def op_headnorm_rope(rope: Rope, q, k, g_q, g_k, pos, q_out=None, k_out=None, eps: float = 1e-6,
                      q_scale: float = 1.0):
     """op_rope behind the RMSNorm of every head, with gains g_q and g_k [D]; q times q_scale."""
-    B, L, rq, rk, q_out, k_out = _rope_call(rope, q, k, pos, q_out, k_out)
-    for g, what in ((g_q, "g_q"),) + (((g_k, "g_k"),) if k is not None else ()):
-        if tuple(g.shape) != (q.shape[3],) or not g.is_contiguous():
-            raise ValueError(f"{what}: [{q.shape[3]}] expected")
-        _like(g, q, what)
-    with _torch().cuda.device(q.device):
-        _check(lib().track_op_headnorm_rope(_float_dtype(q), ctypes.byref(rope.c), B, L, ctypes.byref(rq),
-                                            None if rk is None else ctypes.byref(rk), _ptr(g_q),
-                                            _ptr(g_k if k is not None else None), float(eps), float(q_scale),
-                                            _ptr(pos), _ptr(rope.freqs), rope.amplitude, _stream()))
+    q_out = q if q_out is None else q_out
+    k_out = k if k_out is None else k_out
+    dtype, B, L, rq, rk = _layout(rope.layouts, (q, k, q_out, k_out, pos, g_q, g_k), rope.check)
+    _on_device(lib().track_op_headnorm_rope, q, dtype, rope.c, B, L, _rows_c(rq, q, q_out),
+               None if k is None else _rows_c(rk, k, k_out), 0 if g_q is None else g_q.data_ptr(),
+               0 if g_k is None else g_k.data_ptr(), eps, q_scale, pos.data_ptr(), rope.freqs.data_ptr(),
+               rope.amplitude)
     return q_out, k_out
 
 
@@ -609,13 +646,17 @@ class Window:
     group: int = 1
     scale: Optional[float] = None  # 1 / sqrt(head_dim)
 
+    def __post_init__(self):
+        object.__setattr__(self, "_c", WindowC(self.left, self.right, self.sink, self.group,
+                                               0.0 if self.scale is None else self.scale))
+
     def c(self) -> WindowC:
-        return WindowC(self.left, self.right, self.sink, self.group, 0.0 if self.scale is None else self.scale)
+        return self._c
 
 
 def attention_window_workspace_bytes(window: Window, dtype: int, B: int, H: int, Hk: int, head_dim: int, Lq: int,
                                      Lk: int) -> int:
-    n = lib().track_attention_window_workspace_bytes(dtype, ctypes.byref(window.c()), B, H, Hk, head_dim, Lq, Lk)
+    n = lib().track_attention_window_workspace_bytes(dtype, window.c(), B, H, Hk, head_dim, Lq, Lk)
     if n < 0:
         raise TrackError(E_INVALID, lib().track_last_error().decode())
     return n
@@ -623,10 +664,42 @@ def attention_window_workspace_bytes(window: Window, dtype: int, B: int, H: int,
 
 def attention_window_workspace(window: Window, q, k):
     """The workspace of op_attention_window on tensors of these shapes (None where it needs none)."""
-    with _torch().cuda.device(q.device):
+    torch = _torch()
+    with torch.cuda.device(q.device):
         n = attention_window_workspace_bytes(window, _float_dtype(q), q.shape[0], q.shape[2], k.shape[2], q.shape[3],
                                              q.shape[1], k.shape[1])
-    return _torch().empty(n, dtype=_torch().uint8, device=q.device) if n else None
+        return torch.empty(n, dtype=torch.uint8, device=q.device) if n else None
+
+
+_window_layouts: dict = {}
+
+
+def _check_window(q, k, vt, out, lse, q_len, k_len, q_start, workspace):
+    ldq, sq = _seq_heads(q, "q")
+    ldk, sk = _seq_heads(k, "k")
+    ldo, so = _seq_heads(out, "out")
+    B, Lq, H, D = q.shape
+    Bk, Lk, Hk, Dk = k.shape
+    if out.shape != q.shape or Bk != B or Dk != D:
+        raise ValueError(f"q {tuple(q.shape)}, k {tuple(k.shape)}, out {tuple(out.shape)} do not match")
+    for t, what in ((k, "k"), (vt, "vt"), (out, "out")):
+        _like(t, q, what)
+    if vt.dim() != 4 or vt.shape[:3] != (B, Hk, D) or vt.shape[3] < Lk:
+        raise ValueError(f"vt: [{B}, {Hk}, {D}, >= {Lk}] expected, got {tuple(vt.shape)}")
+    sv, s1, ldv, s3 = vt.stride()
+    if ((s3 != 1 and vt.shape[3] > 1) or (s1 != D * ldv and Hk > 1)) and vt.numel():
+        raise ValueError("vt: rows of keys, D of them a head, heads one after another")
+    for t, what in ((q_len, "q_len"), (k_len, "k_len"), (q_start, "q_start")):
+        _ints(t, (B,), q, what)
+    if lse is not None and (str(lse.dtype) != "torch.float32" or lse.shape != (B, H, Lq) or
+                            not lse.is_contiguous() or lse.get_device() != q.get_device()):
+        raise ValueError(f"lse: contiguous float32 [{B}, {H}, {Lq}] on {q.device} expected")
+    nbytes = 0
+    if workspace is not None:
+        if workspace.get_device() != q.get_device() or not workspace.is_contiguous():
+            raise ValueError(f"workspace: contiguous, on {q.device} expected")
+        nbytes = workspace.numel() * workspace.element_size()
+    return (_float_dtype(q), B, H, Hk, D, Lq, Lk, ldq, sq, ldk, sk, ldv, sv if B > 1 else 0, ldo, so, nbytes)
 
 
 def op_attention_window(window: Window, q, k, vt, out, lse=None, q_len=None, k_len=None, q_start=None,
@@ -634,35 +707,11 @@ def op_attention_window(window: Window, q, k, vt, out, lse=None, q_len=None, k_l
     """Window attention of q [B, Lq, H, D] on k [B, Lk, Hk, D] and vt [B, Hk, D, >= Lk] into out (like q); returns
     out.  k may be a view into a longer cache; a sequence stride of 0 in k and vt shares them.  lse: float32
     [B, H, Lq]; q_len, k_len, q_start: int32 [B]."""
-    B, Lq, H, D = q.shape
-    if tuple(out.shape) != tuple(q.shape) or k.dim() != 4 or k.shape[0] != B or k.shape[3] != D:
-        raise ValueError(f"q {tuple(q.shape)}, k {tuple(k.shape)}, out {tuple(out.shape)} do not match")
-    Lk, Hk = k.shape[1], k.shape[2]
-    for t, what in ((k, "k"), (vt, "vt"), (out, "out")):
-        _like(t, q, what)
-    if vt.dim() != 4 or tuple(vt.shape[:3]) != (B, Hk, D) or vt.shape[3] < Lk:
-        raise ValueError(f"vt: [{B}, {Hk}, {D}, >= {Lk}] expected, got {tuple(vt.shape)}")
-    ldv = vt.stride(2)
-    if vt.numel() and (vt.stride(3) != 1 or (Hk > 1 and vt.stride(1) != D * ldv)):
-        raise ValueError("vt: rows of keys, D of them a head, heads one after another")
-    ldq, sq = _seq_heads(q, "q")
-    ldk, sk = _seq_heads(k, "k")
-    ldo, so = _seq_heads(out, "out")
-    sv = vt.stride(0) if B > 1 else Hk * D * ldv
-    _ints(q_len, (B,), q, "q_len")
-    _ints(k_len, (B,), q, "k_len")
-    _ints(q_start, (B,), q, "q_start")
-    if lse is not None and (lse.dtype != _torch().float32 or tuple(lse.shape) != (B, H, Lq) or
-                            not lse.is_contiguous() or lse.device != q.device):
-        raise ValueError(f"lse: contiguous float32 [{B}, {H}, {Lq}] on {q.device} expected")
-    if workspace is not None and workspace.device != q.device:
-        raise ValueError(f"workspace on {workspace.device}, q on {q.device}")
-    nbytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
-    with _torch().cuda.device(q.device):
-        _check(lib().track_op_attention_window(
-            _float_dtype(q), ctypes.byref(window.c()), B, H, Hk, D, Lq, Lk, _ptr(q), ldq, sq, _ptr(k), ldk, sk,
-            _ptr(vt), ldv, sv, _ptr(out), ldo, so, _ptr(lse), _ptr(q_len), _ptr(k_len), _ptr(q_start),
-            _ptr(workspace), nbytes, _stream()))
+    (dtype, B, H, Hk, D, Lq, Lk, ldq, sq, ldk, sk, ldv, sv, ldo, so, nbytes) = _layout(
+        _window_layouts, (q, k, vt, out, lse, q_len, k_len, q_start, workspace), _check_window)
+    _on_device(lib().track_op_attention_window, q, dtype, window.c(), B, H, Hk, D, Lq, Lk, q.data_ptr(), ldq, sq,
+               k.data_ptr(), ldk, sk, vt.data_ptr(), ldv, sv, out.data_ptr(), ldo, so,
+               *[0 if t is None else t.data_ptr() for t in (lse, q_len, k_len, q_start, workspace)], nbytes)
     return out
 
 
