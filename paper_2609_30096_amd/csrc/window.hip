@@ -150,6 +150,18 @@ struct WinMask {
   }
 };
 
+// 16 bytes a lane from the buffer at `off` to LDS, lanes side by side.  (A function of its own: in
+// a template, with arguments that depend on it, the host's pass rejects the builtin.)
+__device__ __forceinline__ void win_copy(__amdgpu_buffer_rsrc_t rs, uint8_t* lds, uint32_t off) {
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (att_lds_ptr_t)lds, 16, off, 0, 0, 0);
+}
+
+template <bool VEC>
+__device__ __forceinline__ f32x4 win_load4(const float* p) {
+  if constexpr (VEC) return *(const f32x4*)p;
+  else return f32x4{p[0], p[1], p[2], p[3]};
+}
+
 // Row block, share, key head and sequence of a workgroup.  Neighbouring row blocks go to one
 // XCD, whose L2 then serves their common keys: over the XCDs in turn, 12 heads 16384 x 16384
 // under a causal mask took 955 us instead of 824, 2 x 12 heads over a 21-frame video 5.2 ms
@@ -577,96 +589,38 @@ __global__ __launch_bounds__(256, 2) void window_rows_kernel(WinArgs a) {
 }
 
 // ---------------------------------------------------------------- float32
-// v_mfma_f32_16x16x4_f32 (float32 products and sums) on 16 rows a wave and 16 keys a step,
-// as the plain float32 attention: K and V^T go from memory to registers, the next step's
-// while this one's are multiplied.  With KS = 4 the workgroup's waves share one row block and
-// take a fourth of its keys each, with KS = 1 they take four row blocks.
-template <int D, int KS, bool VEC, bool SPLIT>
-__global__ __launch_bounds__(256) void window_f32_kernel(WinArgs a) {
-  static_assert(KS == 4 || !SPLIT, "shares of the keys");
-  constexpr int C = D / 16, BKV = 16;
-  __shared__ f32x4 so[KS == 4 ? 4 : 1][KS == 4 ? C : 1][64];
-  __shared__ float sm[4][16], sl[4][16];
-  auto load4 = [](const float* p) {
-    if constexpr (VEC) return *(const f32x4*)p;
-    else return f32x4{p[0], p[1], p[2], p[3]};
-  };
-  const int lane = threadIdx.x & 63;
-  const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
-  const int jq = lane & 15, g = lane >> 4;
-  int rb, sp, h, b;
-  win_place(a, rb, sp, h, b);
-  const WinSeq seq = win_seq(a, b);
-  const int rows = seq.qlen * a.n;
-  const int r0 = KS == 4 ? rb * 16 : (rb * 4 + wave) * 16;
-  if (r0 >= rows) return;  // the whole workgroup (KS = 4), or a wave that no barrier waits for
-
-  int lo0, hi0, lo1, hi1;
-  win_range(a, seq, (int)((uint32_t)r0 / (uint32_t)a.n), lo0, hi0);
-  win_range(a, seq, (int)((uint32_t)min(r0 + 15, rows - 1) / (uint32_t)a.n), lo1, hi1);
-  WinTiles tiles;
-  tiles.init<BKV>(seq, __builtin_amdgcn_readfirstlane(lo0), __builtin_amdgcn_readfirstlane(hi0),
-                  __builtin_amdgcn_readfirstlane(lo1), __builtin_amdgcn_readfirstlane(hi1));
-  int i0 = 0, i1 = tiles.n;
-  if (KS == 4) win_share(tiles.n, (SPLIT ? sp * 4 : 0) + wave, SPLIT ? 4 * a.nsplit : 4, i0, i1);
-
-  const int r = r0 + jq;
-  const uint32_t rr = (uint32_t)min(r, rows - 1), qi = rr / (uint32_t)a.n;
-  const int head = h * a.n + (int)(rr - qi * a.n);
-  int lo, hi;
-  win_range(a, seq, (int)qi, lo, hi);
-  if (tiles.sink == 0 && seq.sink >= lo1) lo = 0;
-  const float* qp = (const float*)a.q + b * a.sq + (int64_t)qi * a.ldq + (int64_t)head * D + 4 * g;
-  const float* kb = (const float*)a.k + b * a.sk + (int64_t)h * D + 4 * g;
-  const float* vb = (const float*)a.vt + b * a.sv + ((int64_t)h * D + jq) * a.ldv + 4 * g;
-  f32x4 qf[C], kf[C], vf[C], o[C];
-  // K row key0 + jq (the last key again past the end) and the V^T columns key0 + 4 g + 0..3,
-  // zero past the end
-  auto load_k = [&](int key0, f32x4 (&d)[C]) {
-    const float* p = kb + min(key0 + jq, seq.klen - 1) * a.ldk;
-#pragma unroll
-    for (int c = 0; c < C; ++c) d[c] = load4(p + 16 * c);
-  };
-  auto load_v = [&](int key0, f32x4 (&d)[C]) {
-    if (key0 + BKV <= seq.klen) {
-#pragma unroll
-      for (int c = 0; c < C; ++c) d[c] = load4(vb + 16 * c * a.ldv + key0);
-    } else {
-#pragma unroll
-      for (int c = 0; c < C; ++c)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) d[c][j] = key0 + 4 * g + j < seq.klen ? vb[16 * c * a.ldv + key0 + j] : 0.0f;
-    }
-  };
-#pragma unroll
-  for (int c = 0; c < C; ++c) {
-    qf[c] = load4(qp + 16 * c);
-    o[c] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-  }
-  float m = -INFINITY, l = 0.0f;  // reference (log2 units), the lane's part of the denominator
-  if (i0 < i1) {
-    load_k(tiles.key<BKV>(i0), kf);
-    load_v(tiles.key<BKV>(i0), vf);
-  }
-  for (int idx = i0; idx < i1; ++idx) {
-    const int key0 = tiles.key<BKV>(idx);
-    const bool edge = idx < tiles.edge;
-    f32x4 kn[C], vn[C];
-    const bool more = idx + 1 < i1;
-    if (more) {
-      const int k1 = tiles.key<BKV>(idx + 1);
-      load_k(k1, kn);
-      load_v(k1, vn);
-    }
+// One wave's 16 rows.  step() takes them against 16 keys with v_mfma_f32_16x16x4_f32 (float32
+// products and sums): lane (jq, g) has row jq, kfrag(c) is channels 16 c + 4 g .. + 3 of key jq,
+// vfrag(c) keys 4 g .. + 3 of channel 16 c + jq, and the logits that a lane holds (keys 4 g .. + 3
+// of its row) are the "B" operand of O^T += V^T P^T as they are.
+template <int D>
+struct WinF32 {
+  static constexpr int C = D / 16;
+  f32x4 qf[C], o[C];
+  float m, l;  // reference (log2 units), the lane's part of the denominator
+  int lo, hi, sink;
+  template <class KF, class VF>
+  __device__ __forceinline__ void step(KF kfrag, VF vfrag, bool edge, int key0, int klen, float scale_log2) {
+    const int lane = att_lane(), jq = lane & 15, g = lane >> 4;
     f32x4 s0 = {0.0f, 0.0f, 0.0f, 0.0f}, s1 = s0;
+    // fragments are read ahead of their products
+    constexpr int LA = C < 3 ? C : 3;
+    f32x4 kf[LA + 1];
+#pragma unroll
+    for (int c = 0; c < LA; ++c) kf[c] = kfrag(c);
 #pragma unroll
     for (int c = 0; c < C; ++c) {
-#pragma unroll
-      for (int i = 0; i < 4; i += 2) {
-        s0 = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[c][i], qf[c][i], s0, 0, 0, 0);
-        s1 = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[c][i + 1], qf[c][i + 1], s1, 0, 0, 0);
-      }
+      if (c + LA < C) kf[(c + LA) % (LA + 1)] = kfrag(c + LA);
+      __builtin_amdgcn_sched_barrier(0);
+      const f32x4 k = kf[c % (LA + 1)];
+      s0 = __builtin_amdgcn_mfma_f32_16x16x4f32(k[0], qf[c][0], s0, 0, 0, 0);
+      s1 = __builtin_amdgcn_mfma_f32_16x16x4f32(k[1], qf[c][1], s1, 0, 0, 0);
+      s0 = __builtin_amdgcn_mfma_f32_16x16x4f32(k[2], qf[c][2], s0, 0, 0, 0);
+      s1 = __builtin_amdgcn_mfma_f32_16x16x4f32(k[3], qf[c][3], s1, 0, 0, 0);
     }
+    f32x4 vf[C];
+#pragma unroll
+    for (int c = 0; c < C; ++c) vf[c] = vfrag(c);
     float x[4];
 #pragma unroll
     for (int e = 0; e < 4; ++e) x[e] = s0[e] + s1[e];
@@ -674,11 +628,11 @@ __global__ __launch_bounds__(256) void window_f32_kernel(WinArgs a) {
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         const int key = key0 + 4 * g + e;
-        x[e] = (key > hi) | ((key < lo) & (key >= tiles.sink)) ? -INFINITY : x[e];
+        x[e] = (key > hi) | ((key < lo) & (key >= sink)) ? -INFINITY : x[e];
       }
     }
     const float t = fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3]));
-    const float mn = fmaxf(m, group_max2(t, t) * a.scale_log2);
+    const float mn = fmaxf(m, group_max2(t, t) * scale_log2);
     if (__ballot(mn > m)) {
       const float alpha = mn == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m - mn);
       l *= alpha;
@@ -690,36 +644,277 @@ __global__ __launch_bounds__(256) void window_f32_kernel(WinArgs a) {
     }
     const float nm = m == -INFINITY ? 0.0f : -m;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) x[e] = __builtin_amdgcn_exp2f(fmaf(x[e], a.scale_log2, nm));
+    for (int e = 0; e < 4; ++e) x[e] = __builtin_amdgcn_exp2f(fmaf(x[e], scale_log2, nm));
     l += (x[0] + x[1]) + (x[2] + x[3]);
-    bool weigh = false;  // key by key where V is not finite and may be hidden from some row
     if (edge) {
+      // V past the last key is cleared, and what else is not finite and may be hidden from some
+      // row is weighed key by key
       float z = 0.0f;
 #pragma unroll
       for (int c = 0; c < C; ++c)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) z = fmaf(vf[c][e], 0.0f, z);
-      weigh = __ballot(z != 0.0f) != 0;
-    }
-    if (weigh) {
-#pragma unroll
-      for (int e = 0; e < 4; ++e)
-        for (int gg = 0; gg < 4; ++gg) {
-          const float p = __shfl(x[e], jq + 16 * gg);
-#pragma unroll
-          for (int c = 0; c < C; ++c)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              const float v = __shfl(vf[c][e], 4 * g + i + 16 * gg);
-              o[c][i] = p != 0.0f ? fmaf(p, v, o[c][i]) : o[c][i];
-            }
+        for (int e = 0; e < 4; ++e) {
+          vf[c][e] = key0 + 4 * g + e < klen ? vf[c][e] : 0.0f;
+          z = fmaf(vf[c][e], 0.0f, z);
         }
+      if (__ballot(z != 0.0f)) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+#pragma unroll 1
+          for (int gg = 0; gg < 4; ++gg) {
+            const float p = __shfl(x[e], jq + 16 * gg);
+#pragma unroll
+            for (int c = 0; c < C; ++c)
+#pragma unroll
+              for (int i = 0; i < 4; ++i) {
+                const float v = __shfl(vf[c][e], 4 * g + i + 16 * gg);
+                o[c][i] = p != 0.0f ? fmaf(p, v, o[c][i]) : o[c][i];
+              }
+          }
+        return;
+      }
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+#pragma unroll
+      for (int c = 0; c < C; ++c) o[c] = __builtin_amdgcn_mfma_f32_16x16x4f32(vf[c][e], x[e], o[c], 0, 0, 0);
+  }
+  // the lane's row of `rows`: window, query, nothing summed yet
+  template <bool VEC>
+  __device__ __forceinline__ void begin(const WinArgs& a, const WinSeq& seq, const WinTiles& tiles, int lo1, int h, int r,
+                                        int rows) {
+    const int g = (int)(threadIdx.x & 63) >> 4;
+    const uint32_t rr = (uint32_t)min(r, rows - 1), qi = rr / (uint32_t)a.n;
+    win_range(a, seq, (int)qi, lo, hi);
+    if (tiles.sink == 0 && seq.sink >= lo1) lo = 0;
+    sink = tiles.sink;
+    const float* qp = (const float*)a.q + seq.b * a.sq + (int64_t)qi * a.ldq + (int64_t)(h * a.n + (rr - qi * a.n)) * D + 4 * g;
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      qf[c] = win_load4<VEC>(qp + 16 * c);
+      o[c] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    }
+    m = -INFINITY;
+    l = 0.0f;
+  }
+  // The sums of each four waves, which have the same rows, joined and stored, through LDS of
+  // so[waves][C][64] and sml[waves][2][16].
+  template <bool VEC, bool SPLIT>
+  __device__ __forceinline__ void end(const WinArgs& a, int b, int h, int sp, int r, int rows, f32x4* so, float* sml) {
+    const int lane = (int)(threadIdx.x & 63), jq = lane & 15, g = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), w0 = wave & ~3;
+    l += __shfl_xor(l, 16);
+    l += __shfl_xor(l, 32);
+#pragma unroll
+    for (int c = 0; c < C; ++c) so[(wave * C + c) * 64 + lane] = o[c];
+    if (g == 0) {
+      sml[wave * 32 + jq] = m;
+      sml[wave * 32 + 16 + jq] = l;
+    }
+    __syncthreads();
+    float mx = -INFINITY, sum = 0.0f, wt[4];
+#pragma unroll
+    for (int w = 0; w < 4; ++w) mx = fmaxf(mx, sml[(w0 + w) * 32 + jq]);
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      const float mi = sml[(w0 + w) * 32 + jq];
+      wt[w] = mi == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(mi - mx);  // a wave without keys
+      sum = fmaf(wt[w], sml[(w0 + w) * 32 + 16 + jq], sum);
+    }
+    if (r >= rows) return;
+    const int qi = (int)((uint32_t)r / (uint32_t)a.n), head = h * a.n + (r - qi * a.n);
+    const int64_t pr = ((((int64_t)sp * a.B + b) * a.Hk + h) * a.Lq) * a.n + r;
+    const float inv = SPLIT ? 1.0f : win_inverse(sum);
+    float* const op = SPLIT ? a.po + pr * D + 4 * g
+                            : (float*)a.out + b * a.so + (int64_t)qi * a.ldo + (int64_t)head * D + 4 * g;
+    for (int c = wave - w0; c < C; c += 4) {
+      f32x4 v = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        const f32x4 u = so[((w0 + w) * C + c) * 64 + lane];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = fmaf(wt[w], u[e], v[e]);
+      }
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] *= inv;
+      if constexpr (VEC || SPLIT) {
+        *(f32x4*)(op + 16 * c) = v;
+      } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) op[16 * c + e] = v[e];
+      }
+    }
+    if (wave == w0 && g == 0) {
+      if constexpr (SPLIT) a.pml[pr] = float2{mx, sum};
+      else if (a.lse) a.lse[((int64_t)b * a.Hk * a.n + head) * a.Lq + qi] = win_lse(mx, sum);
+    }
+  }
+};
+
+// Many rows: 32 a workgroup of 8 waves, K and V^T tiles of 64 keys by DMA into a ring of two
+// slots in LDS.  Four waves have the same 16 rows and 16 keys of a tile each.  LDS rows keep
+// 16-byte units at unit ^ (row & 7), so that the 16 rows of a fragment meet no bank twice in a
+// phase.  What bounds it: the matrix cores (135 - 149 TFLOP/s sustained on this instruction) at
+// 87 - 92 TFLOP/s, the rest a tile's softmax and barrier.  2 x 8 heads, 1500 x 1500: 105 us at 64
+// channels (140 straight from memory), 215 at 128 (303); 8 heads of 64, 1501 queries on 304 keys
+// each 26.3 us (32.5).  With 4 waves instead of 8: 123 and 324 us; with four row groups of 16
+// rows, each wave all keys of a tile: 124 and 219, and twice as long where few rows are there.
+constexpr int WIN_F32_WAVES = 8, WIN_F32_ROWS = 32;
+template <int D, bool SPLIT>
+__global__ __launch_bounds__(64 * WIN_F32_WAVES) void window_f32_tiles_kernel(WinArgs a) {
+  constexpr int C = D / 16, W = WIN_F32_WAVES, TK = 64;
+  constexpr int KU = D / 4, VU = TK / 4;                   // 16-byte units of a K row, of a V^T row
+  constexpr int HALF = TK * D * 4, SLOT = 2 * HALF;
+  constexpr int NI = HALF / 1024 / W;                      // copies of 1 KB a wave, of K and of V^T
+  constexpr int SO = W * C * 1024, LDS = 2 * SLOT > SO + W * 128 ? 2 * SLOT : SO + W * 128;
+  // one object: with a second one the compiler waits for every copy under way before a tile's
+  // first fragment read
+  __shared__ __attribute__((aligned(1024))) uint8_t smem[LDS];
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+  const int jq = lane & 15, g = lane >> 4;
+  int rb, sp, h, b;
+  win_place(a, rb, sp, h, b);
+  const WinSeq seq = win_seq(a, b);
+  const int rows = seq.qlen * a.n;
+  const int r0 = rb * WIN_F32_ROWS;
+  if (r0 >= rows) return;  // the whole workgroup
+  auto range_of = [&](int r, int& lo, int& hi) {
+    win_range(a, seq, (int)((uint32_t)min(r, rows - 1) / (uint32_t)a.n), lo, hi);
+    lo = __builtin_amdgcn_readfirstlane(lo);
+    hi = __builtin_amdgcn_readfirstlane(hi);
+  };
+  int lo0, hi0, lo1, hi1;
+  range_of(r0, lo0, hi0);
+  range_of(r0 + WIN_F32_ROWS - 1, lo1, hi1);
+  WinTiles tiles;
+  tiles.init<TK>(seq, lo0, hi0, lo1, hi1);
+  int i0 = 0, i1 = tiles.n;
+  if (SPLIT) win_share(tiles.n, sp, a.nsplit, i0, i1);
+  const int wr0 = r0 + 16 * (wave >> 2), mine = 16 * (wave & 3);  // first row, first key of a tile
+  int wlo, whi, unused;
+  range_of(wr0, wlo, unused);
+  range_of(wr0 + 15, unused, whi);
+  if (tiles.sink == 0 && seq.sink >= lo1) wlo = 0;
+  const bool live = wr0 < rows;
+
+  const float* const kbase = (const float*)a.k + b * a.sk + (int64_t)h * D;
+  const float* const vbase = (const float*)a.vt + b * a.sv + (int64_t)h * D * a.ldv;
+  uint32_t koff[NI], voff[NI];
+#pragma unroll
+  for (int i = 0; i < NI; ++i) {
+    const int at = (wave * NI + i) * 64 + lane;
+    const int kr = at / KU, vr = at / VU;
+    koff[i] = (uint32_t)(kr * a.ldk * 4 + ((at % KU) ^ (kr & 7)) * 16);
+    voff[i] = (uint32_t)(vr * a.ldv * 4 + ((at % VU) ^ (vr & 7)) * 16);
+  }
+  // the tile at key0 into the slot at byte `slot`: K rows past the last key read as zero, V^T
+  // columns past the row's end as the next row's (step() clears them) or zero
+  auto issue = [&](int key0, int slot) {
+    const __amdgpu_buffer_rsrc_t rsK = __builtin_amdgcn_make_buffer_rsrc(
+        (void*)(kbase + key0 * a.ldk), (short)0, (int)(uint32_t)(min(TK, seq.klen - key0) * a.ldk * 4), 0x00020000);
+    const __amdgpu_buffer_rsrc_t rsV = __builtin_amdgcn_make_buffer_rsrc(
+        (void*)(vbase + key0), (short)0, (int)(uint32_t)((D * a.ldv - key0) * 4), 0x00020000);
+#pragma unroll
+    for (int i = 0; i < NI; ++i)
+      win_copy(rsK, smem + slot + (wave * NI + i) * 1024, koff[i]);
+#pragma unroll
+    for (int i = 0; i < NI; ++i)
+      win_copy(rsV, smem + slot + HALF + (wave * NI + i) * 1024, voff[i]);
+  };
+  auto barrier = [&]() {
+    att_wait_vmcnt<0>();
+    __builtin_amdgcn_s_waitcnt((15 << 0) | (3 << 14) | (7 << 4) | (0 << 8));  // lgkmcnt(0)
+    __builtin_amdgcn_s_barrier();
+  };
+
+  WinF32<D> st;
+  st.template begin<true>(a, seq, tiles, lo1, h, wr0 + jq, rows);
+  if (i0 < i1) {
+    issue(tiles.key<TK>(i0), 0);
+    barrier();
+    int slot = 0;
+    for (int idx = i0; idx < i1; ++idx, slot ^= SLOT) {
+      const int key0 = tiles.key<TK>(idx);
+      if (idx + 1 < i1) issue(tiles.key<TK>(idx + 1), slot ^ SLOT);
+      const bool edge = idx < tiles.edge;
+      const int k0 = key0 + mine;
+      if (live && (!edge || (k0 <= whi && (k0 + 16 > wlo || k0 < tiles.sink)))) {
+        const uint8_t* const kt = smem + slot + (mine + jq) * (D * 4);
+        const uint8_t* const vt = smem + slot + HALF + jq * (TK * 4) + ((((mine >> 2) + g) ^ (jq & 7)) << 4);
+        st.step([&](int c) { return *(const f32x4*)(kt + (((4 * c + g) ^ (jq & 7)) << 4)); },
+                [&](int c) { return *(const f32x4*)(vt + 16 * c * (TK * 4)); }, edge, k0, seq.klen, a.scale_log2);
+      }
+      barrier();
+    }
+  }
+  st.template end<true, SPLIT>(a, b, h, sp, wr0 + jq, rows, (f32x4*)smem, (float*)(smem + SO));
+}
+
+// Straight from memory: few rows or keys, and rows that are not 16-byte aligned (VEC false:
+// loads of single elements).  The four waves share a row
+// block and take a fourth of its keys each, 16 a step, the next step's under way.
+template <int D, bool VEC, bool SPLIT>
+__global__ __launch_bounds__(256) void window_f32_kernel(WinArgs a) {
+  constexpr int C = D / 16, BKV = 16;
+  __shared__ f32x4 so[4 * C * 64];
+  __shared__ float sml[4 * 32];
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+  const int jq = lane & 15, g = lane >> 4;
+  int rb, sp, h, b;
+  win_place(a, rb, sp, h, b);
+  const WinSeq seq = win_seq(a, b);
+  const int rows = seq.qlen * a.n;
+  const int r0 = rb * 16;
+  if (r0 >= rows) return;  // the whole workgroup
+
+  int lo0, hi0, lo1, hi1;
+  win_range(a, seq, (int)((uint32_t)r0 / (uint32_t)a.n), lo0, hi0);
+  win_range(a, seq, (int)((uint32_t)min(r0 + 15, rows - 1) / (uint32_t)a.n), lo1, hi1);
+  WinTiles tiles;
+  tiles.init<BKV>(seq, __builtin_amdgcn_readfirstlane(lo0), __builtin_amdgcn_readfirstlane(hi0),
+                  __builtin_amdgcn_readfirstlane(lo1), __builtin_amdgcn_readfirstlane(hi1));
+  int i0, i1;
+  win_share(tiles.n, (SPLIT ? sp * 4 : 0) + wave, SPLIT ? 4 * a.nsplit : 4, i0, i1);
+  WinF32<D> st;
+  st.template begin<VEC>(a, seq, tiles, lo1, h, r0 + jq, rows);
+
+  const float* kb = (const float*)a.k + b * a.sk + (int64_t)h * D + 4 * g;
+  const float* vb = (const float*)a.vt + b * a.sv + ((int64_t)h * D + jq) * a.ldv + 4 * g;
+  f32x4 kf[C], vf[C];
+  // K row key0 + jq (the last key again past the end) and the V^T columns key0 + 4 g + 0..3,
+  // zero past the end
+  auto load_k = [&](int key0, f32x4 (&d)[C]) {
+    const float* p = kb + min(key0 + jq, seq.klen - 1) * a.ldk;
+#pragma unroll
+    for (int c = 0; c < C; ++c) d[c] = win_load4<VEC>(p + 16 * c);
+  };
+  auto load_v = [&](int key0, f32x4 (&d)[C]) {
+    if (key0 + BKV <= seq.klen) {
+#pragma unroll
+      for (int c = 0; c < C; ++c) d[c] = win_load4<VEC>(vb + 16 * c * a.ldv + key0);
     } else {
 #pragma unroll
-      for (int e = 0; e < 4; ++e)
+      for (int c = 0; c < C; ++c)
 #pragma unroll
-        for (int c = 0; c < C; ++c) o[c] = __builtin_amdgcn_mfma_f32_16x16x4f32(vf[c][e], x[e], o[c], 0, 0, 0);
+        for (int j = 0; j < 4; ++j) d[c][j] = key0 + 4 * g + j < seq.klen ? vb[16 * c * a.ldv + key0 + j] : 0.0f;
     }
+  };
+  if (i0 < i1) {
+    load_k(tiles.key<BKV>(i0), kf);
+    load_v(tiles.key<BKV>(i0), vf);
+  }
+  for (int idx = i0; idx < i1; ++idx) {
+    f32x4 kn[C], vn[C];
+    const bool more = idx + 1 < i1;
+    if (more) {
+      const int k1 = tiles.key<BKV>(idx + 1);
+      load_k(k1, kn);
+      load_v(k1, vn);
+    }
+    st.step([&](int c) { return kf[c]; }, [&](int c) { return vf[c]; }, idx < tiles.edge, tiles.key<BKV>(idx), seq.klen,
+            a.scale_log2);
     if (more) {
 #pragma unroll
       for (int c = 0; c < C; ++c) {
@@ -728,60 +923,7 @@ __global__ __launch_bounds__(256) void window_f32_kernel(WinArgs a) {
       }
     }
   }
-  l += __shfl_xor(l, 16);
-  l += __shfl_xor(l, 32);
-  float* op = (float*)a.out + b * a.so + (int64_t)qi * a.ldo + (int64_t)head * D + 4 * g;
-  auto store = [&](int c, const f32x4& v) {
-    if (r >= rows) return;
-    if constexpr (VEC) {
-      *(f32x4*)(op + 16 * c) = v;
-    } else {
-#pragma unroll
-      for (int e = 0; e < 4; ++e) op[16 * c + e] = v[e];
-    }
-  };
-  float* const lse = a.lse && g == 0 && r < rows ? a.lse + ((int64_t)b * a.Hk * a.n + head) * a.Lq + qi : nullptr;
-  if constexpr (KS == 1) {
-    const float inv = win_inverse(l);
-#pragma unroll
-    for (int c = 0; c < C; ++c) store(c, f32x4{o[c][0] * inv, o[c][1] * inv, o[c][2] * inv, o[c][3] * inv});
-    if (lse) *lse = win_lse(m, l);
-  } else {
-#pragma unroll
-    for (int c = 0; c < C; ++c) so[wave][c][lane] = o[c];
-    if (g == 0) {
-      sm[wave][jq] = m;
-      sl[wave][jq] = l;
-    }
-    __syncthreads();
-    const float mx = fmaxf(fmaxf(sm[0][jq], sm[1][jq]), fmaxf(sm[2][jq], sm[3][jq]));
-    float wt[4], sum = 0.0f;
-#pragma unroll
-    for (int w = 0; w < 4; ++w) {
-      wt[w] = sm[w][jq] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(sm[w][jq] - mx);  // a wave without keys
-      sum = fmaf(wt[w], sl[w][jq], sum);
-    }
-    const float inv = win_inverse(sum);
-    const int64_t pr = ((((int64_t)sp * a.B + b) * a.Hk + h) * a.Lq) * a.n + r;
-    for (int c = wave; c < C; c += 4) {
-      f32x4 v = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-      for (int w = 0; w < 4; ++w) {
-        const f32x4 u = so[w][c][lane];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = fmaf(wt[w], u[e], v[e]);
-      }
-      if constexpr (SPLIT) {
-        if (r < rows) *(f32x4*)(a.po + pr * D + 16 * c + 4 * g) = v;
-      } else {
-        store(c, f32x4{v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv});
-      }
-    }
-    if (wave == 0 && g == 0 && r < rows) {
-      if constexpr (SPLIT) a.pml[pr] = float2{mx, sum};
-      else if (lse) *lse = win_lse(mx, sum);
-    }
-  }
+  st.template end<VEC, SPLIT>(a, b, h, sp, r0 + jq, rows, so, sml);
 }
 
 // The shares of each row joined: D / 4 threads a row and G groups of them, each with every
@@ -841,7 +983,7 @@ __global__ __launch_bounds__(256) void window_join_kernel(WinArgs a, int D) {
 
 // ---------------------------------------------------------------- host
 struct WinPlan {
-  enum Form { BLOCKS, ROWS, F32_SHARED, F32_APART } form;
+  enum Form { BLOCKS, ROWS, F32_ROWS, F32_TILES } form;
   int64_t nrb;
   int nsplit;
 };
@@ -886,20 +1028,19 @@ static int blocks_split(int64_t tiles, int64_t blocks, int64_t rows, int64_t cus
   return best;
 }
 
-static WinPlan win_plan(int dtype, const track_window& w, int64_t B, int Hk, int n, int64_t Lq, int64_t Lk) {
+static WinPlan win_plan(int dtype, const track_window& w, int64_t B, int Hk, int n, int64_t Lq, int64_t Lk, bool vec) {
   const int64_t rows = Lq * n, cus = device_cus();
   WinPlan p;
   if (dtype == TRACK_DTYPE_F32) {
+    // the tiles kernel from 12000 steps of 16 rows and 16 keys on (8 heads of 64: 300 x 300,
+    // 2900 steps, 11.8 us straight and 12.7 by tiles; 1501 x 304, 15000, 32.5 and 26.3; 1000 x
+    // 1000, 31000, 31.3 and 30.4), shares of the keys up to two workgroups a CU
     p.nrb = (rows + 15) / 16;
-    if (p.nrb * Hk * B >= 4 * cus) {
-      p.form = WinPlan::F32_APART;
-      p.nrb = (p.nrb + 3) / 4;
-      p.nsplit = 1;
-      return p;
-    }
-    p.form = WinPlan::F32_SHARED;
-    const int64_t steps = (win_span(w, 16, n, Lk) + 15) / 16;
-    p.nsplit = (int)std::max<int64_t>(1, std::min<int64_t>(2 * cus / (p.nrb * Hk * B), steps / 32));
+    const int64_t steps = (win_span(w, std::min<int64_t>(rows, 16), n, Lk) + 15) / 16;
+    p.form = vec && p.nrb * Hk * B * steps >= 12000 && rows > 16 ? WinPlan::F32_TILES : WinPlan::F32_ROWS;
+    if (p.form == WinPlan::F32_TILES) p.nrb = (rows + WIN_F32_ROWS - 1) / WIN_F32_ROWS;
+    const int64_t most = p.form == WinPlan::F32_TILES ? steps / 16 : steps / 32;
+    p.nsplit = (int)std::max<int64_t>(1, std::min<int64_t>(2 * cus / (p.nrb * Hk * B), most));
     return p;
   }
   if (rows <= 16) {
@@ -940,7 +1081,10 @@ static track_status win_check(int dtype, const track_window* w, int B, int H, in
 int64_t attention_window_bytes(int dtype, const track_window* w, int B, int H, int Hk, int D, int64_t Lq, int64_t Lk) {
   if (win_check(dtype, w, B, H, Hk, D, Lq, Lk) != TRACK_OK) return -1;
   if (B == 0 || Lq == 0) return 0;
-  return (int64_t)win_bytes(win_plan(dtype, *w, B, Hk, H / Hk, Lq, Lk), B, Hk, H / Hk, D, Lq);
+  size_t bytes = 0;
+  for (bool vec : {true, false})  // whatever the rows' alignment turns out to be
+    bytes = std::max(bytes, win_bytes(win_plan(dtype, *w, B, Hk, H / Hk, Lq, Lk, vec), B, Hk, H / Hk, D, Lq));
+  return (int64_t)bytes;
 }
 
 track_status attention_window(int dtype, const track_window* w, int B, int H, int Hk, int D, int64_t Lq, int64_t Lk,
@@ -959,8 +1103,9 @@ track_status attention_window(int dtype, const track_window* w, int B, int H, in
     return fail(TRACK_E_SHAPE, "attention_window: sequences overlap in out, or a negative stride");
   if (((uintptr_t)lse | (uintptr_t)q_len | (uintptr_t)k_len | (uintptr_t)q_start) & 3)
     return fail(TRACK_E_INVALID, "attention_window: lse and lengths need 4-byte alignment");
-  if (ldk > ((int64_t)1 << 23) || ldv > ((int64_t)1 << 23))
-    return fail(TRACK_E_SHAPE, "attention_window: ldk and ldv are at most 2^23");
+  // (offsets inside a tile and a head's V^T are 32 bits)
+  if (ldk > ((int64_t)1 << 22) || ldv > ((int64_t)1 << 22))
+    return fail(TRACK_E_SHAPE, "attention_window: ldk and ldv are at most 2^22");
   const uintptr_t ptrs = (uintptr_t)q | (uintptr_t)k | (uintptr_t)vt | (uintptr_t)out;
   const int64_t strides = ldq | ldk | ldv | ldo | (B > 1 ? sq | sk | sv | so : 0);
   bool vec = true;
@@ -970,7 +1115,7 @@ track_status attention_window(int dtype, const track_window* w, int B, int H, in
     if (ptrs & 3) return fail(TRACK_E_INVALID, "attention_window: float32 path needs 4-byte aligned rows");
     vec = !(ptrs & 15) && !(strides & 3);
   }
-  const WinPlan p = win_plan(dtype, *w, B, Hk, n, Lq, Lk);
+  const WinPlan p = win_plan(dtype, *w, B, Hk, n, Lq, Lk, vec);
   const size_t need = win_bytes(p, B, Hk, n, D, Lq);
   if (need && (!ws || ws_bytes < need)) return fail(TRACK_E_NOMEM, "attention_window: workspace of %zu bytes needed", need);
   if (need && ((uintptr_t)ws & 255)) return fail(TRACK_E_INVALID, "attention_window: workspace must be 256-byte aligned");
@@ -990,16 +1135,16 @@ track_status attention_window(int dtype, const track_window* w, int B, int H, in
   const bool split = p.nsplit > 1, log2q = a.scale_log2 == 1.0f;
   ProfScope prof(TRACK_PROF_ATTN_SELF, s);
   const unsigned gr = (unsigned)grid;
-#define TRACK_WIN_F32_K(DH, KS, SPLIT)                                             \
-  do {                                                                             \
-    if (vec) window_f32_kernel<DH, KS, true, SPLIT><<<gr, 256, 0, s>>>(a);         \
-    else window_f32_kernel<DH, KS, false, SPLIT><<<gr, 256, 0, s>>>(a);            \
-  } while (0)
-#define TRACK_WIN_F32(DH)                                                          \
-  do {                                                                             \
-    if (p.form == WinPlan::F32_APART) TRACK_WIN_F32_K(DH, 1, false);               \
-    else if (split) TRACK_WIN_F32_K(DH, 4, true);                                  \
-    else TRACK_WIN_F32_K(DH, 4, false);                                            \
+#define TRACK_WIN_F32(DH)                                                                             \
+  do {                                                                                                \
+    if (p.form == WinPlan::F32_TILES && split)                                                        \
+      window_f32_tiles_kernel<DH, true><<<gr, 64 * WIN_F32_WAVES, 0, s>>>(a);                         \
+    else if (p.form == WinPlan::F32_TILES)                                                            \
+      window_f32_tiles_kernel<DH, false><<<gr, 64 * WIN_F32_WAVES, 0, s>>>(a);                        \
+    else if (vec && split) window_f32_kernel<DH, true, true><<<gr, 256, 0, s>>>(a);                   \
+    else if (vec) window_f32_kernel<DH, true, false><<<gr, 256, 0, s>>>(a);                           \
+    else if (split) window_f32_kernel<DH, false, true><<<gr, 256, 0, s>>>(a);                         \
+    else window_f32_kernel<DH, false, false><<<gr, 256, 0, s>>>(a);                                   \
   } while (0)
   switch (p.form) {
     case WinPlan::BLOCKS:
@@ -1018,7 +1163,6 @@ track_status attention_window(int dtype, const track_window* w, int B, int H, in
       else TRACK_WIN_F32(128);
   }
 #undef TRACK_WIN_F32
-#undef TRACK_WIN_F32_K
   TRACK_LAUNCH_CHECK();
   if (split) {
     // groups of shares while the rows alone do not fill the chip
