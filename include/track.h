@@ -431,7 +431,7 @@ int64_t track_attention_window_workspace_bytes(int32_t dtype, const track_window
  * bfloat16: head_dim 128, 16-byte aligned rows (bases, and strides in multiples
  * of 8); probabilities are rounded to bfloat16 for the product with V, their
  * sum is that of the rounded ones.  float32: head_dim 32, 64, 128.
- * ldk, ldv <= 2^22; lengths, window limits <= 2^30.  workspace: 256-byte
+ * ldk, ldv <= 2^22; lengths, window limits <= 2^28 (q_start is cut to that range).  workspace: 256-byte
  * aligned; calls that may overlap on the GPU need one each.  B == 0 or Lq == 0
  * is a no-op; Lk == 0 gives zeros.  Asynchronous. */
 track_status track_op_attention_window(int32_t dtype, const track_window* window, int32_t B, int32_t H, int32_t Hk,

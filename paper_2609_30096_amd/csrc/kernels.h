@@ -50,7 +50,7 @@ track_status attention_f32_vrows(int B, int H, int head_dim, int64_t Lq, int64_t
 float attn_log2_scale(int head_dim);
 
 // window.hip (track_op_attention_window)
-constexpr int64_t WIN_MAX = (int64_t)1 << 30;  // largest length and window limit
+constexpr int64_t WIN_MAX = (int64_t)1 << 28;  // largest length, position and window limit
 // Workspace of attention_window, -1 for what it refuses.
 int64_t attention_window_bytes(int dtype, const track_window* w, int B, int H, int Hk, int D, int64_t Lq, int64_t Lk);
 track_status attention_window(int dtype, const track_window* w, int B, int H, int Hk, int D, int64_t Lq, int64_t Lk,

@@ -25,6 +25,22 @@
 
 namespace track {
 
+// Division by a number that the host knows, for dividends below 2^31: with s = ceil(log2 d) and
+// m = ceil(2^(31 + s) / d) < 2^32, floor(x m / 2^(31 + s)) = floor(x / d), since m d exceeds
+// 2^(31 + s) by less than d <= 2^s (a hardware division is some 30 instructions, and the limits
+// of a block's, a wave's and a lane's rows take a dozen: 1 - 2 us of a single token's call).
+struct WinDiv {
+  uint32_t d, m, s;
+  __device__ __forceinline__ uint32_t operator()(uint32_t x) const { return d == 1 ? x : __umulhi(x, m) >> s; }
+};
+
+static WinDiv win_div(int64_t d) {
+  uint32_t s = 0;
+  while (((int64_t)1 << s) < d) ++s;
+  if (d == 1) return WinDiv{1, 0, 0};
+  return WinDiv{(uint32_t)d, (uint32_t)((((uint64_t)1 << (31 + s)) + (uint64_t)d - 1) / (uint64_t)d), s - 1};
+}
+
 // One call's arguments as the kernels take them.
 struct WinArgs {
   const void *q, *k, *vt;
@@ -32,21 +48,24 @@ struct WinArgs {
   int64_t ldq, sq, ldk, sk, ldv, sv, ldo, so;
   float* lse;
   const int32_t *q_len, *k_len, *q_start;
-  int64_t left, right;  // groups; negative: no limit
-  uint32_t group;
+  // limits in tokens: from a group's first key back, and on to the first key past them (2^31 - 1:
+  // no limit; all else is below 2^30)
+  int before, past;
+  int lift;           // multiple of the group that makes every position positive
   int sink;
-  int B, Hk, n;  // sequences, key heads, query heads of each
+  int B, Hk, n;       // sequences, key heads, query heads of each
   int Lq, Lk;
-  int nrb, nsplit;  // row blocks, shares of the keys
+  int nrb, nsplit;    // row blocks, shares of the keys
+  WinDiv by_group, by_n, by_nrb, by_nsplit, by_Hk;
   float scale_log2;
-  float* po;   // [nsplit][B][Hk][Lq n][D]: a share's sums
-  float2* pml;  // [nsplit][B][Hk][Lq n]: its reference (log2 units) and its denominator
+  float* po;          // [nsplit][B][Hk][Lq n][D]: a share's sums
+  float2* pml;        // [nsplit][B][Hk][Lq n]: its reference (log2 units) and its denominator
 };
 
 // One sequence of the batch, in wave-uniform registers.
 struct WinSeq {
   int b, qlen, klen, sink;
-  int64_t start;  // position of its first query
+  int start;  // position of its first query
 };
 
 __device__ __forceinline__ WinSeq win_seq(const WinArgs& a, int b) {
@@ -55,19 +74,24 @@ __device__ __forceinline__ WinSeq win_seq(const WinArgs& a, int b) {
   // lengths from device memory are cut to the buffers
   s.qlen = a.q_len ? __builtin_amdgcn_readfirstlane(max(0, min(a.q_len[b], a.Lq))) : a.Lq;
   s.klen = a.k_len ? __builtin_amdgcn_readfirstlane(max(0, min(a.k_len[b], a.Lk))) : a.Lk;
-  s.start = a.q_start ? __builtin_amdgcn_readfirstlane(a.q_start[b]) : s.klen - s.qlen;
+  s.start = a.q_start ? __builtin_amdgcn_readfirstlane(max(-(int)WIN_MAX, min(a.q_start[b], (int)WIN_MAX))) : s.klen - s.qlen;
   s.sink = min(a.sink, s.klen);
   return s;
 }
 
 // The window [lo, hi] of query i, cut to [0, klen) (lo = klen or hi = -1: nothing left).
 __device__ __forceinline__ void win_range(const WinArgs& a, const WinSeq& s, int i, int& lo, int& hi) {
-  const int64_t p = s.start + i, G = a.group;
-  int64_t g = p;
-  if (a.group != 1)  // floor; -2^31 <= p < 2^32
-    g = p >= 0 ? (int64_t)((uint32_t)p / a.group) : ~(int64_t)((uint32_t)~p / a.group);
-  hi = a.right < 0 ? s.klen - 1 : (int)max((int64_t)-1, min((g + a.right + 1) * G - 1, (int64_t)s.klen - 1));
-  lo = a.left < 0 ? 0 : (int)max((int64_t)0, min((g - a.left) * G, (int64_t)s.klen));
+  const uint32_t p = (uint32_t)(s.start + i + a.lift);  // in [0, 2^30 + 2^28)
+  const int first = (int)(a.by_group(p) * a.by_group.d) - a.lift;  // of the query's group
+  lo = first > a.before ? min(first - a.before, s.klen) : 0;
+  hi = a.past - 1 < s.klen - 1 - first ? max(first + a.past - 1, -1) : s.klen - 1;
+}
+
+// Query of row r, and the row's head among those of its key head.
+__device__ __forceinline__ int win_query(const WinArgs& a, int r, int& e) {
+  const int i = (int)a.by_n((uint32_t)r);
+  e = r - i * a.n;
+  return i;
 }
 
 // The tiles of TK keys that rows with windows from [lo0, hi0] (the first row's) to [lo1, hi1]
@@ -168,18 +192,12 @@ __device__ __forceinline__ f32x4 win_load4(const float* p) {
 // instead of 4.8.  The last rows of a sequence, which see most keys under a causal mask, start
 // first.
 __device__ __forceinline__ void win_place(const WinArgs& a, int& rb, int& sp, int& h, int& b) {
-  uint32_t id = (uint32_t)xcd_remap((int)blockIdx.x, (int)gridDim.x);
-  uint32_t t = id / (uint32_t)a.nrb;
+  const uint32_t id = (uint32_t)xcd_remap((int)blockIdx.x, (int)gridDim.x);
+  const uint32_t t = a.by_nrb(id), u = a.by_nsplit(t), v = a.by_Hk(u);
   rb = a.nrb - 1 - (int)(id - t * a.nrb);
-  id = t;
-  t = id / (uint32_t)a.nsplit;
-  sp = (int)(id - t * a.nsplit);
-  b = (int)(t / (uint32_t)a.Hk);
-  h = (int)(t - b * a.Hk);
-  rb = __builtin_amdgcn_readfirstlane(rb);
-  sp = __builtin_amdgcn_readfirstlane(sp);
-  h = __builtin_amdgcn_readfirstlane(h);
-  b = __builtin_amdgcn_readfirstlane(b);
+  sp = (int)(t - u * a.nsplit);
+  h = (int)(u - v * a.Hk);
+  b = (int)v;
 }
 
 // ---------------------------------------------------------------- many rows, bfloat16
@@ -206,7 +224,7 @@ __global__ __launch_bounds__(512) void window_blocks_kernel(WinArgs a) {
 
   // windows of the block's first and last row, and of the wave's
   auto range_of = [&](int r, int& lo, int& hi) {
-    win_range(a, seq, (int)((uint32_t)min(r, rows - 1) / (uint32_t)a.n), lo, hi);
+    win_range(a, seq, (int)a.by_n((uint32_t)min(r, rows - 1)), lo, hi);
     lo = __builtin_amdgcn_readfirstlane(lo);
     hi = __builtin_amdgcn_readfirstlane(hi);
   };
@@ -229,10 +247,11 @@ __global__ __launch_bounds__(512) void window_blocks_kernel(WinArgs a) {
   mask.sink = tiles.sink;
 #pragma unroll
   for (int i = 0; i < ATT_QB; ++i) {
-    const uint32_t r = (uint32_t)min(wr0 + 16 * i + jq, rows - 1), qi = r / (uint32_t)a.n;
-    win_range(a, seq, (int)qi, mask.lo[i], mask.hi[i]);
+    int e;
+    const int qi = win_query(a, min(wr0 + 16 * i + jq, rows - 1), e);
+    win_range(a, seq, qi, mask.lo[i], mask.hi[i]);
     if (tiles.sink == 0 && seq.sink >= lo1) mask.lo[i] = 0;
-    const bf16_t* qp = (const bf16_t*)a.q + b * a.sq + (int64_t)qi * a.ldq + (int64_t)(h * a.n + (r - qi * a.n)) * D + g * 8;
+    const bf16_t* qp = (const bf16_t*)a.q + b * a.sq + (int64_t)qi * a.ldq + (int64_t)(h * a.n + e) * D + g * 8;
 #pragma unroll
     for (int kc = 0; kc < D / 32; ++kc) qf[kc][i] = __builtin_bit_cast(bf16x8, *(const u32x4*)(qp + kc * 32));
   }
@@ -361,7 +380,8 @@ __global__ __launch_bounds__(512) void window_blocks_kernel(WinArgs a) {
       }
       if (g == 0) a.pml[pr] = float2{m, l};
     } else {
-      const int qi = (int)((uint32_t)r / (uint32_t)a.n), head = h * a.n + (r - qi * a.n);
+      int e;
+      const int qi = win_query(a, r, e), head = h * a.n + e;
       const float inv = win_inverse(l);
       bf16_t* o = (bf16_t*)a.out + b * a.so + (int64_t)qi * a.ldo + (int64_t)head * D + 8 * g;
 #pragma unroll
@@ -411,8 +431,8 @@ __global__ __launch_bounds__(256, 2) void window_rows_kernel(WinArgs a) {
   if (SPLIT) win_share(tiles.n, sp, a.nsplit, i0, i1);
 
   // the lane's row (the last one again past the end)
-  const uint32_t row = (uint32_t)min(jq, rows - 1);
-  const int qi = (int)(row / (uint32_t)a.n), head = h * a.n + (int)(row - qi * a.n);
+  int e;
+  const int qi = win_query(a, min(jq, rows - 1), e), head = h * a.n + e;
   WinMask<1> mask;
   mask.sink = tiles.sink;
   win_range(a, seq, qi, mask.lo[0], mask.hi[0]);
@@ -684,11 +704,12 @@ struct WinF32 {
   __device__ __forceinline__ void begin(const WinArgs& a, const WinSeq& seq, const WinTiles& tiles, int lo1, int h, int r,
                                         int rows) {
     const int g = (int)(threadIdx.x & 63) >> 4;
-    const uint32_t rr = (uint32_t)min(r, rows - 1), qi = rr / (uint32_t)a.n;
-    win_range(a, seq, (int)qi, lo, hi);
+    int e;
+    const int qi = win_query(a, min(r, rows - 1), e);
+    win_range(a, seq, qi, lo, hi);
     if (tiles.sink == 0 && seq.sink >= lo1) lo = 0;
     sink = tiles.sink;
-    const float* qp = (const float*)a.q + seq.b * a.sq + (int64_t)qi * a.ldq + (int64_t)(h * a.n + (rr - qi * a.n)) * D + 4 * g;
+    const float* qp = (const float*)a.q + seq.b * a.sq + (int64_t)qi * a.ldq + (int64_t)(h * a.n + e) * D + 4 * g;
 #pragma unroll
     for (int c = 0; c < C; ++c) {
       qf[c] = win_load4<VEC>(qp + 16 * c);
@@ -722,7 +743,8 @@ struct WinF32 {
       sum = fmaf(wt[w], sml[(w0 + w) * 32 + 16 + jq], sum);
     }
     if (r >= rows) return;
-    const int qi = (int)((uint32_t)r / (uint32_t)a.n), head = h * a.n + (r - qi * a.n);
+    int e;
+    const int qi = win_query(a, r, e), head = h * a.n + e;
     const int64_t pr = ((((int64_t)sp * a.B + b) * a.Hk + h) * a.Lq) * a.n + r;
     const float inv = SPLIT ? 1.0f : win_inverse(sum);
     float* const op = SPLIT ? a.po + pr * D + 4 * g
@@ -780,7 +802,7 @@ __global__ __launch_bounds__(64 * WIN_F32_WAVES) void window_f32_tiles_kernel(Wi
   const int r0 = rb * WIN_F32_ROWS;
   if (r0 >= rows) return;  // the whole workgroup
   auto range_of = [&](int r, int& lo, int& hi) {
-    win_range(a, seq, (int)((uint32_t)min(r, rows - 1) / (uint32_t)a.n), lo, hi);
+    win_range(a, seq, (int)a.by_n((uint32_t)min(r, rows - 1)), lo, hi);
     lo = __builtin_amdgcn_readfirstlane(lo);
     hi = __builtin_amdgcn_readfirstlane(hi);
   };
@@ -870,8 +892,8 @@ __global__ __launch_bounds__(256) void window_f32_kernel(WinArgs a) {
   if (r0 >= rows) return;  // the whole workgroup
 
   int lo0, hi0, lo1, hi1;
-  win_range(a, seq, (int)((uint32_t)r0 / (uint32_t)a.n), lo0, hi0);
-  win_range(a, seq, (int)((uint32_t)min(r0 + 15, rows - 1) / (uint32_t)a.n), lo1, hi1);
+  win_range(a, seq, (int)a.by_n((uint32_t)r0), lo0, hi0);
+  win_range(a, seq, (int)a.by_n((uint32_t)min(r0 + 15, rows - 1)), lo1, hi1);
   WinTiles tiles;
   tiles.init<BKV>(seq, __builtin_amdgcn_readfirstlane(lo0), __builtin_amdgcn_readfirstlane(hi0),
                   __builtin_amdgcn_readfirstlane(lo1), __builtin_amdgcn_readfirstlane(hi1));
@@ -939,11 +961,11 @@ __global__ __launch_bounds__(256) void window_join_kernel(WinArgs a, int D) {
   const int64_t pr = (int64_t)blockIdx.x * (256 / per / G) + t / (per * G);
   float m = -INFINITY, l = 0.0f;
   f32x4 v = {0.0f, 0.0f, 0.0f, 0.0f};
-  const uint32_t per_head = (uint32_t)(a.Lq * a.n);  // < 2^31
-  const int64_t row = pr < all ? pr : all - 1;
-  const uint32_t bh = (uint32_t)(row / per_head), r = (uint32_t)(row - (int64_t)bh * per_head);
-  const int b = (int)(bh / (uint32_t)a.Hk), h = (int)(bh - b * a.Hk);
-  const int qi = (int)(r / (uint32_t)a.n), head = h * a.n + (int)(r - qi * a.n);
+  const int64_t row = pr < all ? pr : all - 1;  // below 2^25
+  const uint32_t per_head = (uint32_t)(a.Lq * a.n), bh = (uint32_t)row / per_head;
+  const int b = (int)a.by_Hk(bh), h = (int)bh - b * a.Hk;
+  int e;
+  const int qi = win_query(a, (int)((uint32_t)row - bh * per_head), e), head = h * a.n + e;
   const bool there = pr < all && !(a.q_len && qi >= min(a.q_len[b], a.Lq));
   auto add = [&](float m1, float l1, const f32x4& u) {
     const float mx = fmaxf(m, m1);
@@ -1068,7 +1090,7 @@ static track_status win_check(int dtype, const track_window* w, int B, int H, in
     return fail(TRACK_E_INVALID, "attention_window: window of %lld / %lld groups of %lld, %lld first tokens, scale %g",
                 (long long)w->left, (long long)w->right, (long long)w->group, (long long)w->sink, w->scale);
   if (w->left > WIN_MAX || w->right > WIN_MAX || w->group > WIN_MAX || w->sink > WIN_MAX)
-    return fail(TRACK_E_SHAPE, "attention_window: window limits are at most 2^30");
+    return fail(TRACK_E_SHAPE, "attention_window: window limits are at most 2^28");
   if (B < 0 || H < 1 || Hk < 1 || Lq < 0 || Lk < 0)
     return fail(TRACK_E_SHAPE, "attention_window: bad sizes B=%d H=%d Hk=%d Lq=%lld Lk=%lld", B, H, Hk, (long long)Lq, (long long)Lk);
   if (H % Hk) return fail(TRACK_E_SHAPE, "attention_window: %d query heads over %d key heads", H, Hk);
@@ -1126,9 +1148,14 @@ track_status attention_window(int dtype, const track_window* w, int B, int H, in
   a.q = q, a.k = k, a.vt = vt, a.out = out;
   a.ldq = ldq, a.sq = sq, a.ldk = ldk, a.sk = sk, a.ldv = ldv, a.sv = sv, a.ldo = ldo, a.so = so;
   a.lse = lse, a.q_len = q_len, a.k_len = k_len, a.q_start = q_start;
-  a.left = w->left, a.right = w->right, a.group = (uint32_t)w->group, a.sink = (int)w->sink;
+  a.before = w->left < 0 ? INT32_MAX : (int)std::min<int64_t>(w->left * w->group, INT32_MAX);
+  a.past = w->right < 0 ? INT32_MAX : (int)std::min<int64_t>((w->right + 1) * w->group, INT32_MAX);
+  a.lift = (int)((2 * WIN_MAX + w->group - 1) / w->group * w->group);
+  a.sink = (int)w->sink;
   a.B = B, a.Hk = Hk, a.n = n, a.Lq = (int)Lq, a.Lk = (int)Lk;
   a.nrb = (int)p.nrb, a.nsplit = p.nsplit;
+  a.by_group = win_div(w->group), a.by_n = win_div(n);
+  a.by_nrb = win_div(a.nrb), a.by_nsplit = win_div(a.nsplit), a.by_Hk = win_div(Hk);
   a.scale_log2 = w->scale > 0.0 ? (float)(w->scale * 1.4426950408889634) : attn_log2_scale(D);
   a.po = (float*)ws;
   a.pml = need ? (float2*)(a.po + (int64_t)p.nsplit * joined * D) : nullptr;

@@ -468,6 +468,12 @@ ATTN = [
     (1, 1, 1, 70, 4000, W(), {}),                                          # shares of the keys, blocks
     (1, 2, 1, 200, 9000, W(left=2500, sink=130), {}),
     (1, 1, 1, 257, 257, W(sink=1000), {}),
+    # limits at the ends of their ranges
+    (1, 2, 1, 100, 300, W(left=1 << 28, right=1 << 28, group=1 << 28, sink=1 << 28), {}),
+    (1, 2, 1, 100, 300, W(left=0, right=0, group=1 << 28), {}),
+    (1, 2, 1, 100, 300, W(left=0, right=1 << 28, group=3), {}),
+    (3, 2, 1, 20, 300, W(left=100, right=0, sink=7), dict(q_start=[-(1 << 28), 1 << 28, 290])),
+    (2, 2, 1, 20, 300, W(left=3, right=0, group=100), dict(q_start=[-250, 250])),
 ]
 
 
