@@ -57,6 +57,7 @@ struct WinArgs {
   int Lq, Lk;
   int nrb, nsplit;    // row blocks, shares of the keys
   WinDiv by_group, by_n, by_nrb, by_nsplit, by_Hk;
+  WinDiv by_inner;    // sequences of a head, or heads of a sequence (win_place)
   float scale_log2;
   float* po;          // [nsplit][B][Hk][Lq n][D]: a share's sums
   float2* pml;        // [nsplit][B][Hk][Lq n]: its reference (log2 units) and its denominator
@@ -186,18 +187,22 @@ __device__ __forceinline__ f32x4 win_load4(const float* p) {
   else return f32x4{p[0], p[1], p[2], p[3]};
 }
 
-// Row block, share, key head and sequence of a workgroup.  Neighbouring row blocks go to one
-// XCD, whose L2 then serves their common keys: over the XCDs in turn, 12 heads 16384 x 16384
+// Row block, share, key head and sequence of a workgroup.  LOCAL: neighbouring row blocks go to
+// one XCD, whose L2 then serves their common keys (over the XCDs in turn, 12 heads 16384 x 16384
 // under a causal mask took 955 us instead of 824, 2 x 12 heads over a 21-frame video 5.2 ms
-// instead of 4.8.  The last rows of a sequence, which see most keys under a causal mask, start
-// first.
+// instead of 4.8), and the sequences follow each other inside a head, so that short ones do
+// not leave one XCD idle (4 sequences of 5000 to 3100 queries: 439 -> 385 us).  Single tokens use
+// a key once: they go over the XCDs in turn (8 sequences of 100003 to 56000 keys: 519 -> 466
+// us).  The last rows of a sequence, which see most keys under a causal mask, start first.
+template <bool LOCAL>
 __device__ __forceinline__ void win_place(const WinArgs& a, int& rb, int& sp, int& h, int& b) {
-  const uint32_t id = (uint32_t)xcd_remap((int)blockIdx.x, (int)gridDim.x);
-  const uint32_t t = a.by_nrb(id), u = a.by_nsplit(t), v = a.by_Hk(u);
+  const uint32_t id = LOCAL ? (uint32_t)xcd_remap((int)blockIdx.x, (int)gridDim.x) : blockIdx.x;
+  const uint32_t t = a.by_nrb(id), u = a.by_nsplit(t), v = a.by_inner(u);
   rb = a.nrb - 1 - (int)(id - t * a.nrb);
   sp = (int)(t - u * a.nsplit);
-  h = (int)(u - v * a.Hk);
-  b = (int)v;
+  const int w = (int)(u - v * a.by_inner.d);
+  h = LOCAL ? (int)v : w;
+  b = LOCAL ? w : (int)v;
 }
 
 // ---------------------------------------------------------------- many rows, bfloat16
@@ -215,7 +220,7 @@ __global__ __launch_bounds__(512) void window_blocks_kernel(WinArgs a) {
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int jq = lane & 15, g = lane >> 4;
   int rb, sp, h, b;
-  win_place(a, rb, sp, h, b);
+  win_place<true>(a, rb, sp, h, b);
   const WinSeq seq = win_seq(a, b);
   const int rows = seq.qlen * a.n;
   const int r0 = rb * ATT_BQ;
@@ -416,7 +421,7 @@ __global__ __launch_bounds__(256, 2) void window_rows_kernel(WinArgs a) {
   const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   const int jq = lane & 15, g = lane >> 4;
   int rb, sp, h, b;
-  win_place(a, rb, sp, h, b);
+  win_place<false>(a, rb, sp, h, b);
   const WinSeq seq = win_seq(a, b);
   const int rows = seq.qlen * a.n;  // at most 16
   if (rows == 0) return;            // the whole workgroup
@@ -796,7 +801,7 @@ __global__ __launch_bounds__(64 * WIN_F32_WAVES) void window_f32_tiles_kernel(Wi
   const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   const int jq = lane & 15, g = lane >> 4;
   int rb, sp, h, b;
-  win_place(a, rb, sp, h, b);
+  win_place<true>(a, rb, sp, h, b);
   const WinSeq seq = win_seq(a, b);
   const int rows = seq.qlen * a.n;
   const int r0 = rb * WIN_F32_ROWS;
@@ -885,7 +890,7 @@ __global__ __launch_bounds__(256) void window_f32_kernel(WinArgs a) {
   const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   const int jq = lane & 15, g = lane >> 4;
   int rb, sp, h, b;
-  win_place(a, rb, sp, h, b);
+  win_place<true>(a, rb, sp, h, b);
   const WinSeq seq = win_seq(a, b);
   const int rows = seq.qlen * a.n;
   const int r0 = rb * 16;
@@ -1018,14 +1023,14 @@ static int64_t win_span(const track_window& w, int64_t rows, int n, int64_t Lk) 
 }
 
 // Shares of the keys for few rows, `blocks` row blocks of `tiles` tiles each.  Up to 8 tiles a
-// wave on a full chip, a workgroup on every CU, but two tiles a share; beyond, three workgroups
-// a CU, which evens out lengths.  One token, 8 key heads of 4096 keys: 59 us with one share,
-// 14.1 with 8, 11.2 with 16, 9.3 with 32, 10.2 with 64; 32 of 1027: 18.9 with 1, 11.1 with 5,
-// 10.4 with 8, 12.2 with 16; 8 of 16384: 17.8 with 32, 18.9 with 64; 64 of 100003: 619 with 8,
-// 568 with 12, 585 with 64.
+// wave on a full chip, a workgroup on every CU, but two tiles a share; beyond, six workgroups
+// a CU with 16 tiles at least, which evens out lengths.  One token, 8 key heads of 4096 keys: 59 us
+// with one share, 14.1 with 8, 11.2 with 16, 9.3 with 32, 10.2 with 64; 32 of 1027: 18.9 with 1,
+// 11.1 with 5, 10.4 with 8, 12.2 with 16; 8 of 16384: 17.8 with 32, 18.9 with 64; 48 of 32760: 198
+// with 8, 163 with 16, 148 with 32; 64 of 100003: 613 with 8, 590 with 12, 582 with 32.
 static int rows_split(int64_t tiles, int64_t blocks, int64_t cus) {
   const bool large = blocks * tiles >= 64 * cus;
-  const int64_t s = large ? (3 * cus + blocks - 1) / blocks : std::min(cus / blocks, (tiles + 1) / 2);
+  const int64_t s = large ? std::min((6 * cus + blocks - 1) / blocks, tiles / 16) : std::min(cus / blocks, (tiles + 1) / 2);
   return (int)std::max<int64_t>(1, s);
 }
 
@@ -1156,6 +1161,7 @@ track_status attention_window(int dtype, const track_window* w, int B, int H, in
   a.nrb = (int)p.nrb, a.nsplit = p.nsplit;
   a.by_group = win_div(w->group), a.by_n = win_div(n);
   a.by_nrb = win_div(a.nrb), a.by_nsplit = win_div(a.nsplit), a.by_Hk = win_div(Hk);
+  a.by_inner = win_div(p.form == WinPlan::ROWS ? Hk : B);
   a.scale_log2 = w->scale > 0.0 ? (float)(w->scale * 1.4426950408889634) : attn_log2_scale(D);
   a.po = (float*)ws;
   a.pml = need ? (float2*)(a.po + (int64_t)p.nsplit * joined * D) : nullptr;
