@@ -1,8 +1,9 @@
 // Rotary positions of queries and keys, with or without the RMSNorm of each head in the
 // same pass: y = m A R(pos f) n(x), n(x) = x / sqrt(mean(x^2) + eps) g over a head (or x).
 //
-// Each element is read once and written once, so HBM bounds it; what is left to decide is
-// how little else a wave does.  A wave takes one token and walks its heads (of q, then of
+// Each element is read once and written once, so HBM bounds it (65520 tokens: 24 heads of 128
+// 141 us, 5.7 TB/s; 80 heads with the norm, out of fused rows, 511 us, 5.2 TB/s); what is left to
+// decide is how little else a wave does.  A wave takes one token and walks its heads (of q, then of
 // k).  It forms the token's angles itself, one pair a lane: the position times the float64
 // frequency in turns, reduced to half a turn in float64 (a float32 product is off by 0.06
 // radian at position 10^6), one sincospi.  LDS hands every lane the angles of its own
@@ -10,8 +11,10 @@
 // of [tokens, pairs] would be as many bytes again as a head, and no scratch memory.
 //
 // A head is D / (2 V) units of two V-element loads (16 bytes each in the wide form) that
-// hold whole pairs: channels V u .. and rot / 2 + V u .. of the half layout, 2 V u .. of the
-// interleaved one, so no lane needs another's elements.  A head takes the next power of two
+// hold whole pairs, so no lane needs another's elements, and that lie V elements apart from
+// lane to lane, so that a load covers whole lines: channels V u .. and rot / 2 + V u .. of the
+// half layout (copied ones likewise, by halves), V u .. and D / 2 + V u .. of the interleaved one
+// (as 2 V u .. and 2 V u + V .. a load took every other 16 bytes).  A head takes the next power of two
 // of lanes (8 for 128 bfloat16 channels, 8 heads a step); the sum of squares meets by DPP
 // moves and lane swaps.
 #include <math.h>
@@ -25,7 +28,7 @@ namespace track {
 
 // Pairs of the widest head: one wave's angles in LDS.
 constexpr int ROPE_MAX_PAIRS = ROPE_MAX_DIM / 2;
-constexpr int ROPE_STEPS = 4;  // head groups whose loads a wave has under way together
+constexpr int ROPE_STEPS = 2;  // head groups whose loads a wave has under way together (4: up to 12% slower)
 
 struct RopeArgs {
   const void* x[2];  // q, k
@@ -106,7 +109,7 @@ __device__ __forceinline__ float group_sum(float v, int n) {
 }
 
 // NU units a lane: 2 only where a head of more than 128 channels moves element by element.
-template <typename T, int V, int NU, bool NORM, bool HALF>
+template <typename T, int V, int NU, bool NORM, bool HALF, bool STREAM>
 __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a) {
   typedef typename RopeVec<T, V>::type Raw;
   constexpr int ST = NU == 1 ? ROPE_STEPS : 1;
@@ -126,12 +129,15 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a) {
 #pragma unroll
   for (int i = 0; i < NU; ++i) {
     const int u = u0 + 64 * i;
-    if (u < rot_units) {
-      e0[i] = HALF ? V * u : 2 * V * u;
-      e1[i] = HALF ? a.pairs + V * u : 2 * V * u + V;
-    } else {
-      e0[i] = 2 * V * u;  // 2 pairs = 2 V rot_units
-      e1[i] = e0[i] + V;
+    if (!HALF && V > 1) {
+      e0[i] = V * u;
+      e1[i] = V * (units + u);
+    } else if (u < rot_units) {
+      e0[i] = HALF ? V * u : 2 * u;
+      e1[i] = HALF ? a.pairs + V * u : 2 * u + 1;
+    } else {  // copied channels, from 2 pairs = 2 V rot_units on
+      e0[i] = V * (rot_units + u);
+      e1[i] = V * (units + u);
     }
   }
   const int total = a.heads[0] + a.heads[1];
@@ -190,9 +196,12 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a) {
   for (int i = 0; i < NU; ++i)
 #pragma unroll
     for (int j = 0; j < V; ++j) {
+      // pair j of the lane: of the unit, or of its first load's V / 2 pairs and its second's
       const int u = u0 + 64 * i;
-      c[i][j] = u < rot_units ? cs[wv][0][V * u + j] : 1.0f;
-      s[i][j] = u < rot_units ? cs[wv][1][V * u + j] : 0.0f;
+      const int p = HALF || V == 1 ? V * u + j : (j < V / 2 ? e0[i] / 2 + j : e1[i] / 2 + j - V / 2);
+      const bool turned = p < a.pairs;
+      c[i][j] = turned ? cs[wv][0][p] : 1.0f;
+      s[i][j] = turned ? cs[wv][1][p] : 0.0f;
     }
 
   for (int h0 = part * hp; h0 < total; h0 += ST * (int)a.wpt * hp) {
@@ -250,8 +259,14 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a) {
               xh[i][2 * j + 1] = x0 * s[i][V / 2 + j] + x1 * c[i][V / 2 + j];
             }
           }
-          *(Raw*)(p + e0[i]) = rope_pack<T, V>(xl[i]);
-          *(Raw*)(p + e1[i]) = rope_pack<T, V>(xh[i]);
+          const Raw rl = rope_pack<T, V>(xl[i]), rh = rope_pack<T, V>(xh[i]);
+          if constexpr (STREAM) {
+            __builtin_nontemporal_store(rl, (Raw*)(p + e0[i]));
+            __builtin_nontemporal_store(rh, (Raw*)(p + e1[i]));
+          } else {
+            *(Raw*)(p + e0[i]) = rl;
+            *(Raw*)(p + e1[i]) = rh;
+          }
         }
       }
     }
@@ -266,12 +281,12 @@ static uint32_t rope_waves_per_token(int64_t tokens, int groups) {
   return (uint32_t)std::max<int64_t>(1, std::min<int64_t>(want, groups));
 }
 
-template <typename T, int V, int NU>
+template <typename T, int V, int NU, bool STREAM>
 static void rope_launch(const RopeArgs& a, bool norm, bool half, unsigned grid, hipStream_t s) {
-  if (norm && half) rope_kernel<T, V, NU, true, true><<<grid, 256, 0, s>>>(a);
-  else if (norm) rope_kernel<T, V, NU, true, false><<<grid, 256, 0, s>>>(a);
-  else if (half) rope_kernel<T, V, NU, false, true><<<grid, 256, 0, s>>>(a);
-  else rope_kernel<T, V, NU, false, false><<<grid, 256, 0, s>>>(a);
+  if (norm && half) rope_kernel<T, V, NU, true, true, STREAM><<<grid, 256, 0, s>>>(a);
+  else if (norm) rope_kernel<T, V, NU, true, false, STREAM><<<grid, 256, 0, s>>>(a);
+  else if (half) rope_kernel<T, V, NU, false, true, STREAM><<<grid, 256, 0, s>>>(a);
+  else rope_kernel<T, V, NU, false, false, STREAM><<<grid, 256, 0, s>>>(a);
 }
 
 track_status rope_heads(int dtype, const track_rope_config& c, int64_t B, int64_t L, const track_head_rows& q,
@@ -310,29 +325,38 @@ track_status rope_heads(int dtype, const track_rope_config& c, int64_t B, int64_
   a.sec1 = c.axes > 2 ? c.section[0] + c.section[1] : a.pairs;
   a.tokens = (uint32_t)tokens;
   a.L = (uint32_t)L;
-  // the widest units that hold whole pairs and that every address allows
+  // the widest units that hold whole pairs, all rotated or all copied, and that every address allows
+  const bool norm = g_q != nullptr, half = c.layout == TRACK_ROPE_HALF;
   auto fits = [&](int v) {
-    return a.pairs % v == 0 && (a.D - 2 * a.pairs) % (2 * v) == 0 && (bits | (uintptr_t)(a.D * es)) % (v * es) == 0;
+    const bool whole = half ? a.pairs % v == 0 && (a.D - 2 * a.pairs) % (2 * v) == 0 : 2 * a.pairs % v == 0 && a.D % (2 * v) == 0;
+    return whole && (bits | (uintptr_t)(a.D * es)) % (v * es) == 0;
   };
   const int V = es == 2 && fits(8) ? 8 : (fits(4) ? 4 : 1);
   const int units = a.D / (2 * V);
   while ((1 << a.lph_log2) < std::min(units, 64)) ++a.lph_log2;
+  // Stores past the caches where a store covers whole 128-byte lines.  With shorter runs a line
+  // is left half written between two stores: 16 heads of 64 channels 42 us, 46 past the caches;
+  // with whole ones 2 x 4099 x 16 heads of 64 float32 channels 12.5 -> 10.1 us, 65520 x 24 heads
+  // of 128 148 -> 142, 8192 x 48 heads 35.5 -> 35, float32 64-channel norms 91 -> 76.
+  const bool stream = V > 1 && (half ? a.pairs : a.D / 2) * es >= 128;
   const int hp = 64 >> a.lph_log2, total = a.heads[0] + a.heads[1];
   a.wpt = rope_waves_per_token(tokens, (total + hp - 1) / hp);
   const int64_t grid = (tokens * a.wpt + 3) / 4;
   if (grid >= (int64_t)1 << 24)
     return fail(TRACK_E_SHAPE, "rope: %lld tokens are too many", (long long)tokens);
-  const bool norm = g_q != nullptr, half = c.layout == TRACK_ROPE_HALF;
   ProfScope prof(TRACK_PROF_NORM, s);
+  const unsigned g1 = (unsigned)grid;
   if (es == 2) {
-    if (V == 8) rope_launch<bf16_t, 8, 1>(a, norm, half, (unsigned)grid, s);
-    else if (V == 4) rope_launch<bf16_t, 4, 1>(a, norm, half, (unsigned)grid, s);
-    else if (units <= 64) rope_launch<bf16_t, 1, 1>(a, norm, half, (unsigned)grid, s);
-    else rope_launch<bf16_t, 1, 2>(a, norm, half, (unsigned)grid, s);
+    if (V == 8 && stream) rope_launch<bf16_t, 8, 1, true>(a, norm, half, g1, s);
+    else if (V == 8) rope_launch<bf16_t, 8, 1, false>(a, norm, half, g1, s);
+    else if (V == 4) rope_launch<bf16_t, 4, 1, false>(a, norm, half, g1, s);
+    else if (units <= 64) rope_launch<bf16_t, 1, 1, false>(a, norm, half, g1, s);
+    else rope_launch<bf16_t, 1, 2, false>(a, norm, half, g1, s);
   } else {
-    if (V == 4) rope_launch<float, 4, 1>(a, norm, half, (unsigned)grid, s);
-    else if (units <= 64) rope_launch<float, 1, 1>(a, norm, half, (unsigned)grid, s);
-    else rope_launch<float, 1, 2>(a, norm, half, (unsigned)grid, s);
+    if (V == 4 && stream) rope_launch<float, 4, 1, true>(a, norm, half, g1, s);
+    else if (V == 4) rope_launch<float, 4, 1, false>(a, norm, half, g1, s);
+    else if (units <= 64) rope_launch<float, 1, 1, false>(a, norm, half, g1, s);
+    else rope_launch<float, 1, 2, false>(a, norm, half, g1, s);
   }
   TRACK_LAUNCH_CHECK();
   return TRACK_OK;
