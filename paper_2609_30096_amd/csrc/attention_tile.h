@@ -258,6 +258,7 @@ __device__ __forceinline__ void att_tile_masked(const uint8_t* kb, const bf16x8 
 #pragma unroll 1
       for (int k = 0; k < 32; ++k) {  // key 32 c + k
         float p[QB];
+        uint32_t on[QB];  // V times 0 where the weight is 0
 #pragma unroll
         for (int b = 0; b < QB; ++b) {
           const u32x4 own = __builtin_bit_cast(u32x4, pf[c][b]);
@@ -265,16 +266,18 @@ __device__ __forceinline__ void att_tile_masked(const uint8_t* kb, const bf16x8 
           const uint32_t w = e == 0 ? own[0] : (e == 1 ? own[1] : (e == 2 ? own[2] : own[3]));
           const uint32_t got = __builtin_amdgcn_ds_bpermute(((lane & 15) + 16 * (k >> 3)) << 2, (int)w);
           p[b] = __uint_as_float(k & 1 ? got & 0xffff0000u : got << 16);
+          on[b] = p[b] != 0.0f ? 0xffffffffu : 0u;
         }
 #pragma unroll
         for (int f = 0; f < ATT_D / 16; ++f)
 #pragma unroll
           for (int r = 0; r < 4; ++r) {
             const int row = 16 * f + 4 * (lane >> 4) + r;
-            const float v =
-                bf2f(*(const bf16_t*)(vt + row * ATT_VROW + (((4 * c + (k >> 3)) ^ att_vswz(row)) << 4) + 2 * (k & 7)));
+            const uint32_t v =
+                *(const bf16_t*)(vt + row * ATT_VROW + (((4 * c + (k >> 3)) ^ att_vswz(row)) << 4) + 2 * (k & 7));
 #pragma unroll
-            for (int b = 0; b < QB; ++b) st.o[f][b][r] = p[b] != 0.0f ? fmaf(p[b], v, st.o[f][b][r]) : st.o[f][b][r];
+            for (int b = 0; b < QB; ++b)
+              st.o[f][b][r] = fmaf(p[b], __uint_as_float((v << 16) & on[b]), st.o[f][b][r]);
           }
       }
     return;

@@ -187,13 +187,17 @@ __device__ __forceinline__ f32x4 win_load4(const float* p) {
   else return f32x4{p[0], p[1], p[2], p[3]};
 }
 
+// Bits of a pair of keys of which `left` are to keep (any number).
+__device__ __forceinline__ uint32_t win_keep(int left) { return (uint32_t)((1ull << (16 * min(max(left, 0), 2))) - 1ull); }
+
 // Row block, share, key head and sequence of a workgroup.  LOCAL: neighbouring row blocks go to
 // one XCD, whose L2 then serves their common keys (over the XCDs in turn, 12 heads 16384 x 16384
 // under a causal mask took 955 us instead of 824, 2 x 12 heads over a 21-frame video 5.2 ms
 // instead of 4.8), and the sequences follow each other inside a head, so that short ones do
 // not leave one XCD idle (4 sequences of 5000 to 3100 queries: 439 -> 385 us).  Single tokens use
 // a key once: they go over the XCDs in turn (8 sequences of 100003 to 56000 keys: 519 -> 466
-// us).  The last rows of a sequence, which see most keys under a causal mask, start first.
+// us with an earlier kernel).  The last rows of a sequence, which see most keys under a causal
+// mask, start first.
 template <bool LOCAL>
 __device__ __forceinline__ void win_place(const WinArgs& a, int& rb, int& sp, int& h, int& b) {
   const uint32_t id = LOCAL ? (uint32_t)xcd_remap((int)blockIdx.x, (int)gridDim.x) : blockIdx.x;
@@ -295,13 +299,10 @@ __global__ __launch_bounds__(512) void window_blocks_kernel(WinArgs a) {
     for (int i = 0; i < 2; ++i) {
       const int unit = tid + 512 * i, row = unit >> 3, c = (unit & 7) ^ att_vswz(row);
       u32x4* p = (u32x4*)(smem + slot + ATT_K_BYTES + unit * 16);
-      const int left = seq.klen - key0 - 8 * c;  // keys of the unit to keep
-      if (left < 8) {
-        u32x4 v = *p;
+      u32x4 v = *p;
 #pragma unroll
-        for (int w = 0; w < 4; ++w) v[w] &= left > 2 * w + 1 ? 0xffffffffu : (left > 2 * w ? 0xffffu : 0u);
-        *p = v;
-      }
+      for (int w = 0; w < 4; ++w) v[w] &= win_keep(seq.klen - key0 - 8 * c - 2 * w);
+      *p = v;
     }
     __syncthreads();
   };
@@ -403,20 +404,24 @@ __global__ __launch_bounds__(512) void window_blocks_kernel(WinArgs a) {
 
 // ---------------------------------------------------------------- few rows, bfloat16
 // At most 16 rows a key head (a token of 16 query heads, four tokens of 4).  The four waves of
-// a workgroup take every fourth 64-key tile of its share straight from memory into the matrix
-// cores' operands: K rows are the "A" operand as they are stored, and so are V^T rows.  No key
-// is used twice, so LDS would only add a stop; the waves' sums meet there at the end.  What
-// bounds it: reading K and V^T (5.4 - 5.8 TB/s over long caches), for short ones the latency of
-// a tile and of the join.  Loads through buffer resources with the row blocks in the scalar
-// offset take one address register for K and one for V^T, so that a SIMD holds two waves (252
-// registers; 64-bit addresses spilled 71): one token over 8 heads of 4096 keys 16.2 -> 11.2 us
-// at 16 shares, 16384 27.6 -> 17.9 at 32.
+// a workgroup take every fourth 64-key tile of its share, each through 32 KB of LDS of its own:
+// copies go by DMA in whole 128-byte lines (operands straight from memory, where adjacent lanes
+// read different rows, pass through the CU's cache 16 bytes a cycle: a tile kept a CU busy
+// for 1 us), and no wave waits for another before the sums meet at the end.  K's half is
+// filled again as soon as its tile's logits are formed, V^T's once its product is, so copies are
+// under way all the time.  What bounds it: reading K and V^T (8 sequences of 100003 keys 538 us,
+// 6.1 TB/s of the 6.5 that a plain read stream reaches; of 100003 to 56000 keys 466 -> 430), and
+// for short windows the latency of a tile and of the join (8 heads of 4096 keys 9.1 -> 8.4 us).
 template <bool SPLIT>
-__global__ __launch_bounds__(256, 2) void window_rows_kernel(WinArgs a) {
+__global__ __launch_bounds__(256) void window_rows_kernel(WinArgs a) {
   constexpr int BKV = ATT_BKV, D = ATT_D, F = D / 16;
   typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
-  __shared__ f32x4 so[4][F][64];
-  __shared__ float sm[4][16], sl[4][16];
+  // one object (see above): four tiles; the sums at the end
+  __shared__ __attribute__((aligned(1024))) uint8_t smem[4 * ATT_SLOT];
+  typedef f32x4 (*Sums)[F][64];
+  typedef float (*Stats)[16];
+  const Sums so = (Sums)smem;                                    // [4][F][64]
+  const Stats sm = (Stats)(smem + 4 * F * 1024), sl = sm + 4;    // [4][16] each
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   const int jq = lane & 15, g = lane >> 4;
@@ -449,45 +454,78 @@ __global__ __launch_bounds__(256, 2) void window_rows_kernel(WinArgs a) {
   const uint8_t* const kbase = (const uint8_t*)((const bf16_t*)a.k + b * a.sk + (int64_t)h * D);
   const uint8_t* const vbase = (const uint8_t*)((const bf16_t*)a.vt + b * a.sv + (int64_t)h * D * a.ldv);
   const uint32_t krow = (uint32_t)a.ldk * 2, vrow = (uint32_t)a.ldv * 2;
-  // att_perm(16 i + jq) = att_perm(16 i) + att_perm(jq): the lane's part of the offsets of its
-  // K and V^T rows, the other part is wave-uniform
-  const uint32_t kl = att_perm(jq) * krow + 16 * g, vl = att_perm(jq) * vrow + 16 * g;
+  // Copy i of 16 fills LDS rows 4 i .. + 3 of K (16 lanes a row of 256 bytes) or 8 i .. + 7 of V^T
+  // (8 lanes a row of 128), laid out as in the block kernel.  The key att_perm(4 i + lane / 16) is
+  // att_perm(4 i) + lane / 16 and the channel att_perm(8 i + lane / 8) likewise, and the
+  // swizzles' bits of i and of the lane do not meet: one offset a lane for V^T, one for each i % 4 for
+  // K, the rest is wave-uniform.
+  uint8_t* const tile = smem + wave * ATT_SLOT;
+  uint32_t kl[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) kl[i] = g * krow + (((jq ^ g) ^ (4 * i)) << 4);
+  const uint32_t vl = att_perm(lane >> 3) * vrow + (((lane & 7) ^ ((lane >> 3) & 6)) << 4);
+  const uint32_t ko = jq * 256 + ((g ^ jq) << 4), vo = jq * ATT_VROW + ((g ^ att_vswz(jq)) << 4);
+  // K rows past the last key read as zero, V^T columns as whatever is there (cleared below) or,
+  // past the head's last row, as zero
+  auto copy_k = [&](int key0) {
+    const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc(
+        (void*)(kbase + (int64_t)key0 * krow), (short)0, (int)(min(BKV, seq.klen - key0) * krow), 0x00020000);
+#pragma unroll
+    for (int i = 0; i < 16; ++i)
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (att_lds_ptr_t)(tile + i * 1024), 16, kl[i & 3], att_perm(4 * i) * krow, 0, 0);
+  };
+  auto copy_v = [&](int key0) {
+    const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc(
+        (void*)(vbase + (int64_t)key0 * 2), (short)0, (int)(D * vrow - 2 * key0), 0x00020000);
+#pragma unroll
+    for (int i = 0; i < 16; ++i)
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (att_lds_ptr_t)(tile + ATT_K_BYTES + i * 1024), 16, vl, att_perm(8 * i) * vrow, 0, 0);
+  };
+  // the oldest 16 copies have landed (`more`: 16 younger ones are under way)
+  auto landed = [&](bool more) {
+    if (more) att_wait_vmcnt<16>();
+    else att_wait_vmcnt<0>();
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  // the wave's own LDS reads are done: what they read may be filled again
+  auto read = [&]() {
+    __builtin_amdgcn_s_waitcnt((15 << 0) | (3 << 14) | (7 << 4) | (0 << 8));  // lgkmcnt(0)
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+  };
 
   f32x4 o[F];
   float m = -INFINITY, l = 0.0f;  // reference (log2 units), the lane's part of the denominator
 #pragma unroll
   for (int f = 0; f < F; ++f) o[f] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 
+  if (i0 + wave < i1) {
+    copy_k(tiles.key<BKV>(i0 + wave));
+    copy_v(tiles.key<BKV>(i0 + wave));
+  }
   for (int idx = i0 + wave; idx < i1; idx += 4) {
     const int key0 = tiles.key<BKV>(idx);
-    const bool edge = idx < tiles.edge;
+    const bool edge = idx < tiles.edge, more = idx + 4 < i1;
+    const int next = more ? tiles.key<BKV>(idx + 4) : 0;
     const int last = seq.klen - 1 - key0;  // the last key's place in the tile (or past it)
-    // K rows past the last key read as zero, V^T columns as whatever is there (cleared below)
-    // or, past the head's last row, as zero
-    const __amdgpu_buffer_rsrc_t rsK = __builtin_amdgcn_make_buffer_rsrc(
-        (void*)(kbase + (int64_t)key0 * krow), (short)0, (int)(min(BKV, last + 1) * krow), 0x00020000);
-    const uint8_t* const vt = vbase + (int64_t)key0 * 2;
-    const __amdgpu_buffer_rsrc_t rsV =
-        __builtin_amdgcn_make_buffer_rsrc((void*)vt, (short)0, (int)(D * vrow - 2 * key0), 0x00020000);
-    u32x4 kf[BKV / 16][D / 32], vf[F][BKV / 32];
+    landed(true);                          // K; V^T is under way
+    // all fragments, then the products: read one by one each would wait for LDS
+    u32x4 kf[BKV / 16][D / 32];
 #pragma unroll
-    for (int i = 0; i < BKV / 16; ++i)
+    for (int kc = 0; kc < D / 32; ++kc)
 #pragma unroll
-      for (int kc = 0; kc < D / 32; ++kc)
-        kf[i][kc] = __builtin_amdgcn_raw_buffer_load_b128(rsK, kl + 64 * kc, att_perm(16 * i) * krow, 0);
-#pragma unroll
-    for (int f = 0; f < F; ++f)
-#pragma unroll
-      for (int c = 0; c < BKV / 32; ++c)
-        vf[f][c] = __builtin_amdgcn_raw_buffer_load_b128(rsV, vl + 64 * c, att_perm(16 * f) * vrow, 0);
+      for (int i = 0; i < BKV / 16; ++i) kf[i][kc] = *(const u32x4*)(tile + 4096 * i + (ko ^ (uint32_t)(64 * kc)));
+    __builtin_amdgcn_sched_barrier(0);
     f32x4 s[BKV / 16];
 #pragma unroll
-    for (int i = 0; i < BKV / 16; ++i) {
-      s[i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    for (int kc = 0; kc < D / 32; ++kc)
 #pragma unroll
-      for (int kc = 0; kc < D / 32; ++kc)
-        s[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kf[i][kc]), qf[kc], s[i], 0, 0, 0);
-    }
+      for (int i = 0; i < BKV / 16; ++i)
+        s[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kf[i][kc]), qf[kc],
+                                                       kc ? s[i] : f32x4{0.0f, 0.0f, 0.0f, 0.0f}, 0, 0, 0);
+    read();
+    if (more) copy_k(next);
     if (edge) {
       WinMask<1> mk = mask;
       mk.key0 = key0;
@@ -525,6 +563,14 @@ __global__ __launch_bounds__(256, 2) void window_rows_kernel(WinArgs a) {
         // the denominator adds the weights as rounded for the product with V
         l += __uint_as_float(pw[c][e] << 16) + __uint_as_float(pw[c][e] & 0xffff0000u);
       }
+    landed(more);  // V^T
+    const uint8_t* const vt = tile + ATT_K_BYTES;
+    u32x4 vf[F][BKV / 32];
+#pragma unroll
+    for (int c = 0; c < BKV / 32; ++c)
+#pragma unroll
+      for (int f = 0; f < F; ++f) vf[f][c] = *(const u32x4*)(vt + f * 16 * ATT_VROW + (vo ^ (uint32_t)(64 * c)));
+    bool weigh = false;
     if (edge) {
       // V^T past the last key is cleared, and what else is not finite and may be hidden from
       // some row is weighed key by key
@@ -533,41 +579,46 @@ __global__ __launch_bounds__(256, 2) void window_rows_kernel(WinArgs a) {
       for (int c = 0; c < BKV / 32; ++c)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          const int left = last + 1 - (32 * c + 8 * g + 2 * e);
-          const uint32_t keep = left > 1 ? 0xffffffffu : (left > 0 ? 0xffffu : 0u);
+          const uint32_t keep = win_keep(last + 1 - (32 * c + 8 * g + 2 * e));
 #pragma unroll
           for (int f = 0; f < F; ++f) {
             vf[f][c][e] &= keep;
             top = __builtin_elementwise_max(top, __builtin_bit_cast(u16x2, vf[f][c][e] & 0x7f807f80u));
           }
         }
-      if (__ballot(top[0] == 0x7f80 || top[1] == 0x7f80)) {
-        const int ln = att_lane();  // the offsets below are formed here, not kept across the tiles
-#pragma unroll 1
-        for (int key = 0; key < min(BKV, last + 1); ++key) {
-          const u32x4 own = key < 32 ? pw[0] : pw[1];
-          const int e = (key >> 1) & 3;
-          const uint32_t w = e == 0 ? own[0] : (e == 1 ? own[1] : (e == 2 ? own[2] : own[3]));
-          const uint32_t got = __builtin_amdgcn_ds_bpermute(((ln & 15) + 16 * ((key >> 3) & 3)) << 2, (int)w);
-          const float p = __uint_as_float(key & 1 ? got & 0xffff0000u : got << 16);
-#pragma unroll
-          for (int f = 0; f < F; ++f)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-              const float v = bf2f(*(const bf16_t*)(vt + att_perm(16 * f + 4 * (ln >> 4) + r) * vrow + 2 * key));
-              o[f][r] = p != 0.0f ? fmaf(p, v, o[f][r]) : o[f][r];
-            }
-        }
-        continue;
-      }
+      weigh = __ballot(top[0] == 0x7f80 || top[1] == 0x7f80) != 0;
     }
+    if (weigh) {
+      const int ln = att_lane();
+#pragma unroll 1
+      for (int key = 0; key < BKV; ++key) {
+        const u32x4 own = key < 32 ? pw[0] : pw[1];
+        const int e = (key >> 1) & 3;
+        const uint32_t w = e == 0 ? own[0] : (e == 1 ? own[1] : (e == 2 ? own[2] : own[3]));
+        const uint32_t got = __builtin_amdgcn_ds_bpermute(((ln & 15) + 16 * ((key >> 3) & 3)) << 2, (int)w);
+        const float p = __uint_as_float(key & 1 ? got & 0xffff0000u : got << 16);
+        const uint32_t on = p != 0.0f ? 0xffffffffu : 0u;  // V times 0 where the weight is 0
 #pragma unroll
-    for (int c = 0; c < BKV / 32; ++c)
+        for (int f = 0; f < F; ++f)
 #pragma unroll
-      for (int f = 0; f < F; ++f)
-        o[f] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, vf[f][c]),
-                                                       __builtin_bit_cast(bf16x8, pw[c]), o[f], 0, 0, 0);
+          for (int r = 0; r < 4; ++r) {
+            const int vr = 16 * f + 4 * (ln >> 4) + r;
+            const uint32_t v = *(const bf16_t*)(vt + vr * ATT_VROW + (((key >> 3) ^ att_vswz(vr)) << 4) + 2 * (key & 7));
+            o[f][r] = fmaf(p, __uint_as_float((v << 16) & on), o[f][r]);
+          }
+      }
+    } else {
+#pragma unroll
+      for (int c = 0; c < BKV / 32; ++c)
+#pragma unroll
+        for (int f = 0; f < F; ++f)
+          o[f] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, vf[f][c]),
+                                                         __builtin_bit_cast(bf16x8, pw[c]), o[f], 0, 0, 0);
+    }
+    read();
+    if (more) copy_v(next);
   }
+  __syncthreads();  // the tiles' space takes the sums
 
   // join the four waves: each takes two of the eight 16-channel blocks
   l += __shfl_xor(l, 16);
@@ -688,12 +739,13 @@ struct WinF32 {
 #pragma unroll 1
           for (int gg = 0; gg < 4; ++gg) {
             const float p = __shfl(x[e], jq + 16 * gg);
+            const uint32_t on = p != 0.0f ? 0xffffffffu : 0u;  // V times 0 where the weight is 0
 #pragma unroll
             for (int c = 0; c < C; ++c)
 #pragma unroll
               for (int i = 0; i < 4; ++i) {
-                const float v = __shfl(vf[c][e], 4 * g + i + 16 * gg);
-                o[c][i] = p != 0.0f ? fmaf(p, v, o[c][i]) : o[c][i];
+                const uint32_t v = __float_as_uint(__shfl(vf[c][e], 4 * g + i + 16 * gg));
+                o[c][i] = fmaf(p, __uint_as_float(v & on), o[c][i]);
               }
           }
         return;
@@ -1022,13 +1074,17 @@ static int64_t win_span(const track_window& w, int64_t rows, int n, int64_t Lk) 
   return std::min(Lk, groups * w.group + w.sink);
 }
 
-// Shares of the keys for few rows, `blocks` row blocks of `tiles` tiles each.  Up to 8 tiles a
-// wave on a full chip, a workgroup on every CU, but two tiles a share; beyond, six workgroups
-// a CU with 16 tiles at least, which evens out lengths.  One token, 8 key heads of 4096 keys: 59 us
-// with one share, 14.1 with 8, 11.2 with 16, 9.3 with 32, 10.2 with 64; 32 of 1027: 18.9 with 1,
-// 11.1 with 5, 10.4 with 8, 12.2 with 16; 8 of 16384: 17.8 with 32, 18.9 with 64; 48 of 32760: 198
-// with 8, 163 with 16, 148 with 32; 64 of 100003: 613 with 8, 590 with 12, 582 with 32.
+// Shares of the keys for few rows, `blocks` row blocks of `tiles` tiles each.  None up to 16
+// tiles, four a wave: the join is a launch more (calls one after another, 8 heads of 1024 keys: 9.1
+// us with one share, 11.1 with 2 or more; 2048: 14.4, 12.1 with 2, 11.1 with 4).  Then up to 8
+// tiles a wave on a full chip a workgroup on every CU, but two tiles a share; beyond, six
+// workgroups a CU with 16 tiles at least, which evens out lengths.  Kernel times, 8 key heads of
+// 4096 keys: 24.9 us with one share, 10.0 with 8, 8.9 with 16, 8.4 with 32, 12.4 with 48; 32 of
+// 1027: 11.8 with 1, 9.6 with 6, 13.8 with 12; 8 of 16384: 17.8 with 16, 17.1 with 32, 20.6 with
+// 48; 48 of 32760: 158 with 4, 152 with 16, 138 with 32; 64 of 100003: 571 with 6, 541 with 16, 538
+// with 32.
 static int rows_split(int64_t tiles, int64_t blocks, int64_t cus) {
+  if (tiles <= 16) return 1;
   const bool large = blocks * tiles >= 64 * cus;
   const int64_t s = large ? std::min((6 * cus + blocks - 1) / blocks, tiles / 16) : std::min(cus / blocks, (tiles + 1) / 2);
   return (int)std::max<int64_t>(1, s);
