@@ -363,8 +363,30 @@ __global__ __launch_bounds__(512) void window_blocks_kernel(WinArgs a) {
         barrier();
       }
     }
+    // the tiles seen whole, the next one's address formed from this one's: they lie one after
+    // another but for the step from the first tokens to the window
+    const int jump = tiles.edge + tiles.fs;
+    const bf16_t* kp = kbase + tiles.key<BKV>(ie) * a.ldk;
+    uint32_t vp = 2 * (uint32_t)tiles.key<BKV>(ie);
+    const bf16_t* const kj = kbase + tiles.key<BKV>(jump) * a.ldk;
+    const uint32_t vj = 2 * (uint32_t)tiles.key<BKV>(jump);
+    const int64_t kstep = BKV * a.ldk;
+    const __amdgpu_buffer_rsrc_t rsV =
+        __builtin_amdgcn_make_buffer_rsrc((void*)vbase, (short)0, (int)(uint32_t)(D * a.ldv * 2), 0x00020000);
     for (int idx = ie; idx < i1; ++idx) {
-      issue(tiles.key<BKV>(min(idx + 1, i1 - 1)), slot ^ SLOT);
+      if (idx + 1 < i1) {  // (past the share: this tile again)
+        kp = idx + 1 == jump ? kj : kp + kstep;
+        vp = idx + 1 == jump ? vj : vp + 2 * BKV;
+      }
+      const __amdgpu_buffer_rsrc_t rsK =
+          __builtin_amdgcn_make_buffer_rsrc((void*)kp, (short)0, (int)(uint32_t)(kstep * 2), 0x00020000);
+      uint8_t* const to = smem + (slot ^ SLOT) + wave * 2048;
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(rsK, (att_lds_ptr_t)(to + i * 1024), 16, koffg[i], 0, 0, 0);
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(rsV, (att_lds_ptr_t)(to + ATT_K_BYTES + i * 1024), 16, voffg[i], vp, 0, 0);
       if (live) att_tile_masked<AttAll, QLOG2, 4, true, false>(smem, qf, ko, vo, st, AttAll{}, a.scale_log2);
       next();
     }
