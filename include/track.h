@@ -408,7 +408,7 @@ typedef struct track_window {
   int64_t left, right;  /* groups before and after the query's own; -1: no limit */
   int64_t sink;         /* first tokens that stay visible, >= 0 */
   int64_t group;        /* tokens of a group, >= 1 */
-  double  scale;        /* of the logits; 0: 1 / sqrt(head_dim).  ln 2 takes log2 queries (as track_op_attention_log2q) */
+  double  scale;        /* of the logits, 1e-30 .. 1e30; 0: 1 / sqrt(head_dim).  ln 2 takes log2 queries (as track_op_attention_log2q) */
 } track_window;
 
 /* Workspace of the call below in bytes, 0 where it needs none, -1 for what it
@@ -421,7 +421,9 @@ int64_t track_attention_window_workspace_bytes(int32_t dtype, const track_window
  * h / (H/Hk)).  Row i of q for sequence b is q[b*sq + i*ldq + h*head_dim + c],
  * likewise k with Hk heads, ldk, sk, and out; v is given transposed,
  * vt[b*sv + (h*head_dim + c)*ldv + key] (a cache that track_op_linear_vt
- * appends to), ldv >= Lk.  sk = sv = 0: keys that all sequences share.
+ * appends to), ldv >= Lk, its rows readable up to the multiple of 16 bytes at
+ * or past key Lk.  sk = sv = 0: keys that all sequences share.  out overlaps
+ * none of the inputs, and its sequences not each other.
  * Lq, Lk: the most queries and keys of a sequence.  q_len, k_len (device int32
  * [B], cut to [0, Lq] and [0, Lk]; NULL: all) and q_start (device int32 [B];
  * NULL: k_len - q_len, the queries are the newest tokens) are read when the

@@ -895,7 +895,9 @@ static track_status op_rope(const char* what, int32_t dtype, const track_rope_co
     if (r->heads < 1 || r->ldx < width || r->ldy < width || r->sx < 0 || r->sy < 0)
       return fail(TRACK_E_SHAPE, "%s: rows of %lld and %lld elements for %d heads of %d", what, (long long)r->ldx,
                   (long long)r->ldy, r->heads, cfg->head_dim);
-    if (B > 1 && L > 0 && r->sy < width) return fail(TRACK_E_SHAPE, "%s: sequences overlap in the output", what);
+    // sequences after each other, or their rows in turn
+    if (B > 1 && L > 0 && r->sy < (L - 1) * r->ldy + width && (r->sy < width || r->ldy < (B - 1) * r->sy + width))
+      return fail(TRACK_E_SHAPE, "%s: sequences overlap in the output", what);
     if (B * L == 0) continue;
     if (!r->x || !r->y) return fail(TRACK_E_INVALID, "%s: null pointer", what);
     if (((uintptr_t)r->x | (uintptr_t)r->y) & mask) return fail(TRACK_E_INVALID, "%s: rows are not aligned to their elements", what);

@@ -58,6 +58,7 @@ struct WinArgs {
   int nrb, nsplit;    // row blocks, shares of the keys
   WinDiv by_group, by_n, by_nrb, by_nsplit, by_Hk;
   WinDiv by_inner;    // sequences of a head, or heads of a sequence (win_place)
+  int64_t vend;       // elements of a head's V^T up to its last row's last key, rounded up to 16 bytes
   float scale_log2;
   float* po;          // [nsplit][B][Hk][Lq n][D]: a share's sums
   float2* pml;        // [nsplit][B][Hk][Lq n]: its reference (log2 units) and its denominator
@@ -278,7 +279,7 @@ __global__ __launch_bounds__(512) void window_blocks_kernel(WinArgs a) {
     const __amdgpu_buffer_rsrc_t rsK = __builtin_amdgcn_make_buffer_rsrc(
         (void*)(kbase + key0 * a.ldk), (short)0, (int)(uint32_t)(min(BKV, seq.klen - key0) * a.ldk * 2), 0x00020000);
     const __amdgpu_buffer_rsrc_t rsV = __builtin_amdgcn_make_buffer_rsrc(
-        (void*)(vbase + key0), (short)0, (int)(uint32_t)((D * a.ldv - key0) * 2), 0x00020000);
+        (void*)(vbase + key0), (short)0, (int)(uint32_t)((a.vend - key0) * 2), 0x00020000);
 #pragma unroll
     for (int i = 0; i < 2; ++i)
       __builtin_amdgcn_raw_ptr_buffer_load_lds(rsK, (att_lds_ptr_t)(smem + slot + wave * 2048 + i * 1024), 16, koffg[i], 0, 0, 0);
@@ -372,7 +373,7 @@ __global__ __launch_bounds__(512) void window_blocks_kernel(WinArgs a) {
     const uint32_t vj = 2 * (uint32_t)tiles.key<BKV>(jump);
     const int64_t kstep = BKV * a.ldk;
     const __amdgpu_buffer_rsrc_t rsV =
-        __builtin_amdgcn_make_buffer_rsrc((void*)vbase, (short)0, (int)(uint32_t)(D * a.ldv * 2), 0x00020000);
+        __builtin_amdgcn_make_buffer_rsrc((void*)vbase, (short)0, (int)(uint32_t)(a.vend * 2), 0x00020000);
     for (int idx = ie; idx < i1; ++idx) {
       if (idx + 1 < i1) {  // (past the share: this tile again)
         kp = idx + 1 == jump ? kj : kp + kstep;
@@ -498,7 +499,7 @@ __global__ __launch_bounds__(256) void window_rows_kernel(WinArgs a) {
   };
   auto copy_v = [&](int key0) {
     const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc(
-        (void*)(vbase + (int64_t)key0 * 2), (short)0, (int)(D * vrow - 2 * key0), 0x00020000);
+        (void*)(vbase + (int64_t)key0 * 2), (short)0, (int)(uint32_t)((a.vend - key0) * 2), 0x00020000);
 #pragma unroll
     for (int i = 0; i < 16; ++i)
       __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (att_lds_ptr_t)(tile + ATT_K_BYTES + i * 1024), 16, vl, att_perm(8 * i) * vrow, 0, 0);
@@ -915,7 +916,7 @@ __global__ __launch_bounds__(64 * WIN_F32_WAVES) void window_f32_tiles_kernel(Wi
     const __amdgpu_buffer_rsrc_t rsK = __builtin_amdgcn_make_buffer_rsrc(
         (void*)(kbase + key0 * a.ldk), (short)0, (int)(uint32_t)(min(TK, seq.klen - key0) * a.ldk * 4), 0x00020000);
     const __amdgpu_buffer_rsrc_t rsV = __builtin_amdgcn_make_buffer_rsrc(
-        (void*)(vbase + key0), (short)0, (int)(uint32_t)((D * a.ldv - key0) * 4), 0x00020000);
+        (void*)(vbase + key0), (short)0, (int)(uint32_t)((a.vend - key0) * 4), 0x00020000);
 #pragma unroll
     for (int i = 0; i < NI; ++i)
       win_copy(rsK, smem + slot + (wave * NI + i) * 1024, koff[i]);
@@ -1169,7 +1170,7 @@ static track_status win_check(int dtype, const track_window* w, int B, int H, in
   if (!w) return fail(TRACK_E_INVALID, "attention_window: null window");
   if (dtype != TRACK_DTYPE_F32 && dtype != TRACK_DTYPE_BF16)
     return fail(TRACK_E_INVALID, "attention_window: bad dtype %d", dtype);
-  if (w->group < 1 || w->sink < 0 || w->left < -1 || w->right < -1 || !(w->scale >= 0.0) || !(w->scale < 1e30))
+  if (w->group < 1 || w->sink < 0 || w->left < -1 || w->right < -1 || !(w->scale == 0.0 || (w->scale >= 1e-30 && w->scale <= 1e30)))
     return fail(TRACK_E_INVALID, "attention_window: window of %lld / %lld groups of %lld, %lld first tokens, scale %g",
                 (long long)w->left, (long long)w->right, (long long)w->group, (long long)w->sink, w->scale);
   if (w->left > WIN_MAX || w->right > WIN_MAX || w->group > WIN_MAX || w->sink > WIN_MAX)
@@ -1204,7 +1205,8 @@ track_status attention_window(int dtype, const track_window* w, int B, int H, in
   const int n = H / Hk;
   if (ldq < (int64_t)H * D || ldo < (int64_t)H * D || ldk < (int64_t)Hk * D || ldv < Lk)
     return fail(TRACK_E_SHAPE, "attention_window: leading dimension too small");
-  if (sq < 0 || sk < 0 || sv < 0 || so < 0 || (B > 1 && so < (Lq - 1) * ldo + (int64_t)H * D))
+  const int64_t wo = (int64_t)H * D;  // sequences after each other, or their rows in turn
+  if (sq < 0 || sk < 0 || sv < 0 || so < 0 || (B > 1 && so < (Lq - 1) * ldo + wo && (so < wo || ldo < (B - 1) * so + wo)))
     return fail(TRACK_E_SHAPE, "attention_window: sequences overlap in out, or a negative stride");
   if (((uintptr_t)lse | (uintptr_t)q_len | (uintptr_t)k_len | (uintptr_t)q_start) & 3)
     return fail(TRACK_E_INVALID, "attention_window: lse and lengths need 4-byte alignment");
@@ -1233,6 +1235,8 @@ track_status attention_window(int dtype, const track_window* w, int B, int H, in
   a.lse = lse, a.q_len = q_len, a.k_len = k_len, a.q_start = q_start;
   a.before = w->left < 0 ? INT32_MAX : (int)std::min<int64_t>(w->left * w->group, INT32_MAX);
   a.past = w->right < 0 ? INT32_MAX : (int)std::min<int64_t>((w->right + 1) * w->group, INT32_MAX);
+  const int64_t piece = dtype == TRACK_DTYPE_BF16 ? 8 : (vec ? 4 : 1);
+  a.vend = (D - 1) * ldv + (Lk + piece - 1) / piece * piece;
   a.lift = (int)((2 * WIN_MAX + w->group - 1) / w->group * w->group);
   a.sink = (int)w->sink;
   a.B = B, a.Hk = Hk, a.n = n, a.Lq = (int)Lq, a.Lk = (int)Lk;

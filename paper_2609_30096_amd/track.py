@@ -485,6 +485,9 @@ class RopeConfig:
         sec = (rot // 2,) if self.sections is None else tuple(self.sections)
         if len(sec) > 3:
             raise ValueError("rotary positions have at most 3 axes")
+        if self.layout not in ROPE_LAYOUTS or self.scaling not in ROPE_SCALINGS:
+            raise ValueError(f"layout {self.layout!r} of {list(ROPE_LAYOUTS)}, scaling {self.scaling!r} of "
+                             f"{list(ROPE_SCALINGS)}")
         return RopeConfigC(self.head_dim, rot, ROPE_LAYOUTS[self.layout], len(sec),
                            (ctypes.c_int32 * 3)(*sec), ROPE_SCALINGS[self.scaling], self.base, self.factor,
                            self.orig_len, self.beta_fast, self.beta_slow)
@@ -528,7 +531,8 @@ def _like(t, other, what):
 
 def _ints(t, shape, ref, what):
     """An int32 tensor of the given shape, contiguous, on ref's device (None passes)."""
-    if t is not None and (t.shape != shape or str(t.dtype) != "torch.int32" or not t.is_contiguous() or t.get_device() != ref.get_device()):
+    if t is not None and (t.shape != shape or str(t.dtype) != "torch.int32" or not t.is_contiguous() or
+                          t.get_device() != ref.get_device()):
         raise ValueError(f"{what}: contiguous int32 {tuple(shape)} on {ref.device} expected")
 
 
@@ -690,6 +694,8 @@ def _check_window(q, k, vt, out, lse, q_len, k_len, q_start, workspace):
     sv, s1, ldv, s3 = vt.stride()
     if ((s3 != 1 and vt.shape[3] > 1) or (s1 != D * ldv and Hk > 1)) and vt.numel():
         raise ValueError("vt: rows of keys, D of them a head, heads one after another")
+    if Lk == 0:  # no key is read, whatever strides an empty tensor has
+        ldk, sk, ldv, sv = Hk * D, 0, 8, 0
     for t, what in ((q_len, "q_len"), (k_len, "k_len"), (q_start, "q_start")):
         _ints(t, (B,), q, what)
     if lse is not None and (str(lse.dtype) != "torch.float32" or lse.shape != (B, H, Lq) or

@@ -96,6 +96,7 @@ def test_rope_refusals(L):
     assert call(c) == I
     assert call(B=-1) == S and call(Ln=-1) == S and call(B=1 << 20, Ln=1 << 20) == S
     assert call(B=1, Ln=1 << 28) == S  # more tokens than a launch holds
+    assert call(q=rows(sy=512 * 10 - 1, y=p + 4096)) == S  # sequences overlap by one element
     assert call(q=rows(heads=0)) == S and call(q=rows(ldx=511)) == S and call(q=rows(ldy=511)) == S
     assert call(q=rows(sx=-1)) == S and call(q=rows(y=p + 4096, sy=511)) == S
     assert call(q=rows(x=0)) == I and call(q=rows(x=p + 1)) == I and call(q=rows(y=p + 1)) == I
@@ -111,8 +112,9 @@ def test_rope_refusals(L):
     assert L.track_rope_freqs(ctypes.byref(_rope_c()), None, None) == I
     with pytest.raises(track.TrackError):
         track.rope_freqs(track.RopeConfig(head_dim=128, sections=(10,)))
-    with pytest.raises(ValueError):
-        track.RopeConfig(head_dim=128, sections=(16, 16, 16, 16)).c()
+    for bad in (dict(sections=(16, 16, 16, 16)), dict(layout="whole"), dict(scaling="dynamic")):
+        with pytest.raises(ValueError):
+            track.RopeConfig(head_dim=128, **bad).c()
     assert np.all(out == 0)
 
 
@@ -135,7 +137,8 @@ def test_window_refusals(L):
     W = track.Window
     assert L.track_op_attention_window(E, None, *([1] * 6), *([None, 1, 1] * 4), *([None] * 5), 0, None) == I
     assert call(dtype=2) == I
-    for w in (W(group=0), W(sink=-1), W(left=-2), W(right=-2), W(scale=-1.0), W(scale=math.nan), W(scale=math.inf)):
+    for w in (W(group=0), W(sink=-1), W(left=-2), W(right=-2), W(scale=-1.0), W(scale=math.nan), W(scale=math.inf),
+              W(scale=1e-31), W(scale=1e31)):
         assert call(win=w) == I, w
     for w in (W(group=1 << 31), W(sink=1 << 31), W(left=1 << 31), W(right=1 << 31)):
         assert call(win=w) == S, w
@@ -149,6 +152,7 @@ def test_window_refusals(L):
     assert call(ldq=1016) == S and call(ldk=504) == S and call(ldo=1016) == S and call(ldv=4992) == S
     assert call(ldq=1028) == I and call(ldk=516) == I and call(sk=512 * 5000 + 4) == I and call(ldv=5004) == I
     assert call(sq=-8) == S and call(so=512) == S
+    assert call(Lq=3, so=3 * 1024 - 8) == S and call(Lq=3, ldo=2040, so=1024) == S  # sequences overlap
     assert call(ldk=(1 << 23) + 8) == S and call(ldv=(1 << 23) + 8) == S
     assert call(lse=p + 2) == I and call(q_len=p + 1) == I and call(k_len=p + 1) == I and call(q_start=p + 1) == I
     need = track.attention_window_workspace_bytes(W(), E, 2, 8, 4, 128, 1, 5000)
@@ -579,6 +583,81 @@ def test_window_strides(dtype):
     kc, vcc = ks.contiguous(), vs.contiguous()
     track.op_attention_window(win, c.tq, kc, vcc, full, workspace=track.attention_window_workspace(win, c.tq, kc))
     assert torch.equal(shared, full)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("Lq", [1, 3, 90])
+def test_window_no_keys(dtype, Lq):
+    """Caches without a key yet: zeros, and a log-sum-exp of -inf."""
+    import torch
+    q = torch.ones(2, Lq, 4, 128, device="cuda").to(track.torch_dtype(dtype))
+    k, vt = q.new_empty(2, 0, 2, 128), q.new_empty(2, 2, 128, 0)
+    out, lse = torch.full_like(q, 3.0), torch.zeros(2, 4, Lq, device="cuda")
+    track.op_attention_window(W(), q, k, vt, out, lse=lse, workspace=track.attention_window_workspace(W(), q, k))
+    assert bool((out == 0).all()) and bool((lse == -math.inf).all())
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("Lq", [1, 70])
+def test_sequences_in_turn(dtype, Lq):
+    """Rows of the sequences in turn ([tokens, sequences, ..] seen as [sequences, tokens, ..]) for all three operators:
+    the same bits as for one sequence after another."""
+    import torch
+    B, H, Hk, Lk, D = 3, 4, 2, 300, 128
+    c = Case(dtype, B, H, Hk, Lq, Lk)
+    def turn(t):
+        return t.transpose(0, 1).contiguous().transpose(0, 1)
+    rope = track.Rope(track.RopeConfig(head_dim=D))
+    g = torch.ones(D, dtype=c.tq.dtype, device="cuda")
+    pos = torch.arange(B * Lq, dtype=torch.int32, device="cuda").view(1, B, Lq)
+    a, b = c.tq.clone(), turn(c.tq)
+    track.op_headnorm_rope(rope, a, None, g, None, pos)
+    track.op_headnorm_rope(rope, b, None, g, None, pos)
+    assert torch.equal(a, b)
+    track.op_rope(rope, a, None, pos)
+    track.op_rope(rope, b, None, pos)
+    assert torch.equal(a, b)
+    win = W(left=120, sink=2)
+    c.tq.copy_(a)
+    want, _ = c.run(win)
+    out, k = turn(c.out.clone()), turn(c.tk)[:, :Lk]
+    track.op_attention_window(win, b, k, c.tv, out, workspace=track.attention_window_workspace(win, b, k))
+    assert np.array_equal(host(out), want)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("Lq", [4, 300])
+def test_window_query_not_finite(dtype, Lq):
+    """A query that is not finite gives NaN to its own row alone."""
+    c = Case(dtype, 1, 2, 2, Lq, 500)
+    win = W(left=77, sink=3)
+    c.tq[0, 2, 1, 7] = float("nan")
+    got, lse = c.run(win)
+    assert np.isnan(got[0, 2, 1]).all() and np.isnan(lse[0, 1, 2])
+    rows = np.array([i for i in range(Lq) if i != 2])
+    _check(c, win, got, lse, rows=rows)
+
+
+@gpu
+@pytest.mark.parametrize("Lq", [1, 90])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_window_cache_ends_with_its_keys(dtype, Lq):
+    """The last V^T row of the last head ends with its keys (rounded up to 16 bytes), the memory behind it is not part
+    of any result: the same bits whatever lies there."""
+    import torch
+    B, H, Hk, D, Lk = 1, 2, 2, 128, 133
+    win = W(left=90)
+    c = Case(dtype, B, H, Hk, Lq, Lk, cap=136, poison=0.0)
+    want, _ = c.run(win)
+    n = Hk * D * 136
+    flat = torch.full((n + 4096,), float("nan"), dtype=c.tq.dtype, device="cuda")
+    flat[:n] = c.tv.reshape(-1)
+    c.tv = flat[:n].view(B, Hk, D, 136)
+    got, _ = c.run(win)
+    assert np.array_equal(got, want)
 
 
 @gpu
