@@ -35,9 +35,8 @@ struct WinDiv {
 };
 
 static WinDiv win_div(int64_t d) {
-  uint32_t s = 0;
-  while (((int64_t)1 << s) < d) ++s;
   if (d == 1) return WinDiv{1, 0, 0};
+  const uint32_t s = 32 - (uint32_t)__builtin_clz((uint32_t)d - 1);  // ceil(log2 d)
   return WinDiv{(uint32_t)d, (uint32_t)((((uint64_t)1 << (31 + s)) + (uint64_t)d - 1) / (uint64_t)d), s - 1};
 }
 
@@ -853,22 +852,24 @@ struct WinF32 {
   }
 };
 
-// Many rows: 32 a workgroup of 8 waves, K and V^T tiles of 64 keys by DMA into a ring of two
-// slots in LDS.  Four waves have the same 16 rows and 16 keys of a tile each.  LDS rows keep
-// 16-byte units at unit ^ (row & 7), so that the 16 rows of a fragment meet no bank twice in a
-// phase.  What bounds it: the matrix cores (135 - 149 TFLOP/s sustained on this instruction) at
-// 87 - 92 TFLOP/s, the rest a tile's softmax and barrier.  2 x 8 heads, 1500 x 1500: 105 us at 64
-// channels (140 straight from memory), 215 at 128 (303); 8 heads of 64, 1501 queries on 304 keys
-// each 26.3 us (32.5).  With 4 waves instead of 8: 123 and 324 us; with four row groups of 16
-// rows, each wave all keys of a tile: 124 and 219, and twice as long where few rows are there.
-constexpr int WIN_F32_WAVES = 8, WIN_F32_ROWS = 32;
-template <int D, bool SPLIT>
-__global__ __launch_bounds__(64 * WIN_F32_WAVES) void window_f32_tiles_kernel(WinArgs a) {
-  constexpr int C = D / 16, W = WIN_F32_WAVES, TK = 64;
+// Many rows: tiles of 64 keys of K and V^T by DMA into LDS, 16 rows to each four of a workgroup's
+// W waves, which take 16 keys of a tile each.  LDS rows keep 16-byte units at unit ^ (row & 7), so
+// that the 16 rows of a fragment meet no bank twice in a phase.  8 waves share a ring of two
+// slots, the next tile on its way while this one is computed on; 4 waves have one slot and rely
+// on the other workgroups of their CU meanwhile, which are twice as many and half as large:
+// where the former do not fill the chip twice that counts more (win_plan).  What bounds
+// it: the matrix cores (135 - 149 TFLOP/s sustained on this instruction) at 87 - 92 TFLOP/s, the
+// rest a tile's softmax and barrier.  2 x 8 heads, 1500 x 1500: 103 us at 64 channels with 8 waves,
+// 117 with 4 (140 straight from memory), 213 and 213 at 128 (303); 8 heads of 64, 1501 queries on
+// 304 keys each 25.2 and 22.2 us (32.5); 8 of 128, 100 x 8000 63.9 and 56.4 (72).
+template <int D, int W, bool SPLIT>
+__global__ __launch_bounds__(64 * W) void window_f32_tiles_kernel(WinArgs a) {
+  static_assert(W == 4 || W == 8, "waves");
+  constexpr int C = D / 16, TK = 64, SLOTS = W / 4, ROWS = 4 * W;
   constexpr int KU = D / 4, VU = TK / 4;                   // 16-byte units of a K row, of a V^T row
   constexpr int HALF = TK * D * 4, SLOT = 2 * HALF;
   constexpr int NI = HALF / 1024 / W;                      // copies of 1 KB a wave, of K and of V^T
-  constexpr int SO = W * C * 1024, LDS = 2 * SLOT > SO + W * 128 ? 2 * SLOT : SO + W * 128;
+  constexpr int SO = W * C * 1024, LDS = SLOTS * SLOT > SO + W * 128 ? SLOTS * SLOT : SO + W * 128;
   // one object: with a second one the compiler waits for every copy under way before a tile's
   // first fragment read
   __shared__ __attribute__((aligned(1024))) uint8_t smem[LDS];
@@ -879,7 +880,7 @@ __global__ __launch_bounds__(64 * WIN_F32_WAVES) void window_f32_tiles_kernel(Wi
   win_place<true>(a, rb, sp, h, b);
   const WinSeq seq = win_seq(a, b);
   const int rows = seq.qlen * a.n;
-  const int r0 = rb * WIN_F32_ROWS;
+  const int r0 = rb * ROWS;
   if (r0 >= rows) return;  // the whole workgroup
   auto range_of = [&](int r, int& lo, int& hi) {
     win_range(a, seq, (int)a.by_n((uint32_t)min(r, rows - 1)), lo, hi);
@@ -888,7 +889,7 @@ __global__ __launch_bounds__(64 * WIN_F32_WAVES) void window_f32_tiles_kernel(Wi
   };
   int lo0, hi0, lo1, hi1;
   range_of(r0, lo0, hi0);
-  range_of(r0 + WIN_F32_ROWS - 1, lo1, hi1);
+  range_of(r0 + ROWS - 1, lo1, hi1);
   WinTiles tiles;
   tiles.init<TK>(seq, lo0, hi0, lo1, hi1);
   int i0 = 0, i1 = tiles.n;
@@ -936,9 +937,9 @@ __global__ __launch_bounds__(64 * WIN_F32_WAVES) void window_f32_tiles_kernel(Wi
     issue(tiles.key<TK>(i0), 0);
     barrier();
     int slot = 0;
-    for (int idx = i0; idx < i1; ++idx, slot ^= SLOT) {
+    for (int idx = i0; idx < i1; ++idx) {
       const int key0 = tiles.key<TK>(idx);
-      if (idx + 1 < i1) issue(tiles.key<TK>(idx + 1), slot ^ SLOT);
+      if (SLOTS == 2 && idx + 1 < i1) issue(tiles.key<TK>(idx + 1), slot ^ SLOT);
       const bool edge = idx < tiles.edge;
       const int k0 = key0 + mine;
       if (live && (!edge || (k0 <= whi && (k0 + 16 > wlo || k0 < tiles.sink)))) {
@@ -948,14 +949,20 @@ __global__ __launch_bounds__(64 * WIN_F32_WAVES) void window_f32_tiles_kernel(Wi
                 [&](int c) { return *(const f32x4*)(vt + 16 * c * (TK * 4)); }, edge, k0, seq.klen, a.scale_log2);
       }
       barrier();
+      if constexpr (SLOTS == 2) {
+        slot ^= SLOT;
+      } else if (idx + 1 < i1) {
+        issue(tiles.key<TK>(idx + 1), 0);
+        barrier();
+      }
     }
   }
   st.template end<true, SPLIT>(a, b, h, sp, wr0 + jq, rows, (f32x4*)smem, (float*)(smem + SO));
 }
 
 // Straight from memory: few rows or keys, and rows that are not 16-byte aligned (VEC false:
-// loads of single elements).  The four waves share a row
-// block and take a fourth of its keys each, 16 a step, the next step's under way.
+// loads of single elements).  The four waves share a row block and take a fourth of its keys
+// each, 16 a step, the next step's under way.
 template <int D, bool VEC, bool SPLIT>
 __global__ __launch_bounds__(256) void window_f32_kernel(WinArgs a) {
   constexpr int C = D / 16, BKV = 16;
@@ -1085,7 +1092,7 @@ __global__ __launch_bounds__(256) void window_join_kernel(WinArgs a, int D) {
 
 // ---------------------------------------------------------------- host
 struct WinPlan {
-  enum Form { BLOCKS, ROWS, F32_ROWS, F32_TILES } form;
+  enum Form { BLOCKS, ROWS, F32_ROWS, F32_TILES4, F32_TILES8 } form;
   int64_t nrb;
   int nsplit;
 };
@@ -1120,12 +1127,14 @@ static int rows_split(int64_t tiles, int64_t blocks, int64_t cus) {
 // heads): 256 rows of 12 heads, 32760 keys 732 us with one share, 106 with 10, 69 with 21, 83
 // with 42; 400 rows of 40 heads, 2000 keys 53 with one, 38 with 3, 52 with 4.
 static int blocks_split(int64_t tiles, int64_t blocks, int64_t rows, int64_t cus) {
+  const uint32_t n = (uint32_t)tiles, most = std::max<uint32_t>(1, std::min<uint32_t>(n / 2, 64));
+  const double join = (double)(2 * rows * (4 * ATT_D + 8)) / 4e6;
   int best = 1;
   double best_t = 0.0;
-  for (int64_t s = 1; s <= std::max<int64_t>(1, std::min<int64_t>(tiles / 2, 64)); ++s) {
-    const double rounds = (double)((blocks * s + cus - 1) / cus);
-    double t = rounds * ((double)((tiles + s - 1) / s) * 1.6 + 5.0);
-    if (s > 1) t += 3.0 + (double)(2 * s * rows * (4 * ATT_D + 8)) / 4e6;
+  for (uint32_t s = 1; s <= most && blocks * s <= 16 * cus; ++s) {  // (32-bit divisions: a call's own time)
+    const uint32_t rounds = ((uint32_t)blocks * s + (uint32_t)cus - 1) / (uint32_t)cus;
+    double t = rounds * ((n + s - 1) / s * 1.6 + 5.0);
+    if (s > 1) t += 3.0 + s * join;
     if (s == 1 || t < best_t) {
       best = (int)s;
       best_t = t;
@@ -1134,19 +1143,21 @@ static int blocks_split(int64_t tiles, int64_t blocks, int64_t rows, int64_t cus
   return best;
 }
 
-static WinPlan win_plan(int dtype, const track_window& w, int64_t B, int Hk, int n, int64_t Lq, int64_t Lk, bool vec) {
+static WinPlan win_plan(int dtype, const track_window& w, int64_t B, int Hk, int n, int D, int64_t Lq, int64_t Lk, bool vec) {
   const int64_t rows = Lq * n, cus = device_cus();
   WinPlan p;
   if (dtype == TRACK_DTYPE_F32) {
-    // the tiles kernel from 12000 steps of 16 rows and 16 keys on (8 heads of 64: 300 x 300,
-    // 2900 steps, 11.8 us straight and 12.7 by tiles; 1501 x 304, 15000, 32.5 and 26.3; 1000 x
-    // 1000, 31000, 31.3 and 30.4), shares of the keys up to two workgroups a CU
+    // the tiles kernel from 180000 steps of 16 rows, 16 keys and a channel on (8 heads, 300 x 300,
+    // 2900 steps: 32 channels 7.8 us straight and 8.4 by tiles, 64 11.4 and 11.1, 128 20.0 and 16.0; 64,
+    // 1501 x 304, 15000 steps, 32.5 and 22.2), with 8 waves where those make two workgroups a CU
+    // (above), shares of the keys up to that number
     p.nrb = (rows + 15) / 16;
     const int64_t steps = (win_span(w, std::min<int64_t>(rows, 16), n, Lk) + 15) / 16;
-    p.form = vec && p.nrb * Hk * B * steps >= 12000 && rows > 16 ? WinPlan::F32_TILES : WinPlan::F32_ROWS;
-    if (p.form == WinPlan::F32_TILES) p.nrb = (rows + WIN_F32_ROWS - 1) / WIN_F32_ROWS;
-    const int64_t most = p.form == WinPlan::F32_TILES ? steps / 16 : steps / 32;
-    p.nsplit = (int)std::max<int64_t>(1, std::min<int64_t>(2 * cus / (p.nrb * Hk * B), most));
+    const bool tiles = vec && p.nrb * Hk * B * steps * D >= 180000 && rows > 16;
+    const int64_t nrb8 = (rows + 31) / 32;
+    p.form = !tiles ? WinPlan::F32_ROWS : (nrb8 * Hk * B >= 2 * cus ? WinPlan::F32_TILES8 : WinPlan::F32_TILES4);
+    if (p.form == WinPlan::F32_TILES8) p.nrb = nrb8;
+    p.nsplit = (int)std::max<int64_t>(1, std::min<int64_t>(2 * cus / (p.nrb * Hk * B), tiles ? steps / 16 : steps / 32));
     return p;
   }
   if (rows <= 16) {
@@ -1189,7 +1200,7 @@ int64_t attention_window_bytes(int dtype, const track_window* w, int B, int H, i
   if (B == 0 || Lq == 0) return 0;
   size_t bytes = 0;
   for (bool vec : {true, false})  // whatever the rows' alignment turns out to be
-    bytes = std::max(bytes, win_bytes(win_plan(dtype, *w, B, Hk, H / Hk, Lq, Lk, vec), B, Hk, H / Hk, D, Lq));
+    bytes = std::max(bytes, win_bytes(win_plan(dtype, *w, B, Hk, H / Hk, D, Lq, Lk, vec), B, Hk, H / Hk, D, Lq));
   return (int64_t)bytes;
 }
 
@@ -1222,7 +1233,7 @@ track_status attention_window(int dtype, const track_window* w, int B, int H, in
     if (ptrs & 3) return fail(TRACK_E_INVALID, "attention_window: float32 path needs 4-byte aligned rows");
     vec = !(ptrs & 15) && !(strides & 3);
   }
-  const WinPlan p = win_plan(dtype, *w, B, Hk, n, Lq, Lk, vec);
+  const WinPlan p = win_plan(dtype, *w, B, Hk, n, D, Lq, Lk, vec);
   const size_t need = win_bytes(p, B, Hk, n, D, Lq);
   if (need && (!ws || ws_bytes < need)) return fail(TRACK_E_NOMEM, "attention_window: workspace of %zu bytes needed", need);
   if (need && ((uintptr_t)ws & 255)) return fail(TRACK_E_INVALID, "attention_window: workspace must be 256-byte aligned");
@@ -1252,10 +1263,9 @@ track_status attention_window(int dtype, const track_window* w, int B, int H, in
   const unsigned gr = (unsigned)grid;
 #define TRACK_WIN_F32(DH)                                                                             \
   do {                                                                                                \
-    if (p.form == WinPlan::F32_TILES && split)                                                        \
-      window_f32_tiles_kernel<DH, true><<<gr, 64 * WIN_F32_WAVES, 0, s>>>(a);                         \
-    else if (p.form == WinPlan::F32_TILES)                                                            \
-      window_f32_tiles_kernel<DH, false><<<gr, 64 * WIN_F32_WAVES, 0, s>>>(a);                        \
+    if (p.form == WinPlan::F32_TILES8) window_f32_tiles_kernel<DH, 8, false><<<gr, 512, 0, s>>>(a);   \
+    else if (p.form == WinPlan::F32_TILES4 && split) window_f32_tiles_kernel<DH, 4, true><<<gr, 256, 0, s>>>(a); \
+    else if (p.form == WinPlan::F32_TILES4) window_f32_tiles_kernel<DH, 4, false><<<gr, 256, 0, s>>>(a); \
     else if (vec && split) window_f32_kernel<DH, true, true><<<gr, 256, 0, s>>>(a);                   \
     else if (vec) window_f32_kernel<DH, true, false><<<gr, 256, 0, s>>>(a);                           \
     else if (split) window_f32_kernel<DH, false, true><<<gr, 256, 0, s>>>(a);                         \

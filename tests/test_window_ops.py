@@ -472,6 +472,7 @@ ATTN = [
     (1, 1, 1, 70, 4000, W(), {}),                                          # shares of the keys, blocks
     (1, 2, 1, 200, 9000, W(left=2500, sink=130), {}),
     (1, 1, 1, 257, 257, W(sink=1000), {}),
+    (2, 8, 8, 1040, 1040, W(left=300, sink=5), dict(q_len=[1040, 900], k_len=[1040, 1000])),  # more blocks than CUs hold
     # limits at the ends of their ranges
     (1, 2, 1, 100, 300, W(left=1 << 28, right=1 << 28, group=1 << 28, sink=1 << 28), {}),
     (1, 2, 1, 100, 300, W(left=0, right=0, group=1 << 28), {}),
