@@ -2,7 +2,7 @@
 // same pass: y = m A R(pos f) n(x), n(x) = x / sqrt(mean(x^2) + eps) g over a head (or x).
 //
 // Each element is read once and written once, so HBM bounds it (65520 tokens: 24 heads of 128
-// 141 us, 5.7 TB/s; 80 heads with the norm, out of fused rows, 511 us, 5.2 TB/s); what is left to
+// 133 us, 6.1 TB/s; 80 heads with the norm, out of fused rows, 494 us, 5.4 TB/s); what is left to
 // decide is how little else a wave does.  A wave takes one token and walks its heads (of q, then of
 // k).  It forms the token's angles itself, one pair a lane: the position times the float64
 // frequency in turns, reduced to half a turn in float64 (a float32 product is off by 0.06
@@ -28,7 +28,7 @@ namespace track {
 
 // Pairs of the widest head: one wave's angles in LDS.
 constexpr int ROPE_MAX_PAIRS = ROPE_MAX_DIM / 2;
-constexpr int ROPE_STEPS = 2;  // head groups whose loads a wave has under way together (4: up to 12% slower)
+constexpr int ROPE_STEPS = 2;  // head groups whose loads a wave has under way together (4: up to 13% slower, 2% faster at most)
 
 struct RopeArgs {
   const void* x[2];  // q, k
@@ -109,7 +109,8 @@ __device__ __forceinline__ float group_sum(float v, int n) {
 }
 
 // NU units a lane: 2 only where a head of more than 128 channels moves element by element.
-template <typename T, int V, int NU, bool NORM, bool HALF, bool STREAM>
+// PAST: 0 through the caches, 1 stores past them, 2 loads too (rope_heads).
+template <typename T, int V, int NU, bool NORM, bool HALF, int PAST>
 __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a) {
   typedef typename RopeVec<T, V>::type Raw;
   constexpr int ST = NU == 1 ? ROPE_STEPS : 1;
@@ -155,8 +156,13 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a) {
         hi[s][i] = Raw{};
         if (h < total && u0 + 64 * i < units) {
           const T* p = h < a.heads[0] ? xr[0] + (int64_t)h * a.D : xr[1] + (int64_t)(h - a.heads[0]) * a.D;
-          lo[s][i] = *(const Raw*)(p + e0[i]);
-          hi[s][i] = *(const Raw*)(p + e1[i]);
+          if constexpr (PAST > 1) {
+            lo[s][i] = __builtin_nontemporal_load((const Raw*)(p + e0[i]));
+            hi[s][i] = __builtin_nontemporal_load((const Raw*)(p + e1[i]));
+          } else {
+            lo[s][i] = *(const Raw*)(p + e0[i]);
+            hi[s][i] = *(const Raw*)(p + e1[i]);
+          }
         }
       }
     }
@@ -260,7 +266,7 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a) {
             }
           }
           const Raw rl = rope_pack<T, V>(xl[i]), rh = rope_pack<T, V>(xh[i]);
-          if constexpr (STREAM) {
+          if constexpr (PAST > 0) {
             __builtin_nontemporal_store(rl, (Raw*)(p + e0[i]));
             __builtin_nontemporal_store(rh, (Raw*)(p + e1[i]));
           } else {
@@ -281,12 +287,12 @@ static uint32_t rope_waves_per_token(int64_t tokens, int groups) {
   return (uint32_t)std::max<int64_t>(1, std::min<int64_t>(want, groups));
 }
 
-template <typename T, int V, int NU, bool STREAM>
+template <typename T, int V, int NU, int PAST>
 static void rope_launch(const RopeArgs& a, bool norm, bool half, unsigned grid, hipStream_t s) {
-  if (norm && half) rope_kernel<T, V, NU, true, true, STREAM><<<grid, 256, 0, s>>>(a);
-  else if (norm) rope_kernel<T, V, NU, true, false, STREAM><<<grid, 256, 0, s>>>(a);
-  else if (half) rope_kernel<T, V, NU, false, true, STREAM><<<grid, 256, 0, s>>>(a);
-  else rope_kernel<T, V, NU, false, false, STREAM><<<grid, 256, 0, s>>>(a);
+  if (norm && half) rope_kernel<T, V, NU, true, true, PAST><<<grid, 256, 0, s>>>(a);
+  else if (norm) rope_kernel<T, V, NU, true, false, PAST><<<grid, 256, 0, s>>>(a);
+  else if (half) rope_kernel<T, V, NU, false, true, PAST><<<grid, 256, 0, s>>>(a);
+  else rope_kernel<T, V, NU, false, false, PAST><<<grid, 256, 0, s>>>(a);
 }
 
 track_status rope_heads(int dtype, const track_rope_config& c, int64_t B, int64_t L, const track_head_rows& q,
@@ -338,8 +344,15 @@ track_status rope_heads(int dtype, const track_rope_config& c, int64_t B, int64_
   // is left half written between two stores: 16 heads of 64 channels 42 us, 46 past the caches;
   // with whole ones 2 x 4099 x 16 heads of 64 float32 channels 12.5 -> 10.1 us, 65520 x 24 heads
   // of 128 148 -> 142, 8192 x 48 heads 35.5 -> 35, float32 64-channel norms 91 -> 76.
-  const bool stream = V > 1 && (half ? a.pairs : a.D / 2) * es >= 128;
+  const bool lines = V > 1 && (half ? a.pairs : a.D / 2) * es >= 128;
   const int hp = 64 >> a.lph_log2, total = a.heads[0] + a.heads[1];
+  // Loads too where the heads are more than the 256 MB that the Infinity Cache holds, so that the
+  // call would push out its own.  Kept and past the caches, one buffer again and again, after 1 GiB
+  // written elsewhere, and with heads just written: 65520 x 24 heads of 128 (403 MB) 140 and 133 us,
+  // 192 and 138, 152 and 135; 80 heads with the norm 509 and 494, 559 and 499, 558 and 499.  Smaller ones
+  // may still be there: 20000 x 48 (246 MB) 73 and 88, 138 and 92, 75 and 75; 4680 x 24 (29 MB) 10.0 and 9.7,
+  // 19.4 and 15.0, 13.0 and 14.8.
+  const int past = !lines ? 0 : (tokens * total * a.D * es > ((int64_t)256 << 20) ? 2 : 1);
   a.wpt = rope_waves_per_token(tokens, (total + hp - 1) / hp);
   const int64_t grid = (tokens * a.wpt + 3) / 4;
   if (grid >= (int64_t)1 << 24)
@@ -347,16 +360,18 @@ track_status rope_heads(int dtype, const track_rope_config& c, int64_t B, int64_
   ProfScope prof(TRACK_PROF_NORM, s);
   const unsigned g1 = (unsigned)grid;
   if (es == 2) {
-    if (V == 8 && stream) rope_launch<bf16_t, 8, 1, true>(a, norm, half, g1, s);
-    else if (V == 8) rope_launch<bf16_t, 8, 1, false>(a, norm, half, g1, s);
-    else if (V == 4) rope_launch<bf16_t, 4, 1, false>(a, norm, half, g1, s);
-    else if (units <= 64) rope_launch<bf16_t, 1, 1, false>(a, norm, half, g1, s);
-    else rope_launch<bf16_t, 1, 2, false>(a, norm, half, g1, s);
+    if (past == 2 && V == 8) rope_launch<bf16_t, 8, 1, 2>(a, norm, half, g1, s);
+    else if (past && V == 8) rope_launch<bf16_t, 8, 1, 1>(a, norm, half, g1, s);
+    else if (V == 8) rope_launch<bf16_t, 8, 1, 0>(a, norm, half, g1, s);
+    else if (V == 4) rope_launch<bf16_t, 4, 1, 0>(a, norm, half, g1, s);
+    else if (units <= 64) rope_launch<bf16_t, 1, 1, 0>(a, norm, half, g1, s);
+    else rope_launch<bf16_t, 1, 2, 0>(a, norm, half, g1, s);
   } else {
-    if (V == 4 && stream) rope_launch<float, 4, 1, true>(a, norm, half, g1, s);
-    else if (V == 4) rope_launch<float, 4, 1, false>(a, norm, half, g1, s);
-    else if (units <= 64) rope_launch<float, 1, 1, false>(a, norm, half, g1, s);
-    else rope_launch<float, 1, 2, false>(a, norm, half, g1, s);
+    if (past == 2 && V == 4) rope_launch<float, 4, 1, 2>(a, norm, half, g1, s);
+    else if (past && V == 4) rope_launch<float, 4, 1, 1>(a, norm, half, g1, s);
+    else if (V == 4) rope_launch<float, 4, 1, 0>(a, norm, half, g1, s);
+    else if (units <= 64) rope_launch<float, 1, 1, 0>(a, norm, half, g1, s);
+    else rope_launch<float, 1, 2, 0>(a, norm, half, g1, s);
   }
   TRACK_LAUNCH_CHECK();
   return TRACK_OK;

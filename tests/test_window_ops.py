@@ -333,6 +333,41 @@ def test_rope_strided(dtype, off):
 
 
 @gpu
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("layout", ["half", "interleaved"])
+@pytest.mark.parametrize("norm", [False, True])
+def test_rope_more_than_the_caches_hold(dtype, layout, norm):
+    """Heads of more than 256 MB, which are read past the caches: bit for bit what calls on parts of the tokens give."""
+    import torch
+    B, H, Hk, D = 2, 70, 40, 128
+    Ln = 5003 if dtype == BF16 else 2503
+    t = torch.bfloat16 if dtype == BF16 else torch.float32
+    gen = torch.Generator(device="cuda").manual_seed(41)
+    q = torch.randn(B, Ln, H, D, device="cuda", generator=gen).to(t)
+    k = torch.randn(B, Ln, Hk, D, device="cuda", generator=gen).to(t)
+    assert q.nbytes + k.nbytes > 256 << 20
+    pos = torch.randint(0, 1 << 20, (1, B, Ln), dtype=torch.int32, device="cuda", generator=gen)
+    g = torch.randn(D, device="cuda", generator=gen).to(t)
+    rope = track.Rope(track.RopeConfig(head_dim=D, layout=layout))
+
+    def call(q, k, pos, qo, ko):
+        if norm:
+            track.op_headnorm_rope(rope, q, k, g, g, pos, qo, ko)
+        else:
+            track.op_rope(rope, q, k, pos, qo, ko)
+
+    wq, wk = torch.empty_like(q), torch.empty_like(k)
+    for i in range(0, Ln, 1000):
+        j = min(Ln, i + 1000)
+        call(q[:, i:j], k[:, i:j], pos[..., i:j].contiguous(), wq[:, i:j], wk[:, i:j])
+    qo, ko = torch.empty_like(q), torch.empty_like(k)
+    call(q, k, pos, qo, ko)
+    assert torch.equal(qo, wq) and torch.equal(ko, wk)
+    call(q, k, pos, q, k)  # in place
+    assert torch.equal(q, wq) and torch.equal(k, wk)
+
+
+@gpu
 def test_rope_far_positions_and_inverse():
     """At position 10^9 the angle still matches float64, and the inverse undoes the rotation."""
     import torch
@@ -675,6 +710,20 @@ def test_window_f32_unaligned():
     k = odd(c.tk)
     track.op_attention_window(win, odd(c.tq), k, odd(c.tv), out, workspace=track.attention_window_workspace(win, c.tq, k))
     assert np.array_equal(host(out), want)
+
+
+@gpu
+@pytest.mark.parametrize("dtype,H,Lq,Lk", [(BF16, 12, 120, 6000), (F32, 8, 150, 3000)])
+def test_window_shares_of_many_rows(dtype, H, Lq, Lk):
+    """Rows enough to fill the join by themselves, and shares of the keys all the same; a cut sequence beside a whole one."""
+    c = Case(dtype, 1, H, H, Lq, Lk)
+    win = W(left=-1, right=-1)
+    t = track.DTYPE_BF16 if dtype == BF16 else track.DTYPE_F32
+    assert track.attention_window_workspace_bytes(win, t, 1, H, H, 128, Lq, Lk) > 2 * H * Lq * (4 * 128 + 8)
+    for lens in ({}, dict(q_len=[Lq - 7], k_len=[Lk // 3 + 1])):
+        c.out.fill_(9.0), c.lse.fill_(9.0)
+        got, lse = c.run(win, **lens)
+        _check(c, win, got, lse, **lens)
 
 
 @gpu
