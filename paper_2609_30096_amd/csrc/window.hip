@@ -195,8 +195,8 @@ __device__ __forceinline__ uint32_t win_keep(int left) { return (uint32_t)((1ull
 // under a causal mask took 955 us instead of 824, 2 x 12 heads over a 21-frame video 5.2 ms
 // instead of 4.8), and the sequences follow each other inside a head, so that short ones do
 // not leave one XCD idle (4 sequences of 5000 to 3100 queries: 439 -> 385 us).  Single tokens use
-// a key once: they go over the XCDs in turn (8 sequences of 100003 to 56000 keys: 519 -> 466
-// us with an earlier kernel).  The last rows of a sequence, which see most keys under a causal
+// a key once and go over the XCDs in turn (48 x 32760 keys 143 us, 147 the other way; 8 of 100003
+// to 56000 keys 437 and 436).  The last rows of a sequence, which see most keys under a causal
 // mask, start first.
 template <bool LOCAL>
 __device__ __forceinline__ void win_place(const WinArgs& a, int& rb, int& sp, int& h, int& b) {
@@ -425,15 +425,22 @@ __global__ __launch_bounds__(512) void window_blocks_kernel(WinArgs a) {
 }
 
 // ---------------------------------------------------------------- few rows, bfloat16
+// Cache policy of the copies below: past the caches (the `nt` bit).  Each key is read once a call, so
+// keeping it only puts out what others left there.  Replays of one buffer, kept and past the
+// caches: 8 sequences of 100003 keys 548 and 490 us, 8 of 16384 101 and 89, 48 x 32760 143 and 128, 8
+// x 32760 27.0 and 26.9; after 1 GiB written elsewhere 609 and 496, 153 and 93, 201 and 132, 55 and 31;
+// with keys just written, 67 MB of them, 27.8 and 28.5 (the worst of nine sizes).
+constexpr int WIN_PAST = 2;
+
 // At most 16 rows a key head (a token of 16 query heads, four tokens of 4).  The four waves of
 // a workgroup take every fourth 64-key tile of its share, each through 32 KB of LDS of its own:
 // copies go by DMA in whole 128-byte lines (operands straight from memory, where adjacent lanes
 // read different rows, pass through the CU's cache 16 bytes a cycle: a tile kept a CU busy
 // for 1 us), and no wave waits for another before the sums meet at the end.  K's half is
 // filled again as soon as its tile's logits are formed, V^T's once its product is, so copies are
-// under way all the time.  What bounds it: reading K and V^T (8 sequences of 100003 keys 538 us,
-// 6.1 TB/s of the 6.5 that a plain read stream reaches; of 100003 to 56000 keys 466 -> 430), and
-// for short windows the latency of a tile and of the join (8 heads of 4096 keys 9.1 -> 8.4 us).
+// under way all the time.  What bounds it: reading K and V^T (8 sequences of 100003 keys 490 us,
+// 6.7 TB/s; 6.2 - 6.5 is what a plain read stream through the caches reaches), and for short windows the
+// latency of a tile and of the join (8 heads of 4096 keys 8.2 us).
 template <bool SPLIT>
 __global__ __launch_bounds__(256) void window_rows_kernel(WinArgs a) {
   constexpr int BKV = ATT_BKV, D = ATT_D, F = D / 16;
@@ -494,14 +501,14 @@ __global__ __launch_bounds__(256) void window_rows_kernel(WinArgs a) {
         (void*)(kbase + (int64_t)key0 * krow), (short)0, (int)(min(BKV, seq.klen - key0) * krow), 0x00020000);
 #pragma unroll
     for (int i = 0; i < 16; ++i)
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (att_lds_ptr_t)(tile + i * 1024), 16, kl[i & 3], att_perm(4 * i) * krow, 0, 0);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (att_lds_ptr_t)(tile + i * 1024), 16, kl[i & 3], att_perm(4 * i) * krow, 0, WIN_PAST);
   };
   auto copy_v = [&](int key0) {
     const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc(
         (void*)(vbase + (int64_t)key0 * 2), (short)0, (int)(uint32_t)((a.vend - key0) * 2), 0x00020000);
 #pragma unroll
     for (int i = 0; i < 16; ++i)
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (att_lds_ptr_t)(tile + ATT_K_BYTES + i * 1024), 16, vl, att_perm(8 * i) * vrow, 0, 0);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (att_lds_ptr_t)(tile + ATT_K_BYTES + i * 1024), 16, vl, att_perm(8 * i) * vrow, 0, WIN_PAST);
   };
   // the oldest 16 copies have landed (`more`: 16 younger ones are under way)
   auto landed = [&](bool more) {
@@ -1036,8 +1043,10 @@ __global__ __launch_bounds__(256) void window_f32_kernel(WinArgs a) {
 }
 
 // The shares of each row joined: D / 4 threads a row and G groups of them, each with every
-// G-th share, so that a token's few rows do not wait for one share after another (with one
-// group 3.9 us at 160 rows of 5 shares, ... ).
+// G-th share, so that few rows do not wait for one share after another.  Whole calls with one
+// group and with eight: 8 heads of 4096 keys, a token 10.6 and 8.2 us, 64 rows 17.3 and 15.5, 128 rows
+// 19.2 and 18.7; 160 rows 22.2 and 22.5, 256 rows 24.5 and 25.3, 12 heads of 200 rows on 32760 keys 59.1
+// and 60.8: eight below 128 threads a CU (1024 rows of 128 channels).
 template <typename T, int G>
 __global__ __launch_bounds__(256) void window_join_kernel(WinArgs a, int D) {
   __shared__ f32x4 so[G > 1 ? 256 : 1];
@@ -1291,7 +1300,7 @@ track_status attention_window(int dtype, const track_window* w, int B, int H, in
   TRACK_LAUNCH_CHECK();
   if (split) {
     // groups of shares while the rows alone do not fill the chip
-    const int per = D / 4, G = joined * D / 4 < 512 * (int64_t)device_cus() && p.nsplit > 2 ? 8 : 1;
+    const int per = D / 4, G = joined * D / 4 < 128 * (int64_t)device_cus() && p.nsplit > 2 ? 8 : 1;
     const int rows_wg = 256 / per / G;
     const unsigned jg = (unsigned)((joined + rows_wg - 1) / rows_wg);
 #define TRACK_WIN_JOIN(T)                                               \
