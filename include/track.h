@@ -370,7 +370,7 @@ typedef struct track_head_rows {
   int64_t ldx, sx;
   void* y;
   int64_t ldy, sy;
-  int32_t heads;       /* >= 1 */
+  int32_t heads;       /* 1..2^19 */
 } track_head_rows;
 
 /* The rotation of queries and keys in one launch.  k may be NULL.  pos: device

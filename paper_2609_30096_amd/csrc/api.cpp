@@ -895,8 +895,8 @@ static track_status op_rope(const char* what, int32_t dtype, const track_rope_co
     if (r->heads < 1 || r->ldx < width || r->ldy < width || r->sx < 0 || r->sy < 0)
       return fail(TRACK_E_SHAPE, "%s: rows of %lld and %lld elements for %d heads of %d", what, (long long)r->ldx,
                   (long long)r->ldy, r->heads, cfg->head_dim);
-    // sequences after each other, or their rows in turn
-    if (B > 1 && L > 0 && r->sy < (L - 1) * r->ldy + width && (r->sy < width || r->ldy < (B - 1) * r->sy + width))
+    if (r->heads > ROPE_MAX_HEADS) return fail(TRACK_E_SHAPE, "%s: %d heads, at most %d", what, r->heads, ROPE_MAX_HEADS);
+    if (sequences_overlap(B, L, r->ldy, r->sy, width))
       return fail(TRACK_E_SHAPE, "%s: sequences overlap in the output", what);
     if (B * L == 0) continue;
     if (!r->x || !r->y) return fail(TRACK_E_INVALID, "%s: null pointer", what);

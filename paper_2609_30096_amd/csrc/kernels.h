@@ -49,6 +49,15 @@ track_status attention_f32_vrows(int B, int H, int head_dim, int64_t Lq, int64_t
 // The softmax scale in log2 units, log2(e) / sqrt(head_dim).
 float attn_log2_scale(int head_dim);
 
+// Rows of `width` elements, L of them `ld` apart in each of B sequences `s` apart: whether sequences
+// share elements (they lie after each other, or their rows in turn).  128 bits: the caller's
+// strides may be any.
+inline bool sequences_overlap(int64_t B, int64_t L, int64_t ld, int64_t s, int64_t width) {
+  if (B < 2 || L < 1) return false;
+  const __int128 seq = (__int128)(L - 1) * ld + width, turn = (__int128)(B - 1) * s + width;
+  return s < seq && (s < width || ld < turn);
+}
+
 // window.hip (track_op_attention_window)
 constexpr int64_t WIN_MAX = (int64_t)1 << 28;  // largest length, position and window limit
 // Workspace of attention_window, -1 for what it refuses.
@@ -61,6 +70,7 @@ track_status attention_window(int dtype, const track_window* w, int B, int H, in
 
 // rope.hip (track_op_rope; with gains track_op_headnorm_rope).  k may be null.
 constexpr int ROPE_MAX_DIM = 256;  // channels of a head
+constexpr int ROPE_MAX_HEADS = 1 << 19;  // of q, of k: sums and bytes of a call stay in their types
 track_status rope_heads(int dtype, const track_rope_config& c, int64_t B, int64_t L, const track_head_rows& q,
                         const track_head_rows* k, const void* g_q, const void* g_k, float eps, float q_scale,
                         const int32_t* pos, const double* freqs, float amplitude, bool inverse, hipStream_t s);

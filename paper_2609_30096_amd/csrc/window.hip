@@ -1186,6 +1186,11 @@ static size_t win_bytes(const WinPlan& p, int64_t B, int Hk, int n, int D, int64
   return (size_t)(p.nsplit * B * Hk * Lq * n) * (size_t)(4 * D + 8);
 }
 
+// Whether a launch and the join hold the plan.
+static bool win_fits(const WinPlan& p, int64_t B, int Hk, int n, int64_t Lq) {
+  return p.nrb * p.nsplit * Hk * B < (int64_t)1 << 23 && (p.nsplit == 1 || B * Hk * n * Lq < (int64_t)1 << 25);
+}
+
 static track_status win_check(int dtype, const track_window* w, int B, int H, int Hk, int D, int64_t Lq, int64_t Lk) {
   if (!w) return fail(TRACK_E_INVALID, "attention_window: null window");
   if (dtype != TRACK_DTYPE_F32 && dtype != TRACK_DTYPE_BF16)
@@ -1201,16 +1206,22 @@ static track_status win_check(int dtype, const track_window* w, int B, int H, in
   if (dtype == TRACK_DTYPE_BF16 ? D != ATT_D : (D != 32 && D != 64 && D != 128))
     return fail(TRACK_E_UNSUPPORTED, "attention_window: head_dim %d (bfloat16: 128; float32: 32, 64, 128)", D);
   if (Lk > WIN_MAX || Lq > WIN_MAX / (H / Hk)) return fail(TRACK_E_SHAPE, "attention_window: sequence too long");
+  // each has a workgroup at least, and the launch holds fewer than 2^23 (products below stay in 64 bits)
+  if ((int64_t)B * Hk >= (int64_t)1 << 23)
+    return fail(TRACK_E_SHAPE, "attention_window: %d sequences of %d key heads are too many", B, Hk);
   return TRACK_OK;
 }
 
 int64_t attention_window_bytes(int dtype, const track_window* w, int B, int H, int Hk, int D, int64_t Lq, int64_t Lk) {
   if (win_check(dtype, w, B, H, Hk, D, Lq, Lk) != TRACK_OK) return -1;
   if (B == 0 || Lq == 0) return 0;
-  size_t bytes = 0;
-  for (bool vec : {true, false})  // whatever the rows' alignment turns out to be
-    bytes = std::max(bytes, win_bytes(win_plan(dtype, *w, B, Hk, H / Hk, D, Lq, Lk, vec), B, Hk, H / Hk, D, Lq));
-  return (int64_t)bytes;
+  int64_t bytes = -1;
+  for (bool vec : {true, false}) {  // whatever the rows' alignment turns out to be
+    const WinPlan p = win_plan(dtype, *w, B, Hk, H / Hk, D, Lq, Lk, vec);
+    if (win_fits(p, B, Hk, H / Hk, Lq)) bytes = std::max(bytes, (int64_t)win_bytes(p, B, Hk, H / Hk, D, Lq));
+  }
+  if (bytes < 0) fail(TRACK_E_SHAPE, "attention_window: too many row blocks");
+  return bytes;
 }
 
 track_status attention_window(int dtype, const track_window* w, int B, int H, int Hk, int D, int64_t Lq, int64_t Lk,
@@ -1225,8 +1236,7 @@ track_status attention_window(int dtype, const track_window* w, int B, int H, in
   const int n = H / Hk;
   if (ldq < (int64_t)H * D || ldo < (int64_t)H * D || ldk < (int64_t)Hk * D || ldv < Lk)
     return fail(TRACK_E_SHAPE, "attention_window: leading dimension too small");
-  const int64_t wo = (int64_t)H * D;  // sequences after each other, or their rows in turn
-  if (sq < 0 || sk < 0 || sv < 0 || so < 0 || (B > 1 && so < (Lq - 1) * ldo + wo && (so < wo || ldo < (B - 1) * so + wo)))
+  if (sq < 0 || sk < 0 || sv < 0 || so < 0 || sequences_overlap(B, Lq, ldo, so, (int64_t)H * D))
     return fail(TRACK_E_SHAPE, "attention_window: sequences overlap in out, or a negative stride");
   if (((uintptr_t)lse | (uintptr_t)q_len | (uintptr_t)k_len | (uintptr_t)q_start) & 3)
     return fail(TRACK_E_INVALID, "attention_window: lse and lengths need 4-byte alignment");
@@ -1243,12 +1253,11 @@ track_status attention_window(int dtype, const track_window* w, int B, int H, in
     vec = !(ptrs & 15) && !(strides & 3);
   }
   const WinPlan p = win_plan(dtype, *w, B, Hk, n, D, Lq, Lk, vec);
+  if (!win_fits(p, B, Hk, n, Lq)) return fail(TRACK_E_SHAPE, "attention_window: too many row blocks");
   const size_t need = win_bytes(p, B, Hk, n, D, Lq);
   if (need && (!ws || ws_bytes < need)) return fail(TRACK_E_NOMEM, "attention_window: workspace of %zu bytes needed", need);
   if (need && ((uintptr_t)ws & 255)) return fail(TRACK_E_INVALID, "attention_window: workspace must be 256-byte aligned");
   const int64_t grid = p.nrb * p.nsplit * Hk * B, joined = (int64_t)B * H * Lq;
-  if (grid >= ((int64_t)1 << 23) || (need && joined >= ((int64_t)1 << 25)))
-    return fail(TRACK_E_SHAPE, "attention_window: too many row blocks");
   WinArgs a = {};
   a.q = q, a.k = k, a.vt = vt, a.out = out;
   a.ldq = ldq, a.sq = sq, a.ldk = ldk, a.sk = sk, a.ldv = ldv, a.sv = sv, a.ldo = ldo, a.so = so;

@@ -600,6 +600,8 @@ def _rope_layout(rope):
             _like(k, q, "k")
         elif k_out is not None or g_k is not None:
             raise ValueError("k_out or g_k without k")
+        if pos is None:
+            raise ValueError("pos: positions are needed")
         _ints(pos, (rope.axes, B, L), q, "pos")
         if rope.freqs.get_device() != q.get_device():
             raise ValueError(f"rope on {rope.freqs.device}, q on {q.device}")

@@ -206,6 +206,40 @@ def test_binding_refusals():
     bad(k_len=torch.zeros(B + 1, dtype=torch.int32))
 
 
+def test_sizes_whose_products_wrap(L):
+    """Sizes and strides whose products pass 64 (or 32) bits are refused and not taken for small ones."""
+    p, S = 1 << 20, track.E_SHAPE
+
+    def rope(B, Ln, heads, ld, sy):
+        r = track.HeadRowsC(p, ld, sy, p, ld, sy, heads)
+        return L.track_op_rope(track.DTYPE_BF16, ctypes.byref(_rope_c()), B, Ln, ctypes.byref(r), ctypes.byref(r), p, p, 1.0, 0, None)
+
+    assert rope(2, 9, 4, 1 << 61, (1 << 61) + 512) == S       # 8 rows of 2^61 are 2^64
+    assert rope(1, 1, (1 << 31) - 1, 1 << 40, 1 << 40) == S   # the heads of q and k in 32 bits
+    assert rope(1, 1, (1 << 19) + 1, 1 << 40, 1 << 40) == S
+
+    def window(B, H, Hk, Lq, ldo, so):
+        return L.track_op_attention_window(
+            track.DTYPE_BF16, ctypes.byref(track.Window().c()), B, H, Hk, 128, Lq, 64, p, 1 << 40, 0, p, 1 << 22, 0, p, 64, 0,
+            p, ldo, so, *([None] * 4), p, (1 << 63) - 1, None)
+
+    for B, H in ((1 << 30, 1 << 30), (1 << 30, 1 << 20), (1 << 23, 1), (1 << 12, 1 << 11)):
+        assert track.lib().track_attention_window_workspace_bytes(
+            track.DTYPE_BF16, ctypes.byref(track.Window().c()), B, H, H, 128, 1 << 28, 64) == -1, (B, H)
+    assert window(1 << 30, 1 << 15, 1 << 15, 1, 1 << 40, 1 << 22) == S
+    assert window(2, 8, 4, 9, 1 << 61, (1 << 61) + 1024) == S
+
+
+def test_binding_needs_positions():
+    import torch
+    rope = track.Rope(track.RopeConfig(head_dim=128), device="cpu")
+    q, g = torch.zeros(1, 2, 4, 128), torch.ones(128)
+    with pytest.raises(ValueError):
+        track.op_rope(rope, q, None, None)
+    with pytest.raises(ValueError):
+        track.op_headnorm_rope(rope, q, None, g, None, None)
+
+
 # ---------------------------------------------------------------- rotation on the GPU
 gpu = pytest.mark.gpu
 
