@@ -884,3 +884,39 @@ def test_streaming_run(dtype):
     for a, b in [(0, total)] + [(i, i + 1) for i in range(total, n)]:
         want, _, mag, big = ref.attention(host(qr)[:, a:b], host(cache)[:, :b], v[:, :b], 2, 0, group, group)
         _close(host(out)[:, a:b], want, 2.1 * _eta(dtype, D, big, b) * mag + 1.01 * U[dtype] * np.abs(want), f"out {a}")
+
+
+@gpu
+@pytest.mark.parametrize("Lq", [1, 40, 500])
+def test_two_calls_at_once(Lq):
+    """Two streams, each with its outputs and workspace, over one cache, appended to right before: as one after another."""
+    import torch
+    B, H, Hk, Lk, D = 2, 8, 2, 6000, 128
+    win = W(left=-1, right=0, sink=4)
+    c = Case(BF16, B, H, Hk, Lq, Lk)
+    k = c.tk[:, :Lk]
+    qs = [c.tq, c.tq.flip(1).contiguous()]
+    rope = track.Rope(track.RopeConfig(head_dim=D))
+    pos = torch.arange(Lq, dtype=torch.int32, device="cuda").expand(1, B, Lq).contiguous()
+    wss = [track.attention_window_workspace(win, c.tq, k) for _ in qs]
+
+    def call(i, out, rq):
+        track.op_rope(rope, qs[i], None, pos, rq)
+        return track.op_attention_window(win, rq, k, c.tv, out, workspace=wss[i])
+
+    for turn in range(3):
+        k[:, -1] = 0.1 * turn + 1.0  # written on the current stream right before the calls
+        want = [call(i, torch.empty_like(c.tq), torch.empty_like(c.tq)) for i in range(2)]
+        k[:, -1] = 7.0
+        k[:, -1] = 0.1 * turn + 1.0
+        outs = [(torch.empty_like(c.tq), torch.empty_like(c.tq)) for _ in range(2)]
+        streams = [torch.cuda.Stream() for _ in range(2)]
+        for i, s in enumerate(streams):
+            s.wait_stream(torch.cuda.current_stream())
+            with torch.cuda.stream(s):
+                call(i, *outs[i])
+        for s in streams:
+            torch.cuda.current_stream().wait_stream(s)
+        torch.cuda.synchronize()
+        for (o, _), w in zip(outs, want):
+            assert torch.equal(o, w)
