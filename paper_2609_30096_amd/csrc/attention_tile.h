@@ -7,6 +7,7 @@
 #include <type_traits>
 
 #include "common.h"
+#include "tile_copy.h"
 
 namespace track {
 
@@ -43,11 +44,7 @@ __device__ __forceinline__ float group_max2(float a, float b) {
 // 16-key blocks are
 // then 8 consecutive keys, the P operand's k-block, which meets one contiguous
 // 16-byte V^T chunk, and its outputs of a pair of 16-channel blocks are 8
-// consecutive channels, one 16-byte store.
-__device__ __forceinline__ int att_perm(int row) {
-  return (row & ~31) | (((row >> 2) & 3) << 3) | (((row >> 4) & 1) << 2) | (row & 3);
-}
-
+// consecutive channels, one 16-byte store (att_perm and att_vswz: tile_copy.h).
 typedef __attribute__((address_space(3))) void* att_lds_ptr_t;
 
 // The lane index, computed where it is used (opaque to the compiler, which would
@@ -73,8 +70,6 @@ constexpr int ATT_V_BYTES = ATT_D * ATT_VROW;       // V^T tile, 16 KB
 constexpr int ATT_SLOT = ATT_K_BYTES + ATT_V_BYTES;  // one ring slot, 32 KB
 // key sequences of at most this many 64-key tiles (an even number) take the item-loop kernel
 constexpr int ATT_ITEMS_MAX_TILES = 32;
-
-__device__ __forceinline__ int att_vswz(int row) { return ((row & 7) ^ ((row >> 3) & 1)) & 6; }
 
 constexpr int ATT_LA = 3;  // fragments read ahead of their MFMAs
 constexpr int ATT_QB = 2;  // 16-query blocks per wave

@@ -483,32 +483,48 @@ __global__ __launch_bounds__(256) void window_rows_kernel(WinArgs a) {
   const uint8_t* const kbase = (const uint8_t*)((const bf16_t*)a.k + b * a.sk + (int64_t)h * D);
   const uint8_t* const vbase = (const uint8_t*)((const bf16_t*)a.vt + b * a.sv + (int64_t)h * D * a.ldv);
   const uint32_t krow = (uint32_t)a.ldk * 2, vrow = (uint32_t)a.ldv * 2;
-  // Copy i of 16 fills LDS rows 4 i .. + 3 of K (16 lanes a row of 256 bytes) or 8 i .. + 7 of V^T
-  // (8 lanes a row of 128), laid out as in the block kernel.  The key att_perm(4 i + lane / 16) is
-  // att_perm(4 i) + lane / 16 and the channel att_perm(8 i + lane / 8) likewise, and the
-  // swizzles' bits of i and of the lane do not meet: one offset a lane for V^T, one for each i % 4 for
-  // K, the rest is wave-uniform.
   uint8_t* const tile = smem + wave * ATT_SLOT;
   uint32_t kl[4];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) kl[i] = g * krow + (((jq ^ g) ^ (4 * i)) << 4);
-  const uint32_t vl = att_perm(lane >> 3) * vrow + (((lane & 7) ^ ((lane >> 3) & 6)) << 4);
+  for (int i = 0; i < 4; ++i) kl[i] = tile_k_lane(i, lane, krow);
+  const uint32_t vl = tile_v_lane(lane, vrow);
   const uint32_t ko = jq * 256 + ((g ^ jq) << 4), vo = jq * ATT_VROW + ((g ^ att_vswz(jq)) << 4);
   // K rows past the last key read as zero, V^T columns as whatever is there (cleared below) or,
-  // past the head's last row, as zero
+  // past the head's last row, as zero.  Whole tiles take the row's offset as a scalar: no
+  // instruction of the vector unit a copy.
   auto copy_k = [&](int key0) {
     const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc(
         (void*)(kbase + (int64_t)key0 * krow), (short)0, (int)(min(BKV, seq.klen - key0) * krow), 0x00020000);
+    if (tile_whole(key0, seq.klen)) {
 #pragma unroll
-    for (int i = 0; i < 16; ++i)
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (att_lds_ptr_t)(tile + i * 1024), 16, kl[i & 3], att_perm(4 * i) * krow, 0, WIN_PAST);
+      for (int i = 0; i < 16; ++i) {
+        const TileOffset at = tile_offset(true, kl[i & 3], tile_k_row(i, krow));
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (att_lds_ptr_t)(tile + i * 1024), 16, at.vec, at.scalar, 0, WIN_PAST);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const TileOffset at = tile_offset(false, kl[i & 3], tile_k_row(i, krow));
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (att_lds_ptr_t)(tile + i * 1024), 16, at.vec, 0, 0, WIN_PAST);
+      }
+    }
   };
   auto copy_v = [&](int key0) {
     const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc(
         (void*)(vbase + (int64_t)key0 * 2), (short)0, (int)(uint32_t)((a.vend - key0) * 2), 0x00020000);
+    if (tile_whole(key0, seq.klen)) {
 #pragma unroll
-    for (int i = 0; i < 16; ++i)
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (att_lds_ptr_t)(tile + ATT_K_BYTES + i * 1024), 16, vl, att_perm(8 * i) * vrow, 0, WIN_PAST);
+      for (int i = 0; i < 16; ++i) {
+        const TileOffset at = tile_offset(true, vl, tile_v_row(i, vrow));
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (att_lds_ptr_t)(tile + ATT_K_BYTES + i * 1024), 16, at.vec, at.scalar, 0, WIN_PAST);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const TileOffset at = tile_offset(false, vl, tile_v_row(i, vrow));
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (att_lds_ptr_t)(tile + ATT_K_BYTES + i * 1024), 16, at.vec, 0, 0, WIN_PAST);
+      }
+    }
   };
   // the oldest 16 copies have landed (`more`: 16 younger ones are under way)
   auto landed = [&](bool more) {
