@@ -17,6 +17,9 @@
 // (as 2 V u .. and 2 V u + V .. a load took every other 16 bytes).  A head takes the next power of two
 // of lanes (8 for 128 bfloat16 channels, 8 heads a step); the sum of squares meets by DPP
 // moves and lane swaps.
+//
+// Channels past rot_dim go out as they came (behind the norm as it leaves them): turned by cos 1 and
+// sin 0 an infinity or a NaN in one would reach the channel beside it, and -0 would become 0.
 #include <math.h>
 
 #include <algorithm>
@@ -198,17 +201,20 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a) {
   __builtin_amdgcn_wave_barrier();
   __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
   float c[NU][V], s[NU][V];
+  bool turn0[NU], turn1[NU];  // whether the first load's channels are rotated, the second's (whole units are)
 #pragma unroll
-  for (int i = 0; i < NU; ++i)
+  for (int i = 0; i < NU; ++i) {
+    const int u = u0 + 64 * i;
+    turn0[i] = HALF || V == 1 ? u < rot_units : e0[i] < 2 * a.pairs;
+    turn1[i] = HALF || V == 1 ? u < rot_units : e1[i] < 2 * a.pairs;
 #pragma unroll
     for (int j = 0; j < V; ++j) {
       // pair j of the lane: of the unit, or of its first load's V / 2 pairs and its second's
-      const int u = u0 + 64 * i;
       const int p = HALF || V == 1 ? V * u + j : (j < V / 2 ? e0[i] / 2 + j : e1[i] / 2 + j - V / 2);
-      const bool turned = p < a.pairs;
-      c[i][j] = turned ? cs[wv][0][p] : 1.0f;
-      s[i][j] = turned ? cs[wv][1][p] : 0.0f;
+      c[i][j] = p < a.pairs ? cs[wv][0][p] : 1.0f;
+      s[i][j] = p < a.pairs ? cs[wv][1][p] : 0.0f;
     }
+  }
 
   for (int h0 = part * hp; h0 < total; h0 += ST * (int)a.wpt * hp) {
     if (h0 != part * hp) load(h0);
@@ -247,25 +253,36 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a) {
 #pragma unroll
         for (int i = 0; i < NU; ++i) {
           if (u0 + 64 * i >= units) continue;
+          Raw rl = lo[st][i], rh = hi[st][i];
           if constexpr (HALF || V == 1) {
+            if (turn0[i]) {
 #pragma unroll
-            for (int j = 0; j < V; ++j) {
-              const float x0 = xl[i][j], x1 = xh[i][j];
-              xl[i][j] = x0 * c[i][j] - x1 * s[i][j];
-              xh[i][j] = x0 * s[i][j] + x1 * c[i][j];
+              for (int j = 0; j < V; ++j) {
+                const float x0 = xl[i][j], x1 = xh[i][j];
+                xl[i][j] = x0 * c[i][j] - x1 * s[i][j];
+                xh[i][j] = x0 * s[i][j] + x1 * c[i][j];
+              }
             }
           } else {
+            if (turn0[i]) {
 #pragma unroll
-            for (int j = 0; j < V / 2; ++j) {
-              float x0 = xl[i][2 * j], x1 = xl[i][2 * j + 1];
-              xl[i][2 * j] = x0 * c[i][j] - x1 * s[i][j];
-              xl[i][2 * j + 1] = x0 * s[i][j] + x1 * c[i][j];
-              x0 = xh[i][2 * j], x1 = xh[i][2 * j + 1];
-              xh[i][2 * j] = x0 * c[i][V / 2 + j] - x1 * s[i][V / 2 + j];
-              xh[i][2 * j + 1] = x0 * s[i][V / 2 + j] + x1 * c[i][V / 2 + j];
+              for (int j = 0; j < V / 2; ++j) {
+                const float x0 = xl[i][2 * j], x1 = xl[i][2 * j + 1];
+                xl[i][2 * j] = x0 * c[i][j] - x1 * s[i][j];
+                xl[i][2 * j + 1] = x0 * s[i][j] + x1 * c[i][j];
+              }
+            }
+            if (turn1[i]) {
+#pragma unroll
+              for (int j = 0; j < V / 2; ++j) {
+                const float x0 = xh[i][2 * j], x1 = xh[i][2 * j + 1];
+                xh[i][2 * j] = x0 * c[i][V / 2 + j] - x1 * s[i][V / 2 + j];
+                xh[i][2 * j + 1] = x0 * s[i][V / 2 + j] + x1 * c[i][V / 2 + j];
+              }
             }
           }
-          const Raw rl = rope_pack<T, V>(xl[i]), rh = rope_pack<T, V>(xh[i]);
+          if (NORM || turn0[i]) rl = rope_pack<T, V>(xl[i]);
+          if (NORM || turn1[i]) rh = rope_pack<T, V>(xh[i]);
           if constexpr (PAST > 0) {
             __builtin_nontemporal_store(rl, (Raw*)(p + e0[i]));
             __builtin_nontemporal_store(rh, (Raw*)(p + e1[i]));

@@ -920,3 +920,60 @@ def test_two_calls_at_once(Lq):
         torch.cuda.synchronize()
         for (o, _), w in zip(outs, want):
             assert torch.equal(o, w)
+
+
+# dtype, H, D, rot, elements a load
+COPIED = [(BF16, 3, 128, 64, 8), (BF16, 3, 80, 40, 4), (BF16, 3, 64, 10, 1), (BF16, 2, 250, 66, 1), (F32, 3, 64, 32, 4),
+          (F32, 3, 20, 6, 1), (F32, 2, 254, 100, 1)]
+
+
+@gpu
+@pytest.mark.parametrize("layout", ["half", "interleaved"])
+@pytest.mark.parametrize("place", ["in place", "out", "norm"])
+@pytest.mark.parametrize("case", COPIED, ids=str)
+def test_copied_channels(case, place, layout):
+    """Channels past rot_dim come out bit for bit, infinities, NaN, -0 and denormals among them, and change no other
+    channel's bits; behind the norm an infinity or a NaN stays in its head, and -0 stays -0."""
+    import torch
+    dtype, H, D, rot, _ = case
+    say(f"copied channels {case} {place} {layout}")
+    ints = torch.int16 if dtype == BF16 else torch.int32
+    Ln = 9
+    rope = track.Rope(track.RopeConfig(head_dim=D, rot_dim=rot, sections=(rot // 2,), layout=layout))
+    pos = torch.arange(5, 5 + Ln, dtype=torch.int32, device="cuda").view(1, 1, Ln)
+    plain = dev(normal([91, D], (1, Ln, H, D), bf16=dtype == BF16), dtype)
+    x = plain.clone()
+    tiny = 1e-40
+    odd = [float("inf"), float("nan"), -float("inf"), -0.0, tiny, -tiny, torch.finfo(x.dtype).max]
+    at = [rot, rot + 3, rot + (D - rot) // 2, D - 1]  # in either half of the copied channels
+    if place == "norm":
+        g = torch.full((D,), 1.25, dtype=x.dtype, device="cuda")
+        for i in range(Ln):
+            x[0, i, i % H, at[i % 4]] = -0.0
+        got, _ = track.op_headnorm_rope(rope, x, None, g, None, pos, torch.empty_like(x))
+        zero = x.view(ints) == (-32768 if dtype == BF16 else -2 ** 31)
+        assert int(zero.sum()) == Ln and torch.equal(got.view(ints)[zero], x.view(ints)[zero])
+        # infinity: the root is infinite, the other channels of the head are 0; NaN: all are NaN
+        for value, rest in ((float("inf"), 0.0), (float("nan"), float("nan"))):
+            y = plain.clone()
+            y[0, 4, 1, rot + 3] = value
+            got, _ = track.op_headnorm_rope(rope, y, None, g, None, pos, torch.empty_like(x))
+            clean, _ = track.op_headnorm_rope(rope, plain, None, g, None, pos, torch.empty_like(x))
+            head = got[0, 4, 1].float()
+            assert bool(torch.isnan(head[rot + 3]))
+            head = torch.cat([head[:rot + 3], head[rot + 4:]])
+            assert bool(torch.isnan(head).all() if math.isnan(rest) else (head == 0).all())
+            got[0, 4, 1] = clean[0, 4, 1]
+            assert torch.equal(got.view(ints), clean.view(ints))
+        return
+    for i in range(Ln):
+        for h in range(H):
+            x[0, i, h, at[(i + h) % 4]] = odd[(i + 2 * h) % len(odd)]
+    # a NaN that is not the usual one
+    x.view(ints)[0, 0, 0, D - 2] = 0x7fa1 if dtype == BF16 else 0x7fa12345
+    want = plain.clone()
+    track.op_rope(rope, want, None, pos)
+    want[..., rot:] = x[..., rot:]
+    want.view(ints)[..., rot:] = x.view(ints)[..., rot:]
+    got, _ = track.op_rope(rope, x, None, pos, None if place == "in place" else torch.empty_like(x))
+    assert torch.equal(got.view(ints), want.view(ints))
