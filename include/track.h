@@ -333,9 +333,11 @@ track_status track_op_rmsnorm_rope_qk(int32_t dtype, int64_t rows, int32_t heads
  *   NTK     base' = base factor^(n_a / (n_a - 1)) (n_a > 1): the fastest pair
  *           kept, the slowest squeezed by factor;
  *   YARN    (1 - r) f_i + r f_i / factor, r the ramp from 0 at
- *           max(floor(c(beta_fast)), 0) to 1 at min(ceil(c(beta_slow)), n_a - 1)
+ *           max(floor(c(beta_fast)), 0) to 1 at min(ceil(c(beta_slow)), m)
  *           over i, c(t) = n_a ln(orig_len / (2 pi t)) / ln(base) the pair that
- *           makes t turns over orig_len; amplitude A = 1 + 0.1 ln(factor).
+ *           makes t turns over orig_len; m = rot_dim - 1 for one axis (as
+ *           published: the ramp may end past the last pair, which then is not
+ *           squeezed whole), n_a - 1 for each of several; A = 1 + 0.1 ln(factor).
  * rotated pair (a, b) -> A (a cos - b sin, a sin + b cos). */
 #define TRACK_ROPE_INTERLEAVED 0
 #define TRACK_ROPE_HALF        1

@@ -861,7 +861,9 @@ track_status track_rope_freqs(const track_rope_config* c, double* freqs, float* 
     if (c->scaling == TRACK_ROPE_YARN) {
       auto pair = [&](double turns) { return n * std::log(c->orig_len / (2.0 * M_PI * turns)) / std::log(c->base); };
       lo = std::max(std::floor(pair(c->beta_fast)), 0.0);
-      hi = std::min(std::ceil(pair(c->beta_slow)), n - 1.0);
+      // one axis: the published ramp, which may end past the last pair (at most at rot_dim - 1); it knows
+      // no axes, and with several each one's slowest pair is squeezed whole
+      hi = std::min(std::ceil(pair(c->beta_slow)), (c->axes == 1 ? 2 * n : n) - 1.0);
     }
     for (int i = 0; i < n; ++i) {
       double f = std::pow(base, -(double)i / n);

@@ -977,3 +977,25 @@ def test_copied_channels(case, place, layout):
     want.view(ints)[..., rot:] = x.view(ints)[..., rot:]
     got, _ = track.op_rope(rope, x, None, pos, None if place == "in place" else torch.empty_like(x))
     assert torch.equal(got.view(ints), want.view(ints))
+
+
+@pytest.mark.parametrize("base,orig,factor", [(256.0, 4096.0, 8.0), (10000.0, 131072.0, 4.0), (10.0, 4096.0, 2.0),
+                                              (10000.0, 4096.0, 8.0), (500000.0, 8192.0, 16.0)])
+@pytest.mark.parametrize("n", [64, 32, 5])
+def test_yarn_one_axis(base, orig, factor, n):
+    """The published ramp of one axis: it ends at the pair that makes beta_slow turns over orig_len, also where that is past
+    the last pair, and at 2 n - 1 at most.  float64 throughout, some ten roundings."""
+    got, _ = track.rope_freqs(track.RopeConfig(head_dim=2 * n, sections=(n,), scaling="yarn", factor=factor, base=base,
+                                               orig_len=orig))
+    pair = [n * math.log(orig / (turns * 2.0 * math.pi)) / math.log(base) for turns in (32.0, 1.0)]
+    low, high = max(math.floor(pair[0]), 0), min(math.ceil(pair[1]), 2 * n - 1)
+    if (base, orig, n) == (256.0, 4096.0, 64):
+        assert high == 75
+    if (base, orig, n) == (10000.0, 131072.0, 64):
+        assert high == 70
+    if base == 10.0:
+        assert high == 2 * n - 1
+    i = np.arange(n)
+    plain = base ** (-i / n)
+    ramp = np.clip((i - low) / max(high - low, 0.001), 0.0, 1.0)
+    np.testing.assert_allclose(got, plain * (1.0 - ramp) + plain / factor * ramp, rtol=1e-13)
