@@ -414,8 +414,12 @@ typedef struct track_window {
 } track_window;
 
 /* Workspace of the call below in bytes, 0 where it needs none, -1 for what it
- * refuses.  The size belongs to this build of the library and to the current
- * device. */
+ * refuses.  The size belongs to this build of the library, to the current
+ * device and to this Lq; it serves calls of fewer keys too, so one made for the
+ * longest Lk lasts (bfloat16 calls of more than 16 rows a key head, Lq H / Hk,
+ * divide their keys into as many shares as the workspace given holds, without
+ * one not at all, which may take longer; the others need no more for fewer keys, and are
+ * refused with less than their size). */
 int64_t track_attention_window_workspace_bytes(int32_t dtype, const track_window* window, int32_t B, int32_t H,
                                                int32_t Hk, int32_t head_dim, int64_t Lq, int64_t Lk);
 

@@ -1268,8 +1268,15 @@ track_status attention_window(int dtype, const track_window* w, int B, int H, in
     if (ptrs & 3) return fail(TRACK_E_INVALID, "attention_window: float32 path needs 4-byte aligned rows");
     vec = !(ptrs & 15) && !(strides & 3);
   }
-  const WinPlan p = win_plan(dtype, *w, B, Hk, n, D, Lq, Lk, vec);
+  WinPlan p = win_plan(dtype, *w, B, Hk, n, D, Lq, Lk, vec);
   if (!win_fits(p, B, Hk, n, Lq)) return fail(TRACK_E_SHAPE, "attention_window: too many row blocks");
+  // Blocks' shares do not always grow with the keys (12 heads of 200 rows: four for 512, three for 576), so a
+  // workspace that was made for more keys may hold fewer than these would take: as many as it
+  // holds.  The other forms' grow.
+  if (p.form == WinPlan::BLOCKS && p.nsplit > 1) {
+    const int64_t share = B * (int64_t)Hk * Lq * n * (4 * D + 8), held = ws ? (int64_t)(std::min<size_t>(ws_bytes, INT64_MAX) / share) : 0;
+    p.nsplit = (int)std::max<int64_t>(1, std::min<int64_t>(p.nsplit, held));
+  }
   const size_t need = win_bytes(p, B, Hk, n, D, Lq);
   if (need && (!ws || ws_bytes < need)) return fail(TRACK_E_NOMEM, "attention_window: workspace of %zu bytes needed", need);
   if (need && ((uintptr_t)ws & 255)) return fail(TRACK_E_INVALID, "attention_window: workspace must be 256-byte aligned");

@@ -670,7 +670,8 @@ def attention_window_workspace_bytes(window: Window, dtype: int, B: int, H: int,
 
 
 def attention_window_workspace(window: Window, q, k):
-    """The workspace of op_attention_window on tensors of these shapes (None where it needs none)."""
+    """The workspace of op_attention_window on tensors of these shapes (None where it needs none); it serves calls of the
+    same q on fewer keys too."""
     torch = _torch()
     with torch.cuda.device(q.device):
         n = attention_window_workspace_bytes(window, _float_dtype(q), q.shape[0], q.shape[2], k.shape[2], q.shape[3],

@@ -999,3 +999,40 @@ def test_yarn_one_axis(base, orig, factor, n):
     plain = base ** (-i / n)
     ramp = np.clip((i - low) / max(high - low, 0.001), 0.0, 1.0)
     np.testing.assert_allclose(got, plain * (1.0 - ramp) + plain / factor * ramp, rtol=1e-13)
+
+
+@pytest.mark.parametrize("dtype,B,H,Hk,D,Lq", [
+    (BF16, 1, 8, 8, 128, 1), (BF16, 8, 40, 8, 128, 1), (BF16, 64, 8, 1, 128, 1), (BF16, 3, 4, 1, 128, 4), (BF16, 1, 1, 1, 128, 16),
+    (F32, 1, 1, 1, 32, 1), (F32, 2, 8, 2, 64, 9), (F32, 1, 4, 4, 128, 40), (F32, 1, 2, 1, 64, 300), (F32, 4, 12, 12, 128, 150),
+    (F32, 1, 8, 4, 64, 1501)], ids=str)
+@pytest.mark.parametrize("win", [track.Window(), track.Window(left=700, sink=4), track.Window(left=3, right=1, group=64)],
+                         ids=lambda w: f"l{w.left}g{w.group}")
+def test_workspace_grows_with_the_keys(dtype, B, H, Hk, D, Lq, win):
+    """Where a call is refused with less than its size, a size for more keys is enough for fewer (the rest: the next test)."""
+    t = track.DTYPE_BF16 if dtype == BF16 else track.DTYPE_F32
+    last = 0
+    for Lk in [*range(0, 3000, 7), *range(3000, 40000, 97), *range(40000, 400000, 2999)]:
+        n = track.attention_window_workspace_bytes(win, t, B, H, Hk, D, Lq, Lk)
+        assert n >= last, Lk
+        last = n
+
+
+@gpu
+@pytest.mark.parametrize("H,Hk,Lq,Lk,longer", [(12, 12, 200, 512, 576), (40, 8, 60, 510, 576), (2, 1, 200, 3000, 9000)])
+def test_workspace_of_more_keys(H, Hk, Lq, Lk, longer):
+    """Blocks of rows take the shares that their workspace holds: one made for more keys, less than that, none; the bytes
+    behind it stay as they were."""
+    import torch
+    c = Case(BF16, 1, H, Hk, Lq, Lk)
+    win = W(left=-1, right=0, sink=3)
+    size = [track.attention_window_workspace_bytes(win, track.DTYPE_BF16, 1, H, Hk, 128, Lq, n) for n in (Lk, longer)]
+    assert size[0] > 0
+    if longer == 576:
+        assert size[1] < size[0]
+    share = H * Lq * (4 * 128 + 8)
+    for held in sorted({size[0], size[1], size[0] - 1, 2 * share, 2 * share - 1, share, 256, 0}):
+        ws = torch.full((held + 4096,), 77, dtype=torch.uint8, device="cuda")
+        c.out.fill_(9.0), c.lse.fill_(9.0)
+        track.op_attention_window(win, c.tq, c.tk[:, :Lk], c.tv, c.out, lse=c.lse, workspace=ws[:held] if held else None)
+        _check(c, win, host(c.out), host(c.lse))
+        assert bool((ws[held // share * share if held < size[0] else held:] == 77).all()), held
