@@ -654,6 +654,8 @@ class Window:
     scale: Optional[float] = None  # 1 / sqrt(head_dim)
 
     def __post_init__(self):
+        if self.scale == 0.0:  # the library's mark for 1 / sqrt(head_dim), which is None here
+            raise ValueError("window: a scale of 0")
         object.__setattr__(self, "_c", WindowC(self.left, self.right, self.sink, self.group,
                                                0.0 if self.scale is None else self.scale))
 

@@ -1036,3 +1036,11 @@ def test_workspace_of_more_keys(H, Hk, Lq, Lk, longer):
         track.op_attention_window(win, c.tq, c.tk[:, :Lk], c.tv, c.out, lse=c.lse, workspace=ws[:held] if held else None)
         _check(c, win, host(c.out), host(c.lse))
         assert bool((ws[held // share * share if held < size[0] else held:] == 77).all()), held
+
+
+def test_window_scale_zero():
+    """A scale of 0 is not taken for the default one."""
+    for scale in (0, 0.0, -0.0):
+        with pytest.raises(ValueError, match="scale of 0"):
+            W(scale=scale)
+    assert W().c().scale == 0.0 and W(scale=0.5).c().scale == 0.5
