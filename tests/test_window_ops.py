@@ -1044,3 +1044,114 @@ def test_window_scale_zero():
         with pytest.raises(ValueError, match="scale of 0"):
             W(scale=scale)
     assert W().c().scale == 0.0 and W(scale=0.5).c().scale == 0.5
+
+
+def _on_cpu():
+    """Tensors that op_rope's and op_attention_window's checks accept (but for their device, which is looked at last)."""
+    import torch
+    B, Ln, Lk, H, Hk, D = 2, 5, 7, 4, 2, 128
+    rope = track.Rope(track.RopeConfig(head_dim=D), device="cpu")
+    q, k = torch.zeros(B, Ln, H, D), torch.zeros(B, Ln, Hk, D)
+    ok = dict(q=q, k=k, q_out=q, k_out=k, pos=torch.zeros(1, B, Ln, dtype=torch.int32), g_q=torch.ones(D), g_k=torch.ones(D))
+    win = dict(q=q, k=torch.zeros(B, Lk, Hk, D), vt=torch.zeros(B, Hk, D, 8), out=torch.zeros_like(q), lse=torch.zeros(B, H, Ln),
+               q_len=torch.zeros(B, dtype=torch.int32), k_len=torch.zeros(B, dtype=torch.int32),
+               q_start=torch.zeros(B, dtype=torch.int32), workspace=torch.zeros(64, dtype=torch.uint8))
+    return rope, ok, win
+
+
+def test_rope_layout_refusals():
+    """Each refusal by its own message, behind arguments that are accepted."""
+    import torch
+    rope, ok, _ = _on_cpu()
+    assert rope.check(**ok) == (track.DTYPE_F32, 2, 5, (512, 2560, 512, 2560, 4), (256, 1280, 256, 1280, 2))
+    assert rope.check(**dict(ok, k=None, k_out=None, g_q=None, g_k=None))[4] is None
+    q, k, pos = ok["q"], ok["k"], ok["pos"]
+    for match, kw in (
+            (r"^pos: contiguous int32 \(1, 2, 5\)", dict(pos=pos.long())), (r"^pos: contiguous", dict(pos=pos[:, :, :4])),
+            (r"^pos: contiguous", dict(pos=pos.expand(3, 2, 5))), (r"^pos: contiguous", dict(pos=pos[0])),
+            (r"^pos: contiguous", dict(pos=pos.new_zeros(1, 2, 10)[..., ::2])), (r"^pos: positions are needed", dict(pos=None)),
+            (r"^k of shape", dict(k=k[:, :4], k_out=k[:, :4])), (r"^k of shape", dict(k=k[:1], k_out=k[:1])),
+            (r"^k: torch.bfloat16 on cpu beside", dict(k=k.bfloat16(), k_out=k.bfloat16())),
+            (r"^k: torch.bfloat16 on cpu beside", dict(k_out=k.bfloat16())),
+            (r"^q: torch.bfloat16 on cpu beside", dict(q_out=q.bfloat16())),
+            (r"^q: output of shape", dict(q_out=q[:, :, :2])), (r"^k: output of shape", dict(k_out=q)),
+            (r"^k_out or g_k without k", dict(k=None)), (r"^k_out or g_k without k", dict(k=None, k_out=None)),
+            (r"^q: heads of a token must lie side by side", dict(q=q.transpose(1, 2).contiguous().transpose(1, 2))),
+            (r"^q: heads of a token must lie side by side", dict(q_out=torch.zeros(2, 5, 4, 256)[..., ::2])),
+            (r"^q: \[sequences, tokens, heads, channels\]", dict(q=q[0], q_out=q[0])),
+            (r"^q: heads of 64 channels, 128 configured", dict(q=q[..., :64].contiguous(), q_out=q[..., :64].contiguous())),
+            (r"^g_q: \[128\]", dict(g_q=torch.ones(64))), (r"^g_k: \[128\]", dict(g_k=torch.ones(256)[::2])),
+            (r"^g_q: torch.bfloat16", dict(g_q=torch.ones(128).bfloat16())),
+            (r"^float32 or bfloat16", {n: t if n == "pos" else t.half() for n, t in ok.items()})):
+        say(f"{match} {list(kw)}")
+        with pytest.raises((ValueError, TypeError), match=match):
+            rope.check(**dict(ok, **kw))
+
+
+def test_window_layout_refusals():
+    import torch
+    _, _, ok = _on_cpu()
+    assert track._check_window(**ok) == (track.DTYPE_F32, 2, 4, 2, 128, 5, 7, 512, 2560, 256, 1792, 8, 2048, 512, 2560, 64)
+    rest = ("lse", "q_len", "k_len", "q_start", "workspace")
+    assert track._check_window(**dict(ok, **dict.fromkeys(rest)))[-1] == 0
+    q, k, vt = ok["q"], ok["k"], ok["vt"]
+    cases = [
+        (r"do not match$", dict(out=ok["out"][:, :4])), (r"do not match$", dict(k=k[:1])),
+        (r"do not match$", dict(k=k[..., :64].contiguous())),
+        (r"^vt: \[2, 2, 128, >= 7\]", dict(vt=vt[..., :6])), (r"^vt: \[2, 2, 128, >= 7\]", dict(vt=vt[:1])),
+        (r"^vt: \[2, 2, 128, >= 7\]", dict(vt=vt[:, :1])), (r"^vt: \[2, 2, 128, >= 7\]", dict(vt=vt[:, :, :64])),
+        (r"^vt: \[2, 2, 128, >= 7\]", dict(vt=vt.flatten(1, 2))),
+        (r"^vt: rows of keys", dict(vt=torch.zeros(2, 2, 8, 128).transpose(2, 3))),
+        (r"^vt: rows of keys", dict(vt=torch.zeros(2, 4, 128, 8)[:, ::2])),
+        (r"^vt: torch.bfloat16 on cpu beside", dict(vt=vt.bfloat16())), (r"^k: torch.bfloat16 on", dict(k=k.bfloat16())),
+        (r"^out: torch.bfloat16 on", dict(out=q.bfloat16())),
+        (r"^k: heads of a token", dict(k=k.transpose(1, 2).contiguous().transpose(1, 2))),
+        (r"^out: heads of a token", dict(out=torch.zeros(2, 5, 4, 256)[..., ::2])),
+        (r"^lse: contiguous float32 \[2, 4, 5\]", dict(lse=torch.zeros(2, 4, 4))), (r"^lse:", dict(lse=ok["lse"].double())),
+        (r"^lse:", dict(lse=torch.zeros(2, 5, 4).transpose(1, 2))),
+        (r"^workspace: contiguous", dict(workspace=ok["workspace"][::2])),
+        (r"^float32 or bfloat16", dict(q=q.half(), k=k.half(), vt=vt.half(), out=q.half()))]
+    for name in ("q_len", "k_len", "q_start"):
+        cases += [(rf"^{name}: contiguous int32 \(2,\)", {name: v}) for v in
+                  (torch.zeros(2, dtype=torch.int64), torch.zeros(3, dtype=torch.int32), torch.zeros(2, 1, dtype=torch.int32),
+                   torch.zeros(4, dtype=torch.int32)[::2])]
+    for match, kw in cases:
+        say(f"{match} {list(kw)}")
+        with pytest.raises((ValueError, TypeError), match=match):
+            track._check_window(**dict(ok, **kw))
+
+
+def test_cpu_tensors_are_refused():
+    rope, r, w = _on_cpu()
+    with pytest.raises(ValueError, match="^GPU tensors expected"):
+        track.op_rope(rope, r["q"], r["k"], r["pos"])
+    with pytest.raises(ValueError, match="^GPU tensors expected"):
+        track.op_headnorm_rope(rope, r["q"], r["k"], r["g_q"], r["g_k"], r["pos"])
+    with pytest.raises(ValueError, match="^GPU tensors expected"):
+        track.op_attention_window(W(), **w)
+
+
+@gpu
+def test_tensors_on_other_devices_are_refused():
+    """Each tensor in turn on the CPU beside the others on the GPU; nothing is launched."""
+    import torch
+    _, r, w = _on_cpu()
+    r, w = ({n: t.cuda() for n, t in d.items()} for d in (r, w))
+    rope = track.Rope(track.RopeConfig(head_dim=128))
+    rope.check(**r), track._check_window(**w)
+    for check, args in ((rope.check, r), (track._check_window, w)):
+        for n in args:
+            with pytest.raises((ValueError, TypeError), match="cuda:0"):
+                check(**dict(args, **{n: args[n].cpu()}))
+    with pytest.raises(ValueError, match="rope on cpu, q on cuda:0"):
+        track.op_rope(track.Rope(track.RopeConfig(head_dim=128), device="cpu"), r["q"], r["k"], r["pos"])
+
+
+def test_rope_freqs_failed_call_writes_nothing(L):
+    out, amp = np.full(64, 3.0), ctypes.c_float(5.0)
+    p = out.ctypes.data_as(ctypes.POINTER(ctypes.c_double))
+    for bad in (dict(sections=(63,)), dict(base=1.0), dict(rot_dim=130, sections=(65,)), dict(scaling="yarn", factor=0.5)):
+        assert L.track_rope_freqs(ctypes.byref(_rope_c(**bad)), p, ctypes.byref(amp)) != 0
+        assert np.all(out == 3.0) and amp.value == 5.0
+    assert L.track_rope_freqs(ctypes.byref(_rope_c()), p, None) == track.E_INVALID and np.all(out == 3.0)
+    assert L.track_rope_freqs(ctypes.byref(_rope_c()), p, ctypes.byref(amp)) == 0 and out[0] == 1.0 and amp.value == 1.0
