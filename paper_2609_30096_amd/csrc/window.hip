@@ -48,7 +48,7 @@ struct WinArgs {
   float* lse;
   const int32_t *q_len, *k_len, *q_start;
   // limits in tokens: from a group's first key back, and on to the first key past them (2^31 - 1:
-  // no limit; all else is below 2^30)
+  // no limit, or one that no key is as far away as: lengths are at most 2^28, positions within +- 2^29)
   int before, past;
   int lift;           // multiple of the group that makes every position positive
   int sink;

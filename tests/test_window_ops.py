@@ -1155,3 +1155,28 @@ def test_rope_freqs_failed_call_writes_nothing(L):
         assert np.all(out == 3.0) and amp.value == 5.0
     assert L.track_rope_freqs(ctypes.byref(_rope_c()), p, None) == track.E_INVALID and np.all(out == 3.0)
     assert L.track_rope_freqs(ctypes.byref(_rope_c()), p, ctypes.byref(amp)) == 0 and out[0] == 1.0 and amp.value == 1.0
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("Lq,Lk,shares", [(1, 200, False), (1, 6000, True), (4, 6000, True), (70, 300, False), (70, 4000, True),
+                                          (300, 451, None)])  # bfloat16 alone takes shares
+def test_window_lengths_out_of_range(dtype, Lq, Lk, shares):
+    """Lengths and positions in device memory that are out of range are cut to it, in the kernels and in the join: the
+    results of the cut ones bit for bit, rows behind them left as they were."""
+    import torch
+    c = Case(dtype, 3, 4, 2, Lq, Lk)
+    win = W(left=-1, right=0, sink=3)
+    t = track.DTYPE_BF16 if dtype == BF16 else track.DTYPE_F32
+    assert (track.attention_window_workspace_bytes(win, t, 3, 4, 2, 128, Lq, Lk) > 0) == (dtype == BF16 if shares is None else shares)
+    big = 2 ** 31 - 1
+    lens = [(dict(q_len=[Lq + 5, -3, big], k_len=[Lk + 100, Lk, -1]), dict(q_len=[Lq, 0, Lq], k_len=[Lk, Lk, 0])),
+            (dict(q_len=[-big - 1, 1, Lq], k_len=[big, -big - 1, Lk + 1]), dict(q_len=[0, 1, Lq], k_len=[Lk, 0, Lk])),
+            (dict(q_start=[big, -big - 1, Lk - Lq]), dict(q_start=[1 << 28, -(1 << 28), Lk - Lq]))]
+    for raw, cut in lens:
+        c.out.fill_(9.0), c.lse.fill_(9.0)
+        got, lse = c.run(win, **raw)
+        _check(c, win, got, lse, **cut)
+        c.out.fill_(9.0), c.lse.fill_(9.0)
+        want, wlse = c.run(win, **cut)
+        assert np.array_equal(got, want) and np.array_equal(lse, wlse)
