@@ -1180,3 +1180,44 @@ def test_window_lengths_out_of_range(dtype, Lq, Lk, shares):
         c.out.fill_(9.0), c.lse.fill_(9.0)
         want, wlse = c.run(win, **cut)
         assert np.array_equal(got, want) and np.array_equal(lse, wlse)
+
+
+@gpu
+@pytest.mark.parametrize("H,Hk,Lq,Lk,lens", [
+    (8, 2, 1, 5000, {}), (8, 2, 1, 100003, dict(k_len=[100003, 56000, 17])), (4, 4, 4, 3001, dict(k_len=[3001, 2944, 2945])),
+    (4, 2, 20, 5000, {}), (2, 1, 200, 9000, dict(k_len=[9000, 8999, 4097])), (12, 12, 120, 6000, {}),
+    (3, 3, 700, 1500, dict(q_len=[700, 511, 1])), (2, 2, 40, 32000, {})], ids=str)
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("win", [W(), W(left=1000, sink=70), W(left=3, right=2, group=100, sink=130)],
+                         ids=lambda w: f"l{w.left}g{w.group}")
+def test_window_counts_each_key_once(dtype, H, Hk, Lq, Lk, lens, win):
+    """Queries of zero weigh every key 1, exactly in either type: the log-sum-exp is the log of the keys' number, and V that
+    is 1 in one key in 64 (another one for each channel, so every key counts somewhere) gives an exact count over it.
+    Sums of whole numbers below 2^24 are exact in any order, so what is left is the logarithm (a unit in the last place, 2^-23),
+    its factor and their product (2^-24 each) for lse, and a division and the output's rounding for out: one key too many or too few of 100003 is 1e-5 in the former."""
+    import torch
+    B, D = 3, 128
+    say(f"count {dtype} {H} {Lq} {Lk} {lens} {win}")
+    dt = track.torch_dtype(dtype)
+    q = torch.zeros(B, Lq, H, D, dtype=dt, device="cuda")
+    k = torch.randn(B, Lk, Hk, D, device="cuda", generator=torch.Generator("cuda").manual_seed(3)).to(dt)
+    cap = (Lk + 7) // 8 * 8
+    hit = (torch.arange(cap, device="cuda")[None, :] - torch.arange(D, device="cuda")[:, None]) % 64 == 0
+    vt = hit.to(dt).expand(B, Hk, D, cap).contiguous()
+    out, lse = torch.full_like(q, 9.0), torch.full((B, H, Lq), 9.0, device="cuda")
+    dl = {n: torch.tensor(v, dtype=torch.int32, device="cuda") for n, v in lens.items()}
+    ws = track.attention_window_workspace(win, q, k)
+    track.op_attention_window(win, q, k, vt, out, lse=lse, workspace=ws, **dl)
+    got, glse = host(out), host(lse)
+    hits = hit[:, :Lk].cpu().numpy().astype(np.float64)  # [D, Lk]
+    for b in range(B):
+        lq, lk = (lens[n][b] if n in lens else full for n, full in (("q_len", Lq), ("k_len", Lk)))
+        seen = np.stack([ref.seen(lk - lq + i, lk, win.left, win.right, win.sink, win.group) for i in range(lq)])
+        n = seen.sum(1)
+        want = np.where(n[:, None] > 0, (seen @ hits[:, :lk].T) / np.maximum(n, 1)[:, None], 0.0)
+        wlse = np.log(np.maximum(n, 1))
+        for h in range(H):
+            _close(got[b, :lq, h], want, (U[dtype] + 2.0 ** -22) * want, f"out {b} {h}")
+            some = n > 0
+            _close(glse[b, h, :lq][some], wlse[some], 1.01 * 2.0 ** -22 * wlse[some] + 1e-30, f"lse {b} {h}")
+            assert np.all(glse[b, h, :lq][~some] == -np.inf)
