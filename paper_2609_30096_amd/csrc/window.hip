@@ -175,10 +175,15 @@ struct WinMask {
   }
 };
 
-// 16 bytes a lane from the buffer at `off` to LDS, lanes side by side.  (A function of its own: in
-// a template, with arguments that depend on it, the host's pass rejects the builtin.)
-__device__ __forceinline__ void win_copy(__amdgpu_buffer_rsrc_t rs, uint8_t* lds, uint32_t off) {
-  __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (att_lds_ptr_t)lds, 16, off, 0, 0, 0);
+// 16 bytes a lane from the buffer at `off` (and the wave's `scalar` more) to LDS, lanes side by side.
+// (Functions of their own: in a template, with arguments that depend on it, the host's pass rejects
+// the builtin.)
+__device__ __forceinline__ void win_copy(__amdgpu_buffer_rsrc_t rs, uint8_t* lds, uint32_t off, uint32_t scalar = 0) {
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (att_lds_ptr_t)lds, 16, off, scalar, 0, 0);
+}
+// The same past the caches (the `nt` bit).
+__device__ __forceinline__ void win_copy_past(__amdgpu_buffer_rsrc_t rs, uint8_t* lds, uint32_t off, uint32_t scalar) {
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (att_lds_ptr_t)lds, 16, off, scalar, 0, 2);
 }
 
 template <bool VEC>
@@ -425,12 +430,16 @@ __global__ __launch_bounds__(512) void window_blocks_kernel(WinArgs a) {
 }
 
 // ---------------------------------------------------------------- few rows, bfloat16
-// Cache policy of the copies below: past the caches (the `nt` bit).  Each key is read once a call, so
-// keeping it only puts out what others left there.  Replays of one buffer, kept and past the
+// Cache policy of the copies below.  Past the caches where each key is read once a call, so that
+// keeping it would only put out what others left there.  Replays of one buffer, kept and past the
 // caches: 8 sequences of 100003 keys 548 and 490 us, 8 of 16384 101 and 89, 48 x 32760 143 and 128, 8
 // x 32760 27.0 and 26.9; after 1 GiB written elsewhere 609 and 496, 153 and 93, 201 and 132, 55 and 31;
 // with keys just written, 67 MB of them, 27.8 and 28.5 (the worst of nine sizes).
-constexpr int WIN_PAST = 2;
+// Through the caches from WIN_SHARED sequences on that share their keys, each of which reads them: 8 key
+// heads of 8192 keys, 32 sequences replayed 71 us and past the caches 100, after 1 GiB written elsewhere
+// 80 and 97; 32 of 32760 keys 200 and 457, 403 and 450; 16 of 8192 40 and 51, 49 and 50; 16 of 32760 181 and
+// 270, 293 and 265; but 8 of 32760 137 and 150, 178 and 152, 2 of 32760 27 and 35, 63 and 38.
+constexpr int WIN_SHARED = 16;
 
 // At most 16 rows a key head (a token of 16 query heads, four tokens of 4).  The four waves of
 // a workgroup take every fourth 64-key tile of its share, each through 32 KB of LDS of its own:
@@ -441,7 +450,7 @@ constexpr int WIN_PAST = 2;
 // under way all the time.  What bounds it: reading K and V^T (8 sequences of 100003 keys 490 us,
 // 6.7 TB/s; 6.2 - 6.5 is what a plain read stream through the caches reaches), and for short windows the
 // latency of a tile and of the join (8 heads of 4096 keys 8.2 us).
-template <bool SPLIT>
+template <bool SPLIT, bool PAST>
 __global__ __launch_bounds__(256) void window_rows_kernel(WinArgs a) {
   constexpr int BKV = ATT_BKV, D = ATT_D, F = D / 16;
   typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
@@ -492,21 +501,19 @@ __global__ __launch_bounds__(256) void window_rows_kernel(WinArgs a) {
   // K rows past the last key read as zero, V^T columns as whatever is there (cleared below) or,
   // past the head's last row, as zero.  Whole tiles take the row's offset as a scalar: no
   // instruction of the vector unit a copy.
+  auto copy = [&](__amdgpu_buffer_rsrc_t rs, uint8_t* to, TileOffset at) {
+    if constexpr (PAST) win_copy_past(rs, to, at.vec, at.scalar);
+    else win_copy(rs, to, at.vec, at.scalar);
+  };
   auto copy_k = [&](int key0) {
     const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc(
         (void*)(kbase + (int64_t)key0 * krow), (short)0, (int)(min(BKV, seq.klen - key0) * krow), 0x00020000);
     if (tile_whole(key0, seq.klen)) {
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const TileOffset at = tile_offset(true, kl[i & 3], tile_k_row(i, krow));
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (att_lds_ptr_t)(tile + i * 1024), 16, at.vec, at.scalar, 0, WIN_PAST);
-      }
+      for (int i = 0; i < 16; ++i) copy(rs, tile + i * 1024, tile_offset(true, kl[i & 3], tile_k_row(i, krow)));
     } else {
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const TileOffset at = tile_offset(false, kl[i & 3], tile_k_row(i, krow));
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (att_lds_ptr_t)(tile + i * 1024), 16, at.vec, 0, 0, WIN_PAST);
-      }
+      for (int i = 0; i < 16; ++i) copy(rs, tile + i * 1024, tile_offset(false, kl[i & 3], tile_k_row(i, krow)));
     }
   };
   auto copy_v = [&](int key0) {
@@ -514,16 +521,10 @@ __global__ __launch_bounds__(256) void window_rows_kernel(WinArgs a) {
         (void*)(vbase + (int64_t)key0 * 2), (short)0, (int)(uint32_t)((a.vend - key0) * 2), 0x00020000);
     if (tile_whole(key0, seq.klen)) {
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const TileOffset at = tile_offset(true, vl, tile_v_row(i, vrow));
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (att_lds_ptr_t)(tile + ATT_K_BYTES + i * 1024), 16, at.vec, at.scalar, 0, WIN_PAST);
-      }
+      for (int i = 0; i < 16; ++i) copy(rs, tile + ATT_K_BYTES + i * 1024, tile_offset(true, vl, tile_v_row(i, vrow)));
     } else {
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const TileOffset at = tile_offset(false, vl, tile_v_row(i, vrow));
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (att_lds_ptr_t)(tile + ATT_K_BYTES + i * 1024), 16, at.vec, 0, 0, WIN_PAST);
-      }
+      for (int i = 0; i < 16; ++i) copy(rs, tile + ATT_K_BYTES + i * 1024, tile_offset(false, vl, tile_v_row(i, vrow)));
     }
   };
   // the oldest 16 copies have landed (`more`: 16 younger ones are under way)
@@ -1320,8 +1321,13 @@ track_status attention_window(int dtype, const track_window* w, int B, int H, in
       else window_blocks_kernel<false, false><<<gr, 512, 0, s>>>(a);
       break;
     case WinPlan::ROWS:
-      if (split) window_rows_kernel<true><<<gr, 256, 0, s>>>(a);
-      else window_rows_kernel<false><<<gr, 256, 0, s>>>(a);
+      if (B >= WIN_SHARED && sk == 0 && sv == 0) {
+        if (split) window_rows_kernel<true, false><<<gr, 256, 0, s>>>(a);
+        else window_rows_kernel<false, false><<<gr, 256, 0, s>>>(a);
+      } else {
+        if (split) window_rows_kernel<true, true><<<gr, 256, 0, s>>>(a);
+        else window_rows_kernel<false, true><<<gr, 256, 0, s>>>(a);
+      }
       break;
     default:
       if (D == 32) TRACK_WIN_F32(32);

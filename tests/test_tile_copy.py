@@ -28,16 +28,15 @@ def test_scalar_rows_of_a_partial_tile_are_found(program):
 
 
 def test_kernel_takes_the_checked_offsets():
-    """Every copy of the single-token kernel goes through tile_offset, and a scalar part stands only behind tile_whole."""
+    """Every copy of the single-token kernel takes its address from tile_offset, that of whole tiles behind tile_whole alone."""
     with open(os.path.join(CSRC, "window.hip")) as f:
         src = f.read()
     body = src[src.index("void window_rows_kernel"):src.index("// ---------------------------------------------------------------- float32")]
-    loads = [i for i in range(len(body)) if body.startswith("raw_ptr_buffer_load_lds(", i)]
-    assert len(loads) == 4
-    for i in loads:
-        before, call = body[:i], body[i:body.index(";", i)]
-        offset = before[before.rindex("tile_offset("):]
-        if "at.scalar" in call:
-            assert offset.startswith("tile_offset(true") and before.rindex("if (tile_whole(") > before.rindex("auto copy_")
-        else:
-            assert offset.startswith("tile_offset(false") and "at.vec, 0, 0," in call
+    assert "raw_ptr_buffer_load" not in body and body.count("win_copy(") == body.count("win_copy_past(") == 1
+    copies = [line.strip() for line in body.splitlines() if " copy(rs, " in line]
+    assert len(copies) == 4 and all("tile_offset(" in line for line in copies)
+    for whole, other in (copies[:2], copies[2:]):
+        assert "tile_offset(true, " in whole and other == whole.replace("true", "false")
+        at = [body.index(line) for line in (whole, other)]
+        assert body.rindex("if (tile_whole(key0, seq.klen)) {", 0, at[0]) > body.rindex("make_buffer_rsrc", 0, at[0])
+        assert body[at[0]:at[1]].count("} else {") == 1

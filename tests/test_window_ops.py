@@ -1221,3 +1221,26 @@ def test_window_counts_each_key_once(dtype, H, Hk, Lq, Lk, lens, win):
             some = n > 0
             _close(glse[b, h, :lq][some], wlse[some], 1.01 * 2.0 ** -22 * wlse[some] + 1e-30, f"lse {b} {h}")
             assert np.all(glse[b, h, :lq][~some] == -np.inf)
+
+
+@gpu
+@pytest.mark.parametrize("B", [15, 16, 40])
+@pytest.mark.parametrize("Lq,Lk", [(1, 200), (1, 6000), (3, 1100)])
+def test_window_keys_of_many_sequences(B, Lq, Lk):
+    """Keys that many sequences share (sequence strides of 0), of ragged lengths: the bits of a copy for each."""
+    import torch
+    H, Hk, D = 8, 2, 128
+    win = W(left=4000, sink=3)
+    c = Case(BF16, 1, H, Hk, Lq, Lk)
+    q = dev(normal([97, B], (B, Lq, H, D), bf16=True), BF16)
+    k_len = torch.tensor([Lk - (b * 37) % Lk for b in range(B)], dtype=torch.int32, device="cuda")
+    got = []
+    for copies in (False, True):
+        k, vt = c.tk[:, :Lk].expand(B, -1, -1, -1), c.tv.expand(B, -1, -1, -1)
+        if copies:
+            k, vt = k.contiguous(), vt.contiguous()
+        out, lse = torch.full_like(q, 9.0), torch.full((B, H, Lq), 9.0, device="cuda")
+        ws = track.attention_window_workspace(win, q, k)
+        got.append((track.op_attention_window(win, q, k, vt, out, lse=lse, k_len=k_len, workspace=ws), lse))
+    assert torch.equal(got[0][0], got[1][0]) and torch.equal(got[0][1], got[1][1])
+    assert bool(torch.isfinite(got[0][0]).all())
