@@ -184,20 +184,25 @@ def main():
                                                                  h0=hist[0], h1=hist[1], vel_S=velS, partial=part,
                                                                  r_out=rout), None,
                                      n_step * (8 * B + 4 * 4 + 3 * 4))
-    # streaming: the q and k of the step normed per head and rotated (into log2 queries), rotated alone, the last
-    # three frames on the last twelve and the first, the whole video with four frames on either side, and one token
-    # for each sequence on everything
+    # streaming: the q and k of the step normed per head and rotated (into log2 queries), rotated alone; and on the normed
+    # ones (formed once here, scale ln 2) the last three frames on the last twelve and the first, the whole video with four
+    # frames on either side, and one token for each sequence on everything
     fr = 30 * 52
     heads = qkv.view(B, L, 3, H, dh)
     vrope = track.Rope(track.RopeConfig(head_dim=dh, sections=(dh // 2 - 2 * (dh // 6), dh // 6, dh // 6)))
     at = torch.arange(L, device=dev)
     vpos = torch.stack([at // fr, at // 52 % 30, at % 52])[:, None].expand(3, B, L).to(torch.int32).contiguous()
     gh = rnd(dh, scale=0.1) + 1
-    hq, hk = (torch.empty(B, L, H, dh, device=dev, dtype=bf) for _ in range(2))
+    hq, hk, rq, rk = (torch.empty(B, L, H, dh, device=dev, dtype=bf) for _ in range(4))
     hbytes = 2 * M * d * (2 + 2) + 3 * 4 * M
-    cases["headnorm_rope"] = (lambda: track.op_headnorm_rope(vrope, heads[:, :, 0], heads[:, :, 1], gh, gh, vpos, hq, hk,
-                                                             q_scale=1.4426950408889634 / dh ** 0.5), None, hbytes)
-    cases["rope"] = (lambda: track.op_rope(vrope, heads[:, :, 0], heads[:, :, 1], vpos, hq, hk), None, hbytes)
+
+    def headnorm(q_out, k_out):
+        track.op_headnorm_rope(vrope, heads[:, :, 0], heads[:, :, 1], gh, gh, vpos, q_out, k_out,
+                               q_scale=1.4426950408889634 / dh ** 0.5)
+
+    headnorm(hq, hk)
+    cases["headnorm_rope"] = (lambda: headnorm(rq, rk), None, hbytes)
+    cases["rope"] = (lambda: track.op_rope(vrope, heads[:, :, 0], heads[:, :, 1], vpos, rq, rk), None, hbytes)
 
     def window(name, win, Lq, pairs=None, nbytes=None):
         q, o = hq[:, L - Lq:], ao.view(B, L, H, dh)[:, L - Lq:]
@@ -205,13 +210,14 @@ def main():
         cases[name] = (lambda: track.op_attention_window(win, q, hk, vt, o, workspace=ws),
                        pairs and 4 * B * H * dh * pairs, nbytes)
 
+    ln2 = 0.6931471805599453
     if L % fr == 0:
         n = L // fr
         seen = [len(set(range(max(0, i - 4), min(n, i + 5))) | {0}) for i in range(n)]
-        window("attn_window_video", track.Window(left=4, right=4, sink=fr, group=fr), L, fr * fr * sum(seen))
+        window("attn_window_video", track.Window(left=4, right=4, sink=fr, group=fr, scale=ln2), L, fr * fr * sum(seen))
         seen = [len(set(range(max(0, i - 11), i + 1)) | {0}) for i in range(n - 3, n)]
-        window("attn_window_stream", track.Window(left=11, sink=fr, group=fr), 3 * fr, fr * fr * sum(seen))
-    window("attn_window_token", track.Window(), 1, None, 2 * B * L * d * 2)
+        window("attn_window_stream", track.Window(left=11, sink=fr, group=fr, scale=ln2), 3 * fr, fr * fr * sum(seen))
+    window("attn_window_token", track.Window(scale=ln2), 1, None, 2 * B * L * d * 2)
     only = set(a.only.split(",")) if a.only else None
     results = []
     for name, (fn, flops, nbytes) in cases.items():
