@@ -390,7 +390,8 @@ track_status track_op_rope(int32_t dtype, const track_rope_config* cfg, int64_t 
 /* The same behind the RMSNorm of each head: x / sqrt(mean over the head of x^2
  * + eps) * g with gains g_q, g_k [head_dim] (dtype, shared by all heads), then
  * the rotation; q is multiplied by q_scale inside its one rounding (1, or
- * log2(e) / sqrt(head_dim) for attention on log2 queries).  eps > 0. */
+ * log2(e) / sqrt(head_dim) for attention on log2 queries).  eps > 0.  The squares' sum
+ * is float32: |x| below 2^63 / sqrt(head_dim). */
 track_status track_op_headnorm_rope(int32_t dtype, const track_rope_config* cfg, int64_t B, int64_t L,
                                     const track_head_rows* q, const track_head_rows* k, const void* g_q,
                                     const void* g_k, float eps, float q_scale, const int32_t* pos, const double* freqs,
@@ -426,8 +427,9 @@ int64_t track_attention_window_workspace_bytes(int32_t dtype, const track_window
 /* H query heads over Hk key heads (H % Hk == 0; head h reads key head
  * h / (H/Hk)).  Row i of q for sequence b is q[b*sq + i*ldq + h*head_dim + c],
  * likewise k with Hk heads, ldk, sk, and out; v is given transposed,
- * vt[b*sv + (h*head_dim + c)*ldv + key] (a cache that track_op_linear_vt
- * appends to), ldv >= Lk, its rows readable up to the multiple of 16 bytes at
+ * vt[b*sv + (h*head_dim + c)*ldv + key] (the layout that track_op_linear_vt
+ * writes, which appends bfloat16 chunks of 128 tokens and more at columns in
+ * multiples of 8; other tokens the caller stores there), ldv >= Lk, its rows readable up to the multiple of 16 bytes at
  * or past key Lk.  sk = sv = 0: keys that all sequences share.  out overlaps
  * none of the inputs, and its sequences not each other.
  * Lq, Lk: the most queries and keys of a sequence.  q_len, k_len (device int32
@@ -438,7 +440,9 @@ int64_t track_attention_window_workspace_bytes(int32_t dtype, const track_window
  * [B][H][Lq], log of the sum of exp of the seen logits (natural), or NULL.
  * bfloat16: head_dim 128, 16-byte aligned rows (bases, and strides in multiples
  * of 8); probabilities are rounded to bfloat16 for the product with V, their
- * sum is that of the rounded ones.  float32: head_dim 32, 64, 128.
+ * sum (and with it lse) is that of the rounded ones.  Scaled logits have to lie within
+ * float32's range, and in bfloat16 |v| of seen keys below 2^63 / Lk: before the division
+ * weights reach 2^64.  float32: head_dim 32, 64, 128.
  * ldk, ldv <= 2^22; lengths, window limits <= 2^28 (q_start is cut to that range).  workspace: 256-byte
  * aligned; calls that may overlap on the GPU need one each.  B == 0 or Lq == 0
  * is a no-op; Lk == 0 gives zeros.  Asynchronous. */

@@ -1244,3 +1244,20 @@ def test_window_keys_of_many_sequences(B, Lq, Lk):
         got.append((track.op_attention_window(win, q, k, vt, out, lse=lse, k_len=k_len, workspace=ws), lse))
     assert torch.equal(got[0][0], got[1][0]) and torch.equal(got[0][1], got[1][1])
     assert bool(torch.isfinite(got[0][0]).all())
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("Lq", [1, 20, 300])
+@pytest.mark.parametrize("scale", [1.0, 4.0])
+def test_window_large_values(dtype, Lq, scale):
+    """V up to the documented 2^63 / Lk (5.5 sigma of it) under logits that the weights' reference lags behind: finite, and
+    a power of two times the result of V itself."""
+    c = Case(dtype, 1, 2, 1, Lq, 900, scale=scale)
+    win = W(left=400, sink=2)
+    want, _ = c.run(win)
+    big = 2.0 ** 50
+    assert np.abs(c.v).max() * big < 2.0 ** 63 / 900
+    c.tv *= big
+    got, _ = c.run(win)
+    assert np.array_equal(got, want * np.float32(big))
