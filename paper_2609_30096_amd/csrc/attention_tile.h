@@ -120,8 +120,10 @@ struct AttBelow {  // keys at or past the end
 // tile, the online-softmax update (lazy rescale), and O^T += V^T P^T from the
 // slot's V^T tile.  ko / vo are the lane's fragment offsets (depth step 0, key chunk
 // 0; the others differ in one XOR); keys that the mask hides get
-// probability zero.  KB 16-key blocks of the tile (2: the half that ko and vo point at).  With SAFE
-// a row whose logits so far are all -inf (a wave of a split sequence can begin with
+// probability zero.  The probabilities are rounded to bfloat16, the type that the matrix cores multiply at
+// full rate (float32 runs at a thirteenth of it), and the row sums add the rounded ones: the weights
+// that meet V then add up to one, and a V of equal rows comes out as it is.  KB 16-key blocks of the tile
+// (2: the half that ko and vo point at).  With SAFE a row whose logits so far are all -inf (a wave of a split sequence can begin with
 // such a tile) takes reference 0 instead.
 // FIRST: the sequence's first tile, which starts O and the sums (no rescale, nothing to
 // zero) and the references: 212.7 -> 207.3 us at 2 x 12 heads, 32760 x 512, 12 times a CU.

@@ -200,8 +200,8 @@ __device__ __forceinline__ uint32_t win_keep(int left) { return (uint32_t)((1ull
 // under a causal mask took 955 us instead of 824, 2 x 12 heads over a 21-frame video 5.2 ms
 // instead of 4.8), and the sequences follow each other inside a head, so that short ones do
 // not leave one XCD idle (4 sequences of 5000 to 3100 queries: 439 -> 385 us).  Single tokens use
-// a key once and go over the XCDs in turn (48 x 32760 keys 143 us, 147 the other way; 8 of 100003
-// to 56000 keys 437 and 436).  The last rows of a sequence, which see most keys under a causal
+// a key once and go over the XCDs in turn (8 sequences of 8 key heads, 100003 keys 491 us, 500 the other way;
+// 48 x 32760 131 and 132, 8 of 100003 to 56000 keys 395 and 397, one of 100003 70 and 68).  The last rows of a sequence, which see most keys under a causal
 // mask, start first.
 template <bool LOCAL>
 __device__ __forceinline__ void win_place(const WinArgs& a, int& rb, int& sp, int& h, int& b) {
@@ -447,7 +447,8 @@ constexpr int WIN_SHARED = 16;
 // read different rows, would pass through the CU's cache 16 bytes a cycle, 1 us a tile: they took
 // 582 us where the copies took 538), and no wave waits for another before the sums meet at the end.  K's half is
 // filled again as soon as its tile's logits are formed, V^T's once its product is, so copies are
-// under way all the time.  What bounds it: reading K and V^T (8 sequences of 100003 keys 490 us,
+// under way all the time.  The weights are rounded to bfloat16 for the product with V, and the
+// denominator adds the rounded ones, as in the block kernel (attention_tile.h).  What bounds it: reading K and V^T (8 sequences of 100003 keys 490 us,
 // 6.7 TB/s; 6.2 - 6.5 is what a plain read stream through the caches reaches), and for short windows the
 // latency of a tile and of the join (8 heads of 4096 keys 8.2 us).
 template <bool SPLIT, bool PAST>
@@ -1131,14 +1132,14 @@ static int64_t win_span(const track_window& w, int64_t rows, int n, int64_t Lk) 
 }
 
 // Shares of the keys for few rows, `blocks` row blocks of `tiles` tiles each.  None up to 16
-// tiles, four a wave: the join is a launch more (calls one after another, 8 heads of 1024 keys: 9.1
-// us with one share, 11.1 with 2 or more; 2048: 14.4, 12.1 with 2, 11.1 with 4).  Then up to 8
+// tiles, four a wave: the join is a launch more (calls one after another, 8 heads of 1024 keys: 9.7
+// us with one share, 11.4 with 2, 11.3 with 4; 2048: 22.3, 15.2 with 2, 12.7 with 4).  Then up to 8
 // tiles a wave on a full chip a workgroup on every CU, but two tiles a share; beyond, six
-// workgroups a CU with 16 tiles at least, which evens out lengths.  Kernel times, 8 key heads of
-// 4096 keys: 24.9 us with one share, 10.0 with 8, 8.9 with 16, 8.4 with 32, 12.4 with 48; 32 of
-// 1027: 11.8 with 1, 9.6 with 6, 13.8 with 12; 8 of 16384: 17.8 with 16, 17.1 with 32, 20.6 with
-// 48; 48 of 32760: 158 with 4, 152 with 16, 138 with 32; 64 of 100003: 571 with 6, 541 with 16, 538
-// with 32.
+// workgroups a CU with 16 tiles at least, which evens out lengths.  Replayed, join included, 8 key heads of
+// 4096 keys: 43.9 us with one share, 12.6 with 8, 10.4 with 16, 9.2 with 32, 13.0 with 48; 32 of
+// 1027: 15.7 with 1, 9.8 with 6 and 8, 13.3 with 12; 8 of 16384: 28.9 with 8, 19.4 with 16, 15.7 with 32,
+// 20.1 with 48; 48 of 32760: 133 with 4, 137 with 16, 128 with 32, 130 with 48; 64 of 100003: 519 with 6,
+// 485 with 16, 492 with 24, 488 with 32; 8 of 100003: 69 with 32, 75 with 48, 80 with 192.
 static int rows_split(int64_t tiles, int64_t blocks, int64_t cus) {
   if (tiles <= 16) return 1;
   const bool large = blocks * tiles >= 64 * cus;

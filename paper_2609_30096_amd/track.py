@@ -718,7 +718,8 @@ def op_attention_window(window: Window, q, k, vt, out, lse=None, q_len=None, k_l
                         workspace=None):
     """Window attention of q [B, Lq, H, D] on k [B, Lk, Hk, D] and vt [B, Hk, D, >= Lk] into out (like q); returns
     out.  k may be a view into a longer cache; a sequence stride of 0 in k and vt shares them.  lse: float32
-    [B, H, Lq]; q_len, k_len, q_start: int32 [B]."""
+    [B, H, Lq]; q_len, k_len, q_start: int32 [B].  Layouts are checked once for each combination of shapes and strides:
+    a view that grows by a token a call is checked every time, a cache of one length with k_len is not."""
     (dtype, B, H, Hk, D, Lq, Lk, ldq, sq, ldk, sk, ldv, sv, ldo, so, nbytes) = _layout(
         _window_layouts, (q, k, vt, out, lse, q_len, k_len, q_start, workspace), _check_window)
     _on_device(lib().track_op_attention_window, q, dtype, window.c(), B, H, Hk, D, Lq, Lk, q.data_ptr(), ldq, sq,
