@@ -453,6 +453,74 @@ track_status track_op_attention_window(int32_t dtype, const track_window* window
                                        const int32_t* k_len, const int32_t* q_start, void* workspace,
                                        size_t workspace_bytes, void* stream);
 
+/* A paged cache that holds keys and values in 4 bits, for long videos.  32
+ * channels of a token's head share a power of two 2^e, kept as the byte e + 127;
+ * each of their values is a sign and one of 0, 0.5, 1, 1.5, 2, 3, 4, 6 times 2^e,
+ * the nearest, ties to the even code of 0..7.  e is the smallest of -124..125 at
+ * which the group's largest magnitude rounds to 6 2^e or less (it is below
+ * 7 2^e), so nothing is cut off below 7 2^125.  A group that holds an infinity or
+ * a NaN is kept as byte 255, 32 NaNs.  head_dim/2 + head_dim/32 bytes a token's
+ * head, for K and for V: 136 at 128 channels, 512 in bfloat16.
+ *
+ * Place x of sequence b lies in page table[b*ld_table + x / page_tokens], at token
+ * x % page_tokens.  Sequences may share pages.  Places at or past table_pages *
+ * page_tokens, and those of a page id outside [0, n_pages) (-1, say, for a page
+ * given back behind a window), are not there: nothing is written to them, they
+ * read as zero, and no query sees them.
+ * A page: blocks of 64 tokens one after another; a block: its heads; a head of D
+ * channels, 68 D bytes: K codes [64][D/2] (channel 2 i the low half of byte i), at
+ * 32 D V codes [D/32][4 r][16 j][2 s][8 c], byte j of a group the channels 2 j and
+ * 2 j + 1 of token 32 s + 8 r + c, at 64 D K's exponents [4 r][4 c][D/32][2 s][2 h] of
+ * token 32 s + 8 r + 4 h + c, at 66 D V's [D/32][4 r][2 s][8 c]. */
+typedef struct track_cache4 {
+  void* pages;           /* device, 128-byte aligned: n_pages of track_cache4_page_bytes */
+  int64_t n_pages;       /* 1..2^31-1 */
+  int32_t page_tokens;   /* a multiple of 64, at most 65536 */
+  int32_t heads;         /* key heads, 1..2^19 */
+  int32_t head_dim;      /* 32, 64 or 128 */
+  int32_t table_pages;   /* pages of a sequence; 2^28 tokens at most */
+  const int32_t* table;  /* device: page ids, read when a call runs on the stream */
+  int64_t ld_table;      /* entries from sequence to sequence, >= table_pages */
+} track_cache4;
+
+/* Bytes of a page (a multiple of 128), 0 for sizes that are refused. */
+int64_t track_cache4_page_bytes(int32_t heads, int32_t head_dim, int32_t page_tokens);
+
+/* Rows of keys and values into the cache: row i of sequence b, k[b*sk + i*ldk +
+ * h*head_dim + c] and v likewise, to place start[b] + i, for i < n[b] (device int32
+ * [B]; n is cut to [0, L], NULL: L).  With rope (of this head_dim) the keys are
+ * rotated on the way as track_op_rope does, by pos (device int32 [axes][B*L]),
+ * freqs and amplitude; rotation and rounding are float64, so a key is rounded once.
+ * rope NULL: as they are, pos and freqs unused.  No two rows of a call, or of calls
+ * that overlap on the GPU, go to one place.  What the cache holds in other places
+ * stays as it was.  B*L == 0 is a no-op.  Asynchronous, no workspace. */
+track_status track_op_cache4_append(int32_t dtype, const track_cache4* cache, const track_rope_config* rope, int64_t B,
+                                    int64_t L, const void* k, int64_t ldk, int64_t sk, const void* v, int64_t ldv,
+                                    int64_t sv, const int32_t* start, const int32_t* n, const int32_t* pos,
+                                    const double* freqs, float amplitude, void* stream);
+
+/* The way back: places start[b] + i of the cache as rows of k and v (exact in
+ * both types).  Rows at or past n[b] are left as they were.  k and v overlap neither
+ * each other nor the cache. */
+track_status track_op_cache4_read(int32_t dtype, const track_cache4* cache, int64_t B, int64_t L, void* k, int64_t ldk,
+                                  int64_t sk, void* v, int64_t ldv, int64_t sv, const int32_t* start, const int32_t* n,
+                                  void* stream);
+
+/* track_op_attention_window on keys and values of a cache: sequence b's keys are
+ * the places 0 .. k_len[b] - 1 (Lk the most of a sequence, at most table_pages *
+ * page_tokens), Hk and head_dim the cache's; all else, window, rows, lengths, types
+ * and lse, as there (bfloat16: head_dim 128; float32: 32, 64, 128).  A key or value
+ * group that holds no number reaches the rows that see it.  The workspace
+ * (256-byte aligned; -1 for what the call refuses) grows with Lk, and one made for the longest
+ * serves calls of fewer keys.  Asynchronous. */
+int64_t track_attention_cache4_workspace_bytes(int32_t dtype, const track_window* window, int32_t B, int32_t H,
+                                               int32_t Hk, int32_t head_dim, int64_t Lq, int64_t Lk);
+track_status track_op_attention_cache4(int32_t dtype, const track_window* window, const track_cache4* cache, int32_t B,
+                                       int32_t H, int64_t Lq, int64_t Lk, const void* q, int64_t ldq, int64_t sq,
+                                       void* out, int64_t ldo, int64_t so, float* lse, const int32_t* q_len,
+                                       const int32_t* k_len, const int32_t* q_start, void* workspace,
+                                       size_t workspace_bytes, void* stream);
+
 /* Step kernels on token-layout velocities vel [B, n] float32 (B = 2: cond
  * then uncond; B = 1: no guidance).  Guided p = u + w (c - u) (Eq. 1).
  * Sample mode: x[n] += dsigma * p.  Calibration mode also takes the small

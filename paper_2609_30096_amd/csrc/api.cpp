@@ -944,6 +944,39 @@ track_status track_op_attention_window(int32_t dtype, const track_window* window
                           lse, q_len, k_len, q_start, workspace, workspace_bytes, (hipStream_t)stream);
 }
 
+int64_t track_cache4_page_bytes(int32_t heads, int32_t head_dim, int32_t page_tokens) {
+  return cache4_page_bytes(heads, head_dim, page_tokens);
+}
+
+track_status track_op_cache4_append(int32_t dtype, const track_cache4* cache, const track_rope_config* rope, int64_t B,
+                                    int64_t L, const void* k, int64_t ldk, int64_t sk, const void* v, int64_t ldv,
+                                    int64_t sv, const int32_t* start, const int32_t* n, const int32_t* pos,
+                                    const double* freqs, float amplitude, void* stream) {
+  if (rope) TRY(check_rope(rope));
+  return cache4_append(dtype, cache, rope, B, L, k, ldk, sk, v, ldv, sv, start, n, pos, freqs, amplitude,
+                       (hipStream_t)stream);
+}
+
+track_status track_op_cache4_read(int32_t dtype, const track_cache4* cache, int64_t B, int64_t L, void* k, int64_t ldk,
+                                  int64_t sk, void* v, int64_t ldv, int64_t sv, const int32_t* start, const int32_t* n,
+                                  void* stream) {
+  return cache4_read(dtype, cache, B, L, k, ldk, sk, v, ldv, sv, start, n, (hipStream_t)stream);
+}
+
+int64_t track_attention_cache4_workspace_bytes(int32_t dtype, const track_window* window, int32_t B, int32_t H,
+                                               int32_t Hk, int32_t head_dim, int64_t Lq, int64_t Lk) {
+  return attention_cache4_bytes(dtype, window, B, H, Hk, head_dim, Lq, Lk);
+}
+
+track_status track_op_attention_cache4(int32_t dtype, const track_window* window, const track_cache4* cache, int32_t B,
+                                       int32_t H, int64_t Lq, int64_t Lk, const void* q, int64_t ldq, int64_t sq,
+                                       void* out, int64_t ldo, int64_t so, float* lse, const int32_t* q_len,
+                                       const int32_t* k_len, const int32_t* q_start, void* workspace,
+                                       size_t workspace_bytes, void* stream) {
+  return attention_cache4(dtype, window, cache, B, H, Lq, Lk, q, ldq, sq, out, ldo, so, lse, q_len, k_len, q_start,
+                          workspace, workspace_bytes, (hipStream_t)stream);
+}
+
 int64_t track_step_partial_count(int64_t n) { return step_partial_count(n); }
 
 track_status track_op_step(int64_t n, int32_t B, float guidance, float dsigma, const float* vel_L, const float* vel_S,

@@ -1,0 +1,1144 @@
+// A paged cache that holds keys and values in 4 bits: rows into it with the rotation on the way, rows back out of it,
+// and window attention that reads it as it lies.
+//
+// 32 channels of a token's head share a power of two 2^e, kept as the byte e + 127; a value is a sign and a magnitude
+// code 0..7 for 0, 0.5, 1, 1.5, 2, 3, 4, 6 times 2^e (the 4-bit floats with one exponent a group that the matrix and
+// conversion units know): v_cvt_scalef32_pk_bf16_fp4 turns a byte of two codes into two bfloat16 values, exactly, one instruction
+// at the full rate (35.7 T lanes a second).  e is the smallest of -124..125 at which the largest magnitude of the group does not
+// pass 6 when it is rounded, so no value moves by more than half a step.
+//
+// 64 tokens of a head lie together (68 D bytes, whole 128-byte lines), K, V, exponents of K, of V, each in the order
+// in which a lane of v_mfma_f32_16x16x32_bf16 takes it:
+//   K codes      [64 tokens][D / 2]                       16 bytes: a key's group of 32 channels, 4 steps' operands
+//   V codes      [D / 32 groups][4 r][16 j][2 s][8 c]     a byte: channels 32 group + 2 j, + 1 of token 32 s + 8 r + c;
+//                                                         16 bytes: two channels of the 16 keys whose weights a lane holds
+//   K exponents  [4 r][4 c][D / 32][2 s][2 h]             of token 32 s + 8 r + 4 h + c; 4 bytes: those of a lane's 4 keys
+//   V exponents  [D / 32][4 r][2 s][8 c]
+// A page is its blocks of 64 tokens one after another, a block its heads.
+#include "cache4_layout.h"
+#include "window.h"
+
+namespace track {
+
+constexpr int C4_MIN = -124, C4_MAX = 125;  // exponents: half of 2^-124 and six of 2^125 are normal bfloat16 values
+constexpr int64_t C4_HEADS = 1 << 19;
+
+// The cache as the kernels take it.
+struct CacheArgs {
+  uint8_t* pages;
+  const int32_t* table;
+  int64_t ld_table, stride;  // entries between sequences; bytes of 64 tokens of all heads
+  int table_pages, n_pages, blocks, cap;  // pages of a sequence, of the pool; 64-token blocks a page; places of a sequence
+  WinDiv by_blocks;
+};
+
+// The 64 places from 64 t on of sequence b and head h, or null where no page holds them.  All wave-uniform.
+template <int D>
+__device__ __forceinline__ uint8_t* c4_at(const CacheArgs& c, int b, int h, int t) {
+  const int slot = (int)c.by_blocks((uint32_t)t);
+  if (slot >= c.table_pages) return nullptr;
+  const int page = __builtin_amdgcn_readfirstlane(c.table[b * c.ld_table + slot]);
+  if (!c4_page(page, c.n_pages)) return nullptr;
+  return c.pages + c4_block(page, c.blocks, t, slot, c.stride) + (int64_t)h * C4<D>::BYTES;
+}
+
+// ---------------------------------------------------------------- rounding to 4 bits
+// The exponent byte of a group whose largest magnitude is m (255: an infinity or a NaN in it).
+__device__ __forceinline__ int c4_exponent(double m) {
+  const uint32_t hi = (uint32_t)(__builtin_bit_cast(uint64_t, m) >> 32);
+  const int x = (int)(hi >> 20) - 1023;                    // m = f 2^x, f in [1, 2)
+  const int e = x - 2 + ((hi & 0xfffff) >= 0xc0000);       // 7 2^(x - 2) = 1.75 2^x
+  return x == 1024 ? 255 : 127 + min(max(e, C4_MIN), C4_MAX);
+}
+__device__ __forceinline__ int c4_exponent(float m) {
+  const uint32_t w = __float_as_uint(m);
+  const int x = (int)(w >> 23) - 127;
+  const int e = x - 2 + ((w & 0x7fffff) >= 0x600000);
+  return x == 128 ? 255 : 127 + min(max(e, C4_MIN), C4_MAX);
+}
+
+// The code of x at the power of two whose reciprocal is given, ties to the even code (x is finite).
+__device__ __forceinline__ uint32_t c4_code(double x, double inv) {
+  const double y = fabs(x) * inv;  // exact
+  const double f = y < 2.0 ? 2.0 : (y < 4.0 ? 1.0 : 0.5);
+  const double q = rint(y * f) + (y < 2.0 ? 0.0 : (y < 4.0 ? 2.0 : 4.0));
+  return (uint32_t)fmin(q, 7.0) | ((uint32_t)(__builtin_bit_cast(uint64_t, x) >> 60) & 8u);
+}
+__device__ __forceinline__ uint32_t c4_code(float x, float inv) {
+  const float y = fabsf(x) * inv;
+  const float f = y < 2.0f ? 2.0f : (y < 4.0f ? 1.0f : 0.5f);
+  const float q = rintf(y * f) + (y < 2.0f ? 0.0f : (y < 4.0f ? 2.0f : 4.0f));
+  return (uint32_t)fminf(q, 7.0f) | ((__float_as_uint(x) >> 28) & 8u);
+}
+
+// 2^(127 - byte).
+__device__ __forceinline__ float c4_inverse(int byte, float) { return __uint_as_float((uint32_t)(254 - byte) << 23); }
+__device__ __forceinline__ double c4_inverse(int byte, double) {
+  return __builtin_bit_cast(double, (uint64_t)(1023 + 127 - byte) << 52);
+}
+
+// Four bytes of codes of the lane's 8 channels, and the exponent byte of the group that they and those of the 3 lanes beside it make.
+template <typename F>
+__device__ __forceinline__ uint32_t c4_round8(const F (&x)[8], int& byte) {
+  constexpr F most = sizeof(F) == 4 ? (F)3.4028234663852886e38 : (F)1.7976931348623157e308;
+  F m = fabs(x[0]);
+  bool odd = !(m <= most);  // an infinity or a NaN
+#pragma unroll
+  for (int i = 1; i < 8; ++i) {
+    const F a = fabs(x[i]);
+    odd |= !(a <= most);
+    m = fmax(m, a);
+  }
+  int e = odd ? 255 : c4_exponent(m);
+  // the largest exponent of the four lanes is that of the largest magnitude
+  e = max(e, __builtin_amdgcn_update_dpp(0, e, 0xb1, 0xf, 0xf, true));  // quad_perm [1, 0, 3, 2]
+  e = max(e, __builtin_amdgcn_update_dpp(0, e, 0x4e, 0xf, 0xf, true));  // quad_perm [2, 3, 0, 1]
+  byte = e;
+  if (e == 255) return 0;
+  const F inv = c4_inverse(e, F());
+  uint32_t w = 0;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) w |= c4_code(x[i], inv) << (4 * i);
+  return w;
+}
+
+// ---------------------------------------------------------------- rows in and out
+struct RowsArgs {
+  CacheArgs c;
+  void *k, *v;
+  int64_t ldk, sk, ldv, sv;
+  const int32_t *start, *n;
+  int B, L, heads, nblk;  // 64-token blocks that a sequence's rows can touch
+  int hsplit;             // workgroups that share a block's heads
+  bool vec;               // 16-byte aligned rows
+  // rotation
+  const int32_t* pos;
+  const double* freqs;
+  double amp;
+  int pairs, sec0, sec1;
+};
+
+// The 16 tokens of a wave in a block of 64: slot 8 s + c is token 32 s + 8 r + c, wave r.
+struct RowsWave {
+  int b, r, first;       // place of the block's first token, less the sequence's start
+  int n;                 // rows of the sequence
+  uint32_t there;        // slots that hold a row of the call, in a place that the cache has
+  template <int D>
+  __device__ __forceinline__ uint8_t* init(const RowsArgs& a, int item) {
+    b = item / a.nblk;
+    r = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    n = a.n ? __builtin_amdgcn_readfirstlane(max(0, min(a.n[b], a.L))) : a.L;
+    const int start = __builtin_amdgcn_readfirstlane(max(-(int)WIN_MAX, min(a.start[b], (int)WIN_MAX)));
+    const int t = (start >> 6) + item % a.nblk;
+    first = t * C4_BLOCK - start;
+    there = 0;
+    if (t < 0 || t * (int64_t)C4_BLOCK >= a.c.cap) return nullptr;
+#pragma unroll
+    for (int s = 0; s < 16; ++s) {
+      const int i = row(s);
+      there |= (uint32_t)(i >= 0 && i < n) << s;
+    }
+    return there ? c4_at<D>(a.c, b, 0, t) : nullptr;
+  }
+  __device__ __forceinline__ int token(int slot) const { return c4_token(r, slot); }
+  __device__ __forceinline__ int row(int slot) const { return first + token(slot); }
+};
+
+template <typename T>
+__device__ __forceinline__ void c4_load8(const T* p, bool vec, float (&x)[8]) {
+  if (!vec) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = ldf(p + i);
+  } else if constexpr (sizeof(T) == 2) {
+    const u32x4 w = *(const u32x4*)p;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      x[2 * i] = __uint_as_float(w[i] << 16);
+      x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+    }
+  } else {
+    const f32x4 a = *(const f32x4*)p, b = *(const f32x4*)(p + 4);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = a[i], x[4 + i] = b[i];
+  }
+}
+
+// Appends.  A wave takes 16 tokens of a block and walks its heads; a lane has 8 channels of a token, D / 8 lanes a
+// token.  Angles are formed once for all heads, in float64 as the products behind them are: a key next to the border of
+// two codes would otherwise fall to one or the other by how float32 rounds (about one in 10^6, each a whole step off).
+// V's codes change places through LDS (a lane of the output has two channels of 16 tokens).
+template <typename T, int D, int ROT>
+__global__ __launch_bounds__(256) void cache_append_kernel(RowsArgs a) {
+  constexpr int LPT = D / 8, TPS = 64 / LPT, STEPS = 16 / TPS;
+  __shared__ double cs[ROT ? 4 : 1][ROT ? 16 * (D / 2) : 1][2];
+  __shared__ uint32_t codes[4][16 * (D / 8)];
+  const int lane = threadIdx.x & 63;
+  const int item = (int)blockIdx.x / a.hsplit, part = (int)blockIdx.x - item * a.hsplit;
+  RowsWave w;
+  uint8_t* const block = w.init<D>(a, item);
+  if (!block) return;  // the wave has no barrier below
+  if constexpr (ROT != 0) {
+    for (int s = 0; s < 16; ++s) {
+      if (!(w.there >> s & 1)) continue;
+      for (int p = lane; p < a.pairs; p += 64) {
+        const int axis = (p >= a.sec0) + (p >= a.sec1);
+        const double turns = (double)a.pos[((int64_t)axis * a.B + w.b) * a.L + w.row(s)] * (a.freqs[p] * 0.15915494309189533577);
+        double sn, cn;
+        sincospi(2.0 * (turns - rint(turns)), &sn, &cn);
+        cs[w.r][s * (D / 2) + p][0] = cn * a.amp;
+        cs[w.r][s * (D / 2) + p][1] = sn * a.amp;
+      }
+    }
+  }
+  auto settle = [&]() {  // the wave's own LDS writes, before its reads
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+  };
+  settle();
+  const int u = lane % LPT, sub = lane / LPT;
+  const bool all = w.there == 0xffff;
+  for (int h = part; h < a.heads; h += a.hsplit) {
+    uint8_t* const to = block + (int64_t)h * C4<D>::BYTES;
+#pragma unroll
+    for (int st = 0; st < STEPS; ++st) {
+      const int slot = st * TPS + sub, tok = w.token(slot);
+      const bool there = w.there >> slot & 1;
+      const int64_t row = there ? w.row(slot) : 0;
+      // keys
+      const T* const kp = (const T*)a.k + w.b * a.sk + row * a.ldk + (int64_t)h * D;
+      float x[8];
+      c4_load8(kp + 8 * u, a.vec, x);
+      uint32_t word;
+      int byte;
+      if constexpr (ROT == 0) {
+        word = c4_round8(x, byte);
+      } else {
+        double y[8];
+        const double(*const at)[2] = &cs[w.r][slot * (D / 2)];
+        if constexpr (ROT == 1) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const int p = 4 * u + i;
+            if (p < a.pairs) {
+              const double c = at[p][0], s = at[p][1];
+              y[2 * i] = x[2 * i] * c - x[2 * i + 1] * s;
+              y[2 * i + 1] = x[2 * i] * s + x[2 * i + 1] * c;
+            } else {
+              y[2 * i] = x[2 * i];
+              y[2 * i + 1] = x[2 * i + 1];
+            }
+          }
+        } else {
+          float z[8];  // the other channel of each one's pair
+          if (a.vec && (a.pairs & 7) == 0) {
+            const int o = 8 * u < a.pairs ? a.pairs : (8 * u < 2 * a.pairs ? -a.pairs : 0);
+            c4_load8(kp + 8 * u + o, true, z);
+          } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+              const int ch = 8 * u + i;
+              z[i] = ldf(kp + (ch < a.pairs ? ch + a.pairs : (ch < 2 * a.pairs ? ch - a.pairs : ch)));
+            }
+          }
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            const int ch = 8 * u + i;
+            if (ch < 2 * a.pairs) {
+              const bool low = ch < a.pairs;
+              const int p = low ? ch : ch - a.pairs;
+              const double c = at[p][0], s = at[p][1];
+              y[i] = low ? x[i] * c - z[i] * s : z[i] * s + x[i] * c;
+            } else {
+              y[i] = x[i];
+            }
+          }
+        }
+        word = c4_round8(y, byte);
+      }
+      if (there) {
+        *(uint32_t*)(to + C4<D>::k_code(tok, 8 * u)) = word;
+        if ((u & 3) == 0) to[C4<D>::k_exp(tok, u >> 2)] = (uint8_t)byte;
+      }
+      // values
+      const T* const vp = (const T*)a.v + w.b * a.sv + row * a.ldv + (int64_t)h * D;
+      c4_load8(vp + 8 * u, a.vec, x);
+      word = c4_round8(x, byte);
+      codes[w.r][slot * LPT + u] = word;
+      if (there && (u & 3) == 0) to[C4<D>::v_exp(tok, u >> 2)] = (uint8_t)byte;
+    }
+    settle();
+    if (lane < D / 2) {
+      // lane: group lane / 16, byte lane % 16 of a group's 16
+      const uint8_t* const from = (const uint8_t*)codes[w.r] + lane;
+      uint8_t* const vt = to + C4<D>::v_code(8 * w.r, 2 * lane);
+      if (all) {
+        u32x4 o;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          o[i] = (uint32_t)from[(4 * i) * (D / 2)] | (uint32_t)from[(4 * i + 1) * (D / 2)] << 8 |
+                 (uint32_t)from[(4 * i + 2) * (D / 2)] << 16 | (uint32_t)from[(4 * i + 3) * (D / 2)] << 24;
+        *(u32x4*)vt = o;
+      } else {
+        for (int s = 0; s < 16; ++s)
+          if (w.there >> s & 1) vt[s] = from[s * (D / 2)];
+      }
+    }
+    settle();
+  }
+}
+
+// ---------------------------------------------------------------- 4 bits back to values
+// Byte SEL of w as the two values that it stands for at scale s.
+template <int SEL>
+__device__ __forceinline__ uint32_t c4_pair(uint32_t w, float s) {
+  return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, SEL));
+}
+template <int SEL>
+__device__ __forceinline__ f32x2 c4_pair_f32(uint32_t w, float s) {
+  return __builtin_bit_cast(f32x2, __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, s, SEL));
+}
+// Byte I of w as a float whose exponent it is (255 gives NaN in the conversions).
+template <int I>
+__device__ __forceinline__ float c4_scale(uint32_t w) {
+  return __uint_as_float(((w >> (8 * I)) & 0xffu) << 23);
+}
+// Four bytes of codes, 8 channels of one group, as bfloat16.
+__device__ __forceinline__ u32x4 c4_eight(uint32_t w, float s) {
+  return u32x4{c4_pair<0>(w, s), c4_pair<1>(w, s), c4_pair<2>(w, s), c4_pair<3>(w, s)};
+}
+// Two channels (a byte each key) of four keys with exponents e: the channels' four keys, two words each.
+__device__ __forceinline__ void c4_four(uint32_t w, uint32_t e, uint32_t (&lo)[2], uint32_t (&hi)[2]) {
+  const uint32_t a = c4_pair<0>(w, c4_scale<0>(e)), b = c4_pair<1>(w, c4_scale<1>(e));
+  const uint32_t c = c4_pair<2>(w, c4_scale<2>(e)), d = c4_pair<3>(w, c4_scale<3>(e));
+  lo[0] = __builtin_amdgcn_perm(b, a, 0x05040100), hi[0] = __builtin_amdgcn_perm(b, a, 0x07060302);
+  lo[1] = __builtin_amdgcn_perm(d, c, 0x05040100), hi[1] = __builtin_amdgcn_perm(d, c, 0x07060302);
+}
+
+template <typename T>
+__device__ __forceinline__ void c4_store8(T* p, bool vec, uint32_t w, float s) {
+  if constexpr (sizeof(T) == 2) {
+    const u32x4 x = c4_eight(w, s);
+    if (vec) {
+      *(u32x4*)p = x;
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) p[i] = (bf16_t)(i & 1 ? x[i >> 1] >> 16 : x[i >> 1]);
+    }
+  } else {
+    const f32x2 a = c4_pair_f32<0>(w, s), b = c4_pair_f32<1>(w, s), c = c4_pair_f32<2>(w, s), d = c4_pair_f32<3>(w, s);
+    if (vec) {
+      *(f32x4*)p = f32x4{a[0], a[1], b[0], b[1]};
+      *(f32x4*)(p + 4) = f32x4{c[0], c[1], d[0], d[1]};
+    } else {
+      p[0] = a[0], p[1] = a[1], p[2] = b[0], p[3] = b[1], p[4] = c[0], p[5] = c[1], p[6] = d[0], p[7] = d[1];
+    }
+  }
+}
+
+// Rows out of the cache: the append's shape the other way round.  Places without a page read as zero.
+template <typename T, int D>
+__global__ __launch_bounds__(256) void cache_read_kernel(RowsArgs a) {
+  constexpr int LPT = D / 8, TPS = 64 / LPT, STEPS = 16 / TPS;
+  __shared__ u32x4 codes[4][D / 2];
+  const int lane = threadIdx.x & 63;
+  const int item = (int)blockIdx.x / a.hsplit, part = (int)blockIdx.x - item * a.hsplit;
+  RowsWave w;
+  const uint8_t* const block = w.init<D>(a, item);
+  const int u = lane % LPT, sub = lane / LPT;
+  if (!block) {  // rows in places that the cache does not have
+#pragma unroll
+    for (int st = 0; st < STEPS; ++st) {
+      const int row = w.row(st * TPS + sub);
+      if (row < 0 || row >= w.n) continue;
+      for (int h = part; h < a.heads; h += a.hsplit) {
+        c4_store8((T*)a.k + w.b * a.sk + (int64_t)row * a.ldk + (int64_t)h * D + 8 * u, a.vec, 0, 1.0f);
+        c4_store8((T*)a.v + w.b * a.sv + (int64_t)row * a.ldv + (int64_t)h * D + 8 * u, a.vec, 0, 1.0f);
+      }
+    }
+    return;
+  }
+  auto settle = [&]() {
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+  };
+  for (int h = part; h < a.heads; h += a.hsplit) {
+    const uint8_t* const from = block + (int64_t)h * C4<D>::BYTES;
+    if (lane < D / 2) codes[w.r][lane] = *(const u32x4*)(from + C4<D>::v_code(8 * w.r, 2 * lane));
+    settle();
+#pragma unroll
+    for (int st = 0; st < STEPS; ++st) {
+      const int slot = st * TPS + sub, tok = w.token(slot);
+      if (!(w.there >> slot & 1)) continue;
+      const int64_t row = w.row(slot);
+      const uint32_t kw = *(const uint32_t*)(from + C4<D>::k_code(tok, 8 * u));
+      const int ke = from[C4<D>::k_exp(tok, u >> 2)];
+      c4_store8((T*)a.k + w.b * a.sk + row * a.ldk + (int64_t)h * D + 8 * u, a.vec, kw, __uint_as_float((uint32_t)ke << 23));
+      const uint8_t* const p = (const uint8_t*)&codes[w.r][4 * u] + slot;
+      const uint32_t vw = (uint32_t)p[0] | (uint32_t)p[16] << 8 | (uint32_t)p[32] << 16 | (uint32_t)p[48] << 24;
+      const int ve = from[C4<D>::v_exp(tok, u >> 2)];
+      c4_store8((T*)a.v + w.b * a.sv + row * a.ldv + (int64_t)h * D + 8 * u, a.vec, vw, __uint_as_float((uint32_t)ve << 23));
+    }
+    settle();
+  }
+}
+
+// ---------------------------------------------------------------- few rows, bfloat16
+// A byte of 0x80 for each byte of x that is 255.
+__device__ __forceinline__ uint32_t c4_nan_bytes(uint32_t x) { return ((x & 0x7f7f7f7fu) + 0x01010101u) & x & 0x80808080u; }
+// Bytes of four keys of which `left` are to keep (any number).
+__device__ __forceinline__ uint32_t c4_keep(int left) { return (uint32_t)((1ull << (8 * min(max(left, 0), 4))) - 1ull); }
+
+// What a lane takes of a 64-key tile: 4 keys' groups of K with their exponents, two channels of each V group for its 16 keys, and these keys'
+// exponents of every group.
+struct C4Raw {
+  u32x4 k[4], v[4], e[4];
+  uint32_t ke;
+};
+
+// At most 16 rows a key head (a token of 16 query heads, four tokens of 4).  The four waves of a workgroup take every
+// fourth tile of its share.  The layout makes every operand a lane's own bytes, so a tile goes from memory to
+// registers, 16 bytes a lane and whole lines a load, and there to bfloat16; nothing passes through LDS until the waves' sums meet.
+// The next tile's loads are under way while one is computed on.
+template <bool SPLIT>
+__global__ __launch_bounds__(256) void cache_rows_kernel(WinArgs a, CacheArgs ca) {
+  constexpr int BKV = C4_BLOCK, D = ATT_D, F = D / 16;
+  __shared__ f32x4 so[4][F][64];
+  __shared__ float sm[4][16], sl[4][16];
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+  const int jq = lane & 15, g = lane >> 4;
+  int rb, sp, h, b;
+  win_place<false>(a, rb, sp, h, b);
+  const WinSeq seq = win_seq(a, b);
+  const int rows = seq.qlen * a.n;  // at most 16
+  if (rows == 0) return;            // the whole workgroup
+
+  int lo0, hi0, lo1, hi1;
+  win_range(a, seq, 0, lo0, hi0);
+  win_range(a, seq, seq.qlen - 1, lo1, hi1);
+  WinTiles tiles;
+  tiles.init<BKV>(seq, __builtin_amdgcn_readfirstlane(lo0), __builtin_amdgcn_readfirstlane(hi0),
+                  __builtin_amdgcn_readfirstlane(lo1), __builtin_amdgcn_readfirstlane(hi1));
+  int i0 = 0, i1 = tiles.n;
+  if (SPLIT) win_share(tiles.n, sp, a.nsplit, i0, i1);
+
+  // the lane's row (the last one again past the end)
+  int e;
+  const int qi = win_query(a, min(jq, rows - 1), e), head = h * a.n + e;
+  WinMask<1> mask;
+  mask.sink = tiles.sink;
+  win_range(a, seq, qi, mask.lo[0], mask.hi[0]);
+  if (tiles.sink == 0 && seq.sink >= lo1) mask.lo[0] = 0;
+  // a lane's channels 32 g + 8 step .. + 7, as its bytes of K hold them
+  const bf16_t* qp = (const bf16_t*)a.q + b * a.sq + (int64_t)qi * a.ldq + (int64_t)head * D + 32 * g;
+  bf16x8 qf[D / 32];
+#pragma unroll
+  for (int kc = 0; kc < D / 32; ++kc) qf[kc] = __builtin_bit_cast(bf16x8, *(const u32x4*)(qp + kc * 8));
+  const uint32_t koff = c4_row_k(lane), keoff = c4_row_ke(lane), voff = c4_row_v(lane, 0), veoff = c4_row_ve(lane, 0);
+  // Loads that are not needed (no page, past the share) read the pool's first block: as many for every
+  // tile, so that the wait for the older ones can count.
+  auto fetch = [&](int idx, C4Raw& r) {
+    const uint8_t* p = idx < i1 ? c4_at<D>(ca, b, h, tiles.key<BKV>(idx) >> 6) : nullptr;
+    const bool there = p != nullptr;
+    if (!there) p = ca.pages;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) r.k[i] = __builtin_nontemporal_load((const u32x4*)(p + (koff + c4_row_k_block(i))));
+    r.ke = __builtin_nontemporal_load((const uint32_t*)(p + keoff));
+#pragma unroll
+    for (int m = 0; m < 4; ++m) r.v[m] = __builtin_nontemporal_load((const u32x4*)(p + (voff + (c4_row_v(0, m) - c4_row_v(0, 0)))));
+#pragma unroll
+    for (int m = 0; m < 4; ++m) r.e[m] = __builtin_nontemporal_load((const u32x4*)(p + (veoff + (c4_row_ve(0, m) - c4_row_ve(0, 0)))));
+    return there;
+  };
+
+  f32x4 o[F];
+  float m = -INFINITY, l = 0.0f;  // reference (log2 units), the lane's part of the denominator
+#pragma unroll
+  for (int f = 0; f < F; ++f) o[f] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+
+  auto tile = [&](int idx, C4Raw& r) {
+    const int key0 = tiles.key<BKV>(idx);
+    const bool edge = idx < tiles.edge;
+    const float ks[4] = {c4_scale<0>(r.ke), c4_scale<1>(r.ke), c4_scale<2>(r.ke), c4_scale<3>(r.ke)};
+    f32x4 s[BKV / 16];
+#pragma unroll
+    for (int kc = 0; kc < D / 32; ++kc)
+#pragma unroll
+      for (int i = 0; i < BKV / 16; ++i)
+        s[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, c4_eight(r.k[i][kc], ks[i])), qf[kc],
+                                                       kc ? s[i] : f32x4{0.0f, 0.0f, 0.0f, 0.0f}, 0, 0, 0);
+    uint32_t lost = 0;  // groups of V in which a key that the row sees holds no number
+    if (edge) {
+      WinMask<1> mk = mask;
+      mk.key0 = key0;
+      mk.begin();
+#pragma unroll
+      for (int i = 0; i < BKV / 16; ++i)
+#pragma unroll
+        for (int x = 0; x < 4; ++x) s[i][x] = mk.apply(0, 32 * (i >> 1) + 4 * (i & 1) + x, s[i][x]);
+      // V past the last key, which may be anything, takes exponent 0 (a weight of zero would not remove a NaN), and so do
+      // groups that hold one, whose keys some rows may not see: they are put into the rows that do
+      const int last = seq.klen - key0 - 8 * g;
+      uint32_t any = 0;
+#pragma unroll
+      for (int mm = 0; mm < 4; ++mm)
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+          r.e[mm][w] &= c4_keep(last - 32 * (w >> 1) - 4 * (w & 1));
+          any |= c4_nan_bytes(r.e[mm][w]);
+        }
+      if (__ballot(any != 0)) {
+#pragma unroll
+        for (int mm = 0; mm < 4; ++mm)
+#pragma unroll
+          for (int w = 0; w < 4; ++w) {
+            const uint32_t bad = c4_nan_bytes(r.e[mm][w]) >> 7;
+            const uint32_t seen = ~(mk.bits[0] >> (4 * w));
+            const uint32_t hit = (bad & seen & 1u) | ((bad >> 8) & (seen >> 1) & 1u) | ((bad >> 16) & (seen >> 2) & 1u) |
+                                 ((bad >> 24) & (seen >> 3) & 1u);
+            lost |= hit << mm;
+            r.e[mm][w] &= ~(bad * 255u);
+          }
+        lost |= (uint32_t)__shfl_xor((int)lost, 16);
+        lost |= (uint32_t)__shfl_xor((int)lost, 32);
+      }
+    }
+    float t = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < BKV / 16; ++i)
+#pragma unroll
+      for (int x = 0; x < 4; ++x) t = fmaxf(t, s[i][x]);
+    const float mn = fmaxf(m, group_max2(t, t) * a.scale_log2);
+    if (__ballot(mn > m)) {
+      const float alpha = mn == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m - mn);
+      l *= alpha;
+#pragma unroll
+      for (int f = 0; f < F; ++f)
+#pragma unroll
+        for (int x = 0; x < 4; ++x) o[f][x] *= alpha;
+      m = mn;
+    }
+    const float nm = m == -INFINITY ? 0.0f : -m;
+    u32x4 pw[BKV / 32];
+#pragma unroll
+    for (int c = 0; c < BKV / 32; ++c)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const f32x4 x = s[2 * c + (q >> 1)];
+        const float p0 = __builtin_amdgcn_exp2f(fmaf(x[2 * (q & 1)], a.scale_log2, nm));
+        const float p1 = __builtin_amdgcn_exp2f(fmaf(x[2 * (q & 1) + 1], a.scale_log2, nm));
+        pw[c][q] = pack_bf2(p0, p1);
+        // the denominator adds the weights as rounded for the product with V
+        l += __uint_as_float(pw[c][q] << 16) + __uint_as_float(pw[c][q] & 0xffff0000u);
+      }
+#pragma unroll
+    for (int c = 0; c < BKV / 32; ++c)
+#pragma unroll
+      for (int mm = 0; mm < D / 32; ++mm) {
+        uint32_t lo[2][2], hi[2][2];
+#pragma unroll
+        for (int w = 0; w < 2; ++w) c4_four(r.v[mm][2 * c + w], r.e[mm][2 * c + w], lo[w], hi[w]);
+        const bf16x8 p = __builtin_bit_cast(bf16x8, pw[c]);
+        o[2 * mm] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, u32x4{lo[0][0], lo[0][1], lo[1][0], lo[1][1]}), p, o[2 * mm], 0, 0, 0);
+        o[2 * mm + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, u32x4{hi[0][0], hi[0][1], hi[1][0], hi[1][1]}), p, o[2 * mm + 1], 0, 0, 0);
+      }
+    if (edge && __ballot(lost != 0)) {
+#pragma unroll
+      for (int f = 0; f < F; ++f)
+#pragma unroll
+        for (int x = 0; x < 4; ++x) o[f][x] = lost >> (f >> 1) & 1 ? NAN : o[f][x];
+    }
+  };
+  C4Raw r0, r1;
+  int idx = i0 + wave;
+  bool there = fetch(idx, r0);
+  while (idx < i1) {
+    bool next = fetch(idx + 4, r1);
+    if (there) tile(idx, r0);
+    idx += 4;
+    if (idx >= i1) break;
+    there = fetch(idx + 4, r0);
+    if (next) tile(idx, r1);
+    idx += 4;
+  }
+
+  // join the four waves: each takes one of the four groups of 32 channels; a lane's are 32 wave + 8 g .. + 7
+  l += __shfl_xor(l, 16);
+  l += __shfl_xor(l, 32);
+#pragma unroll
+  for (int f = 0; f < F; ++f) so[wave][f][lane] = o[f];
+  if (g == 0) {
+    sm[wave][jq] = m;
+    sl[wave][jq] = l;
+  }
+  __syncthreads();
+  float mx = -INFINITY, sum = 0.0f, wt[4];
+#pragma unroll
+  for (int w = 0; w < 4; ++w) mx = fmaxf(mx, sm[w][jq]);
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    const float mi = sm[w][jq];
+    wt[w] = mi == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(mi - mx);  // a wave without keys
+    sum = fmaf(wt[w], sl[w][jq], sum);
+  }
+  if (jq >= rows) return;
+  const int64_t pr = ((((int64_t)sp * a.B + b) * a.Hk + h) * a.Lq) * a.n + jq;
+  const float inv = SPLIT ? 1.0f : win_inverse(sum);
+  f32x4 v0 = {0.0f, 0.0f, 0.0f, 0.0f}, v1 = v0;
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    const f32x4 x = so[w][2 * wave][lane], y = so[w][2 * wave + 1][lane];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      v0[i] = fmaf(wt[w], x[i], v0[i]);
+      v1[i] = fmaf(wt[w], y[i], v1[i]);
+    }
+  }
+  const int ch = 32 * wave + 8 * g;
+  if constexpr (SPLIT) {
+    *(f32x4*)(a.po + pr * D + ch) = f32x4{v0[0], v1[0], v0[1], v1[1]};
+    *(f32x4*)(a.po + pr * D + ch + 4) = f32x4{v0[2], v1[2], v0[3], v1[3]};
+  } else {
+    *(u32x4*)((bf16_t*)a.out + b * a.so + (int64_t)qi * a.ldo + (int64_t)head * D + ch) =
+        u32x4{pack_bf2(v0[0] * inv, v1[0] * inv), pack_bf2(v0[1] * inv, v1[1] * inv), pack_bf2(v0[2] * inv, v1[2] * inv),
+              pack_bf2(v0[3] * inv, v1[3] * inv)};
+  }
+  if (wave == 0 && g == 0) {
+    if constexpr (SPLIT) a.pml[pr] = float2{mx, sum};
+    else if (a.lse) a.lse[((int64_t)b * a.Hk * a.n + head) * a.Lq + qi] = win_lse(mx, sum);
+  }
+}
+
+// ---------------------------------------------------------------- many rows, bfloat16
+// 256 rows a workgroup, 32 a wave, and the tile body of the plain attention on tiles that the workgroup turns into bfloat16 in LDS
+// (attention_tile.h's layout): half of the threads take K's 16 bytes each, half V's.  The next tile's bytes are under way while one is computed on.
+template <bool QLOG2, bool SPLIT>
+__global__ __launch_bounds__(512) void cache_blocks_kernel(WinArgs a, CacheArgs ca) {
+  constexpr int BKV = ATT_BKV, D = ATT_D, SLOT = ATT_SLOT;
+  __shared__ __attribute__((aligned(1024))) uint8_t smem[2 * SLOT + 2 * 256];  // two tiles, and where V holds no number
+  const int tid = threadIdx.x;
+  const int lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int jq = lane & 15, g = lane >> 4;
+  int rb, sp, h, b;
+  win_place<true>(a, rb, sp, h, b);
+  const WinSeq seq = win_seq(a, b);
+  const int rows = seq.qlen * a.n;
+  const int r0 = rb * ATT_BQ;
+  if (r0 >= rows) return;  // the whole workgroup
+
+  // windows of the block's first and last row, and of the wave's
+  auto range_of = [&](int r, int& lo, int& hi) {
+    win_range(a, seq, (int)a.by_n((uint32_t)min(r, rows - 1)), lo, hi);
+    lo = __builtin_amdgcn_readfirstlane(lo);
+    hi = __builtin_amdgcn_readfirstlane(hi);
+  };
+  int lo0, hi0, lo1, hi1;
+  range_of(r0, lo0, hi0);
+  range_of(r0 + ATT_BQ - 1, lo1, hi1);
+  WinTiles tiles;
+  tiles.init<BKV>(seq, lo0, hi0, lo1, hi1);
+  const int wr0 = r0 + 32 * wave;
+  int wlo, whi, unused;
+  range_of(wr0, wlo, unused);
+  range_of(wr0 + 31, unused, whi);
+  if (tiles.sink == 0 && seq.sink >= lo1) wlo = 0;
+  const bool live = wr0 < rows;
+
+  bf16x8 qf[D / 32][ATT_QB];
+  WinMask<ATT_QB> mask;
+  mask.sink = tiles.sink;
+#pragma unroll
+  for (int i = 0; i < ATT_QB; ++i) {
+    int e;
+    const int qi = win_query(a, min(wr0 + 16 * i + jq, rows - 1), e);
+    win_range(a, seq, qi, mask.lo[i], mask.hi[i]);
+    if (tiles.sink == 0 && seq.sink >= lo1) mask.lo[i] = 0;
+    const bf16_t* qp = (const bf16_t*)a.q + b * a.sq + (int64_t)qi * a.ldq + (int64_t)(h * a.n + e) * D + g * 8;
+#pragma unroll
+    for (int kc = 0; kc < D / 32; ++kc) qf[kc][i] = __builtin_bit_cast(bf16x8, *(const u32x4*)(qp + kc * 32));
+  }
+
+  // What this thread brings in: 16 bytes of K, group kg of key kt, or 16 of V, channels vc and vc + 1 of the keys
+  // 32 s + 8 vr + 0..7.  The LDS row of key (channel) 8 q + 4 x + j of 32 is 16 x + 4 q + j.
+  auto row_of = [](int x) { return (x & 32) | (x & 64) | (((x >> 2) & 1) << 4) | (((x >> 3) & 3) << 2) | (x & 3); };
+  const bool isv = wave >= 4;
+  const int t8 = tid & 255;
+  const int kt = c4_tile_key(t8), kg = c4_tile_group(t8), vr = c4_tile_r(t8), vc = c4_tile_channel(t8), vm = vc >> 5;
+  const uint32_t from = c4_tile_codes(isv, t8), efrom = c4_tile_exp(isv, t8);
+  const int krow = row_of(kt), vrow[2] = {row_of(vc), row_of(vc + 1)};
+  struct Raw {
+    u32x4 w, e;
+  };
+  auto fetch = [&](const uint8_t* p, Raw& r) {
+    r.w = *(const u32x4*)(p + from);
+    if (isv) r.e = *(const u32x4*)(p + efrom);
+    else r.e[0] = p[efrom];
+  };
+  auto spread = [&](Raw& r, int slot, int key0, bool edge) {
+    if (!isv) {
+      const float s = __uint_as_float(r.e[0] << 23);
+      uint8_t* const to = smem + slot + krow * 256;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) *(u32x4*)(to + (((4 * kg + i) ^ (krow & 15)) << 4)) = c4_eight(r.w[i], s);
+      return;
+    }
+    if (edge) {
+      // V past the last key takes exponent 0, and so do groups that hold no number (below)
+      u32x4 bad;
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        r.e[w] &= c4_keep(seq.klen - key0 - 8 * vr - 32 * (w >> 1) - 4 * (w & 1));
+        bad[w] = c4_nan_bytes(r.e[w]) >> 7;
+        r.e[w] &= ~(bad[w] * 255u);
+      }
+      if ((t8 & 15) == 0) *(u32x4*)(smem + 2 * SLOT + (slot ? 256 : 0) + (vm * 4 + vr) * 16) = bad;
+    }
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+      uint32_t lo[2][2], hi[2][2];
+#pragma unroll
+      for (int w = 0; w < 2; ++w) c4_four(r.w[2 * s + w], r.e[2 * s + w], lo[w], hi[w]);
+      uint8_t* const to = smem + slot + ATT_K_BYTES;
+      *(u32x4*)(to + vrow[0] * ATT_VROW + (((4 * s + vr) ^ att_vswz(vrow[0])) << 4)) = u32x4{lo[0][0], lo[0][1], lo[1][0], lo[1][1]};
+      *(u32x4*)(to + vrow[1] * ATT_VROW + (((4 * s + vr) ^ att_vswz(vrow[1])) << 4)) = u32x4{hi[0][0], hi[0][1], hi[1][0], hi[1][1]};
+    }
+  };
+  auto barrier = [&]() {
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt((15 << 0) | (3 << 14) | (7 << 4) | (0 << 8));  // lgkmcnt(0)
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+  };
+
+  uint32_t ko = jq * 256 + ((g ^ jq) << 4), vo = jq * ATT_VROW + ((g ^ att_vswz(jq)) << 4);
+  int slot = 0;  // byte offset of the slot computed on
+  AttState st;
+  st.reset();
+  int i0 = 0, i1 = tiles.n;
+  if (SPLIT) win_share(tiles.n, sp, a.nsplit, i0, i1);
+  const uint8_t* at = nullptr;
+  auto find = [&](int idx) {  // the next tile that a page holds
+    for (at = nullptr; idx < i1; ++idx) {
+      at = c4_at<D>(ca, b, h, tiles.key<BKV>(idx) >> 6);
+      if (at) break;
+    }
+    return idx;
+  };
+  Raw raw;
+  int idx = find(i0);
+  if (idx < i1) {
+    fetch(at, raw);
+    spread(raw, 0, tiles.key<BKV>(idx), idx < tiles.edge);
+  }
+  barrier();
+  while (idx < i1) {
+    const int next = find(idx + 1);
+    if (next < i1) fetch(at, raw);
+    const int key0 = tiles.key<BKV>(idx);
+    if (idx < tiles.edge) {
+      if (live && key0 <= whi && (key0 + BKV > wlo || key0 < tiles.sink)) {
+        mask.key0 = key0;
+        att_tile_masked<WinMask<ATT_QB>, QLOG2, 4, true, false>(smem, qf, ko, vo, st, mask, a.scale_log2);
+        // rows that see a key whose V holds no number in a group of channels have none there
+        u32x4 bad[4];
+        uint32_t any = 0;
+#pragma unroll
+        for (int m = 0; m < 4; ++m) {
+          bad[m] = *(const u32x4*)(smem + 2 * SLOT + (slot ? 256 : 0) + (m * 4 + g) * 16);
+          any |= bad[m][0] | bad[m][1] | bad[m][2] | bad[m][3];
+        }
+        if (__ballot(any != 0)) {
+          WinMask<ATT_QB> mk = mask;
+          mk.begin();
+#pragma unroll
+          for (int i = 0; i < ATT_QB; ++i) {
+            uint32_t lost = 0;
+#pragma unroll
+            for (int m = 0; m < 4; ++m)
+#pragma unroll
+              for (int w = 0; w < 4; ++w)
+#pragma unroll
+                for (int x = 0; x < 4; ++x)
+                  lost |= ((bad[m][w] >> (8 * x)) & ~(mk.bits[i] >> (4 * w + x)) & 1u) << m;
+            lost |= (uint32_t)__shfl_xor((int)lost, 16);
+            lost |= (uint32_t)__shfl_xor((int)lost, 32);
+#pragma unroll
+            for (int f = 0; f < D / 16; ++f)
+#pragma unroll
+              for (int r = 0; r < 4; ++r) st.o[f][i][r] = lost >> (f >> 1) & 1 ? NAN : st.o[f][i][r];
+          }
+        }
+      }
+    } else if (live) {
+      att_tile_masked<AttAll, QLOG2, 4, true, false>(smem, qf, ko, vo, st, AttAll{}, a.scale_log2);
+    }
+    if (next < i1) spread(raw, slot ^ SLOT, tiles.key<BKV>(next), next < tiles.edge);
+    ko ^= SLOT;
+    vo ^= SLOT;
+    slot ^= SLOT;
+    idx = next;
+    barrier();
+  }
+
+  // lane: query jq of each block, channels 32 p + 8 g .. + 7
+#pragma unroll
+  for (int i = 0; i < ATT_QB; ++i) {
+    const int r = wr0 + 16 * i + jq;
+    const float m = att_of_block(st.ms, i, lane), l = st.lsum[i][0];
+    if (r >= rows) continue;
+    if constexpr (SPLIT) {
+      const int64_t pr = ((((int64_t)sp * a.B + b) * a.Hk + h) * a.Lq) * a.n + r;
+      float* o = a.po + pr * D + 8 * g;
+#pragma unroll
+      for (int p = 0; p < D / 32; ++p) {
+        *(f32x4*)(o + 32 * p) = st.o[2 * p][i];
+        *(f32x4*)(o + 32 * p + 4) = st.o[2 * p + 1][i];
+      }
+      if (g == 0) a.pml[pr] = float2{m, l};
+    } else {
+      int e;
+      const int qi = win_query(a, r, e), head = h * a.n + e;
+      const float inv = win_inverse(l);
+      bf16_t* o = (bf16_t*)a.out + b * a.so + (int64_t)qi * a.ldo + (int64_t)head * D + 8 * g;
+#pragma unroll
+      for (int p = 0; p < D / 32; ++p) {
+        const f32x4 &x = st.o[2 * p][i], &y = st.o[2 * p + 1][i];
+        *(u32x4*)(o + 32 * p) = u32x4{pack_bf2(x[0] * inv, x[1] * inv), pack_bf2(x[2] * inv, x[3] * inv),
+                                      pack_bf2(y[0] * inv, y[1] * inv), pack_bf2(y[2] * inv, y[3] * inv)};
+      }
+      if (a.lse && g == 0) a.lse[((int64_t)b * a.Hk * a.n + head) * a.Lq + qi] = win_lse(m, l);
+    }
+  }
+}
+
+// ---------------------------------------------------------------- float32
+// 16 rows a workgroup; a tile of 64 keys is turned into float32 in LDS (rows of K, rows of V^T, 16-byte units at unit ^ (row & 7)), each of
+// the four waves takes 16 of its keys, and the next tile's bytes are under way meanwhile.
+template <int D, bool VEC, bool SPLIT>
+__global__ __launch_bounds__(256) void cache_f32_kernel(WinArgs a, CacheArgs ca) {
+  constexpr int C = D / 16, TK = C4_BLOCK, W = 4, ROWS = 16;
+  constexpr int HALF = TK * D * 4, NW = D / 32;  // words of codes a thread brings, of K and of V
+  constexpr int SO = W * C * 1024, LDS = 2 * HALF > SO + W * 128 ? 2 * HALF : SO + W * 128;
+  __shared__ __attribute__((aligned(1024))) uint8_t smem[LDS];
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int jq = lane & 15, g = lane >> 4;
+  int rb, sp, h, b;
+  win_place<true>(a, rb, sp, h, b);
+  const WinSeq seq = win_seq(a, b);
+  const int rows = seq.qlen * a.n;
+  const int r0 = rb * ROWS;
+  if (r0 >= rows) return;  // the whole workgroup
+  int lo0, hi0, lo1, hi1;
+  win_range(a, seq, (int)a.by_n((uint32_t)r0), lo0, hi0);
+  win_range(a, seq, (int)a.by_n((uint32_t)min(r0 + ROWS - 1, rows - 1)), lo1, hi1);
+  lo0 = __builtin_amdgcn_readfirstlane(lo0), hi0 = __builtin_amdgcn_readfirstlane(hi0);
+  lo1 = __builtin_amdgcn_readfirstlane(lo1), hi1 = __builtin_amdgcn_readfirstlane(hi1);
+  WinTiles tiles;
+  tiles.init<TK>(seq, lo0, hi0, lo1, hi1);
+  int i0 = 0, i1 = tiles.n;
+  if (SPLIT) win_share(tiles.n, sp, a.nsplit, i0, i1);
+  int wlo = lo0;
+  if (tiles.sink == 0 && seq.sink >= lo1) wlo = 0;
+  const int mine = 16 * wave;
+
+  typedef C4F32<D> At;
+  const int kt = tid >> 2, kc = At::k_channel(tid), vc = At::v_channel(tid);
+  struct Raw {
+    uint32_t k[NW], v[NW], e[NW], ke;
+  };
+  auto fetch = [&](const uint8_t* p, Raw& r) {
+    const uint32_t* kp = (const uint32_t*)(p + At::k_codes(tid));
+    const uint32_t* vp = (const uint32_t*)(p + At::v_codes(tid));
+    const uint32_t* ep = (const uint32_t*)(p + At::v_exp(tid));
+#pragma unroll
+    for (int i = 0; i < NW; ++i) r.k[i] = kp[i], r.v[i] = vp[i], r.e[i] = ep[i];
+    r.ke = p[At::k_exp(tid)];
+  };
+  auto spread = [&](const Raw& r) {
+    const float s = __uint_as_float(r.ke << 23);
+    uint8_t* const kto = smem + kt * (D * 4);
+#pragma unroll
+    for (int i = 0; i < NW; ++i) {
+      const int unit = kc / 4 + 2 * i;
+      const f32x2 x0 = c4_pair_f32<0>(r.k[i], s), x1 = c4_pair_f32<1>(r.k[i], s), x2 = c4_pair_f32<2>(r.k[i], s), x3 = c4_pair_f32<3>(r.k[i], s);
+      *(f32x4*)(kto + ((unit ^ (kt & 7)) << 4)) = f32x4{x0[0], x0[1], x1[0], x1[1]};
+      *(f32x4*)(kto + (((unit + 1) ^ (kt & 7)) << 4)) = f32x4{x2[0], x2[1], x3[0], x3[1]};
+    }
+#pragma unroll
+    for (int i = 0; i < NW; ++i) {
+      const int unit = At::v_key(tid, i) >> 2;
+      const f32x2 x0 = c4_pair_f32<0>(r.v[i], c4_scale<0>(r.e[i])), x1 = c4_pair_f32<1>(r.v[i], c4_scale<1>(r.e[i]));
+      const f32x2 x2 = c4_pair_f32<2>(r.v[i], c4_scale<2>(r.e[i])), x3 = c4_pair_f32<3>(r.v[i], c4_scale<3>(r.e[i]));
+#pragma unroll
+      for (int y = 0; y < 2; ++y)
+        *(f32x4*)(smem + HALF + (vc + y) * (TK * 4) + ((unit ^ ((vc + y) & 7)) << 4)) = f32x4{x0[y], x1[y], x2[y], x3[y]};
+    }
+  };
+  WinF32<D> st;
+  st.template begin<VEC>(a, seq, tiles, lo1, h, r0 + jq, rows);
+  const uint8_t* at = nullptr;
+  auto find = [&](int idx) {  // the next tile that a page holds
+    for (at = nullptr; idx < i1; ++idx) {
+      at = c4_at<D>(ca, b, h, tiles.key<TK>(idx) >> 6);
+      if (at) break;
+    }
+    return idx;
+  };
+  Raw raw;
+  int idx = find(i0);
+  if (idx < i1) fetch(at, raw);
+  while (idx < i1) {
+    spread(raw);
+    __syncthreads();
+    const int next = find(idx + 1);
+    if (next < i1) fetch(at, raw);
+    const int key0 = tiles.key<TK>(idx), k0 = key0 + mine;
+    const bool edge = idx < tiles.edge;
+    if (!edge || (k0 <= hi1 && (k0 + 16 > wlo || k0 < tiles.sink))) {
+      const uint8_t* const kb = smem + (mine + jq) * (D * 4);
+      const uint8_t* const vb = smem + HALF + jq * (TK * 4) + ((((mine >> 2) + g) ^ (jq & 7)) << 4);
+      st.step([&](int c) { return *(const f32x4*)(kb + (((4 * c + g) ^ (jq & 7)) << 4)); },
+              [&](int c) { return *(const f32x4*)(vb + 16 * c * (TK * 4)); }, edge, k0, seq.klen, a.scale_log2);
+    }
+    __syncthreads();
+    idx = next;
+  }
+  st.template end<VEC, SPLIT>(a, b, h, sp, r0 + jq, rows, (f32x4*)smem, (float*)(smem + SO));
+}
+
+// ---------------------------------------------------------------- host
+int64_t cache4_page_bytes(int heads, int head_dim, int page_tokens) {
+  if (heads < 1 || heads > C4_HEADS || (head_dim != 32 && head_dim != 64 && head_dim != 128) || page_tokens < C4_BLOCK ||
+      page_tokens > 65536 || page_tokens % C4_BLOCK)
+    return 0;
+  return (int64_t)(page_tokens / C4_BLOCK) * heads * 68 * head_dim;
+}
+
+static track_status cache_check(const char* what, const track_cache4* c, int64_t B, CacheArgs* a) {
+  if (!c) return fail(TRACK_E_INVALID, "%s: null cache", what);
+  if (!cache4_page_bytes(c->heads, c->head_dim, c->page_tokens))
+    return fail(TRACK_E_UNSUPPORTED, "%s: pages of %d tokens (multiples of 64 up to 65536), %d heads of %d channels (32, 64, 128)", what,
+                c->page_tokens, c->heads, c->head_dim);
+  if (c->n_pages < 1 || c->n_pages > INT32_MAX || c->table_pages < 0 || c->table_pages > WIN_MAX / c->page_tokens ||
+      (B > 1 && c->ld_table < c->table_pages) || c->ld_table < 0)
+    return fail(TRACK_E_SHAPE, "%s: %lld pages, %d of a sequence (2^28 tokens at most), %lld between sequences", what, (long long)c->n_pages,
+                c->table_pages, (long long)c->ld_table);
+  if (!c->pages || (c->table_pages && !c->table)) return fail(TRACK_E_INVALID, "%s: null pointer in the cache", what);
+  if (((uintptr_t)c->pages & 127) || ((uintptr_t)c->table & 3))
+    return fail(TRACK_E_INVALID, "%s: pages need 128-byte alignment, the table 4", what);
+  a->pages = (uint8_t*)c->pages;
+  a->table = c->table;
+  a->ld_table = c->ld_table;
+  a->blocks = c->page_tokens / C4_BLOCK;
+  a->stride = (int64_t)c->heads * 68 * c->head_dim;
+  a->table_pages = c->table_pages;
+  a->n_pages = (int)c->n_pages;
+  a->cap = c->table_pages * c->page_tokens;
+  a->by_blocks = win_div(a->blocks);
+  return TRACK_OK;
+}
+
+// Workgroups that share a block's heads: one while the blocks alone fill the chip twice.
+static int rows_heads(int64_t items, int heads) {
+  return (int)std::max<int64_t>(1, std::min<int64_t>(heads, (2 * (int64_t)device_cus() + items - 1) / items));
+}
+
+template <typename T, int D>
+static void append_launch(const RowsArgs& a, int rot, unsigned grid, hipStream_t s) {
+  if (rot == 0) cache_append_kernel<T, D, 0><<<grid, 256, 0, s>>>(a);
+  else if (rot == 1) cache_append_kernel<T, D, 1><<<grid, 256, 0, s>>>(a);
+  else cache_append_kernel<T, D, 2><<<grid, 256, 0, s>>>(a);
+}
+
+static track_status cache_rows(const char* what, bool read, int dtype, const track_cache4* cache, const track_rope_config* rope,
+                               int64_t B, int64_t L, void* k, int64_t ldk, int64_t sk, void* v, int64_t ldv, int64_t sv,
+                               const int32_t* start, const int32_t* n, const int32_t* pos, const double* freqs, float amplitude,
+                               hipStream_t s) {
+  if (dtype != TRACK_DTYPE_F32 && dtype != TRACK_DTYPE_BF16) return fail(TRACK_E_INVALID, "%s: bad dtype %d", what, dtype);
+  RowsArgs a = {};
+  const track_status st = cache_check(what, cache, B, &a.c);
+  if (st != TRACK_OK) return st;
+  const int D = cache->head_dim;
+  const int64_t width = (int64_t)cache->heads * D;
+  if (B < 0 || L < 0 || L > WIN_MAX) return fail(TRACK_E_SHAPE, "%s: %lld x %lld tokens", what, (long long)B, (long long)L);
+  if (rope && rope->head_dim != D) return fail(TRACK_E_SHAPE, "%s: rotation of %d channels, %d in the cache", what, rope->head_dim, D);
+  if (ldk < width || ldv < width || sk < 0 || sv < 0)
+    return fail(TRACK_E_SHAPE, "%s: rows of %lld and %lld elements for %d heads of %d", what, (long long)ldk, (long long)ldv, cache->heads, D);
+  if (read && (sequences_overlap(B, L, ldk, sk, width) || sequences_overlap(B, L, ldv, sv, width)))
+    return fail(TRACK_E_SHAPE, "%s: sequences overlap in the output", what);
+  if (B == 0 || L == 0) return TRACK_OK;
+  const uintptr_t es = dtype == TRACK_DTYPE_BF16 ? 2 : 4;
+  if (!k || !v || !start || (rope && (!pos || !freqs))) return fail(TRACK_E_INVALID, "%s: null pointer", what);
+  if (((uintptr_t)k | (uintptr_t)v) & (es - 1) || ((uintptr_t)start | (uintptr_t)n | (uintptr_t)pos) & 3 || (uintptr_t)freqs & 7)
+    return fail(TRACK_E_INVALID, "%s: rows, lengths, positions or frequencies are not aligned to their elements", what);
+  if (!std::isfinite(amplitude)) return fail(TRACK_E_INVALID, "%s: scale is not finite", what);
+  a.k = k, a.v = v, a.ldk = ldk, a.sk = sk, a.ldv = ldv, a.sv = sv;
+  a.start = start, a.n = n;
+  a.B = (int)B, a.L = (int)L, a.heads = cache->heads;
+  a.nblk = (int)((L + C4_BLOCK - 2) / C4_BLOCK + 1);
+  a.vec = !((((uintptr_t)k | (uintptr_t)v) & 15) || ((ldk | ldv | (B > 1 ? sk | sv : 0)) * (int64_t)es & 15));
+  if (B > INT32_MAX || B * a.nblk >= (int64_t)1 << 23) return fail(TRACK_E_SHAPE, "%s: %lld x %lld tokens are too many", what, (long long)B, (long long)L);
+  a.hsplit = rows_heads(B * a.nblk, a.heads);
+  int rot = 0;
+  if (rope) {
+    rot = rope->layout == TRACK_ROPE_HALF ? 2 : 1;
+    a.pos = pos, a.freqs = freqs, a.amp = amplitude;
+    a.pairs = rope->rot_dim / 2;
+    a.sec0 = rope->axes > 1 ? rope->section[0] : a.pairs;
+    a.sec1 = rope->axes > 2 ? rope->section[0] + rope->section[1] : a.pairs;
+  }
+  ProfScope prof(TRACK_PROF_OTHER, s);
+  const unsigned grid = (unsigned)(B * a.nblk * a.hsplit);
+#define TRACK_C4_ROWS(T, DH)                                              \
+  do {                                                                    \
+    if (read) cache_read_kernel<T, DH><<<grid, 256, 0, s>>>(a);           \
+    else append_launch<T, DH>(a, rot, grid, s);                           \
+  } while (0)
+  if (es == 2) {
+    if (D == 32) TRACK_C4_ROWS(bf16_t, 32);
+    else if (D == 64) TRACK_C4_ROWS(bf16_t, 64);
+    else TRACK_C4_ROWS(bf16_t, 128);
+  } else {
+    if (D == 32) TRACK_C4_ROWS(float, 32);
+    else if (D == 64) TRACK_C4_ROWS(float, 64);
+    else TRACK_C4_ROWS(float, 128);
+  }
+#undef TRACK_C4_ROWS
+  TRACK_LAUNCH_CHECK();
+  return TRACK_OK;
+}
+
+track_status cache4_append(int dtype, const track_cache4* cache, const track_rope_config* rope, int64_t B, int64_t L, const void* k,
+                           int64_t ldk, int64_t sk, const void* v, int64_t ldv, int64_t sv, const int32_t* start, const int32_t* n,
+                           const int32_t* pos, const double* freqs, float amplitude, hipStream_t s) {
+  return cache_rows("cache4_append", false, dtype, cache, rope, B, L, (void*)k, ldk, sk, (void*)v, ldv, sv, start, n, pos, freqs,
+                    amplitude, s);
+}
+
+track_status cache4_read(int dtype, const track_cache4* cache, int64_t B, int64_t L, void* k, int64_t ldk, int64_t sk, void* v,
+                         int64_t ldv, int64_t sv, const int32_t* start, const int32_t* n, hipStream_t s) {
+  return cache_rows("cache4_read", true, dtype, cache, nullptr, B, L, k, ldk, sk, v, ldv, sv, start, n, nullptr, nullptr, 1.0f, s);
+}
+
+// How a call is taken: at most 16 rows a key head, blocks of 256, or 16 float32 rows a workgroup; shares of the keys.
+struct CachePlan {
+  enum Form { BLOCKS, ROWS, F32 } form;
+  int64_t nrb;
+  int nsplit;
+};
+
+static CachePlan cache_plan(int dtype, const track_window& w, int64_t B, int Hk, int n, int D, int64_t Lq, int64_t Lk) {
+  const int64_t rows = Lq * n, cus = device_cus();
+  CachePlan p;
+  p.form = dtype == TRACK_DTYPE_F32 ? CachePlan::F32 : (rows <= 16 ? CachePlan::ROWS : CachePlan::BLOCKS);
+  const int64_t block = p.form == CachePlan::BLOCKS ? ATT_BQ : 16;
+  p.nrb = (rows + block - 1) / block;
+  const int64_t tiles = (win_span(w, std::min(rows, block), n, Lk) + C4_BLOCK - 1) / C4_BLOCK;
+  const int64_t blocks = p.nrb * Hk * B;
+  int64_t s;
+  if (p.form == CachePlan::ROWS) s = tiles <= 16 ? 1 : std::min((4 * cus + blocks - 1) / blocks, tiles / 8);
+  else if (p.form == CachePlan::F32) s = std::min(2 * cus / blocks, tiles / 4);
+  else s = win_blocks_split(tiles, blocks, rows * Hk * B, cus);
+  p.nsplit = (int)std::max<int64_t>(1, std::min<int64_t>(s, 1024));
+  return p;
+}
+
+static size_t cache_plan_bytes(const CachePlan& p, int64_t B, int Hk, int n, int D, int64_t Lq) {
+  return p.nsplit == 1 ? 0 : (size_t)(p.nsplit * B * Hk * Lq * n) * (size_t)(4 * D + 8);
+}
+
+static bool cache_fits(const CachePlan& p, int64_t B, int Hk, int n, int64_t Lq) {
+  return p.nrb * p.nsplit * Hk * B < (int64_t)1 << 23 && (p.nsplit == 1 || B * Hk * n * Lq < (int64_t)1 << 25);
+}
+
+int64_t attention_cache4_bytes(int dtype, const track_window* w, int B, int H, int Hk, int D, int64_t Lq, int64_t Lk) {
+  if (win_check("attention_cache4", dtype, w, B, H, Hk, D, Lq, Lk) != TRACK_OK) return -1;
+  if (B == 0 || Lq == 0) return 0;
+  const CachePlan p = cache_plan(dtype, *w, B, Hk, H / Hk, D, Lq, Lk);
+  if (!cache_fits(p, B, Hk, H / Hk, Lq)) {
+    fail(TRACK_E_SHAPE, "attention_cache4: too many row blocks");
+    return -1;
+  }
+  return (int64_t)cache_plan_bytes(p, B, Hk, H / Hk, D, Lq);
+}
+
+track_status attention_cache4(int dtype, const track_window* w, const track_cache4* cache, int B, int H, int64_t Lq, int64_t Lk,
+                              const void* q, int64_t ldq, int64_t sq, void* out, int64_t ldo, int64_t so, float* lse,
+                              const int32_t* q_len, const int32_t* k_len, const int32_t* q_start, void* ws, size_t ws_bytes,
+                              hipStream_t s) {
+  CacheArgs ca = {};
+  track_status st = cache_check("attention_cache4", cache, B, &ca);
+  if (st != TRACK_OK) return st;
+  const int Hk = cache->heads, D = cache->head_dim;
+  st = win_check("attention_cache4", dtype, w, B, H, Hk, D, Lq, Lk);
+  if (st != TRACK_OK) return st;
+  if (Lk > ca.cap) return fail(TRACK_E_SHAPE, "attention_cache4: %lld keys, the table has places for %d", (long long)Lk, ca.cap);
+  if (B == 0 || Lq == 0) return TRACK_OK;
+  if (!q || !out) return fail(TRACK_E_INVALID, "attention_cache4: null pointer");
+  const int n = H / Hk;
+  if (ldq < (int64_t)H * D || ldo < (int64_t)H * D) return fail(TRACK_E_SHAPE, "attention_cache4: leading dimension too small");
+  if (sq < 0 || so < 0 || sequences_overlap(B, Lq, ldo, so, (int64_t)H * D))
+    return fail(TRACK_E_SHAPE, "attention_cache4: sequences overlap in out, or a negative stride");
+  if (((uintptr_t)lse | (uintptr_t)q_len | (uintptr_t)k_len | (uintptr_t)q_start) & 3)
+    return fail(TRACK_E_INVALID, "attention_cache4: lse and lengths need 4-byte alignment");
+  const uintptr_t ptrs = (uintptr_t)q | (uintptr_t)out;
+  const int64_t strides = ldq | ldo | (B > 1 ? sq | so : 0);
+  const bool vec = !(ptrs & 15) && !(strides & (dtype == TRACK_DTYPE_BF16 ? 7 : 3));
+  if (dtype == TRACK_DTYPE_BF16 && !vec) return fail(TRACK_E_INVALID, "attention_cache4: bf16 path needs 16-byte aligned rows");
+  if (ptrs & 3) return fail(TRACK_E_INVALID, "attention_cache4: float32 path needs 4-byte aligned rows");
+  CachePlan p = cache_plan(dtype, *w, B, Hk, n, D, Lq, Lk);
+  if (!cache_fits(p, B, Hk, n, Lq)) return fail(TRACK_E_SHAPE, "attention_cache4: too many row blocks");
+  if (p.form == CachePlan::BLOCKS) p.nsplit = win_held(p.nsplit, B, Hk, n, D, Lq, ws, ws_bytes);
+  const size_t need = cache_plan_bytes(p, B, Hk, n, D, Lq);
+  if (need && (!ws || ws_bytes < need)) return fail(TRACK_E_NOMEM, "attention_cache4: workspace of %zu bytes needed", need);
+  if (need && ((uintptr_t)ws & 255)) return fail(TRACK_E_INVALID, "attention_cache4: workspace must be 256-byte aligned");
+  const int64_t joined = (int64_t)B * H * Lq;
+  WinArgs a = {};
+  a.q = q, a.out = out, a.ldq = ldq, a.sq = sq, a.ldo = ldo, a.so = so;
+  a.lse = lse, a.q_len = q_len, a.k_len = k_len, a.q_start = q_start;
+  win_visible(a, *w, B, Hk, n, D, Lq, Lk);
+  a.nrb = (int)p.nrb, a.nsplit = p.nsplit;
+  a.by_nrb = win_div(a.nrb), a.by_nsplit = win_div(a.nsplit);
+  a.by_inner = win_div(p.form == CachePlan::ROWS ? Hk : B);
+  a.po = (float*)ws;
+  a.pml = need ? (float2*)(a.po + (int64_t)p.nsplit * joined * D) : nullptr;
+  const bool split = p.nsplit > 1, log2q = a.scale_log2 == 1.0f;
+  ProfScope prof(TRACK_PROF_ATTN_SELF, s);
+  const unsigned gr = (unsigned)(p.nrb * p.nsplit * Hk * B);
+#define TRACK_C4_F32(DH)                                                            \
+  do {                                                                              \
+    if (vec && split) cache_f32_kernel<DH, true, true><<<gr, 256, 0, s>>>(a, ca);   \
+    else if (vec) cache_f32_kernel<DH, true, false><<<gr, 256, 0, s>>>(a, ca);      \
+    else if (split) cache_f32_kernel<DH, false, true><<<gr, 256, 0, s>>>(a, ca);    \
+    else cache_f32_kernel<DH, false, false><<<gr, 256, 0, s>>>(a, ca);              \
+  } while (0)
+  switch (p.form) {
+    case CachePlan::ROWS:
+      if (split) cache_rows_kernel<true><<<gr, 256, 0, s>>>(a, ca);
+      else cache_rows_kernel<false><<<gr, 256, 0, s>>>(a, ca);
+      break;
+    case CachePlan::BLOCKS:
+      if (log2q && split) cache_blocks_kernel<true, true><<<gr, 512, 0, s>>>(a, ca);
+      else if (log2q) cache_blocks_kernel<true, false><<<gr, 512, 0, s>>>(a, ca);
+      else if (split) cache_blocks_kernel<false, true><<<gr, 512, 0, s>>>(a, ca);
+      else cache_blocks_kernel<false, false><<<gr, 512, 0, s>>>(a, ca);
+      break;
+    default:
+      if (D == 32) TRACK_C4_F32(32);
+      else if (D == 64) TRACK_C4_F32(64);
+      else TRACK_C4_F32(128);
+  }
+#undef TRACK_C4_F32
+  TRACK_LAUNCH_CHECK();
+  if (split) {
+    window_join(dtype, a, D, s);
+    TRACK_LAUNCH_CHECK();
+  }
+  return TRACK_OK;
+}
+
+}  // namespace track

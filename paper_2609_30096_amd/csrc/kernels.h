@@ -68,6 +68,19 @@ track_status attention_window(int dtype, const track_window* w, int B, int H, in
                               const int32_t* q_len, const int32_t* k_len, const int32_t* q_start, void* ws,
                               size_t ws_bytes, hipStream_t s);
 
+// cache.hip (track_cache4_page_bytes, track_op_cache4_append, track_op_cache4_read, track_op_attention_cache4)
+int64_t cache4_page_bytes(int heads, int head_dim, int page_tokens);  // 0 for what it refuses
+track_status cache4_append(int dtype, const track_cache4* cache, const track_rope_config* rope, int64_t B, int64_t L, const void* k,
+                           int64_t ldk, int64_t sk, const void* v, int64_t ldv, int64_t sv, const int32_t* start, const int32_t* n,
+                           const int32_t* pos, const double* freqs, float amplitude, hipStream_t s);
+track_status cache4_read(int dtype, const track_cache4* cache, int64_t B, int64_t L, void* k, int64_t ldk, int64_t sk, void* v,
+                         int64_t ldv, int64_t sv, const int32_t* start, const int32_t* n, hipStream_t s);
+int64_t attention_cache4_bytes(int dtype, const track_window* w, int B, int H, int Hk, int D, int64_t Lq, int64_t Lk);
+track_status attention_cache4(int dtype, const track_window* w, const track_cache4* cache, int B, int H, int64_t Lq, int64_t Lk,
+                              const void* q, int64_t ldq, int64_t sq, void* out, int64_t ldo, int64_t so, float* lse,
+                              const int32_t* q_len, const int32_t* k_len, const int32_t* q_start, void* ws, size_t ws_bytes,
+                              hipStream_t s);
+
 // rope.hip (track_op_rope; with gains track_op_headnorm_rope).  k may be null.
 constexpr int ROPE_MAX_DIM = 256;  // channels of a head
 constexpr int ROPE_MAX_HEADS = 1 << 19;  // of q, of k: sums and bytes of a call stay in their types

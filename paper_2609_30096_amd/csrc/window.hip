@@ -15,204 +15,9 @@
 // 0 x inf in the matrix product; the edge tiles are the only place where that can happen, so
 // their sums are looked at once, and only where one is not finite the edge tiles are taken
 // again with the keys weighed one by one.
-#include <math.h>
-
-#include <algorithm>
-
-#include "attention_tile.h"
-#include "common.h"
-#include "kernels.h"
+#include "window.h"
 
 namespace track {
-
-// Division by a number that the host knows, for dividends below 2^31: with s = ceil(log2 d) and
-// m = ceil(2^(31 + s) / d) < 2^32, floor(x m / 2^(31 + s)) = floor(x / d), since m d exceeds
-// 2^(31 + s) by less than d <= 2^s (a hardware division is some 30 instructions, and the limits
-// of a block's, a wave's and a lane's rows take a dozen: 1 - 2 us of a single token's call).
-struct WinDiv {
-  uint32_t d, m, s;
-  __device__ __forceinline__ uint32_t operator()(uint32_t x) const { return d == 1 ? x : __umulhi(x, m) >> s; }
-};
-
-static WinDiv win_div(int64_t d) {
-  if (d == 1) return WinDiv{1, 0, 0};
-  const uint32_t s = 32 - (uint32_t)__builtin_clz((uint32_t)d - 1);  // ceil(log2 d)
-  return WinDiv{(uint32_t)d, (uint32_t)((((uint64_t)1 << (31 + s)) + (uint64_t)d - 1) / (uint64_t)d), s - 1};
-}
-
-// One call's arguments as the kernels take them.
-struct WinArgs {
-  const void *q, *k, *vt;
-  void* out;
-  int64_t ldq, sq, ldk, sk, ldv, sv, ldo, so;
-  float* lse;
-  const int32_t *q_len, *k_len, *q_start;
-  // limits in tokens: from a group's first key back, and on to the first key past them (2^31 - 1:
-  // no limit, or one that no key is as far away as: lengths are at most 2^28, positions within +- 2^29)
-  int before, past;
-  int lift;           // multiple of the group that makes every position positive
-  int sink;
-  int B, Hk, n;       // sequences, key heads, query heads of each
-  int Lq, Lk;
-  int nrb, nsplit;    // row blocks, shares of the keys
-  WinDiv by_group, by_n, by_nrb, by_nsplit, by_Hk;
-  WinDiv by_inner;    // sequences of a head, or heads of a sequence (win_place)
-  int64_t vend;       // elements of a head's V^T up to its last row's last key, rounded up to 16 bytes
-  float scale_log2;
-  float* po;          // [nsplit][B][Hk][Lq n][D]: a share's sums
-  float2* pml;        // [nsplit][B][Hk][Lq n]: its reference (log2 units) and its denominator
-};
-
-// One sequence of the batch, in wave-uniform registers.
-struct WinSeq {
-  int b, qlen, klen, sink;
-  int start;  // position of its first query
-};
-
-__device__ __forceinline__ WinSeq win_seq(const WinArgs& a, int b) {
-  WinSeq s;
-  s.b = b;
-  // lengths from device memory are cut to the buffers
-  s.qlen = a.q_len ? __builtin_amdgcn_readfirstlane(max(0, min(a.q_len[b], a.Lq))) : a.Lq;
-  s.klen = a.k_len ? __builtin_amdgcn_readfirstlane(max(0, min(a.k_len[b], a.Lk))) : a.Lk;
-  s.start = a.q_start ? __builtin_amdgcn_readfirstlane(max(-(int)WIN_MAX, min(a.q_start[b], (int)WIN_MAX))) : s.klen - s.qlen;
-  s.sink = min(a.sink, s.klen);
-  return s;
-}
-
-// The window [lo, hi] of query i, cut to [0, klen) (lo = klen or hi = -1: nothing left).
-__device__ __forceinline__ void win_range(const WinArgs& a, const WinSeq& s, int i, int& lo, int& hi) {
-  const uint32_t p = (uint32_t)(s.start + i + a.lift);  // in [0, 2^30 + 2^28)
-  const int first = (int)(a.by_group(p) * a.by_group.d) - a.lift;  // of the query's group
-  lo = first > a.before ? min(first - a.before, s.klen) : 0;
-  hi = a.past - 1 < s.klen - 1 - first ? max(first + a.past - 1, -1) : s.klen - 1;
-}
-
-// Query of row r, and the row's head among those of its key head.
-__device__ __forceinline__ int win_query(const WinArgs& a, int r, int& e) {
-  const int i = (int)a.by_n((uint32_t)r);
-  e = r - i * a.n;
-  return i;
-}
-
-// The tiles of TK keys that rows with windows from [lo0, hi0] (the first row's) to [lo1, hi1]
-// (the last's) see between them, in the order they are taken: those seen in part by some
-// row, then those seen whole by all.
-struct WinTiles {
-  int sink;          // first tokens, 0 where the window covers them
-  int ns, w0;        // tiles of first tokens, first tile of the window
-  int n, fs, fa, fb;  // all tiles; seen whole: [0, fs) and [fa, fb)
-  int edge;          // tiles seen in part
-  template <int TK>
-  __device__ __forceinline__ void init(const WinSeq& s, int lo0, int hi0, int lo1, int hi1) {
-    sink = s.sink;
-    if (sink >= lo1) sink = lo0 = lo1 = 0;  // every row sees all from key 0 to its hi
-    ns = (min(sink, hi1 + 1) + TK - 1) / TK;
-    w0 = max(lo0 / TK, ns);
-    n = ns + max(0, hi1 / TK + (hi1 >= 0) - w0);
-    fs = min(sink, hi0 + 1) / TK;
-    const int t0 = max((lo1 + TK - 1) / TK, w0), t1 = min((hi0 + 1) / TK, w0 + n - ns);
-    fa = ns + t0 - w0;
-    fb = ns + t1 - w0;
-    if (t1 <= t0) fa = fb = n;
-    edge = n - fs - (fb - fa);
-  }
-  // first key of the tile at place idx of the order
-  template <int TK>
-  __device__ __forceinline__ int key(int idx) const {
-    int m;
-    if (idx < edge) {
-      m = fs + idx;
-      if (m >= fa) m += fb - fa;
-    } else {
-      m = idx - edge;
-      if (m >= fs) m += fa - fs;
-    }
-    return (m < ns ? m : m - ns + w0) * TK;
-  }
-};
-
-// Share s of S of n tiles: [i0, i1).
-__device__ __forceinline__ void win_share(int n, int s, int S, int& i0, int& i1) {
-  const int q = (int)((uint32_t)n / (uint32_t)S), more = n - q * S;
-  i0 = __builtin_amdgcn_readfirstlane(q * s + min(s, more));
-  i1 = __builtin_amdgcn_readfirstlane(i0 + q + (s < more));
-}
-
-__device__ __forceinline__ float win_inverse(float l) { return l == 0.0f ? 0.0f : 1.0f / l; }  // nothing seen: zeros
-__device__ __forceinline__ float win_lse(float m, float l) {
-  return l == 0.0f ? -INFINITY : 0.69314718056f * (m + log2f(l));
-}
-
-// The keys of a tile that a lane's queries do not see.  A lane holds two runs of 8 keys of a
-// tile, 32 apart; a bit for each that is hidden, and a hidden logit's bits replaced by those of
-// -inf: two instructions an element and no branch (as comparisons with && and || the same
-// was compiled to branches around single accumulator elements, and with two query blocks to
-// moves that lost one of them).
-template <int NB, bool WEIGHED_ = false>
-struct WinMask {
-  static constexpr bool ACTIVE = true, BITS = true, WEIGHED = WEIGHED_;
-  int lo[NB], hi[NB];
-  int sink, key0;
-  uint32_t bits[NB];
-  static __device__ __forceinline__ uint32_t below(int n) { return (1u << min(max(n, 0), 8)) - 1u; }
-  __device__ __forceinline__ void begin() {
-    key0 += 8 * (att_lane() >> 4);
-#pragma unroll
-    for (int b = 0; b < NB; ++b) {
-      bits[b] = 0;
-#pragma unroll
-      for (int run = 0; run < 2; ++run) {
-        const int k = key0 + 32 * run;
-        bits[b] |= ((below(lo[b] - k) & ~below(sink - k)) | (below(hi[b] + 1 - k) ^ 0xffu)) << (8 * run);
-      }
-    }
-  }
-  __device__ __forceinline__ float apply(int b, int c, float s) const {
-    const int at = (c & 7) + (c >> 5) * 8;
-    const uint32_t t = (uint32_t)((int32_t)(bits[b] << (31 - at)) >> 31);
-    return __uint_as_float((t & 0xff800000u) | (~t & __float_as_uint(s)));
-  }
-};
-
-// 16 bytes a lane from the buffer at `off` (and the wave's `scalar` more) to LDS, lanes side by side.
-// (Functions of their own: in a template, with arguments that depend on it, the host's pass rejects
-// the builtin.)
-__device__ __forceinline__ void win_copy(__amdgpu_buffer_rsrc_t rs, uint8_t* lds, uint32_t off, uint32_t scalar = 0) {
-  __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (att_lds_ptr_t)lds, 16, off, scalar, 0, 0);
-}
-// The same past the caches (the `nt` bit).
-__device__ __forceinline__ void win_copy_past(__amdgpu_buffer_rsrc_t rs, uint8_t* lds, uint32_t off, uint32_t scalar) {
-  __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (att_lds_ptr_t)lds, 16, off, scalar, 0, 2);
-}
-
-template <bool VEC>
-__device__ __forceinline__ f32x4 win_load4(const float* p) {
-  if constexpr (VEC) return *(const f32x4*)p;
-  else return f32x4{p[0], p[1], p[2], p[3]};
-}
-
-// Bits of a pair of keys of which `left` are to keep (any number).
-__device__ __forceinline__ uint32_t win_keep(int left) { return (uint32_t)((1ull << (16 * min(max(left, 0), 2))) - 1ull); }
-
-// Row block, share, key head and sequence of a workgroup.  LOCAL: neighbouring row blocks go to
-// one XCD, whose L2 then serves their common keys (over the XCDs in turn, 12 heads 16384 x 16384
-// under a causal mask took 955 us instead of 824, 2 x 12 heads over a 21-frame video 5.2 ms
-// instead of 4.8), and the sequences follow each other inside a head, so that short ones do
-// not leave one XCD idle (4 sequences of 5000 to 3100 queries: 439 -> 385 us).  Single tokens use
-// a key once and go over the XCDs in turn (8 sequences of 8 key heads, 100003 keys 491 us, 500 the other way;
-// 48 x 32760 131 and 132, 8 of 100003 to 56000 keys 395 and 397, one of 100003 70 and 68).  The last rows of a sequence, which see most keys under a causal
-// mask, start first.
-template <bool LOCAL>
-__device__ __forceinline__ void win_place(const WinArgs& a, int& rb, int& sp, int& h, int& b) {
-  const uint32_t id = LOCAL ? (uint32_t)xcd_remap((int)blockIdx.x, (int)gridDim.x) : blockIdx.x;
-  const uint32_t t = a.by_nrb(id), u = a.by_nsplit(t), v = a.by_inner(u);
-  rb = a.nrb - 1 - (int)(id - t * a.nrb);
-  sp = (int)(t - u * a.nsplit);
-  const int w = (int)(u - v * a.by_inner.d);
-  h = LOCAL ? (int)v : w;
-  b = LOCAL ? w : (int)v;
-}
 
 // ---------------------------------------------------------------- many rows, bfloat16
 // 256 rows a workgroup, 32 a wave; K and V^T tiles by DMA into a ring of two slots, and the
@@ -712,171 +517,6 @@ __global__ __launch_bounds__(256) void window_rows_kernel(WinArgs a) {
 }
 
 // ---------------------------------------------------------------- float32
-// One wave's 16 rows.  step() takes them against 16 keys with v_mfma_f32_16x16x4_f32 (float32
-// products and sums): lane (jq, g) has row jq, kfrag(c) is channels 16 c + 4 g .. + 3 of key jq,
-// vfrag(c) keys 4 g .. + 3 of channel 16 c + jq, and the logits that a lane holds (keys 4 g .. + 3
-// of its row) are the "B" operand of O^T += V^T P^T as they are.
-template <int D>
-struct WinF32 {
-  static constexpr int C = D / 16;
-  f32x4 qf[C], o[C];
-  float m, l;  // reference (log2 units), the lane's part of the denominator
-  int lo, hi, sink;
-  template <class KF, class VF>
-  __device__ __forceinline__ void step(KF kfrag, VF vfrag, bool edge, int key0, int klen, float scale_log2) {
-    const int lane = att_lane(), jq = lane & 15, g = lane >> 4;
-    f32x4 s0 = {0.0f, 0.0f, 0.0f, 0.0f}, s1 = s0;
-    // fragments are read ahead of their products
-    constexpr int LA = C < 3 ? C : 3;
-    f32x4 kf[LA + 1];
-#pragma unroll
-    for (int c = 0; c < LA; ++c) kf[c] = kfrag(c);
-#pragma unroll
-    for (int c = 0; c < C; ++c) {
-      if (c + LA < C) kf[(c + LA) % (LA + 1)] = kfrag(c + LA);
-      __builtin_amdgcn_sched_barrier(0);
-      const f32x4 k = kf[c % (LA + 1)];
-      s0 = __builtin_amdgcn_mfma_f32_16x16x4f32(k[0], qf[c][0], s0, 0, 0, 0);
-      s1 = __builtin_amdgcn_mfma_f32_16x16x4f32(k[1], qf[c][1], s1, 0, 0, 0);
-      s0 = __builtin_amdgcn_mfma_f32_16x16x4f32(k[2], qf[c][2], s0, 0, 0, 0);
-      s1 = __builtin_amdgcn_mfma_f32_16x16x4f32(k[3], qf[c][3], s1, 0, 0, 0);
-    }
-    f32x4 vf[C];
-#pragma unroll
-    for (int c = 0; c < C; ++c) vf[c] = vfrag(c);
-    float x[4];
-#pragma unroll
-    for (int e = 0; e < 4; ++e) x[e] = s0[e] + s1[e];
-    if (edge) {
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int key = key0 + 4 * g + e;
-        x[e] = (key > hi) | ((key < lo) & (key >= sink)) ? -INFINITY : x[e];
-      }
-    }
-    const float t = fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3]));
-    const float mn = fmaxf(m, group_max2(t, t) * scale_log2);
-    if (__ballot(mn > m)) {
-      const float alpha = mn == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m - mn);
-      l *= alpha;
-#pragma unroll
-      for (int c = 0; c < C; ++c)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) o[c][e] *= alpha;
-      m = mn;
-    }
-    const float nm = m == -INFINITY ? 0.0f : -m;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) x[e] = __builtin_amdgcn_exp2f(fmaf(x[e], scale_log2, nm));
-    l += (x[0] + x[1]) + (x[2] + x[3]);
-    if (edge) {
-      // V past the last key is cleared, and what else is not finite and may be hidden from some
-      // row is weighed key by key
-      float z = 0.0f;
-#pragma unroll
-      for (int c = 0; c < C; ++c)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          vf[c][e] = key0 + 4 * g + e < klen ? vf[c][e] : 0.0f;
-          z = fmaf(vf[c][e], 0.0f, z);
-        }
-      if (__ballot(z != 0.0f)) {
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-#pragma unroll 1
-          for (int gg = 0; gg < 4; ++gg) {
-            const float p = __shfl(x[e], jq + 16 * gg);
-            const uint32_t on = p != 0.0f ? 0xffffffffu : 0u;  // V times 0 where the weight is 0
-#pragma unroll
-            for (int c = 0; c < C; ++c)
-#pragma unroll
-              for (int i = 0; i < 4; ++i) {
-                const uint32_t v = __float_as_uint(__shfl(vf[c][e], 4 * g + i + 16 * gg));
-                o[c][i] = fmaf(p, __uint_as_float(v & on), o[c][i]);
-              }
-          }
-        return;
-      }
-    }
-#pragma unroll
-    for (int e = 0; e < 4; ++e)
-#pragma unroll
-      for (int c = 0; c < C; ++c) o[c] = __builtin_amdgcn_mfma_f32_16x16x4f32(vf[c][e], x[e], o[c], 0, 0, 0);
-  }
-  // the lane's row of `rows`: window, query, nothing summed yet
-  template <bool VEC>
-  __device__ __forceinline__ void begin(const WinArgs& a, const WinSeq& seq, const WinTiles& tiles, int lo1, int h, int r,
-                                        int rows) {
-    const int g = (int)(threadIdx.x & 63) >> 4;
-    int e;
-    const int qi = win_query(a, min(r, rows - 1), e);
-    win_range(a, seq, qi, lo, hi);
-    if (tiles.sink == 0 && seq.sink >= lo1) lo = 0;
-    sink = tiles.sink;
-    const float* qp = (const float*)a.q + seq.b * a.sq + (int64_t)qi * a.ldq + (int64_t)(h * a.n + e) * D + 4 * g;
-#pragma unroll
-    for (int c = 0; c < C; ++c) {
-      qf[c] = win_load4<VEC>(qp + 16 * c);
-      o[c] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-    }
-    m = -INFINITY;
-    l = 0.0f;
-  }
-  // The sums of each four waves, which have the same rows, joined and stored, through LDS of
-  // so[waves][C][64] and sml[waves][2][16].
-  template <bool VEC, bool SPLIT>
-  __device__ __forceinline__ void end(const WinArgs& a, int b, int h, int sp, int r, int rows, f32x4* so, float* sml) {
-    const int lane = (int)(threadIdx.x & 63), jq = lane & 15, g = lane >> 4;
-    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), w0 = wave & ~3;
-    l += __shfl_xor(l, 16);
-    l += __shfl_xor(l, 32);
-#pragma unroll
-    for (int c = 0; c < C; ++c) so[(wave * C + c) * 64 + lane] = o[c];
-    if (g == 0) {
-      sml[wave * 32 + jq] = m;
-      sml[wave * 32 + 16 + jq] = l;
-    }
-    __syncthreads();
-    float mx = -INFINITY, sum = 0.0f, wt[4];
-#pragma unroll
-    for (int w = 0; w < 4; ++w) mx = fmaxf(mx, sml[(w0 + w) * 32 + jq]);
-#pragma unroll
-    for (int w = 0; w < 4; ++w) {
-      const float mi = sml[(w0 + w) * 32 + jq];
-      wt[w] = mi == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(mi - mx);  // a wave without keys
-      sum = fmaf(wt[w], sml[(w0 + w) * 32 + 16 + jq], sum);
-    }
-    if (r >= rows) return;
-    int e;
-    const int qi = win_query(a, r, e), head = h * a.n + e;
-    const int64_t pr = ((((int64_t)sp * a.B + b) * a.Hk + h) * a.Lq) * a.n + r;
-    const float inv = SPLIT ? 1.0f : win_inverse(sum);
-    float* const op = SPLIT ? a.po + pr * D + 4 * g
-                            : (float*)a.out + b * a.so + (int64_t)qi * a.ldo + (int64_t)head * D + 4 * g;
-    for (int c = wave - w0; c < C; c += 4) {
-      f32x4 v = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-      for (int w = 0; w < 4; ++w) {
-        const f32x4 u = so[((w0 + w) * C + c) * 64 + lane];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = fmaf(wt[w], u[e], v[e]);
-      }
-#pragma unroll
-      for (int e = 0; e < 4; ++e) v[e] *= inv;
-      if constexpr (VEC || SPLIT) {
-        *(f32x4*)(op + 16 * c) = v;
-      } else {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) op[16 * c + e] = v[e];
-      }
-    }
-    if (wave == w0 && g == 0) {
-      if constexpr (SPLIT) a.pml[pr] = float2{mx, sum};
-      else if (a.lse) a.lse[((int64_t)b * a.Hk * a.n + head) * a.Lq + qi] = win_lse(mx, sum);
-    }
-  }
-};
-
 // Many rows: tiles of 64 keys of K and V^T by DMA into LDS, 16 rows to each four of a workgroup's
 // W waves, which take 16 keys of a tile each.  LDS rows keep 16-byte units at unit ^ (row & 7), so
 // that the 16 rows of a fragment meet no bank twice in a phase.  8 waves share a ring of two
@@ -1117,19 +757,28 @@ __global__ __launch_bounds__(256) void window_join_kernel(WinArgs a, int D) {
   if (a.lse && c == 0) a.lse[((int64_t)b * a.Hk * a.n + head) * a.Lq + qi] = win_lse(m, l);
 }
 
+void window_join(int dtype, const WinArgs& a, int D, hipStream_t s) {
+  // groups of shares for few rows (window_join_kernel)
+  const int64_t joined = (int64_t)a.B * a.Hk * a.n * a.Lq;
+  const int per = D / 4, G = joined * D / 4 < 128 * (int64_t)device_cus() && a.nsplit > 2 ? 8 : 1;
+  const int rows_wg = 256 / per / G;
+  const unsigned jg = (unsigned)((joined + rows_wg - 1) / rows_wg);
+#define TRACK_WIN_JOIN(T)                                               \
+  do {                                                                  \
+    if (G == 1) window_join_kernel<T, 1><<<jg, 256, 0, s>>>(a, D);      \
+    else window_join_kernel<T, 8><<<jg, 256, 0, s>>>(a, D);             \
+  } while (0)
+  if (dtype == TRACK_DTYPE_BF16) TRACK_WIN_JOIN(bf16_t);
+  else TRACK_WIN_JOIN(float);
+#undef TRACK_WIN_JOIN
+}
+
 // ---------------------------------------------------------------- host
 struct WinPlan {
   enum Form { BLOCKS, ROWS, F32_ROWS, F32_TILES4, F32_TILES8 } form;
   int64_t nrb;
   int nsplit;
 };
-
-// Keys that a block of `rows` rows sees at most.
-static int64_t win_span(const track_window& w, int64_t rows, int n, int64_t Lk) {
-  if (w.left < 0 || w.right < 0) return Lk;
-  const int64_t groups = w.left + w.right + 2 + (rows + n - 1) / n / w.group;
-  return std::min(Lk, groups * w.group + w.sink);
-}
 
 // Shares of the keys for few rows, `blocks` row blocks of `tiles` tiles each.  None up to 16
 // tiles, four a wave: the join is a launch more (calls one after another, 8 heads of 1024 keys: 9.7
@@ -1145,29 +794,6 @@ static int rows_split(int64_t tiles, int64_t blocks, int64_t cus) {
   const bool large = blocks * tiles >= 64 * cus;
   const int64_t s = large ? std::min((6 * cus + blocks - 1) / blocks, tiles / 16) : std::min(cus / blocks, (tiles + 1) / 2);
   return (int)std::max<int64_t>(1, s);
-}
-
-// Shares of the keys for blocks of rows, by an estimate of the time: rounds of workgroups over
-// the CUs, a tile 1.6 us and 5 us beside the tiles, and with shares the join, 3 us and the
-// sums' way out and back at 4 TB/s.  Fits measured times within 10% where the matrix cores
-// are the bound (1 - 42 shares of 2000, 4096 and 32760 keys, 17 - 400 rows of 8, 12 and 40
-// heads): 256 rows of 12 heads, 32760 keys 732 us with one share, 106 with 10, 69 with 21, 83
-// with 42; 400 rows of 40 heads, 2000 keys 53 with one, 38 with 3, 52 with 4.
-static int blocks_split(int64_t tiles, int64_t blocks, int64_t rows, int64_t cus) {
-  const uint32_t n = (uint32_t)tiles, most = std::max<uint32_t>(1, std::min<uint32_t>(n / 2, 64));
-  const double join = (double)(2 * rows * (4 * ATT_D + 8)) / 4e6;
-  int best = 1;
-  double best_t = 0.0;
-  for (uint32_t s = 1; s <= most && blocks * s <= 16 * cus; ++s) {  // (32-bit divisions: a call's own time)
-    const uint32_t rounds = ((uint32_t)blocks * s + (uint32_t)cus - 1) / (uint32_t)cus;
-    double t = rounds * ((n + s - 1) / s * 1.6 + 5.0);
-    if (s > 1) t += 3.0 + s * join;
-    if (s == 1 || t < best_t) {
-      best = (int)s;
-      best_t = t;
-    }
-  }
-  return best;
 }
 
 static WinPlan win_plan(int dtype, const track_window& w, int64_t B, int Hk, int n, int D, int64_t Lq, int64_t Lk, bool vec) {
@@ -1195,7 +821,7 @@ static WinPlan win_plan(int dtype, const track_window& w, int64_t B, int Hk, int
   }
   p.form = WinPlan::BLOCKS;
   p.nrb = (rows + ATT_BQ - 1) / ATT_BQ;
-  p.nsplit = blocks_split((win_span(w, std::min<int64_t>(rows, ATT_BQ), n, Lk) + 63) / 64, p.nrb * Hk * B, rows * Hk * B, cus);
+  p.nsplit = win_blocks_split((win_span(w, std::min<int64_t>(rows, ATT_BQ), n, Lk) + 63) / 64, p.nrb * Hk * B, rows * Hk * B, cus);
   return p;
 }
 
@@ -1209,29 +835,29 @@ static bool win_fits(const WinPlan& p, int64_t B, int Hk, int n, int64_t Lq) {
   return p.nrb * p.nsplit * Hk * B < (int64_t)1 << 23 && (p.nsplit == 1 || B * Hk * n * Lq < (int64_t)1 << 25);
 }
 
-static track_status win_check(int dtype, const track_window* w, int B, int H, int Hk, int D, int64_t Lq, int64_t Lk) {
-  if (!w) return fail(TRACK_E_INVALID, "attention_window: null window");
+track_status win_check(const char* what, int dtype, const track_window* w, int B, int H, int Hk, int D, int64_t Lq, int64_t Lk) {
+  if (!w) return fail(TRACK_E_INVALID, "%s: null window", what);
   if (dtype != TRACK_DTYPE_F32 && dtype != TRACK_DTYPE_BF16)
-    return fail(TRACK_E_INVALID, "attention_window: bad dtype %d", dtype);
+    return fail(TRACK_E_INVALID, "%s: bad dtype %d", what, dtype);
   if (w->group < 1 || w->sink < 0 || w->left < -1 || w->right < -1 || !(w->scale == 0.0 || (w->scale >= 1e-30 && w->scale <= 1e30)))
-    return fail(TRACK_E_INVALID, "attention_window: window of %lld / %lld groups of %lld, %lld first tokens, scale %g",
+    return fail(TRACK_E_INVALID, "%s: window of %lld / %lld groups of %lld, %lld first tokens, scale %g", what,
                 (long long)w->left, (long long)w->right, (long long)w->group, (long long)w->sink, w->scale);
   if (w->left > WIN_MAX || w->right > WIN_MAX || w->group > WIN_MAX || w->sink > WIN_MAX)
-    return fail(TRACK_E_SHAPE, "attention_window: window limits are at most 2^28");
+    return fail(TRACK_E_SHAPE, "%s: window limits are at most 2^28", what);
   if (B < 0 || H < 1 || Hk < 1 || Lq < 0 || Lk < 0)
-    return fail(TRACK_E_SHAPE, "attention_window: bad sizes B=%d H=%d Hk=%d Lq=%lld Lk=%lld", B, H, Hk, (long long)Lq, (long long)Lk);
-  if (H % Hk) return fail(TRACK_E_SHAPE, "attention_window: %d query heads over %d key heads", H, Hk);
+    return fail(TRACK_E_SHAPE, "%s: bad sizes B=%d H=%d Hk=%d Lq=%lld Lk=%lld", what, B, H, Hk, (long long)Lq, (long long)Lk);
+  if (H % Hk) return fail(TRACK_E_SHAPE, "%s: %d query heads over %d key heads", what, H, Hk);
   if (dtype == TRACK_DTYPE_BF16 ? D != ATT_D : (D != 32 && D != 64 && D != 128))
-    return fail(TRACK_E_UNSUPPORTED, "attention_window: head_dim %d (bfloat16: 128; float32: 32, 64, 128)", D);
-  if (Lk > WIN_MAX || Lq > WIN_MAX / (H / Hk)) return fail(TRACK_E_SHAPE, "attention_window: sequence too long");
+    return fail(TRACK_E_UNSUPPORTED, "%s: head_dim %d (bfloat16: 128; float32: 32, 64, 128)", what, D);
+  if (Lk > WIN_MAX || Lq > WIN_MAX / (H / Hk)) return fail(TRACK_E_SHAPE, "%s: sequence too long", what);
   // each has a workgroup at least, and the launch holds fewer than 2^23 (products below stay in 64 bits)
   if ((int64_t)B * Hk >= (int64_t)1 << 23)
-    return fail(TRACK_E_SHAPE, "attention_window: %d sequences of %d key heads are too many", B, Hk);
+    return fail(TRACK_E_SHAPE, "%s: %d sequences of %d key heads are too many", what, B, Hk);
   return TRACK_OK;
 }
 
 int64_t attention_window_bytes(int dtype, const track_window* w, int B, int H, int Hk, int D, int64_t Lq, int64_t Lk) {
-  if (win_check(dtype, w, B, H, Hk, D, Lq, Lk) != TRACK_OK) return -1;
+  if (win_check("attention_window", dtype, w, B, H, Hk, D, Lq, Lk) != TRACK_OK) return -1;
   if (B == 0 || Lq == 0) return 0;
   int64_t bytes = -1;
   for (bool vec : {true, false}) {  // whatever the rows' alignment turns out to be
@@ -1247,7 +873,7 @@ track_status attention_window(int dtype, const track_window* w, int B, int H, in
                               const void* vt, int64_t ldv, int64_t sv, void* out, int64_t ldo, int64_t so, float* lse,
                               const int32_t* q_len, const int32_t* k_len, const int32_t* q_start, void* ws,
                               size_t ws_bytes, hipStream_t s) {
-  const track_status st = win_check(dtype, w, B, H, Hk, D, Lq, Lk);
+  const track_status st = win_check("attention_window", dtype, w, B, H, Hk, D, Lq, Lk);
   if (st != TRACK_OK) return st;
   if (B == 0 || Lq == 0) return TRACK_OK;
   if (!q || !out || (Lk > 0 && (!k || !vt))) return fail(TRACK_E_INVALID, "attention_window: null pointer");
@@ -1272,13 +898,7 @@ track_status attention_window(int dtype, const track_window* w, int B, int H, in
   }
   WinPlan p = win_plan(dtype, *w, B, Hk, n, D, Lq, Lk, vec);
   if (!win_fits(p, B, Hk, n, Lq)) return fail(TRACK_E_SHAPE, "attention_window: too many row blocks");
-  // Blocks' shares do not always grow with the keys (12 heads of 200 rows: four for 512, three for 576), so a
-  // workspace that was made for more keys may hold fewer than these would take: as many as it
-  // holds.  The other forms' grow.
-  if (p.form == WinPlan::BLOCKS && p.nsplit > 1) {
-    const int64_t share = B * (int64_t)Hk * Lq * n * (4 * D + 8), held = ws ? (int64_t)(std::min<size_t>(ws_bytes, INT64_MAX) / share) : 0;
-    p.nsplit = (int)std::max<int64_t>(1, std::min<int64_t>(p.nsplit, held));
-  }
+  if (p.form == WinPlan::BLOCKS) p.nsplit = win_held(p.nsplit, B, Hk, n, D, Lq, ws, ws_bytes);
   const size_t need = win_bytes(p, B, Hk, n, D, Lq);
   if (need && (!ws || ws_bytes < need)) return fail(TRACK_E_NOMEM, "attention_window: workspace of %zu bytes needed", need);
   if (need && ((uintptr_t)ws & 255)) return fail(TRACK_E_INVALID, "attention_window: workspace must be 256-byte aligned");
@@ -1287,18 +907,12 @@ track_status attention_window(int dtype, const track_window* w, int B, int H, in
   a.q = q, a.k = k, a.vt = vt, a.out = out;
   a.ldq = ldq, a.sq = sq, a.ldk = ldk, a.sk = sk, a.ldv = ldv, a.sv = sv, a.ldo = ldo, a.so = so;
   a.lse = lse, a.q_len = q_len, a.k_len = k_len, a.q_start = q_start;
-  a.before = w->left < 0 ? INT32_MAX : (int)std::min<int64_t>(w->left * w->group, INT32_MAX);
-  a.past = w->right < 0 ? INT32_MAX : (int)std::min<int64_t>((w->right + 1) * w->group, INT32_MAX);
+  win_visible(a, *w, B, Hk, n, D, Lq, Lk);
   const int64_t piece = dtype == TRACK_DTYPE_BF16 ? 8 : (vec ? 4 : 1);
   a.vend = (D - 1) * ldv + (Lk + piece - 1) / piece * piece;
-  a.lift = (int)((2 * WIN_MAX + w->group - 1) / w->group * w->group);
-  a.sink = (int)w->sink;
-  a.B = B, a.Hk = Hk, a.n = n, a.Lq = (int)Lq, a.Lk = (int)Lk;
   a.nrb = (int)p.nrb, a.nsplit = p.nsplit;
-  a.by_group = win_div(w->group), a.by_n = win_div(n);
-  a.by_nrb = win_div(a.nrb), a.by_nsplit = win_div(a.nsplit), a.by_Hk = win_div(Hk);
+  a.by_nrb = win_div(a.nrb), a.by_nsplit = win_div(a.nsplit);
   a.by_inner = win_div(p.form == WinPlan::ROWS ? Hk : B);
-  a.scale_log2 = w->scale > 0.0 ? (float)(w->scale * 1.4426950408889634) : attn_log2_scale(D);
   a.po = (float*)ws;
   a.pml = need ? (float2*)(a.po + (int64_t)p.nsplit * joined * D) : nullptr;
   const bool split = p.nsplit > 1, log2q = a.scale_log2 == 1.0f;
@@ -1338,18 +952,7 @@ track_status attention_window(int dtype, const track_window* w, int B, int H, in
 #undef TRACK_WIN_F32
   TRACK_LAUNCH_CHECK();
   if (split) {
-    // groups of shares for few rows (window_join_kernel)
-    const int per = D / 4, G = joined * D / 4 < 128 * (int64_t)device_cus() && p.nsplit > 2 ? 8 : 1;
-    const int rows_wg = 256 / per / G;
-    const unsigned jg = (unsigned)((joined + rows_wg - 1) / rows_wg);
-#define TRACK_WIN_JOIN(T)                                               \
-  do {                                                                  \
-    if (G == 1) window_join_kernel<T, 1><<<jg, 256, 0, s>>>(a, D);      \
-    else window_join_kernel<T, 8><<<jg, 256, 0, s>>>(a, D);             \
-  } while (0)
-    if (dtype == TRACK_DTYPE_BF16) TRACK_WIN_JOIN(bf16_t);
-    else TRACK_WIN_JOIN(float);
-#undef TRACK_WIN_JOIN
+    window_join(dtype, a, D, s);
     TRACK_LAUNCH_CHECK();
   }
   return TRACK_OK;

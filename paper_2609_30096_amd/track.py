@@ -33,7 +33,8 @@ EXPORTS = [
     "track_op_layernorm", "track_rope_table_len", "track_op_rmsnorm_rope", "track_op_rmsnorm_rope_qk", "track_step_partial_count",
     "track_op_step", "track_op_step_noalloc", "track_hbm_stream", "track_mfma_stream", "track_unipc_coefficients", "track_op_unipc_step", "track_profile_enable", "track_profile_reset", "track_profile_read", "track_set_progress",
     "track_rope_freqs", "track_op_rope", "track_op_headnorm_rope", "track_attention_window_workspace_bytes",
-    "track_op_attention_window",
+    "track_op_attention_window", "track_cache4_page_bytes", "track_op_cache4_append", "track_op_cache4_read",
+    "track_attention_cache4_workspace_bytes", "track_op_attention_cache4",
 ]
 
 
@@ -72,6 +73,12 @@ class HeadRowsC(ctypes.Structure):
 
 class WindowC(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int64) for n in ("left", "right", "sink", "group")] + [("scale", ctypes.c_double)]
+
+
+class Cache4C(ctypes.Structure):
+    _fields_ = ([("pages", ctypes.c_void_p), ("n_pages", ctypes.c_int64)] +
+                [(n, ctypes.c_int32) for n in ("page_tokens", "heads", "head_dim", "table_pages")] +
+                [("table", ctypes.c_void_p), ("ld_table", ctypes.c_int64)])
 
 
 SOLVERS = {"euler": 0, "unipc": 1}
@@ -127,6 +134,13 @@ def _declare(L):
         "track_attention_window_workspace_bytes": (_i64, [_i32, P(WindowC), _i32, _i32, _i32, _i32, _i64, _i64]),
         "track_op_attention_window": (_i32, [_i32, P(WindowC), _i32, _i32, _i32, _i32, _i64, _i64] +
                                       [_vp, _i64, _i64] * 4 + [_vp] * 5 + [_sz, _vp]),
+        "track_cache4_page_bytes": (_i64, [_i32, _i32, _i32]),
+        "track_op_cache4_append": (_i32, [_i32, P(Cache4C), P(RopeConfigC), _i64, _i64] + [_vp, _i64, _i64] * 2 +
+                                   [_vp, _vp, _vp, _vp, _f32, _vp]),
+        "track_op_cache4_read": (_i32, [_i32, P(Cache4C), _i64, _i64] + [_vp, _i64, _i64] * 2 + [_vp, _vp, _vp]),
+        "track_attention_cache4_workspace_bytes": (_i64, [_i32, P(WindowC), _i32, _i32, _i32, _i32, _i64, _i64]),
+        "track_op_attention_cache4": (_i32, [_i32, P(WindowC), P(Cache4C), _i32, _i32, _i64, _i64] +
+                                      [_vp, _i64, _i64] * 2 + [_vp] * 5 + [_sz, _vp]),
         "track_step_partial_count": (_i64, [_i64]),
         "track_op_step": (_i32, [_i64, _i32, _f32, _f32, _vp, _vp, _vp, _vp, _f64, _vp, _vp]),
         "track_op_step_noalloc": (_i32, [_i64, _i32, _f32, _f32, _vp, _vp, _vp, _f64, _vp, _vp]),
@@ -681,6 +695,22 @@ def attention_window_workspace(window: Window, q, k):
         return torch.empty(n, dtype=torch.uint8, device=q.device) if n else None
 
 
+def _attention_extras(q, lse, q_len, k_len, q_start, workspace) -> int:
+    """Checks what attention takes beside its rows; bytes of the workspace."""
+    B, Lq, H, _ = q.shape
+    for t, what in ((q_len, "q_len"), (k_len, "k_len"), (q_start, "q_start")):
+        _ints(t, (B,), q, what)
+    if lse is not None and (str(lse.dtype) != "torch.float32" or lse.shape != (B, H, Lq) or
+                            not lse.is_contiguous() or lse.get_device() != q.get_device()):
+        raise ValueError(f"lse: contiguous float32 [{B}, {H}, {Lq}] on {q.device} expected")
+    nbytes = 0
+    if workspace is not None:
+        if workspace.get_device() != q.get_device() or not workspace.is_contiguous():
+            raise ValueError(f"workspace: contiguous, on {q.device} expected")
+        nbytes = workspace.numel() * workspace.element_size()
+    return nbytes
+
+
 _window_layouts: dict = {}
 
 
@@ -701,16 +731,7 @@ def _check_window(q, k, vt, out, lse, q_len, k_len, q_start, workspace):
         raise ValueError("vt: rows of keys, D of them a head, heads one after another")
     if Lk == 0:  # no key is read, whatever strides an empty tensor has
         ldk, sk, ldv, sv = Hk * D, 0, 8, 0
-    for t, what in ((q_len, "q_len"), (k_len, "k_len"), (q_start, "q_start")):
-        _ints(t, (B,), q, what)
-    if lse is not None and (str(lse.dtype) != "torch.float32" or lse.shape != (B, H, Lq) or
-                            not lse.is_contiguous() or lse.get_device() != q.get_device()):
-        raise ValueError(f"lse: contiguous float32 [{B}, {H}, {Lq}] on {q.device} expected")
-    nbytes = 0
-    if workspace is not None:
-        if workspace.get_device() != q.get_device() or not workspace.is_contiguous():
-            raise ValueError(f"workspace: contiguous, on {q.device} expected")
-        nbytes = workspace.numel() * workspace.element_size()
+    nbytes = _attention_extras(q, lse, q_len, k_len, q_start, workspace)
     return (_float_dtype(q), B, H, Hk, D, Lq, Lk, ldq, sq, ldk, sk, ldv, sv if B > 1 else 0, ldo, so, nbytes)
 
 
@@ -724,6 +745,126 @@ def op_attention_window(window: Window, q, k, vt, out, lse=None, q_len=None, k_l
         _window_layouts, (q, k, vt, out, lse, q_len, k_len, q_start, workspace), _check_window)
     _on_device(lib().track_op_attention_window, q, dtype, window.c(), B, H, Hk, D, Lq, Lk, q.data_ptr(), ldq, sq,
                k.data_ptr(), ldk, sk, vt.data_ptr(), ldv, sv, out.data_ptr(), ldo, so,
+               *[0 if t is None else t.data_ptr() for t in (lse, q_len, k_len, q_start, workspace)], nbytes)
+    return out
+
+
+def cache4_page_bytes(heads: int, head_dim: int, page_tokens: int) -> int:
+    n = lib().track_cache4_page_bytes(heads, head_dim, page_tokens)
+    if n == 0:
+        raise ValueError(f"pages of {page_tokens} tokens (multiples of 64 up to 65536), {heads} heads of {head_dim} "
+                         "channels (32, 64, 128)")
+    return n
+
+
+class Cache4:
+    """A paged cache of keys and values in 4 bits (track_cache4): pages uint8 [n_pages, page bytes], made here if not
+    given, and the table of each sequence's pages, int32 [sequences, pages of a sequence], whose entries may change
+    between calls."""
+
+    def __init__(self, heads: int, head_dim: int, page_tokens: int, table, pages=None, n_pages: Optional[int] = None):
+        torch = _torch()
+        size = cache4_page_bytes(heads, head_dim, page_tokens)
+        if table.dim() != 2 or str(table.dtype) != "torch.int32" or (table.shape[1] > 1 and table.stride(1) != 1):
+            raise ValueError("table: int32 [sequences, pages] with entries side by side expected")
+        if pages is None:
+            if n_pages is None:
+                raise ValueError("pages or n_pages is needed")
+            pages = torch.zeros(n_pages, size, dtype=torch.uint8, device=table.device)
+        if pages.dim() != 2 or pages.shape[1] != size or str(pages.dtype) != "torch.uint8" or not pages.is_contiguous():
+            raise ValueError(f"pages: contiguous uint8 [pages, {size}] expected")
+        if n_pages is not None and n_pages != pages.shape[0]:
+            raise ValueError(f"{pages.shape[0]} pages, n_pages {n_pages}")
+        if pages.get_device() != table.get_device():
+            raise TypeError(f"pages on {pages.device} beside a table on {table.device}")
+        self.heads, self.head_dim, self.page_tokens = heads, head_dim, page_tokens
+        self.pages, self.table = pages, table
+        self.tokens = table.shape[1] * page_tokens  # places of a sequence
+        self.c = Cache4C(pages.data_ptr(), pages.shape[0], page_tokens, heads, head_dim, table.shape[1],
+                         table.data_ptr(), max(table.stride(0), table.shape[1]) if table.shape[0] > 1 else table.shape[1])
+        self.layouts = tuple({} for _ in range(5))
+
+    def _rows(self, k, v, start, n, pos, freqs):
+        B, L, H, D = k.shape if k.dim() == 4 else (0, 0, 0, 0)
+        ldk, sk = _seq_heads(k, "k")
+        ldv, sv = _seq_heads(v, "v")
+        if v.shape != k.shape or H != self.heads or D != self.head_dim or B != self.table.shape[0]:
+            raise ValueError(f"k {tuple(k.shape)}, v {tuple(v.shape)} for {self.table.shape[0]} sequences, {self.heads} "
+                             f"heads of {self.head_dim}")
+        _like(v, k, "v")
+        if start is None:
+            raise ValueError("start: the first place of each sequence is needed")
+        _ints(start, (B,), k, "start")
+        _ints(n, (B,), k, "n")
+        for t, what in ((self.pages, "cache"), (freqs, "rope")):
+            if t is not None and t.get_device() != k.get_device():
+                raise TypeError(f"{what} on {t.device}, k on {k.device}")
+        return _float_dtype(k), B, L, ldk, sk, ldv, sv
+
+    def _queries(self, q, out, lse, q_len, k_len, q_start, workspace):
+        ldq, sq = _seq_heads(q, "q")
+        ldo, so = _seq_heads(out, "out")
+        B, Lq, H, D = q.shape
+        if out.shape != q.shape or D != self.head_dim or B != self.table.shape[0]:
+            raise ValueError(f"q {tuple(q.shape)}, out {tuple(out.shape)} for {self.table.shape[0]} sequences, heads of "
+                             f"{self.head_dim}")
+        _like(out, q, "out")
+        if self.pages.get_device() != q.get_device():
+            raise TypeError(f"cache on {self.pages.device}, q on {q.device}")
+        nbytes = _attention_extras(q, lse, q_len, k_len, q_start, workspace)
+        return _float_dtype(q), B, H, Lq, ldq, sq, ldo, so, nbytes
+
+
+def op_cache4_append(cache: Cache4, k, v, start, n=None, rope: Optional[Rope] = None, pos=None):
+    """Rows k and v [B, L, heads, head_dim] into places start[b].. of the cache (int32 [B]), the first n[b] of each
+    sequence (int32 [B]; None: all), the keys rotated by pos (int32 [axes, B, L]) where a rope is given."""
+    if (rope is None) != (pos is None):
+        raise ValueError("rope and pos come together")
+    dtype, B, L, ldk, sk, ldv, sv = _layout(cache.layouts[rope.axes if rope is not None else 0],
+                                            (k, v, start, n, pos, None if rope is None else rope.freqs), cache._rows)
+    if rope is not None:
+        _ints(pos, (rope.axes, B, L), k, "pos")
+    _on_device(lib().track_op_cache4_append, k, dtype, cache.c, None if rope is None else rope.c, B, L, k.data_ptr(), ldk,
+               sk, v.data_ptr(), ldv, sv, start.data_ptr(), 0 if n is None else n.data_ptr(),
+               0 if rope is None else pos.data_ptr(), 0 if rope is None else rope.freqs.data_ptr(),
+               1.0 if rope is None else rope.amplitude)
+
+
+def op_cache4_read(cache: Cache4, k, v, start, n=None):
+    """Places start[b].. of the cache into rows k and v [B, L, heads, head_dim], the first n[b] of each sequence (the
+    others stay as they were); returns them."""
+    dtype, B, L, ldk, sk, ldv, sv = _layout(cache.layouts[0], (k, v, start, n, None, None), cache._rows)
+    _on_device(lib().track_op_cache4_read, k, dtype, cache.c, B, L, k.data_ptr(), ldk, sk, v.data_ptr(), ldv, sv,
+               start.data_ptr(), 0 if n is None else n.data_ptr())
+    return k, v
+
+
+def attention_cache4_workspace_bytes(window: Window, dtype: int, B: int, H: int, Hk: int, head_dim: int, Lq: int,
+                                     Lk: int) -> int:
+    n = lib().track_attention_cache4_workspace_bytes(dtype, window.c(), B, H, Hk, head_dim, Lq, Lk)
+    if n < 0:
+        raise TrackError(E_INVALID, lib().track_last_error().decode())
+    return n
+
+
+def attention_cache4_workspace(window: Window, cache: Cache4, q, Lk: Optional[int] = None):
+    """The workspace of op_attention_cache4 for q and at most Lk keys (None where it needs none); it serves calls of the
+    same q on fewer keys too."""
+    torch = _torch()
+    with torch.cuda.device(q.device):
+        n = attention_cache4_workspace_bytes(window, _float_dtype(q), q.shape[0], q.shape[2], cache.heads, q.shape[3],
+                                             q.shape[1], cache.tokens if Lk is None else Lk)
+        return torch.empty(n, dtype=torch.uint8, device=q.device) if n else None
+
+
+def op_attention_cache4(window: Window, cache: Cache4, q, out, Lk: Optional[int] = None, lse=None, q_len=None,
+                        k_len=None, q_start=None, workspace=None):
+    """Window attention of q [B, Lq, H, D] on the first Lk places of each sequence of the cache (None: all that its
+    table has) into out (like q); returns out.  The rest as op_attention_window."""
+    dtype, B, H, Lq, ldq, sq, ldo, so, nbytes = _layout(cache.layouts[4], (q, out, lse, q_len, k_len, q_start, workspace),
+                                                        cache._queries)
+    _on_device(lib().track_op_attention_cache4, q, dtype, window.c(), cache.c, B, H, Lq,
+               cache.tokens if Lk is None else Lk, q.data_ptr(), ldq, sq, out.data_ptr(), ldo, so,
                *[0 if t is None else t.data_ptr() for t in (lse, q_len, k_len, q_start, workspace)], nbytes)
     return out
 
