@@ -453,6 +453,39 @@ track_status track_op_attention_window(int32_t dtype, const track_window* window
                                        const int32_t* k_len, const int32_t* q_start, void* workspace,
                                        size_t workspace_bytes, void* stream);
 
+/* Attention with changed logits, for sequences packed of several shots or texts:
+ * softmax(x) v with x = scale q k, then, if cap > 0, cap tanh(x / cap), then less
+ * slope[h] |p - j| for the query at place p and the key at place j (tokens), over the
+ * keys that a query sees.  The query at p sees key j < k_len[b] of its document iff
+ *   right < 0 or floor(j/group) <= floor(p/group) + right or j is among the first
+ *   prefix tokens of the document, and
+ *   left < 0 or floor(j/group) >= floor(p/group) - left.
+ * Documents lie one after another: place x is in document d, the number of ends at or
+ * before x; the places past the last end are one more. */
+typedef struct track_scores {
+  int64_t left, right;  /* as track_window */
+  int64_t group;
+  double  scale;
+  double  cap;          /* 0: none; 1e-3 .. 1e3 */
+} track_scores;
+
+int64_t track_attention_scores_workspace_bytes(int32_t dtype, const track_scores* scores, int32_t B, int32_t H,
+                                               int32_t Hk, int32_t head_dim, int64_t Lq, int64_t Lk);
+
+/* Rows, lengths, types, limits, lse (of the changed logits) and the workspace as
+ * track_op_attention_window.  slopes: device float32 [H], finite, or NULL; doc_end:
+ * device int32 [B][docs], ascending, docs in 0..2^20 (NULL for 0); prefix: device int32
+ * [B][docs + 1], cut to [0, 2^28], or NULL.  They are read when the call runs on the stream;
+ * ends that do not ascend give unspecified outputs, nothing else.  scale q k (before
+ * the cap too) and the bias have to lie within float32's range; a capped logit is off by up to cap 2^-20. */
+track_status track_op_attention_scores(int32_t dtype, const track_scores* scores, int32_t B, int32_t H, int32_t Hk,
+                                       int32_t head_dim, int64_t Lq, int64_t Lk, const void* q, int64_t ldq, int64_t sq,
+                                       const void* k, int64_t ldk, int64_t sk, const void* vt, int64_t ldv, int64_t sv,
+                                       void* out, int64_t ldo, int64_t so, float* lse, const float* slopes,
+                                       const int32_t* doc_end, int32_t docs, const int32_t* prefix,
+                                       const int32_t* q_len, const int32_t* k_len, const int32_t* q_start,
+                                       void* workspace, size_t workspace_bytes, void* stream);
+
 /* A paged cache that holds keys and values in 4 bits, for long videos.  32
  * channels of a token's head share a power of two 2^e, kept as the byte e + 127;
  * each of their values is a sign and one of 0, 0.5, 1, 1.5, 2, 3, 4, 6 times 2^e,

@@ -944,6 +944,23 @@ track_status track_op_attention_window(int32_t dtype, const track_window* window
                           lse, q_len, k_len, q_start, workspace, workspace_bytes, (hipStream_t)stream);
 }
 
+int64_t track_attention_scores_workspace_bytes(int32_t dtype, const track_scores* scores, int32_t B, int32_t H,
+                                               int32_t Hk, int32_t head_dim, int64_t Lq, int64_t Lk) {
+  return attention_scores_bytes(dtype, scores, B, H, Hk, head_dim, Lq, Lk);
+}
+
+track_status track_op_attention_scores(int32_t dtype, const track_scores* scores, int32_t B, int32_t H, int32_t Hk,
+                                       int32_t head_dim, int64_t Lq, int64_t Lk, const void* q, int64_t ldq, int64_t sq,
+                                       const void* k, int64_t ldk, int64_t sk, const void* vt, int64_t ldv, int64_t sv,
+                                       void* out, int64_t ldo, int64_t so, float* lse, const float* slopes,
+                                       const int32_t* doc_end, int32_t docs, const int32_t* prefix,
+                                       const int32_t* q_len, const int32_t* k_len, const int32_t* q_start,
+                                       void* workspace, size_t workspace_bytes, void* stream) {
+  return attention_scores(dtype, scores, B, H, Hk, head_dim, Lq, Lk, q, ldq, sq, k, ldk, sk, vt, ldv, sv, out, ldo, so,
+                          lse, slopes, doc_end, docs, prefix, q_len, k_len, q_start, workspace, workspace_bytes,
+                          (hipStream_t)stream);
+}
+
 int64_t track_cache4_page_bytes(int32_t heads, int32_t head_dim, int32_t page_tokens) {
   return cache4_page_bytes(heads, head_dim, page_tokens);
 }

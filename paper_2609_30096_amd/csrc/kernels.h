@@ -68,6 +68,16 @@ track_status attention_window(int dtype, const track_window* w, int B, int H, in
                               const int32_t* q_len, const int32_t* k_len, const int32_t* q_start, void* ws,
                               size_t ws_bytes, hipStream_t s);
 
+// window.hip (track_op_attention_scores)
+constexpr int SCORES_DOCS = 1 << 20;  // documents of a sequence
+int64_t attention_scores_bytes(int dtype, const track_scores* c, int B, int H, int Hk, int D, int64_t Lq, int64_t Lk);
+track_status attention_scores(int dtype, const track_scores* c, int B, int H, int Hk, int D, int64_t Lq, int64_t Lk,
+                              const void* q, int64_t ldq, int64_t sq, const void* k, int64_t ldk, int64_t sk,
+                              const void* vt, int64_t ldv, int64_t sv, void* out, int64_t ldo, int64_t so, float* lse,
+                              const float* slopes, const int32_t* doc_end, int docs, const int32_t* prefix,
+                              const int32_t* q_len, const int32_t* k_len, const int32_t* q_start, void* ws,
+                              size_t ws_bytes, hipStream_t s);
+
 // cache.hip (track_cache4_page_bytes, track_op_cache4_append, track_op_cache4_read, track_op_attention_cache4)
 int64_t cache4_page_bytes(int heads, int head_dim, int page_tokens);  // 0 for what it refuses
 track_status cache4_append(int dtype, const track_cache4* cache, const track_rope_config* rope, int64_t B, int64_t L, const void* k,

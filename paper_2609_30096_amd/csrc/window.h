@@ -46,6 +46,11 @@ struct WinArgs {
   WinDiv by_inner;    // sequences of a head, or heads of a sequence (win_place)
   int64_t vend;       // elements of a head's V^T up to its last row's last key, rounded up to 16 bytes
   float scale_log2;
+  // attention with changed logits (win_score_range, WinScore)
+  const float* slopes;                // [query heads], or null
+  const int32_t *doc_end, *prefix;    // [B][docs], [B][docs + 1], or null
+  int docs;
+  float cap_log2, cap_in;             // cap log2(e) (0: none), 2 scale log2(e) / cap
   float* po;          // [nsplit][B][Hk][Lq n][D]: a share's sums
   float2* pml;        // [nsplit][B][Hk][Lq n]: its reference (log2 units) and its denominator
 };
@@ -73,6 +78,43 @@ __device__ __forceinline__ void win_range(const WinArgs& a, const WinSeq& s, int
   const int first = (int)(a.by_group(p) * a.by_group.d) - a.lift;  // of the query's group
   lo = first > a.before ? min(first - a.before, s.klen) : 0;
   hi = a.past - 1 < s.klen - 1 - first ? max(first + a.past - 1, -1) : s.klen - 1;
+}
+
+// The keys [lo, hi] of query i inside its document, those of the document's prefix among them whatever the window's
+// end is; they grow with the position, like the window.  Ends of documents ascend: the last one at or before the
+// position and the first behind it, all in the wave's lanes at once for 64 at most, by halves beyond (a dependent load each).
+__device__ __forceinline__ void win_score_range(const WinArgs& a, const WinSeq& s, int i, int& lo, int& hi) {
+  win_range(a, s, i, lo, hi);
+  if (!a.docs && !a.prefix) return;
+  const int p = s.start + i;
+  int first = 0, end = INT32_MAX, d = 0;
+  const int32_t* const ends = a.doc_end + (int64_t)s.b * a.docs;
+  if (a.docs > 64) {
+    int n = a.docs;  // ends at or before p: d .. d + n
+    while (n > 0) {
+      const int half = n >> 1;
+      const bool before = ends[d + half] <= p;
+      d = before ? d + half + 1 : d;
+      n = before ? n - half - 1 : half;
+    }
+    if (d > 0) first = ends[d - 1];
+    if (d < a.docs) end = ends[d];
+  } else if (a.docs > 0) {
+    const int all = ends[min(att_lane(), a.docs - 1)];
+    for (int k = 0; k < a.docs; ++k) {
+      const int e = __builtin_amdgcn_readlane(all, k);
+      const bool before = e <= p;
+      d += before;
+      first = before ? e : first;
+      end = before ? end : min(end, e);
+    }
+  }
+  if (a.prefix && a.past != INT32_MAX) {
+    const int n = max(0, min(a.prefix[(int64_t)s.b * (a.docs + 1) + d], (int)WIN_MAX));
+    hi = max(hi, min(max(-(int)WIN_MAX, min(first, (int)WIN_MAX)) + n, s.klen) - 1);
+  }
+  lo = max(lo, min(first, s.klen));
+  hi = min(hi, max(end, 0) - 1);
 }
 
 // Query of row r, and the row's head among those of its key head.
@@ -162,6 +204,61 @@ struct WinMask {
   }
 };
 
+// What becomes of a logit s = q k before the softmax, in log2 units: cap tanh(scale s / cap) or scale s, less
+// slope |p - j| for a query at place p and a key at j.  Both are template values: an element takes 2 instructions without either.
+template <bool CAP_, bool BIAS_>
+struct WinScore {
+  static constexpr bool ON = true, CAP = CAP_, BIAS = BIAS_;
+  // x: the logit, far: p - j, slope: in log2 units
+  // tanh(y) = 1 - 2 / (exp(2 y) + 1): off by some 5 units of 2^-24 of the cap, also where it is near 0, a hundredth of
+  // what the weights' rounding to bfloat16 takes at a cap of 50
+  static __device__ __forceinline__ float apply(const WinArgs& a, float x, float far, float slope) {
+    if constexpr (CAP)
+      x = fmaf(-2.0f * a.cap_log2, __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(x * a.cap_in) + 1.0f), a.cap_log2);
+    else
+      x *= a.scale_log2;
+    if constexpr (BIAS) x = fmaf(-fabsf(far), slope, x);
+    return x;
+  }
+};
+struct WinPlain {
+  static constexpr bool ON = false, CAP = false, BIAS = false;
+};
+
+template <class S>
+__device__ __forceinline__ void win_seen(const WinArgs& a, const WinSeq& s, int i, int& lo, int& hi) {
+  if constexpr (S::ON) win_score_range(a, s, i, lo, hi);
+  else win_range(a, s, i, lo, hi);
+}
+
+// The head's slope in log2 units.
+template <class S>
+__device__ __forceinline__ float win_slope(const WinArgs& a, int head) {
+  if constexpr (S::BIAS) return a.slopes[head] * 1.4426950408889634f;
+  else return 0.0f;
+}
+
+// A mask that changes the logits too; EDGE: it hides keys.
+template <int NB, class S, bool EDGE, bool WEIGHED_ = false>
+struct WinScoreMask : WinMask<NB, WEIGHED_> {
+  const WinArgs* a;
+  int p[NB];          // the lane's queries' places
+  float slope[NB], far[NB];
+  __device__ __forceinline__ void begin() {
+    const int k = this->key0 + 8 * (att_lane() >> 4);
+    if constexpr (EDGE) WinMask<NB, WEIGHED_>::begin();
+    if constexpr (S::BIAS) {
+#pragma unroll
+      for (int b = 0; b < NB; ++b) far[b] = (float)(p[b] - k);
+    }
+  }
+  __device__ __forceinline__ float apply(int b, int c, float s) const {
+    s = S::apply(*a, s, S::BIAS ? far[b] - (float)c : 0.0f, S::BIAS ? slope[b] : 0.0f);
+    if constexpr (EDGE) return WinMask<NB, WEIGHED_>::apply(b, c, s);
+    else return s;
+  }
+};
+
 // 16 bytes a lane from the buffer at `off` (and the wave's `scalar` more) to LDS, lanes side by side.
 // (Functions of their own: in a template, with arguments that depend on it, the host's pass rejects
 // the builtin.)
@@ -205,14 +302,16 @@ __device__ __forceinline__ void win_place(const WinArgs& a, int& rb, int& sp, in
 // products and sums): lane (jq, g) has row jq, kfrag(c) is channels 16 c + 4 g .. + 3 of key jq,
 // vfrag(c) keys 4 g .. + 3 of channel 16 c + jq, and the logits that a lane holds (keys 4 g .. + 3
 // of its row) are the "B" operand of O^T += V^T P^T as they are.
-template <int D>
+template <int D, bool SCORED = false>
 struct WinF32 {
   static constexpr int C = D / 16;
   f32x4 qf[C], o[C];
   float m, l;  // reference (log2 units), the lane's part of the denominator
   int lo, hi, sink;
+  int p;       // SCORED: the row's place and slope
+  float slope;
   template <class KF, class VF>
-  __device__ __forceinline__ void step(KF kfrag, VF vfrag, bool edge, int key0, int klen, float scale_log2) {
+  __device__ __forceinline__ void step(KF kfrag, VF vfrag, bool edge, int key0, int klen, float scale_log2, const WinArgs* a = nullptr) {
     const int lane = att_lane(), jq = lane & 15, g = lane >> 4;
     f32x4 s0 = {0.0f, 0.0f, 0.0f, 0.0f}, s1 = s0;
     // fragments are read ahead of their products
@@ -236,6 +335,20 @@ struct WinF32 {
     float x[4];
 #pragma unroll
     for (int e = 0; e < 4; ++e) x[e] = s0[e] + s1[e];
+    if constexpr (SCORED) {  // in log2 units from here on
+      if (a->cap_log2 > 0.0f) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[e] = a->cap_log2 * tanhf(x[e] * a->cap_in);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[e] *= scale_log2;
+      }
+      if (a->slopes) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[e] = fmaf(-fabsf((float)(p - (key0 + 4 * g + e))), slope, x[e]);
+      }
+      scale_log2 = 1.0f;
+    }
     if (edge) {
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
@@ -299,8 +412,14 @@ struct WinF32 {
     const int g = (int)(threadIdx.x & 63) >> 4;
     int e;
     const int qi = win_query(a, min(r, rows - 1), e);
-    win_range(a, seq, qi, lo, hi);
-    if (tiles.sink == 0 && seq.sink >= lo1) lo = 0;
+    if constexpr (SCORED) {
+      win_score_range(a, seq, qi, lo, hi);
+      p = seq.start + qi;
+      slope = a.slopes ? a.slopes[h * a.n + e] * 1.4426950408889634f : 0.0f;
+    } else {
+      win_range(a, seq, qi, lo, hi);
+      if (tiles.sink == 0 && seq.sink >= lo1) lo = 0;
+    }
     sink = tiles.sink;
     const float* qp = (const float*)a.q + seq.b * a.sq + (int64_t)qi * a.ldq + (int64_t)(h * a.n + e) * D + 4 * g;
 #pragma unroll

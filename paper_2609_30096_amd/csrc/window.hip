@@ -22,8 +22,12 @@ namespace track {
 // ---------------------------------------------------------------- many rows, bfloat16
 // 256 rows a workgroup, 32 a wave; K and V^T tiles by DMA into a ring of two slots, and the
 // tile body of the plain attention.
-template <bool QLOG2, bool SPLIT>
+template <bool QLOG2, bool SPLIT, class S>
 __global__ __launch_bounds__(512) void window_blocks_kernel(WinArgs a) {
+  static_assert(QLOG2 || !S::ON, "changed logits are in log2 units");
+  typedef std::conditional_t<S::ON, WinScoreMask<ATT_QB, S, true>, WinMask<ATT_QB>> Mask;
+  typedef std::conditional_t<S::ON, WinScoreMask<ATT_QB, S, true, true>, WinMask<ATT_QB, true>> Weighed;
+  typedef std::conditional_t<S::ON, WinScoreMask<ATT_QB, S, false>, AttAll> Whole;
   constexpr int BKV = ATT_BKV, D = ATT_D, SLOT = ATT_SLOT;
   // one object: with a second one the compiler waits for every copy under way before a tile's
   // first fragment read (20% slower)
@@ -43,7 +47,7 @@ __global__ __launch_bounds__(512) void window_blocks_kernel(WinArgs a) {
 
   // windows of the block's first and last row, and of the wave's
   auto range_of = [&](int r, int& lo, int& hi) {
-    win_range(a, seq, (int)a.by_n((uint32_t)min(r, rows - 1)), lo, hi);
+    win_seen<S>(a, seq, (int)a.by_n((uint32_t)min(r, rows - 1)), lo, hi);
     lo = __builtin_amdgcn_readfirstlane(lo);
     hi = __builtin_amdgcn_readfirstlane(hi);
   };
@@ -56,20 +60,26 @@ __global__ __launch_bounds__(512) void window_blocks_kernel(WinArgs a) {
   int wlo, whi, unused;
   range_of(wr0, wlo, unused);
   range_of(wr0 + 31, unused, whi);
-  if (tiles.sink == 0 && seq.sink >= lo1) wlo = 0;
+  if (!S::ON && tiles.sink == 0 && seq.sink >= lo1) wlo = 0;
   const bool live = wr0 < rows;
 
   const bf16_t* const kbase = (const bf16_t*)a.k + b * a.sk + (int64_t)h * D;
   const bf16_t* const vbase = (const bf16_t*)a.vt + b * a.sv + (int64_t)h * D * a.ldv;
   bf16x8 qf[D / 32][ATT_QB];
-  WinMask<ATT_QB> mask;
+  Mask mask;
+  Whole whole;
   mask.sink = tiles.sink;
+  if constexpr (S::ON) mask.a = whole.a = &a;
 #pragma unroll
   for (int i = 0; i < ATT_QB; ++i) {
     int e;
     const int qi = win_query(a, min(wr0 + 16 * i + jq, rows - 1), e);
-    win_range(a, seq, qi, mask.lo[i], mask.hi[i]);
-    if (tiles.sink == 0 && seq.sink >= lo1) mask.lo[i] = 0;
+    win_seen<S>(a, seq, qi, mask.lo[i], mask.hi[i]);
+    if (!S::ON && tiles.sink == 0 && seq.sink >= lo1) mask.lo[i] = 0;
+    if constexpr (S::ON) {
+      mask.p[i] = whole.p[i] = seq.start + qi;
+      mask.slope[i] = whole.slope[i] = win_slope<S>(a, h * a.n + e);
+    }
     const bf16_t* qp = (const bf16_t*)a.q + b * a.sq + (int64_t)qi * a.ldq + (int64_t)(h * a.n + e) * D + g * 8;
 #pragma unroll
     for (int kc = 0; kc < D / 32; ++kc) qf[kc][i] = __builtin_bit_cast(bf16x8, *(const u32x4*)(qp + kc * 32));
@@ -141,7 +151,7 @@ __global__ __launch_bounds__(512) void window_blocks_kernel(WinArgs a) {
         if (key0 + BKV > seq.klen) clear_past_end(key0, slot);
         if (live && key0 <= whi && (key0 + BKV > wlo || key0 < tiles.sink)) {
           mask.key0 = key0;
-          att_tile_masked<WinMask<ATT_QB>, QLOG2, 4, true, false>(smem, qf, ko, vo, st, mask, a.scale_log2);
+          att_tile_masked<Mask, QLOG2, 4, true, false>(smem, qf, ko, vo, st, mask, a.scale_log2);
         }
         next();
       }
@@ -156,17 +166,22 @@ __global__ __launch_bounds__(512) void window_blocks_kernel(WinArgs a) {
       __syncthreads();
       if (*not_finite) {  // the whole workgroup
         st.reset();
-        WinMask<ATT_QB, true> weigh;
+        Weighed weigh;
 #pragma unroll
         for (int i = 0; i < ATT_QB; ++i) weigh.lo[i] = mask.lo[i], weigh.hi[i] = mask.hi[i];
         weigh.sink = mask.sink;
+        if constexpr (S::ON) {
+          weigh.a = &a;
+#pragma unroll
+          for (int i = 0; i < ATT_QB; ++i) weigh.p[i] = mask.p[i], weigh.slope[i] = mask.slope[i];
+        }
         for (int idx = i0; idx < ie; ++idx) {
           const int key0 = tiles.key<BKV>(idx);
           issue(key0, slot);
           barrier();
           if (key0 + BKV > seq.klen) clear_past_end(key0, slot);
           weigh.key0 = key0;
-          att_tile_masked<WinMask<ATT_QB, true>, QLOG2, 4, true, false>(smem, qf, ko, vo, st, weigh, a.scale_log2);
+          att_tile_masked<Weighed, QLOG2, 4, true, false>(smem, qf, ko, vo, st, weigh, a.scale_log2);
           __syncthreads();
         }
         issue(tiles.key<BKV>(min(ie, i1 - 1)), slot);
@@ -184,6 +199,7 @@ __global__ __launch_bounds__(512) void window_blocks_kernel(WinArgs a) {
     const __amdgpu_buffer_rsrc_t rsV =
         __builtin_amdgcn_make_buffer_rsrc((void*)vbase, (short)0, (int)(uint32_t)(a.vend * 2), 0x00020000);
     for (int idx = ie; idx < i1; ++idx) {
+      const uint32_t vp0 = vp;
       if (idx + 1 < i1) {  // (past the share: this tile again)
         kp = idx + 1 == jump ? kj : kp + kstep;
         vp = idx + 1 == jump ? vj : vp + 2 * BKV;
@@ -197,7 +213,10 @@ __global__ __launch_bounds__(512) void window_blocks_kernel(WinArgs a) {
 #pragma unroll
       for (int i = 0; i < 2; ++i)
         __builtin_amdgcn_raw_ptr_buffer_load_lds(rsV, (att_lds_ptr_t)(to + ATT_K_BYTES + i * 1024), 16, voffg[i], vp, 0, 0);
-      if (live) att_tile_masked<AttAll, QLOG2, 4, true, false>(smem, qf, ko, vo, st, AttAll{}, a.scale_log2);
+      if (live) {
+        if constexpr (S::ON) whole.key0 = (int)(vp0 >> 1);
+        att_tile_masked<Whole, QLOG2, 4, true, false>(smem, qf, ko, vo, st, whole, a.scale_log2);
+      }
       next();
     }
   }
@@ -256,7 +275,7 @@ constexpr int WIN_SHARED = 16;
 // denominator adds the rounded ones, as in the block kernel (attention_tile.h).  What bounds it: reading K and V^T (8 sequences of 100003 keys 490 us,
 // 6.7 TB/s; 6.2 - 6.5 is what a plain read stream through the caches reaches), and for short windows the
 // latency of a tile and of the join (8 heads of 4096 keys 8.2 us).
-template <bool SPLIT, bool PAST>
+template <bool SPLIT, bool PAST, class S>
 __global__ __launch_bounds__(256) void window_rows_kernel(WinArgs a) {
   constexpr int BKV = ATT_BKV, D = ATT_D, F = D / 16;
   typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
@@ -276,8 +295,8 @@ __global__ __launch_bounds__(256) void window_rows_kernel(WinArgs a) {
   if (rows == 0) return;            // the whole workgroup
 
   int lo0, hi0, lo1, hi1;
-  win_range(a, seq, 0, lo0, hi0);
-  win_range(a, seq, seq.qlen - 1, lo1, hi1);
+  win_seen<S>(a, seq, 0, lo0, hi0);
+  win_seen<S>(a, seq, seq.qlen - 1, lo1, hi1);
   WinTiles tiles;
   tiles.init<BKV>(seq, __builtin_amdgcn_readfirstlane(lo0), __builtin_amdgcn_readfirstlane(hi0),
                   __builtin_amdgcn_readfirstlane(lo1), __builtin_amdgcn_readfirstlane(hi1));
@@ -289,8 +308,9 @@ __global__ __launch_bounds__(256) void window_rows_kernel(WinArgs a) {
   const int qi = win_query(a, min(jq, rows - 1), e), head = h * a.n + e;
   WinMask<1> mask;
   mask.sink = tiles.sink;
-  win_range(a, seq, qi, mask.lo[0], mask.hi[0]);
-  if (tiles.sink == 0 && seq.sink >= lo1) mask.lo[0] = 0;
+  win_seen<S>(a, seq, qi, mask.lo[0], mask.hi[0]);
+  if (!S::ON && tiles.sink == 0 && seq.sink >= lo1) mask.lo[0] = 0;
+  const float slope = win_slope<S>(a, head), scale_log2 = S::ON ? 1.0f : a.scale_log2;  // (changed logits are in log2 units)
   const bf16_t* qp = (const bf16_t*)a.q + b * a.sq + (int64_t)qi * a.ldq + (int64_t)head * D + g * 8;
   bf16x8 qf[D / 32];
 #pragma unroll
@@ -378,6 +398,14 @@ __global__ __launch_bounds__(256) void window_rows_kernel(WinArgs a) {
                                                        kc ? s[i] : f32x4{0.0f, 0.0f, 0.0f, 0.0f}, 0, 0, 0);
     read();
     if (more) copy_k(next);
+    if constexpr (S::ON) {
+      const float far = S::BIAS ? (float)(seq.start + qi - (key0 + 8 * g)) : 0.0f;
+#pragma unroll
+      for (int i = 0; i < BKV / 16; ++i)
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+          s[i][r] = S::apply(a, s[i][r], S::BIAS ? far - (float)(32 * (i >> 1) + 4 * (i & 1) + r) : 0.0f, slope);
+    }
     if (edge) {
       WinMask<1> mk = mask;
       mk.key0 = key0;
@@ -392,7 +420,7 @@ __global__ __launch_bounds__(256) void window_rows_kernel(WinArgs a) {
     for (int i = 0; i < BKV / 16; ++i)
 #pragma unroll
       for (int r = 0; r < 4; ++r) t = fmaxf(t, s[i][r]);
-    const float mn = fmaxf(m, group_max2(t, t) * a.scale_log2);
+    const float mn = fmaxf(m, group_max2(t, t) * scale_log2);
     if (__ballot(mn > m)) {
       const float alpha = mn == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m - mn);
       l *= alpha;
@@ -409,8 +437,8 @@ __global__ __launch_bounds__(256) void window_rows_kernel(WinArgs a) {
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         const f32x4 x = s[2 * c + (e >> 1)];
-        const float p0 = __builtin_amdgcn_exp2f(fmaf(x[2 * (e & 1)], a.scale_log2, nm));
-        const float p1 = __builtin_amdgcn_exp2f(fmaf(x[2 * (e & 1) + 1], a.scale_log2, nm));
+        const float p0 = __builtin_amdgcn_exp2f(fmaf(x[2 * (e & 1)], scale_log2, nm));
+        const float p1 = __builtin_amdgcn_exp2f(fmaf(x[2 * (e & 1) + 1], scale_log2, nm));
         pw[c][e] = pack_bf2(p0, p1);
         // the denominator adds the weights as rounded for the product with V
         l += __uint_as_float(pw[c][e] << 16) + __uint_as_float(pw[c][e] & 0xffff0000u);
@@ -527,7 +555,7 @@ __global__ __launch_bounds__(256) void window_rows_kernel(WinArgs a) {
 // rest a tile's softmax and barrier.  2 x 8 heads, 1500 x 1500: 103 us at 64 channels with 8 waves,
 // 117 with 4 (140 straight from memory), 213 and 213 at 128 (303); 8 heads of 64, 1501 queries on
 // 304 keys each 25.2 and 22.2 us (32.5); 8 of 128, 100 x 8000 63.9 and 56.4 (72).
-template <int D, int W, bool SPLIT>
+template <int D, int W, bool SPLIT, bool SCORED>
 __global__ __launch_bounds__(64 * W) void window_f32_tiles_kernel(WinArgs a) {
   static_assert(W == 4 || W == 8, "waves");
   constexpr int C = D / 16, TK = 64, SLOTS = W / 4, ROWS = 4 * W;
@@ -548,7 +576,7 @@ __global__ __launch_bounds__(64 * W) void window_f32_tiles_kernel(WinArgs a) {
   const int r0 = rb * ROWS;
   if (r0 >= rows) return;  // the whole workgroup
   auto range_of = [&](int r, int& lo, int& hi) {
-    win_range(a, seq, (int)a.by_n((uint32_t)min(r, rows - 1)), lo, hi);
+    win_seen<std::conditional_t<SCORED, WinScore<false, false>, WinPlain>>(a, seq, (int)a.by_n((uint32_t)min(r, rows - 1)), lo, hi);
     lo = __builtin_amdgcn_readfirstlane(lo);
     hi = __builtin_amdgcn_readfirstlane(hi);
   };
@@ -563,7 +591,7 @@ __global__ __launch_bounds__(64 * W) void window_f32_tiles_kernel(WinArgs a) {
   int wlo, whi, unused;
   range_of(wr0, wlo, unused);
   range_of(wr0 + 15, unused, whi);
-  if (tiles.sink == 0 && seq.sink >= lo1) wlo = 0;
+  if (!SCORED && tiles.sink == 0 && seq.sink >= lo1) wlo = 0;
   const bool live = wr0 < rows;
 
   const float* const kbase = (const float*)a.k + b * a.sk + (int64_t)h * D;
@@ -596,7 +624,7 @@ __global__ __launch_bounds__(64 * W) void window_f32_tiles_kernel(WinArgs a) {
     __builtin_amdgcn_s_barrier();
   };
 
-  WinF32<D> st;
+  WinF32<D, SCORED> st;
   st.template begin<true>(a, seq, tiles, lo1, h, wr0 + jq, rows);
   if (i0 < i1) {
     issue(tiles.key<TK>(i0), 0);
@@ -611,7 +639,7 @@ __global__ __launch_bounds__(64 * W) void window_f32_tiles_kernel(WinArgs a) {
         const uint8_t* const kt = smem + slot + (mine + jq) * (D * 4);
         const uint8_t* const vt = smem + slot + HALF + jq * (TK * 4) + ((((mine >> 2) + g) ^ (jq & 7)) << 4);
         st.step([&](int c) { return *(const f32x4*)(kt + (((4 * c + g) ^ (jq & 7)) << 4)); },
-                [&](int c) { return *(const f32x4*)(vt + 16 * c * (TK * 4)); }, edge, k0, seq.klen, a.scale_log2);
+                [&](int c) { return *(const f32x4*)(vt + 16 * c * (TK * 4)); }, edge, k0, seq.klen, a.scale_log2, &a);
       }
       barrier();
       if constexpr (SLOTS == 2) {
@@ -628,7 +656,7 @@ __global__ __launch_bounds__(64 * W) void window_f32_tiles_kernel(WinArgs a) {
 // Straight from memory: few rows or keys, and rows that are not 16-byte aligned (VEC false:
 // loads of single elements).  The four waves share a row block and take a fourth of its keys
 // each, 16 a step, the next step's under way.
-template <int D, bool VEC, bool SPLIT>
+template <int D, bool VEC, bool SPLIT, bool SCORED>
 __global__ __launch_bounds__(256) void window_f32_kernel(WinArgs a) {
   constexpr int C = D / 16, BKV = 16;
   __shared__ f32x4 so[4 * C * 64];
@@ -644,14 +672,15 @@ __global__ __launch_bounds__(256) void window_f32_kernel(WinArgs a) {
   if (r0 >= rows) return;  // the whole workgroup
 
   int lo0, hi0, lo1, hi1;
-  win_range(a, seq, (int)a.by_n((uint32_t)r0), lo0, hi0);
-  win_range(a, seq, (int)a.by_n((uint32_t)min(r0 + 15, rows - 1)), lo1, hi1);
+  typedef std::conditional_t<SCORED, WinScore<false, false>, WinPlain> S;
+  win_seen<S>(a, seq, (int)a.by_n((uint32_t)r0), lo0, hi0);
+  win_seen<S>(a, seq, (int)a.by_n((uint32_t)min(r0 + 15, rows - 1)), lo1, hi1);
   WinTiles tiles;
   tiles.init<BKV>(seq, __builtin_amdgcn_readfirstlane(lo0), __builtin_amdgcn_readfirstlane(hi0),
                   __builtin_amdgcn_readfirstlane(lo1), __builtin_amdgcn_readfirstlane(hi1));
   int i0, i1;
   win_share(tiles.n, (SPLIT ? sp * 4 : 0) + wave, SPLIT ? 4 * a.nsplit : 4, i0, i1);
-  WinF32<D> st;
+  WinF32<D, SCORED> st;
   st.template begin<VEC>(a, seq, tiles, lo1, h, r0 + jq, rows);
 
   const float* kb = (const float*)a.k + b * a.sk + (int64_t)h * D + 4 * g;
@@ -688,7 +717,7 @@ __global__ __launch_bounds__(256) void window_f32_kernel(WinArgs a) {
       load_v(k1, vn);
     }
     st.step([&](int c) { return kf[c]; }, [&](int c) { return vf[c]; }, idx < tiles.edge, tiles.key<BKV>(idx), seq.klen,
-            a.scale_log2);
+            a.scale_log2, &a);
     if (more) {
 #pragma unroll
       for (int c = 0; c < C; ++c) {
@@ -856,52 +885,65 @@ track_status win_check(const char* what, int dtype, const track_window* w, int B
   return TRACK_OK;
 }
 
-int64_t attention_window_bytes(int dtype, const track_window* w, int B, int H, int Hk, int D, int64_t Lq, int64_t Lk) {
-  if (win_check("attention_window", dtype, w, B, H, Hk, D, Lq, Lk) != TRACK_OK) return -1;
+static int64_t rows_bytes(const char* what, int dtype, const track_window* w, int B, int H, int Hk, int D, int64_t Lq, int64_t Lk) {
+  if (win_check(what, dtype, w, B, H, Hk, D, Lq, Lk) != TRACK_OK) return -1;
   if (B == 0 || Lq == 0) return 0;
   int64_t bytes = -1;
   for (bool vec : {true, false}) {  // whatever the rows' alignment turns out to be
     const WinPlan p = win_plan(dtype, *w, B, Hk, H / Hk, D, Lq, Lk, vec);
     if (win_fits(p, B, Hk, H / Hk, Lq)) bytes = std::max(bytes, (int64_t)win_bytes(p, B, Hk, H / Hk, D, Lq));
   }
-  if (bytes < 0) fail(TRACK_E_SHAPE, "attention_window: too many row blocks");
+  if (bytes < 0) fail(TRACK_E_SHAPE, "%s: too many row blocks", what);
   return bytes;
 }
 
-track_status attention_window(int dtype, const track_window* w, int B, int H, int Hk, int D, int64_t Lq, int64_t Lk,
-                              const void* q, int64_t ldq, int64_t sq, const void* k, int64_t ldk, int64_t sk,
-                              const void* vt, int64_t ldv, int64_t sv, void* out, int64_t ldo, int64_t so, float* lse,
-                              const int32_t* q_len, const int32_t* k_len, const int32_t* q_start, void* ws,
-                              size_t ws_bytes, hipStream_t s) {
-  const track_status st = win_check("attention_window", dtype, w, B, H, Hk, D, Lq, Lk);
+int64_t attention_window_bytes(int dtype, const track_window* w, int B, int H, int Hk, int D, int64_t Lq, int64_t Lk) {
+  return rows_bytes("attention_window", dtype, w, B, H, Hk, D, Lq, Lk);
+}
+
+// What attention_scores adds to a window.
+struct ScoreArgs {
+  double cap;
+  const float* slopes;
+  const int32_t *doc_end, *prefix;
+  int docs;
+};
+
+// One call of either kind (`c` null: a window's).
+static track_status attention_rows(const char* what, int dtype, const track_window* w, const ScoreArgs* c, int B, int H, int Hk,
+                                   int D, int64_t Lq, int64_t Lk, const void* q, int64_t ldq, int64_t sq, const void* k,
+                                   int64_t ldk, int64_t sk, const void* vt, int64_t ldv, int64_t sv, void* out, int64_t ldo,
+                                   int64_t so, float* lse, const int32_t* q_len, const int32_t* k_len, const int32_t* q_start,
+                                   void* ws, size_t ws_bytes, hipStream_t s) {
+  const track_status st = win_check(what, dtype, w, B, H, Hk, D, Lq, Lk);
   if (st != TRACK_OK) return st;
   if (B == 0 || Lq == 0) return TRACK_OK;
-  if (!q || !out || (Lk > 0 && (!k || !vt))) return fail(TRACK_E_INVALID, "attention_window: null pointer");
+  if (!q || !out || (Lk > 0 && (!k || !vt))) return fail(TRACK_E_INVALID, "%s: null pointer", what);
   const int n = H / Hk;
   if (ldq < (int64_t)H * D || ldo < (int64_t)H * D || ldk < (int64_t)Hk * D || ldv < Lk)
-    return fail(TRACK_E_SHAPE, "attention_window: leading dimension too small");
+    return fail(TRACK_E_SHAPE, "%s: leading dimension too small", what);
   if (sq < 0 || sk < 0 || sv < 0 || so < 0 || sequences_overlap(B, Lq, ldo, so, (int64_t)H * D))
-    return fail(TRACK_E_SHAPE, "attention_window: sequences overlap in out, or a negative stride");
+    return fail(TRACK_E_SHAPE, "%s: sequences overlap in out, or a negative stride", what);
   if (((uintptr_t)lse | (uintptr_t)q_len | (uintptr_t)k_len | (uintptr_t)q_start) & 3)
-    return fail(TRACK_E_INVALID, "attention_window: lse and lengths need 4-byte alignment");
+    return fail(TRACK_E_INVALID, "%s: lse and lengths need 4-byte alignment", what);
   // (offsets inside a tile and a head's V^T are 32 bits)
   if (ldk > ((int64_t)1 << 22) || ldv > ((int64_t)1 << 22))
-    return fail(TRACK_E_SHAPE, "attention_window: ldk and ldv are at most 2^22");
+    return fail(TRACK_E_SHAPE, "%s: ldk and ldv are at most 2^22", what);
   const uintptr_t ptrs = (uintptr_t)q | (uintptr_t)k | (uintptr_t)vt | (uintptr_t)out;
   const int64_t strides = ldq | ldk | ldv | ldo | (B > 1 ? sq | sk | sv | so : 0);
   bool vec = true;
   if (dtype == TRACK_DTYPE_BF16) {
-    if (ptrs & 15 || strides & 7) return fail(TRACK_E_INVALID, "attention_window: bf16 path needs 16-byte aligned rows");
+    if (ptrs & 15 || strides & 7) return fail(TRACK_E_INVALID, "%s: bf16 path needs 16-byte aligned rows", what);
   } else {
-    if (ptrs & 3) return fail(TRACK_E_INVALID, "attention_window: float32 path needs 4-byte aligned rows");
+    if (ptrs & 3) return fail(TRACK_E_INVALID, "%s: float32 path needs 4-byte aligned rows", what);
     vec = !(ptrs & 15) && !(strides & 3);
   }
   WinPlan p = win_plan(dtype, *w, B, Hk, n, D, Lq, Lk, vec);
-  if (!win_fits(p, B, Hk, n, Lq)) return fail(TRACK_E_SHAPE, "attention_window: too many row blocks");
+  if (!win_fits(p, B, Hk, n, Lq)) return fail(TRACK_E_SHAPE, "%s: too many row blocks", what);
   if (p.form == WinPlan::BLOCKS) p.nsplit = win_held(p.nsplit, B, Hk, n, D, Lq, ws, ws_bytes);
   const size_t need = win_bytes(p, B, Hk, n, D, Lq);
-  if (need && (!ws || ws_bytes < need)) return fail(TRACK_E_NOMEM, "attention_window: workspace of %zu bytes needed", need);
-  if (need && ((uintptr_t)ws & 255)) return fail(TRACK_E_INVALID, "attention_window: workspace must be 256-byte aligned");
+  if (need && (!ws || ws_bytes < need)) return fail(TRACK_E_NOMEM, "%s: workspace of %zu bytes needed", what, need);
+  if (need && ((uintptr_t)ws & 255)) return fail(TRACK_E_INVALID, "%s: workspace must be 256-byte aligned", what);
   const int64_t grid = p.nrb * p.nsplit * Hk * B, joined = (int64_t)B * H * Lq;
   WinArgs a = {};
   a.q = q, a.k = k, a.vt = vt, a.out = out;
@@ -916,33 +958,60 @@ track_status attention_window(int dtype, const track_window* w, int B, int H, in
   a.po = (float*)ws;
   a.pml = need ? (float2*)(a.po + (int64_t)p.nsplit * joined * D) : nullptr;
   const bool split = p.nsplit > 1, log2q = a.scale_log2 == 1.0f;
+  if (c) {
+    a.slopes = c->slopes, a.doc_end = c->doc_end, a.prefix = c->prefix, a.docs = c->docs;
+    const double scale = w->scale > 0.0 ? w->scale : 1.0 / sqrt((double)D), log2e = 1.4426950408889634;
+    a.cap_log2 = (float)(c->cap * log2e);
+    // the argument of exp2 in bfloat16 (exp(2 y)), of tanh in float32
+    a.cap_in = c->cap > 0.0 ? (float)(dtype == TRACK_DTYPE_BF16 ? 2.0 * log2e * scale / c->cap : scale / c->cap) : 0.0f;
+  }
   ProfScope prof(TRACK_PROF_ATTN_SELF, s);
   const unsigned gr = (unsigned)grid;
-#define TRACK_WIN_F32(DH)                                                                             \
-  do {                                                                                                \
-    if (p.form == WinPlan::F32_TILES8) window_f32_tiles_kernel<DH, 8, false><<<gr, 512, 0, s>>>(a);   \
-    else if (p.form == WinPlan::F32_TILES4 && split) window_f32_tiles_kernel<DH, 4, true><<<gr, 256, 0, s>>>(a); \
-    else if (p.form == WinPlan::F32_TILES4) window_f32_tiles_kernel<DH, 4, false><<<gr, 256, 0, s>>>(a); \
-    else if (vec && split) window_f32_kernel<DH, true, true><<<gr, 256, 0, s>>>(a);                   \
-    else if (vec) window_f32_kernel<DH, true, false><<<gr, 256, 0, s>>>(a);                           \
-    else if (split) window_f32_kernel<DH, false, true><<<gr, 256, 0, s>>>(a);                         \
-    else window_f32_kernel<DH, false, false><<<gr, 256, 0, s>>>(a);                                   \
+#define TRACK_WIN_F32_OF(DH, C)                                                                             \
+  do {                                                                                                      \
+    if (p.form == WinPlan::F32_TILES8) window_f32_tiles_kernel<DH, 8, false, C><<<gr, 512, 0, s>>>(a);      \
+    else if (p.form == WinPlan::F32_TILES4 && split) window_f32_tiles_kernel<DH, 4, true, C><<<gr, 256, 0, s>>>(a); \
+    else if (p.form == WinPlan::F32_TILES4) window_f32_tiles_kernel<DH, 4, false, C><<<gr, 256, 0, s>>>(a); \
+    else if (vec && split) window_f32_kernel<DH, true, true, C><<<gr, 256, 0, s>>>(a);                      \
+    else if (vec) window_f32_kernel<DH, true, false, C><<<gr, 256, 0, s>>>(a);                              \
+    else if (split) window_f32_kernel<DH, false, true, C><<<gr, 256, 0, s>>>(a);                            \
+    else window_f32_kernel<DH, false, false, C><<<gr, 256, 0, s>>>(a);                                      \
   } while (0)
+#define TRACK_WIN_F32(DH)              \
+  do {                                 \
+    if (c) TRACK_WIN_F32_OF(DH, true); \
+    else TRACK_WIN_F32_OF(DH, false);  \
+  } while (0)
+  auto blocks = [&](auto qlog2, auto score) {
+    typedef decltype(score) S;
+    if (split) window_blocks_kernel<decltype(qlog2)::value, true, S><<<gr, 512, 0, s>>>(a);
+    else window_blocks_kernel<decltype(qlog2)::value, false, S><<<gr, 512, 0, s>>>(a);
+  };
+  auto few = [&](auto score) {
+    typedef decltype(score) S;
+    if (B >= WIN_SHARED && sk == 0 && sv == 0) {
+      if (split) window_rows_kernel<true, false, S><<<gr, 256, 0, s>>>(a);
+      else window_rows_kernel<false, false, S><<<gr, 256, 0, s>>>(a);
+    } else {
+      if (split) window_rows_kernel<true, true, S><<<gr, 256, 0, s>>>(a);
+      else window_rows_kernel<false, true, S><<<gr, 256, 0, s>>>(a);
+    }
+  };
+  auto scored = [&](auto&& launch) {
+    if (a.cap_log2 > 0.0f && a.slopes) launch(WinScore<true, true>{});
+    else if (a.cap_log2 > 0.0f) launch(WinScore<true, false>{});
+    else if (a.slopes) launch(WinScore<false, true>{});
+    else launch(WinScore<false, false>{});
+  };
   switch (p.form) {
     case WinPlan::BLOCKS:
-      if (log2q && split) window_blocks_kernel<true, true><<<gr, 512, 0, s>>>(a);
-      else if (log2q) window_blocks_kernel<true, false><<<gr, 512, 0, s>>>(a);
-      else if (split) window_blocks_kernel<false, true><<<gr, 512, 0, s>>>(a);
-      else window_blocks_kernel<false, false><<<gr, 512, 0, s>>>(a);
+      if (c) scored([&](auto score) { blocks(std::true_type{}, score); });
+      else if (log2q) blocks(std::true_type{}, WinPlain{});
+      else blocks(std::false_type{}, WinPlain{});
       break;
     case WinPlan::ROWS:
-      if (B >= WIN_SHARED && sk == 0 && sv == 0) {
-        if (split) window_rows_kernel<true, false><<<gr, 256, 0, s>>>(a);
-        else window_rows_kernel<false, false><<<gr, 256, 0, s>>>(a);
-      } else {
-        if (split) window_rows_kernel<true, true><<<gr, 256, 0, s>>>(a);
-        else window_rows_kernel<false, true><<<gr, 256, 0, s>>>(a);
-      }
+      if (c) scored(few);
+      else few(WinPlain{});
       break;
     default:
       if (D == 32) TRACK_WIN_F32(32);
@@ -950,12 +1019,52 @@ track_status attention_window(int dtype, const track_window* w, int B, int H, in
       else TRACK_WIN_F32(128);
   }
 #undef TRACK_WIN_F32
+#undef TRACK_WIN_F32_OF
   TRACK_LAUNCH_CHECK();
   if (split) {
     window_join(dtype, a, D, s);
     TRACK_LAUNCH_CHECK();
   }
   return TRACK_OK;
+}
+
+track_status attention_window(int dtype, const track_window* w, int B, int H, int Hk, int D, int64_t Lq, int64_t Lk,
+                              const void* q, int64_t ldq, int64_t sq, const void* k, int64_t ldk, int64_t sk,
+                              const void* vt, int64_t ldv, int64_t sv, void* out, int64_t ldo, int64_t so, float* lse,
+                              const int32_t* q_len, const int32_t* k_len, const int32_t* q_start, void* ws,
+                              size_t ws_bytes, hipStream_t s) {
+  return attention_rows("attention_window", dtype, w, nullptr, B, H, Hk, D, Lq, Lk, q, ldq, sq, k, ldk, sk, vt, ldv, sv, out,
+                        ldo, so, lse, q_len, k_len, q_start, ws, ws_bytes, s);
+}
+
+static track_status scores_window(const track_scores* c, track_window* w) {
+  if (!c) return fail(TRACK_E_INVALID, "attention_scores: null scores");
+  if (!(c->cap == 0.0 || (c->cap >= 1e-3 && c->cap <= 1e3))) return fail(TRACK_E_INVALID, "attention_scores: cap %g", c->cap);
+  *w = track_window{c->left, c->right, 0, c->group, c->scale};
+  return TRACK_OK;
+}
+
+int64_t attention_scores_bytes(int dtype, const track_scores* c, int B, int H, int Hk, int D, int64_t Lq, int64_t Lk) {
+  track_window w;
+  return scores_window(c, &w) == TRACK_OK ? rows_bytes("attention_scores", dtype, &w, B, H, Hk, D, Lq, Lk) : -1;
+}
+
+track_status attention_scores(int dtype, const track_scores* c, int B, int H, int Hk, int D, int64_t Lq, int64_t Lk,
+                              const void* q, int64_t ldq, int64_t sq, const void* k, int64_t ldk, int64_t sk,
+                              const void* vt, int64_t ldv, int64_t sv, void* out, int64_t ldo, int64_t so, float* lse,
+                              const float* slopes, const int32_t* doc_end, int docs, const int32_t* prefix,
+                              const int32_t* q_len, const int32_t* k_len, const int32_t* q_start, void* ws,
+                              size_t ws_bytes, hipStream_t s) {
+  track_window w;
+  const track_status st = scores_window(c, &w);
+  if (st != TRACK_OK) return st;
+  if (docs < 0 || docs > SCORES_DOCS) return fail(TRACK_E_SHAPE, "attention_scores: %d documents (2^20 at most)", docs);
+  if (docs > 0 && !doc_end && B > 0) return fail(TRACK_E_INVALID, "attention_scores: null pointer");
+  if (((uintptr_t)slopes | (uintptr_t)doc_end | (uintptr_t)prefix) & 3)
+    return fail(TRACK_E_INVALID, "attention_scores: slopes, documents and prefixes need 4-byte alignment");
+  const ScoreArgs args = {c->cap, slopes, doc_end, prefix, docs};
+  return attention_rows("attention_scores", dtype, &w, &args, B, H, Hk, D, Lq, Lk, q, ldq, sq, k, ldk, sk, vt, ldv, sv, out, ldo,
+                        so, lse, q_len, k_len, q_start, ws, ws_bytes, s);
 }
 
 }  // namespace track

@@ -34,7 +34,8 @@ EXPORTS = [
     "track_op_step", "track_op_step_noalloc", "track_hbm_stream", "track_mfma_stream", "track_unipc_coefficients", "track_op_unipc_step", "track_profile_enable", "track_profile_reset", "track_profile_read", "track_set_progress",
     "track_rope_freqs", "track_op_rope", "track_op_headnorm_rope", "track_attention_window_workspace_bytes",
     "track_op_attention_window", "track_cache4_page_bytes", "track_op_cache4_append", "track_op_cache4_read",
-    "track_attention_cache4_workspace_bytes", "track_op_attention_cache4",
+    "track_attention_cache4_workspace_bytes", "track_op_attention_cache4", "track_attention_scores_workspace_bytes",
+    "track_op_attention_scores",
 ]
 
 
@@ -73,6 +74,10 @@ class HeadRowsC(ctypes.Structure):
 
 class WindowC(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int64) for n in ("left", "right", "sink", "group")] + [("scale", ctypes.c_double)]
+
+
+class ScoresC(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int64) for n in ("left", "right", "group")] + [(n, ctypes.c_double) for n in ("scale", "cap")]
 
 
 class Cache4C(ctypes.Structure):
@@ -134,6 +139,9 @@ def _declare(L):
         "track_attention_window_workspace_bytes": (_i64, [_i32, P(WindowC), _i32, _i32, _i32, _i32, _i64, _i64]),
         "track_op_attention_window": (_i32, [_i32, P(WindowC), _i32, _i32, _i32, _i32, _i64, _i64] +
                                       [_vp, _i64, _i64] * 4 + [_vp] * 5 + [_sz, _vp]),
+        "track_attention_scores_workspace_bytes": (_i64, [_i32, P(ScoresC), _i32, _i32, _i32, _i32, _i64, _i64]),
+        "track_op_attention_scores": (_i32, [_i32, P(ScoresC), _i32, _i32, _i32, _i32, _i64, _i64] +
+                                      [_vp, _i64, _i64] * 4 + [_vp, _vp, _vp, _i32] + [_vp] * 5 + [_sz, _vp]),
         "track_cache4_page_bytes": (_i64, [_i32, _i32, _i32]),
         "track_op_cache4_append": (_i32, [_i32, P(Cache4C), P(RopeConfigC), _i64, _i64] + [_vp, _i64, _i64] * 2 +
                                    [_vp, _vp, _vp, _vp, _f32, _vp]),
@@ -746,6 +754,76 @@ def op_attention_window(window: Window, q, k, vt, out, lse=None, q_len=None, k_l
     _on_device(lib().track_op_attention_window, q, dtype, window.c(), B, H, Hk, D, Lq, Lk, q.data_ptr(), ldq, sq,
                k.data_ptr(), ldk, sk, vt.data_ptr(), ldv, sv, out.data_ptr(), ldo, so,
                *[0 if t is None else t.data_ptr() for t in (lse, q_len, k_len, q_start, workspace)], nbytes)
+    return out
+
+
+@dataclasses.dataclass(frozen=True)
+class Scores:
+    """What a query sees and what becomes of its logits (track_scores)."""
+    left: int = -1
+    right: int = 0
+    group: int = 1
+    scale: Optional[float] = None  # 1 / sqrt(head_dim)
+    cap: float = 0.0               # none
+
+    def __post_init__(self):
+        if self.scale == 0.0:  # the library's mark for 1 / sqrt(head_dim), which is None here
+            raise ValueError("scores: a scale of 0")
+        object.__setattr__(self, "_c", ScoresC(self.left, self.right, self.group,
+                                               0.0 if self.scale is None else self.scale, self.cap))
+
+    def c(self) -> ScoresC:
+        return self._c
+
+
+def attention_scores_workspace_bytes(scores: Scores, dtype: int, B: int, H: int, Hk: int, head_dim: int, Lq: int,
+                                     Lk: int) -> int:
+    n = lib().track_attention_scores_workspace_bytes(dtype, scores.c(), B, H, Hk, head_dim, Lq, Lk)
+    if n < 0:
+        raise TrackError(E_INVALID, lib().track_last_error().decode())
+    return n
+
+
+def attention_scores_workspace(scores: Scores, q, k):
+    """The workspace of op_attention_scores on tensors of these shapes (None where it needs none); it serves calls of the
+    same q on fewer keys too."""
+    torch = _torch()
+    with torch.cuda.device(q.device):
+        n = attention_scores_workspace_bytes(scores, _float_dtype(q), q.shape[0], q.shape[2], k.shape[2], q.shape[3],
+                                             q.shape[1], k.shape[1])
+        return torch.empty(n, dtype=torch.uint8, device=q.device) if n else None
+
+
+_scores_layouts: dict = {}
+
+
+def _check_scores(q, k, vt, out, lse, q_len, k_len, q_start, workspace, slopes, doc_end, prefix):
+    got = _check_window(q, k, vt, out, lse, q_len, k_len, q_start, workspace)
+    B, _, H, _ = q.shape
+    if slopes is not None and (str(slopes.dtype) != "torch.float32" or slopes.shape != (H,) or
+                               not slopes.is_contiguous() or slopes.get_device() != q.get_device()):
+        raise ValueError(f"slopes: contiguous float32 [{H}] on {q.device} expected")
+    docs = 0
+    if doc_end is not None:
+        if doc_end.dim() != 2:
+            raise ValueError("doc_end: [sequences, documents] expected")
+        docs = doc_end.shape[1]
+        _ints(doc_end, (B, docs), q, "doc_end")
+    _ints(prefix, (B, docs + 1), q, "prefix")
+    return got, docs
+
+
+def op_attention_scores(scores: Scores, q, k, vt, out, lse=None, slopes=None, doc_end=None, prefix=None, q_len=None,
+                        k_len=None, q_start=None, workspace=None):
+    """op_attention_window's call with capped logits, less slopes[h] (float32 [H]) times the distance in tokens, inside
+    documents that end at doc_end (int32 [B, documents], ascending) and whose first prefix[b, d] tokens (int32
+    [B, documents + 1]) all of their tokens see; returns out."""
+    (dtype, B, H, Hk, D, Lq, Lk, ldq, sq, ldk, sk, ldv, sv, ldo, so, nbytes), docs = _layout(
+        _scores_layouts, (q, k, vt, out, lse, q_len, k_len, q_start, workspace, slopes, doc_end, prefix), _check_scores)
+    _on_device(lib().track_op_attention_scores, q, dtype, scores.c(), B, H, Hk, D, Lq, Lk, q.data_ptr(), ldq, sq,
+               k.data_ptr(), ldk, sk, vt.data_ptr(), ldv, sv, out.data_ptr(), ldo, so,
+               *[0 if t is None else t.data_ptr() for t in (lse, slopes, doc_end)], docs,
+               *[0 if t is None else t.data_ptr() for t in (prefix, q_len, k_len, q_start, workspace)], nbytes)
     return out
 
 
