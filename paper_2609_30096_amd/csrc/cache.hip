@@ -57,6 +57,14 @@ __device__ __forceinline__ int c4_exponent(float m) {
   return x == 128 ? 255 : 127 + min(max(e, C4_MIN), C4_MAX);
 }
 
+// Eight channels' codes at scale 2^e, given as its float (exact for float32 values: the conversion rounds once, ties to the even code).
+__device__ __forceinline__ uint32_t c4_codes(const float (&x)[8], float s) {
+  uint32_t w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(0, x[0], x[1], s, 0);
+  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[2], x[3], s, 1);
+  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[4], x[5], s, 2);
+  return __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[6], x[7], s, 3);
+}
+
 // The code of x at the power of two whose reciprocal is given, ties to the even code (x is finite).
 __device__ __forceinline__ uint32_t c4_code(double x, double inv) {
   const double y = fabs(x) * inv;  // exact
@@ -64,38 +72,40 @@ __device__ __forceinline__ uint32_t c4_code(double x, double inv) {
   const double q = rint(y * f) + (y < 2.0 ? 0.0 : (y < 4.0 ? 2.0 : 4.0));
   return (uint32_t)fmin(q, 7.0) | ((uint32_t)(__builtin_bit_cast(uint64_t, x) >> 60) & 8u);
 }
-__device__ __forceinline__ uint32_t c4_code(float x, float inv) {
-  const float y = fabsf(x) * inv;
-  const float f = y < 2.0f ? 2.0f : (y < 4.0f ? 1.0f : 0.5f);
-  const float q = rintf(y * f) + (y < 2.0f ? 0.0f : (y < 4.0f ? 2.0f : 4.0f));
-  return (uint32_t)fminf(q, 7.0f) | ((__float_as_uint(x) >> 28) & 8u);
+
+// The largest of four lanes beside each other.
+__device__ __forceinline__ uint32_t c4_quad_max(uint32_t v) {
+  v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0xb1, 0xf, 0xf, true));  // quad_perm [1, 0, 3, 2]
+  return max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x4e, 0xf, 0xf, true));  // quad_perm [2, 3, 0, 1]
 }
 
-// 2^(127 - byte).
-__device__ __forceinline__ float c4_inverse(int byte, float) { return __uint_as_float((uint32_t)(254 - byte) << 23); }
-__device__ __forceinline__ double c4_inverse(int byte, double) {
-  return __builtin_bit_cast(double, (uint64_t)(1023 + 127 - byte) << 52);
+// The largest magnitude of a lane's 8 values, as bits (an infinity or a NaN is above all numbers).
+__device__ __forceinline__ uint32_t c4_top(const float (&x)[8]) {
+  uint32_t m = 0;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) m = max(m, __float_as_uint(x[i]) & 0x7fffffffu);
+  return m;
 }
 
 // Four bytes of codes of the lane's 8 channels, and the exponent byte of the group that they and those of the 3 lanes beside it make.
-template <typename F>
-__device__ __forceinline__ uint32_t c4_round8(const F (&x)[8], int& byte) {
-  constexpr F most = sizeof(F) == 4 ? (F)3.4028234663852886e38 : (F)1.7976931348623157e308;
-  F m = fabs(x[0]);
-  bool odd = !(m <= most);  // an infinity or a NaN
+__device__ __forceinline__ uint32_t c4_round8(const float (&x)[8], int& byte) {
+  byte = c4_exponent(__uint_as_float(c4_quad_max(c4_top(x))));
+  const uint32_t w = c4_codes(x, __uint_as_float((uint32_t)byte << 23));
+  return byte == 255 ? 0 : w;
+}
+__device__ __forceinline__ uint32_t c4_round8(const double (&x)[8], int& byte) {
+  double m = fabs(x[0]);
+  bool odd = !(m <= 1.7976931348623157e308);  // an infinity or a NaN
 #pragma unroll
   for (int i = 1; i < 8; ++i) {
-    const F a = fabs(x[i]);
-    odd |= !(a <= most);
+    const double a = fabs(x[i]);
+    odd |= !(a <= 1.7976931348623157e308);
     m = fmax(m, a);
   }
-  int e = odd ? 255 : c4_exponent(m);
   // the largest exponent of the four lanes is that of the largest magnitude
-  e = max(e, __builtin_amdgcn_update_dpp(0, e, 0xb1, 0xf, 0xf, true));  // quad_perm [1, 0, 3, 2]
-  e = max(e, __builtin_amdgcn_update_dpp(0, e, 0x4e, 0xf, 0xf, true));  // quad_perm [2, 3, 0, 1]
-  byte = e;
-  if (e == 255) return 0;
-  const F inv = c4_inverse(e, F());
+  byte = (int)c4_quad_max((uint32_t)(odd ? 255 : c4_exponent(m)));
+  if (byte == 255) return 0;
+  const double inv = __builtin_bit_cast(double, (uint64_t)(1023 + 127 - byte) << 52);
   uint32_t w = 0;
 #pragma unroll
   for (int i = 0; i < 8; ++i) w |= c4_code(x[i], inv) << (4 * i);
@@ -109,7 +119,7 @@ struct RowsArgs {
   int64_t ldk, sk, ldv, sv;
   const int32_t *start, *n;
   int B, L, heads, nblk;  // 64-token blocks that a sequence's rows can touch
-  int hsplit;             // workgroups that share a block's heads
+  int hsplit;             // workgroups that share 16 tokens' heads
   bool vec;               // 16-byte aligned rows
   // rotation
   const int32_t* pos;
@@ -118,18 +128,19 @@ struct RowsArgs {
   int pairs, sec0, sec1;
 };
 
-// The 16 tokens of a wave in a block of 64: slot 8 s + c is token 32 s + 8 r + c, wave r.
-struct RowsWave {
+// The 16 tokens of a workgroup in a block of 64: slot 8 s + c is token 32 s + 8 r + c, r the quarter.  All wave-uniform.
+struct RowsPart {
   int b, r, first;       // place of the block's first token, less the sequence's start
   int n;                 // rows of the sequence
   uint32_t there;        // slots that hold a row of the call, in a place that the cache has
   template <int D>
   __device__ __forceinline__ uint8_t* init(const RowsArgs& a, int item) {
-    b = item / a.nblk;
-    r = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    r = item & 3;
+    const int blk = item >> 2;
+    b = blk / a.nblk;
     n = a.n ? __builtin_amdgcn_readfirstlane(max(0, min(a.n[b], a.L))) : a.L;
     const int start = __builtin_amdgcn_readfirstlane(max(-(int)WIN_MAX, min(a.start[b], (int)WIN_MAX)));
-    const int t = (start >> 6) + item % a.nblk;
+    const int t = (start >> 6) + (blk - b * a.nblk);
     first = t * C4_BLOCK - start;
     there = 0;
     if (t < 0 || t * (int64_t)C4_BLOCK >= a.c.cap) return nullptr;
@@ -144,133 +155,196 @@ struct RowsWave {
   __device__ __forceinline__ int row(int slot) const { return first + token(slot); }
 };
 
+// A lane's 8 channels as they lie in memory.
 template <typename T>
-__device__ __forceinline__ void c4_load8(const T* p, bool vec, float (&x)[8]) {
-  if (!vec) {
+struct C4Unit {
+  u32x4 w[sizeof(T) / 2];
+  __device__ __forceinline__ void load(const T* p, bool vec) {
+    if (vec) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = ldf(p + i);
-  } else if constexpr (sizeof(T) == 2) {
-    const u32x4 w = *(const u32x4*)p;
+      for (int i = 0; i < (int)sizeof(T) / 2; ++i) w[i] = ((const u32x4*)p)[i];
+    } else if constexpr (sizeof(T) == 2) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      x[2 * i] = __uint_as_float(w[i] << 16);
-      x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+      for (int i = 0; i < 4; ++i) w[0][i] = (uint32_t)p[2 * i] | (uint32_t)p[2 * i + 1] << 16;
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) w[i >> 2][i & 3] = __float_as_uint(p[i]);
     }
-  } else {
-    const f32x4 a = *(const f32x4*)p, b = *(const f32x4*)(p + 4);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) x[i] = a[i], x[4 + i] = b[i];
   }
+  __device__ __forceinline__ void get(float (&x)[8]) const {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      if constexpr (sizeof(T) == 2) x[i] = __uint_as_float(i & 1 ? w[0][i >> 1] & 0xffff0000u : w[0][i >> 1] << 16);
+      else x[i] = __uint_as_float(w[i >> 2][i & 3]);
+    }
+  }
+};
+
+// The wave's own LDS writes, before its reads.
+__device__ __forceinline__ void c4_settle() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
 }
 
-// Appends.  A wave takes 16 tokens of a block and walks its heads; a lane has 8 channels of a token, D / 8 lanes a
-// token.  Angles are formed once for all heads, in float64 as the products behind them are: a key next to the border of
-// two codes would otherwise fall to one or the other by how float32 rounds (about one in 10^6, each a whole step off).
-// V's codes change places through LDS (a lane of the output has two channels of 16 tokens).
+// Appends.  A workgroup takes 16 tokens of a block, forms their angles once, and its waves walk the heads; a lane has 8 channels of a
+// token, D / 8 lanes a token.  Codes and exponents change places through LDS into the order of the cache, and leave in 16-byte units.
+// A key is what its rotation in float64 rounds to: next to the border of two codes float32 would fall to either (one in some 10^6, a whole
+// step off).  The rotation is float32 all the same: it is off by at most 4e-7 of the pair's length (angle reduced in float64 and
+// rounded once, sine and cosine 2 units, two products and a sum), below D = 2^-20 of the largest value that goes into the lane's group, and where x - D and x + D
+// round to the same code, and the group's largest value to the same exponent, that is the key's.  Elsewhere (one wave's step in a hundred) the wave takes the step
+// again in float64.
 template <typename T, int D, int ROT>
 __global__ __launch_bounds__(256) void cache_append_kernel(RowsArgs a) {
-  constexpr int LPT = D / 8, TPS = 64 / LPT, STEPS = 16 / TPS;
-  __shared__ double cs[ROT ? 4 : 1][ROT ? 16 * (D / 2) : 1][2];
-  __shared__ uint32_t codes[4][16 * (D / 8)];
+  constexpr int LPT = D / 8, TPS = 64 / LPT, STEPS = 16 / TPS, G = D / 32;
+  __shared__ float2 cs[ROT ? 16 * (D / 2) : 1];
+  __shared__ __attribute__((aligned(16))) uint32_t kcodes[4][16 * LPT], vcodes[4][16 * LPT];
+  __shared__ __attribute__((aligned(16))) uint8_t kexp[4][16 * G], vexp[4][16 * G];  // in the cache's order
   const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   const int item = (int)blockIdx.x / a.hsplit, part = (int)blockIdx.x - item * a.hsplit;
-  RowsWave w;
+  RowsPart w;
   uint8_t* const block = w.init<D>(a, item);
-  if (!block) return;  // the wave has no barrier below
-  if constexpr (ROT != 0) {
-    for (int s = 0; s < 16; ++s) {
-      if (!(w.there >> s & 1)) continue;
-      for (int p = lane; p < a.pairs; p += 64) {
-        const int axis = (p >= a.sec0) + (p >= a.sec1);
-        const double turns = (double)a.pos[((int64_t)axis * a.B + w.b) * a.L + w.row(s)] * (a.freqs[p] * 0.15915494309189533577);
-        double sn, cn;
-        sincospi(2.0 * (turns - rint(turns)), &sn, &cn);
-        cs[w.r][s * (D / 2) + p][0] = cn * a.amp;
-        cs[w.r][s * (D / 2) + p][1] = sn * a.amp;
-      }
-    }
-  }
-  auto settle = [&]() {  // the wave's own LDS writes, before its reads
-    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-  };
-  settle();
+  if (!block) return;  // the whole workgroup
   const int u = lane % LPT, sub = lane / LPT;
-  const bool all = w.there == 0xffff;
-  for (int h = part; h < a.heads; h += a.hsplit) {
-    uint8_t* const to = block + (int64_t)h * C4<D>::BYTES;
+  int h = part * 4 + wave;
+  C4Unit<T> rk[STEPS], rz[ROT == 2 ? STEPS : 1], rv[STEPS];
+  // where the other channels of the lane's pairs lie (half layout), if they are a unit
+  const bool whole = ROT == 2 && a.vec && (a.pairs & 7) == 0;
+  const int other = 8 * u < a.pairs ? a.pairs : (8 * u < 2 * a.pairs ? -a.pairs : 0);
+  auto key_row = [&](int st, int hh) {
+    const int slot = st * TPS + sub;
+    const int64_t row = w.there >> slot & 1 ? w.row(slot) : 0;  // (any row of the sequence in a slot without one)
+    return (const T*)a.k + w.b * a.sk + row * a.ldk + (int64_t)hh * D;
+  };
+  auto load = [&](int hh) {
 #pragma unroll
     for (int st = 0; st < STEPS; ++st) {
-      const int slot = st * TPS + sub, tok = w.token(slot);
-      const bool there = w.there >> slot & 1;
-      const int64_t row = there ? w.row(slot) : 0;
-      // keys
-      const T* const kp = (const T*)a.k + w.b * a.sk + row * a.ldk + (int64_t)h * D;
+      const int slot = st * TPS + sub;
+      const int64_t row = w.there >> slot & 1 ? w.row(slot) : 0;
+      const T* const kp = key_row(st, hh);
+      rk[st].load(kp + 8 * u, a.vec);
+      if constexpr (ROT == 2)
+        if (whole) rz[st].load(kp + 8 * u + other, true);
+      rv[st].load((const T*)a.v + w.b * a.sv + row * a.ldv + (int64_t)hh * D + 8 * u, a.vec);
+    }
+  };
+  if (h < a.heads) load(h);
+  auto turns_of = [&](int slot, int p) {
+    const int axis = (p >= a.sec0) + (p >= a.sec1);
+    const double t = (double)a.pos[((int64_t)axis * a.B + w.b) * a.L + w.row(slot)] * (a.freqs[p] * 0.15915494309189533577);
+    return 2.0 * (t - rint(t));
+  };
+  if constexpr (ROT != 0) {
+    for (int i = threadIdx.x; i < 16 * (D / 2); i += 256) {
+      const int slot = i / (D / 2), p = i % (D / 2);
+      float sn = 0.0f, cn = 1.0f;  // copied channels
+      if (p < a.pairs && (w.there >> slot & 1)) {
+        sincospif((float)turns_of(slot, p), &sn, &cn);
+        sn *= (float)a.amp, cn *= (float)a.amp;
+      }
+      cs[i] = float2{cn, sn};
+    }
+    __syncthreads();
+  }
+  // the lane's pair of channel i of its unit, and whether the channel is the pair's first
+  auto pair_of = [&](int i, bool& low) {
+    if constexpr (ROT == 1) {
+      low = !(i & 1);
+      return 4 * u + (i >> 1);
+    } else {
+      const int ch = 8 * u + i;
+      low = ch < a.pairs;
+      return low ? ch : ch - a.pairs;
+    }
+  };
+  const bool all = w.there == 0xffff;
+  for (; h < a.heads; h += 4 * a.hsplit) {
+    uint8_t* const to = block + (int64_t)h * C4<D>::BYTES;
+    C4Unit<T> ck[STEPS], cz[ROT == 2 ? STEPS : 1], cv[STEPS];
+#pragma unroll
+    for (int st = 0; st < STEPS; ++st) {
+      ck[st] = rk[st], cv[st] = rv[st];
+      if constexpr (ROT == 2) cz[st] = rz[st];
+    }
+    if (h + 4 * a.hsplit < a.heads) load(h + 4 * a.hsplit);  // under way while this head is computed on
+#pragma unroll
+    for (int st = 0; st < STEPS; ++st) {
+      const int slot = st * TPS + sub;
+      // the exponent's place in the cache's order: K [4 c][G][2 s][2 h], V [G][2 s][8 c]
+      const int c = slot & 7, ke = (c & 3) * (4 * G) + 4 * (u >> 2) + 2 * (slot >> 3) + (c >> 2), ve = 16 * (u >> 2) + slot;
       float x[8];
-      c4_load8(kp + 8 * u, a.vec, x);
       uint32_t word;
       int byte;
+      ck[st].get(x);
       if constexpr (ROT == 0) {
         word = c4_round8(x, byte);
       } else {
-        double y[8];
-        const double(*const at)[2] = &cs[w.r][slot * (D / 2)];
+        float z[8];  // the other channel of each one's pair
         if constexpr (ROT == 1) {
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const int p = 4 * u + i;
-            if (p < a.pairs) {
-              const double c = at[p][0], s = at[p][1];
-              y[2 * i] = x[2 * i] * c - x[2 * i + 1] * s;
-              y[2 * i + 1] = x[2 * i] * s + x[2 * i + 1] * c;
-            } else {
-              y[2 * i] = x[2 * i];
-              y[2 * i + 1] = x[2 * i + 1];
-            }
-          }
+          for (int i = 0; i < 8; ++i) z[i] = x[i ^ 1];
+        } else if (whole) {
+          cz[st].get(z);
         } else {
-          float z[8];  // the other channel of each one's pair
-          if (a.vec && (a.pairs & 7) == 0) {
-            const int o = 8 * u < a.pairs ? a.pairs : (8 * u < 2 * a.pairs ? -a.pairs : 0);
-            c4_load8(kp + 8 * u + o, true, z);
-          } else {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-              const int ch = 8 * u + i;
-              z[i] = ldf(kp + (ch < a.pairs ? ch + a.pairs : (ch < 2 * a.pairs ? ch - a.pairs : ch)));
-            }
-          }
+          const T* const kp = key_row(st, h);
 #pragma unroll
           for (int i = 0; i < 8; ++i) {
             const int ch = 8 * u + i;
-            if (ch < 2 * a.pairs) {
-              const bool low = ch < a.pairs;
-              const int p = low ? ch : ch - a.pairs;
-              const double c = at[p][0], s = at[p][1];
-              y[i] = low ? x[i] * c - z[i] * s : z[i] * s + x[i] * c;
-            } else {
-              y[i] = x[i];
-            }
+            z[i] = ldf(kp + (ch < a.pairs ? ch + a.pairs : (ch < 2 * a.pairs ? ch - a.pairs : ch)));
           }
         }
-        word = c4_round8(y, byte);
+        float y[8], lo[8], hi[8];
+        const float2* const at = cs + slot * (D / 2);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          bool low;
+          const int p = pair_of(i, low);
+          const float2 t = p < a.pairs ? at[p] : float2{1.0f, 0.0f};
+          const float sn = p < a.pairs && low ? -t.y : t.y;
+          y[i] = p < a.pairs ? fmaf(x[i], t.x, z[i] * sn) : x[i];
+        }
+        const uint32_t in = c4_quad_max(max(c4_top(x), c4_top(z)));
+        const float off = __uint_as_float(in) * (9.5367431640625e-7f * fabsf((float)a.amp));
+#pragma unroll
+        for (int i = 0; i < 8; ++i) lo[i] = y[i] - off, hi[i] = y[i] + off;
+        const float top = __uint_as_float(c4_quad_max(c4_top(y)));
+        byte = c4_exponent(top + off);
+        const float s = __uint_as_float((uint32_t)byte << 23);
+        word = c4_codes(lo, s);
+        const uint32_t differ = word ^ c4_codes(hi, s);
+        const bool near = byte != c4_exponent(fmaxf(top - off, 0.0f)) || byte == 255 || (differ != 0 && in != 0);
+        if (__ballot(near)) {
+          const T* const kp = key_row(st, h);
+          double r[8];
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            bool low;
+            const int p = pair_of(i, low);
+            r[i] = x[i];
+            if (p < a.pairs) {
+              double sn = 0.0, cn = 1.0;
+              if (w.there >> slot & 1) sincospi(turns_of(slot, p), &sn, &cn);
+              sn *= a.amp, cn *= a.amp;
+              r[i] = low ? x[i] * cn - z[i] * sn : z[i] * sn + x[i] * cn;
+            }
+          }
+          word = c4_round8(r, byte);
+        }
       }
-      if (there) {
-        *(uint32_t*)(to + C4<D>::k_code(tok, 8 * u)) = word;
-        if ((u & 3) == 0) to[C4<D>::k_exp(tok, u >> 2)] = (uint8_t)byte;
-      }
-      // values
-      const T* const vp = (const T*)a.v + w.b * a.sv + row * a.ldv + (int64_t)h * D;
-      c4_load8(vp + 8 * u, a.vec, x);
-      word = c4_round8(x, byte);
-      codes[w.r][slot * LPT + u] = word;
-      if (there && (u & 3) == 0) to[C4<D>::v_exp(tok, u >> 2)] = (uint8_t)byte;
+      kcodes[wave][slot * LPT + u] = word;
+      if ((u & 3) == 0) kexp[wave][ke] = (uint8_t)byte;
+      cv[st].get(x);
+      vcodes[wave][slot * LPT + u] = c4_round8(x, byte);
+      if ((u & 3) == 0) vexp[wave][ve] = (uint8_t)byte;
     }
-    settle();
+    c4_settle();
     if (lane < D / 2) {
-      // lane: group lane / 16, byte lane % 16 of a group's 16
-      const uint8_t* const from = (const uint8_t*)codes[w.r] + lane;
+      // K: 16 bytes of one token; V: group lane / 16, byte lane % 16 of a group's 16, of the 16 tokens
+      const int slot = lane / G;
+      if (w.there >> slot & 1)
+        *(u32x4*)(to + C4<D>::k_code(w.token(slot), 32 * (lane % G))) = *(const u32x4*)&kcodes[wave][4 * lane];
+      const uint8_t* const from = (const uint8_t*)vcodes[wave] + lane;
       uint8_t* const vt = to + C4<D>::v_code(8 * w.r, 2 * lane);
       if (all) {
         u32x4 o;
@@ -284,7 +358,18 @@ __global__ __launch_bounds__(256) void cache_append_kernel(RowsArgs a) {
           if (w.there >> s & 1) vt[s] = from[s * (D / 2)];
       }
     }
-    settle();
+    if (all) {
+      const int i = lane & (4 * G - 1);  // G words of 4 exponents for each of 4 c, or of 4 runs of 4 tokens for each group
+      if (lane < 4 * G) *(uint32_t*)(to + C4<D>::k_exp(8 * w.r, 0) + 4 * i) = ((const uint32_t*)kexp[wave])[i];
+      else if (lane < 8 * G) *(uint32_t*)(to + C4<D>::v_exp(8 * w.r, i >> 2) + 4 * (i & 3)) = ((const uint32_t*)vexp[wave])[i];
+    } else if (lane < 16 * G) {
+      const int slot = lane & 15, grp = lane >> 4, c = slot & 7;
+      if (w.there >> slot & 1) {
+        to[C4<D>::k_exp(w.token(slot), grp)] = kexp[wave][(c & 3) * (4 * G) + 4 * grp + 2 * (slot >> 3) + (c >> 2)];
+        to[C4<D>::v_exp(w.token(slot), grp)] = vexp[wave][lane];
+      }
+    }
+    c4_settle();
   }
 }
 
@@ -339,11 +424,12 @@ __device__ __forceinline__ void c4_store8(T* p, bool vec, uint32_t w, float s) {
 // Rows out of the cache: the append's shape the other way round.  Places without a page read as zero.
 template <typename T, int D>
 __global__ __launch_bounds__(256) void cache_read_kernel(RowsArgs a) {
-  constexpr int LPT = D / 8, TPS = 64 / LPT, STEPS = 16 / TPS;
+  constexpr int LPT = D / 8, TPS = 64 / LPT, STEPS = 16 / TPS, G = D / 32;
   __shared__ u32x4 codes[4][D / 2];
   const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   const int item = (int)blockIdx.x / a.hsplit, part = (int)blockIdx.x - item * a.hsplit;
-  RowsWave w;
+  RowsPart w;
   const uint8_t* const block = w.init<D>(a, item);
   const int u = lane % LPT, sub = lane / LPT;
   if (!block) {  // rows in places that the cache does not have
@@ -351,22 +437,17 @@ __global__ __launch_bounds__(256) void cache_read_kernel(RowsArgs a) {
     for (int st = 0; st < STEPS; ++st) {
       const int row = w.row(st * TPS + sub);
       if (row < 0 || row >= w.n) continue;
-      for (int h = part; h < a.heads; h += a.hsplit) {
+      for (int h = part * 4 + wave; h < a.heads; h += 4 * a.hsplit) {
         c4_store8((T*)a.k + w.b * a.sk + (int64_t)row * a.ldk + (int64_t)h * D + 8 * u, a.vec, 0, 1.0f);
         c4_store8((T*)a.v + w.b * a.sv + (int64_t)row * a.ldv + (int64_t)h * D + 8 * u, a.vec, 0, 1.0f);
       }
     }
     return;
   }
-  auto settle = [&]() {
-    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-  };
-  for (int h = part; h < a.heads; h += a.hsplit) {
+  for (int h = part * 4 + wave; h < a.heads; h += 4 * a.hsplit) {
     const uint8_t* const from = block + (int64_t)h * C4<D>::BYTES;
-    if (lane < D / 2) codes[w.r][lane] = *(const u32x4*)(from + C4<D>::v_code(8 * w.r, 2 * lane));
-    settle();
+    if (lane < D / 2) codes[wave][lane] = *(const u32x4*)(from + C4<D>::v_code(8 * w.r, 2 * lane));
+    c4_settle();
 #pragma unroll
     for (int st = 0; st < STEPS; ++st) {
       const int slot = st * TPS + sub, tok = w.token(slot);
@@ -375,12 +456,12 @@ __global__ __launch_bounds__(256) void cache_read_kernel(RowsArgs a) {
       const uint32_t kw = *(const uint32_t*)(from + C4<D>::k_code(tok, 8 * u));
       const int ke = from[C4<D>::k_exp(tok, u >> 2)];
       c4_store8((T*)a.k + w.b * a.sk + row * a.ldk + (int64_t)h * D + 8 * u, a.vec, kw, __uint_as_float((uint32_t)ke << 23));
-      const uint8_t* const p = (const uint8_t*)&codes[w.r][4 * u] + slot;
+      const uint8_t* const p = (const uint8_t*)&codes[wave][4 * u] + slot;
       const uint32_t vw = (uint32_t)p[0] | (uint32_t)p[16] << 8 | (uint32_t)p[32] << 16 | (uint32_t)p[48] << 24;
       const int ve = from[C4<D>::v_exp(tok, u >> 2)];
       c4_store8((T*)a.v + w.b * a.sv + row * a.ldv + (int64_t)h * D + 8 * u, a.vec, vw, __uint_as_float((uint32_t)ve << 23));
     }
-    settle();
+    c4_settle();
   }
 }
 
@@ -942,9 +1023,9 @@ static track_status cache_check(const char* what, const track_cache4* c, int64_t
   return TRACK_OK;
 }
 
-// Workgroups that share a block's heads: one while the blocks alone fill the chip twice.
+// Workgroups that share 16 tokens' heads, four a turn: one while the tokens alone fill the chip twice.
 static int rows_heads(int64_t items, int heads) {
-  return (int)std::max<int64_t>(1, std::min<int64_t>(heads, (2 * (int64_t)device_cus() + items - 1) / items));
+  return (int)std::max<int64_t>(1, std::min<int64_t>((heads + 3) / 4, (2 * (int64_t)device_cus() + items - 1) / items));
 }
 
 template <typename T, int D>
@@ -981,8 +1062,8 @@ static track_status cache_rows(const char* what, bool read, int dtype, const tra
   a.B = (int)B, a.L = (int)L, a.heads = cache->heads;
   a.nblk = (int)((L + C4_BLOCK - 2) / C4_BLOCK + 1);
   a.vec = !((((uintptr_t)k | (uintptr_t)v) & 15) || ((ldk | ldv | (B > 1 ? sk | sv : 0)) * (int64_t)es & 15));
-  if (B > INT32_MAX || B * a.nblk >= (int64_t)1 << 23) return fail(TRACK_E_SHAPE, "%s: %lld x %lld tokens are too many", what, (long long)B, (long long)L);
-  a.hsplit = rows_heads(B * a.nblk, a.heads);
+  if (B > INT32_MAX || B * a.nblk >= (int64_t)1 << 22) return fail(TRACK_E_SHAPE, "%s: %lld x %lld tokens are too many", what, (long long)B, (long long)L);
+  a.hsplit = rows_heads(4 * B * a.nblk, a.heads);
   int rot = 0;
   if (rope) {
     rot = rope->layout == TRACK_ROPE_HALF ? 2 : 1;
@@ -992,7 +1073,7 @@ static track_status cache_rows(const char* what, bool read, int dtype, const tra
     a.sec1 = rope->axes > 2 ? rope->section[0] + rope->section[1] : a.pairs;
   }
   ProfScope prof(TRACK_PROF_OTHER, s);
-  const unsigned grid = (unsigned)(B * a.nblk * a.hsplit);
+  const unsigned grid = (unsigned)(4 * B * a.nblk * a.hsplit);
 #define TRACK_C4_ROWS(T, DH)                                              \
   do {                                                                    \
     if (read) cache_read_kernel<T, DH><<<grid, 256, 0, s>>>(a);           \
