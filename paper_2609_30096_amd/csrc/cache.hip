@@ -93,24 +93,6 @@ __device__ __forceinline__ uint32_t c4_round8(const float (&x)[8], int& byte) {
   const uint32_t w = c4_codes(x, __uint_as_float((uint32_t)byte << 23));
   return byte == 255 ? 0 : w;
 }
-__device__ __forceinline__ uint32_t c4_round8(const double (&x)[8], int& byte) {
-  double m = fabs(x[0]);
-  bool odd = !(m <= 1.7976931348623157e308);  // an infinity or a NaN
-#pragma unroll
-  for (int i = 1; i < 8; ++i) {
-    const double a = fabs(x[i]);
-    odd |= !(a <= 1.7976931348623157e308);
-    m = fmax(m, a);
-  }
-  // the largest exponent of the four lanes is that of the largest magnitude
-  byte = (int)c4_quad_max((uint32_t)(odd ? 255 : c4_exponent(m)));
-  if (byte == 255) return 0;
-  const double inv = __builtin_bit_cast(double, (uint64_t)(1023 + 127 - byte) << 52);
-  uint32_t w = 0;
-#pragma unroll
-  for (int i = 0; i < 8; ++i) w |= c4_code(x[i], inv) << (4 * i);
-  return w;
-}
 
 // ---------------------------------------------------------------- rows in and out
 struct RowsArgs {
@@ -207,29 +189,9 @@ __global__ __launch_bounds__(256) void cache_append_kernel(RowsArgs a) {
   uint8_t* const block = w.init<D>(a, item);
   if (!block) return;  // the whole workgroup
   const int u = lane % LPT, sub = lane / LPT;
-  int h = part * 4 + wave;
-  C4Unit<T> rk[STEPS], rz[ROT == 2 ? STEPS : 1], rv[STEPS];
-  // where the other channels of the lane's pairs lie (half layout), if they are a unit
-  const bool whole = ROT == 2 && a.vec && (a.pairs & 7) == 0;
-  const int other = 8 * u < a.pairs ? a.pairs : (8 * u < 2 * a.pairs ? -a.pairs : 0);
-  auto key_row = [&](int st, int hh) {
-    const int slot = st * TPS + sub;
-    const int64_t row = w.there >> slot & 1 ? w.row(slot) : 0;  // (any row of the sequence in a slot without one)
-    return (const T*)a.k + w.b * a.sk + row * a.ldk + (int64_t)hh * D;
-  };
-  auto load = [&](int hh) {
-#pragma unroll
-    for (int st = 0; st < STEPS; ++st) {
-      const int slot = st * TPS + sub;
-      const int64_t row = w.there >> slot & 1 ? w.row(slot) : 0;
-      const T* const kp = key_row(st, hh);
-      rk[st].load(kp + 8 * u, a.vec);
-      if constexpr (ROT == 2)
-        if (whole) rz[st].load(kp + 8 * u + other, true);
-      rv[st].load((const T*)a.v + w.b * a.sv + row * a.ldv + (int64_t)hh * D + 8 * u, a.vec);
-    }
-  };
-  if (h < a.heads) load(h);
+  // the lane that has the other channels of this one's pairs (half layout), if they are a unit
+  const bool whole = ROT == 2 && (a.pairs & 7) == 0;
+  const int other = (8 * u < a.pairs ? a.pairs : (8 * u < 2 * a.pairs ? -a.pairs : 0)) / 8;
   auto turns_of = [&](int slot, int p) {
     const int axis = (p >= a.sec0) + (p >= a.sec1);
     const double t = (double)a.pos[((int64_t)axis * a.B + w.b) * a.L + w.row(slot)] * (a.freqs[p] * 0.15915494309189533577);
@@ -247,36 +209,46 @@ __global__ __launch_bounds__(256) void cache_append_kernel(RowsArgs a) {
     }
     __syncthreads();
   }
-  // the lane's pair of channel i of its unit, and whether the channel is the pair's first
-  auto pair_of = [&](int i, bool& low) {
+  // the pair of channel i of unit un, and whether the channel is the pair's first
+  auto pair_of = [&](int un, int i, bool& low) {
     if constexpr (ROT == 1) {
       low = !(i & 1);
-      return 4 * u + (i >> 1);
+      return 4 * un + (i >> 1);
     } else {
-      const int ch = 8 * u + i;
+      const int ch = 8 * un + i;
       low = ch < a.pairs;
       return low ? ch : ch - a.pairs;
     }
   };
+  // the lane's pairs where its unit is all first channels, all second ones or all copied
+  const bool low0 = 8 * u < a.pairs;
+  const int first = low0 ? 8 * u : min(8 * u - a.pairs, D / 2 - 8);
+  // the exponent's place in the cache's order: K [4 c][G][2 s][2 h], V [G][2 s][8 c]
+  auto kexp_at = [&](int un, int slot) {
+    const int c = slot & 7;
+    return (c & 3) * (4 * G) + 4 * (un >> 2) + 2 * (slot >> 3) + (c >> 2);
+  };
   const bool all = w.there == 0xffff;
-  for (; h < a.heads; h += 4 * a.hsplit) {
+  for (int h = part * 4 + wave; h < a.heads; h += 4 * a.hsplit) {
     uint8_t* const to = block + (int64_t)h * C4<D>::BYTES;
-    C4Unit<T> ck[STEPS], cz[ROT == 2 ? STEPS : 1], cv[STEPS];
-#pragma unroll
-    for (int st = 0; st < STEPS; ++st) {
-      ck[st] = rk[st], cv[st] = rv[st];
-      if constexpr (ROT == 2) cz[st] = rz[st];
-    }
-    if (h + 4 * a.hsplit < a.heads) load(h + 4 * a.hsplit);  // under way while this head is computed on
+    const T* kp[STEPS];
+    C4Unit<T> rk[STEPS], rv[STEPS];
 #pragma unroll
     for (int st = 0; st < STEPS; ++st) {
       const int slot = st * TPS + sub;
-      // the exponent's place in the cache's order: K [4 c][G][2 s][2 h], V [G][2 s][8 c]
-      const int c = slot & 7, ke = (c & 3) * (4 * G) + 4 * (u >> 2) + 2 * (slot >> 3) + (c >> 2), ve = 16 * (u >> 2) + slot;
+      const int64_t row = w.there >> slot & 1 ? w.row(slot) : 0;  // (any row of the sequence in a slot without one)
+      kp[st] = (const T*)a.k + w.b * a.sk + row * a.ldk + (int64_t)h * D;
+      rk[st].load(kp[st] + 8 * u, a.vec);
+      rv[st].load((const T*)a.v + w.b * a.sv + row * a.ldv + (int64_t)h * D + 8 * u, a.vec);
+    }
+    uint32_t again = 0;  // steps with a value near a border
+#pragma unroll
+    for (int st = 0; st < STEPS; ++st) {
+      const int slot = st * TPS + sub;
       float x[8];
       uint32_t word;
       int byte;
-      ck[st].get(x);
+      rk[st].get(x);
       if constexpr (ROT == 0) {
         word = c4_round8(x, byte);
       } else {
@@ -285,58 +257,97 @@ __global__ __launch_bounds__(256) void cache_append_kernel(RowsArgs a) {
 #pragma unroll
           for (int i = 0; i < 8; ++i) z[i] = x[i ^ 1];
         } else if (whole) {
-          cz[st].get(z);
+          C4Unit<T> o;  // another lane's
+#pragma unroll
+          for (int j = 0; j < (int)sizeof(T) / 2; ++j)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o.w[j][e] = (uint32_t)__builtin_amdgcn_ds_bpermute(4 * (lane + other), (int)rk[st].w[j][e]);
+          o.get(z);
         } else {
-          const T* const kp = key_row(st, h);
+          const int un = att_lane() % LPT;
 #pragma unroll
           for (int i = 0; i < 8; ++i) {
-            const int ch = 8 * u + i;
-            z[i] = ldf(kp + (ch < a.pairs ? ch + a.pairs : (ch < 2 * a.pairs ? ch - a.pairs : ch)));
+            const int ch = 8 * un + i;
+            z[i] = ldf(kp[st] + (ch < a.pairs ? ch + a.pairs : (ch < 2 * a.pairs ? ch - a.pairs : ch)));
           }
         }
         float y[8], lo[8], hi[8];
         const float2* const at = cs + slot * (D / 2);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          bool low;
-          const int p = pair_of(i, low);
-          const float2 t = p < a.pairs ? at[p] : float2{1.0f, 0.0f};
-          const float sn = p < a.pairs && low ? -t.y : t.y;
-          y[i] = p < a.pairs ? fmaf(x[i], t.x, z[i] * sn) : x[i];
-        }
         const uint32_t in = c4_quad_max(max(c4_top(x), c4_top(z)));
         const float off = __uint_as_float(in) * (9.5367431640625e-7f * fabsf((float)a.amp));
+        auto turn = [&](int i, const float2& t, bool low, bool rotated) {
+          y[i] = fmaf(x[i], t.x, z[i] * (low ? -t.y : t.y));
+          y[i] = rotated ? y[i] : x[i];
+          const float d = !rotated || (t.y == 0.0f && t.x == 1.0f) ? 0.0f : off;  // by angle 0 a key stays as it is, ties included
+          lo[i] = y[i] - d, hi[i] = y[i] + d;
+        };
+        if (ROT == 2 && whole) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) lo[i] = y[i] - off, hi[i] = y[i] + off;
+          for (int i = 0; i < 8; ++i) turn(i, at[first + i], low0, 8 * u < 2 * a.pairs);
+        } else {
+          const int un = ROT == 2 ? att_lane() % LPT : u;  // (formed here: eight pairs' places would stay in registers)
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            bool low;
+            const int p = pair_of(un, i, low);
+            turn(i, at[min(p, D / 2 - 1)], low, p < a.pairs);
+          }
+        }
         const float top = __uint_as_float(c4_quad_max(c4_top(y)));
         byte = c4_exponent(top + off);
         const float s = __uint_as_float((uint32_t)byte << 23);
         word = c4_codes(lo, s);
         const uint32_t differ = word ^ c4_codes(hi, s);
-        const bool near = byte != c4_exponent(fmaxf(top - off, 0.0f)) || byte == 255 || (differ != 0 && in != 0);
-        if (__ballot(near)) {
-          const T* const kp = key_row(st, h);
-          double r[8];
-#pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            bool low;
-            const int p = pair_of(i, low);
-            r[i] = x[i];
-            if (p < a.pairs) {
-              double sn = 0.0, cn = 1.0;
-              if (w.there >> slot & 1) sincospi(turns_of(slot, p), &sn, &cn);
-              sn *= a.amp, cn *= a.amp;
-              r[i] = low ? x[i] * cn - z[i] * sn : z[i] * sn + x[i] * cn;
-            }
-          }
-          word = c4_round8(r, byte);
-        }
+        if (__ballot((byte != c4_exponent(fmaxf(top - off, 0.0f)) || byte == 255 || (differ != 0 && in != 0)) && (w.there >> slot & 1))) again |= 1u << st;
       }
       kcodes[wave][slot * LPT + u] = word;
-      if ((u & 3) == 0) kexp[wave][ke] = (uint8_t)byte;
-      cv[st].get(x);
+      if ((u & 3) == 0) kexp[wave][kexp_at(u, slot)] = (uint8_t)byte;
+      rv[st].get(x);
       vcodes[wave][slot * LPT + u] = c4_round8(x, byte);
-      if ((u & 3) == 0) vexp[wave][ve] = (uint8_t)byte;
+      if ((u & 3) == 0) vexp[wave][16 * (u >> 2) + slot] = (uint8_t)byte;
+      if (ROT == 2) __builtin_amdgcn_sched_barrier(0);
+    }
+    if constexpr (ROT != 0) {
+#pragma unroll 1
+      for (; again; again &= again - 1) {
+        const int un = att_lane() % LPT, slot = __builtin_ctz(again) * TPS + att_lane() / LPT;
+        const bool there = w.there >> slot & 1;
+        const T* const p0 = (const T*)a.k + w.b * a.sk + (there ? w.row(slot) : 0) * a.ldk + (int64_t)h * D;
+        C4Unit<T> unit;
+        float x[8];
+        unit.load(p0 + 8 * un, a.vec);
+        unit.get(x);
+        double r[8], sn = 0.0, cn = 1.0, m = 0.0;
+        bool odd = false;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const int ch = 8 * un + i;
+          bool low;
+          const int p = pair_of(un, i, low);
+          if (ROT == 2 || low) {  // (interleaved: the second channel has the first one's)
+            sn = 0.0, cn = 1.0;
+            if (there && p < a.pairs) sincospi(turns_of(slot, p), &sn, &cn);
+            sn *= a.amp, cn *= a.amp;
+          }
+          r[i] = x[i];
+          if (p < a.pairs) {
+            const double z = ROT == 1 ? x[i ^ 1] : ldf(p0 + (low ? ch + a.pairs : ch - a.pairs));
+            r[i] = low ? x[i] * cn - z * sn : z * sn + x[i] * cn;
+          }
+          odd |= !(fabs(r[i]) <= 1.7976931348623157e308);  // an infinity or a NaN
+          m = fmax(m, fabs(r[i]));
+          if (ROT == 2) __builtin_amdgcn_sched_barrier(0);  // eight angles side by side would take 100 registers more
+        }
+        // the largest exponent of the four lanes is that of the largest magnitude
+        const int byte = (int)c4_quad_max((uint32_t)(odd ? 255 : c4_exponent(m)));
+        const double inv = __builtin_bit_cast(double, (uint64_t)(1023 + 127 - byte) << 52);
+        uint32_t word = 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) word |= c4_code(r[i], inv) << (4 * i);
+        if (byte == 255) word = 0;
+        kcodes[wave][slot * LPT + un] = word;
+        if ((un & 3) == 0) kexp[wave][kexp_at(un, slot)] = (uint8_t)byte;
+      }
     }
     c4_settle();
     if (lane < D / 2) {
