@@ -509,10 +509,11 @@ struct C4Raw {
 // registers, 16 bytes a lane and whole lines a load, and there to bfloat16; nothing passes through LDS until the waves' sums meet.
 // The next tile's K takes the place of this one's as soon as its logits are formed, V that of V.
 template <bool SPLIT>
-__global__ __launch_bounds__(256) void cache_rows_kernel(WinArgs a, CacheArgs ca) {
+__global__ __launch_bounds__(256, 3) void cache_rows_kernel(WinArgs a, CacheArgs ca) {
   constexpr int BKV = C4_BLOCK, D = ATT_D, F = D / 16;
   __shared__ f32x4 so[4][F][64];
   __shared__ float sm[4][16], sl[4][16];
+  __shared__ u32x4 qs[D / 32][64];
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   const int jq = lane & 15, g = lane >> 4;
@@ -540,9 +541,12 @@ __global__ __launch_bounds__(256) void cache_rows_kernel(WinArgs a, CacheArgs ca
   if (tiles.sink == 0 && seq.sink >= lo1) mask.lo[0] = 0;
   // a lane's channels 32 g + 8 step .. + 7, as its bytes of K hold them
   const bf16_t* qp = (const bf16_t*)a.q + b * a.sq + (int64_t)qi * a.ldq + (int64_t)head * D + 32 * g;
-  bf16x8 qf[D / 32];
+  // (the waves have the same rows; from LDS a tile, and in an order that takes V group by group, 168 registers are enough: three waves a SIMD)
+  if (wave == 0) {
 #pragma unroll
-  for (int kc = 0; kc < D / 32; ++kc) qf[kc] = __builtin_bit_cast(bf16x8, *(const u32x4*)(qp + kc * 8));
+    for (int kc = 0; kc < D / 32; ++kc) qs[kc][lane] = *(const u32x4*)(qp + kc * 8);
+  }
+  __syncthreads();
   const uint32_t koff = c4_row_k(lane), keoff = c4_row_ke(lane), voff = c4_row_v(lane, 0), veoff = c4_row_ve(lane, 0);
   // Loads that are not needed (no page, past the share) read the pool's first block: as many for every
   // tile, so that the wait for the older ones can count.
@@ -580,6 +584,9 @@ __global__ __launch_bounds__(256) void cache_rows_kernel(WinArgs a, CacheArgs ca
     const bool edge = idx < tiles.edge || !there;
     const float ks[4] = {c4_scale<0>(r.ke), c4_scale<1>(r.ke), c4_scale<2>(r.ke), c4_scale<3>(r.ke)};
     f32x4 s[BKV / 16];
+    bf16x8 qf[D / 32];
+#pragma unroll
+    for (int kc = 0; kc < D / 32; ++kc) qf[kc] = __builtin_bit_cast(bf16x8, qs[kc][lane]);
 #pragma unroll
     for (int kc = 0; kc < D / 32; ++kc)
 #pragma unroll
@@ -664,6 +671,7 @@ __global__ __launch_bounds__(256) void cache_rows_kernel(WinArgs a, CacheArgs ca
         const bf16x8 p = __builtin_bit_cast(bf16x8, pw[c]);
         o[2 * mm] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, u32x4{lo[0][0], lo[0][1], lo[1][0], lo[1][1]}), p, o[2 * mm], 0, 0, 0);
         o[2 * mm + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, u32x4{hi[0][0], hi[0][1], hi[1][0], hi[1][1]}), p, o[2 * mm + 1], 0, 0, 0);
+        __builtin_amdgcn_sched_barrier(0);
       }
     if (edge && __ballot(lost != 0)) {
 #pragma unroll
@@ -1144,6 +1152,16 @@ struct CachePlan {
   int nsplit;
 };
 
+// Shares of the keys for few rows.  None up to 16 tiles, four a wave: the join is a launch more.  Then as many as make the three
+// workgroups a CU that are resident, of four tiles at least, and twice as many for what takes some 100 us, which evens out lengths.
+// Join included, replayed on three caches in turn: 64 key heads of 100003 to 56000 keys 124 us with 8, 122 with 12, 126 with 16, 118 with 24, 117 with
+// 32, 127 with 64; 48 of 32760 51 with 8, 44 with 16, 48 with 24, 45 with 32; 8 of 100003 36 with 32, 29 with 64 and 96; 64 of
+// 16384 32 with 8, 34 with 12, 37 with 24; 512 of 2000 29 with one, 35 with 2; 8 of 16384 17 with 16, 14 with 32, 13 with 64.
+static int64_t cache_rows_split(int64_t tiles, int64_t blocks, int64_t cus) {
+  if (tiles <= 16) return 1;
+  return std::min((blocks * tiles >= 192 * cus ? 6 : 3) * cus / blocks, tiles / 4);
+}
+
 static CachePlan cache_plan(int dtype, const track_window& w, int64_t B, int Hk, int n, int D, int64_t Lq, int64_t Lk) {
   const int64_t rows = Lq * n, cus = device_cus();
   CachePlan p;
@@ -1153,7 +1171,7 @@ static CachePlan cache_plan(int dtype, const track_window& w, int64_t B, int Hk,
   const int64_t tiles = (win_span(w, std::min(rows, block), n, Lk) + C4_BLOCK - 1) / C4_BLOCK;
   const int64_t blocks = p.nrb * Hk * B;
   int64_t s;
-  if (p.form == CachePlan::ROWS) s = tiles <= 16 ? 1 : std::min((4 * cus + blocks - 1) / blocks, tiles / 8);
+  if (p.form == CachePlan::ROWS) s = cache_rows_split(tiles, blocks, cus);
   else if (p.form == CachePlan::F32) s = std::min(2 * cus / blocks, tiles / 4);
   else s = win_blocks_split(tiles, blocks, rows * Hk * B, cus);
   p.nsplit = (int)std::max<int64_t>(1, std::min<int64_t>(s, 1024));
