@@ -783,31 +783,35 @@ __global__ __launch_bounds__(512) void cache_blocks_kernel(WinArgs a, CacheArgs 
   }
 
   // What this thread brings in: 16 bytes of K, group kg of key kt, or 16 of V, channels vc and vc + 1 of the keys
-  // 32 s + 8 vr + 0..7.  The LDS row of key (channel) 8 q + 4 x + j of 32 is 16 x + 4 q + j.
-  auto row_of = [](int x) { return (x & 32) | (x & 64) | (((x >> 2) & 1) << 4) | (((x >> 3) & 3) << 2) | (x & 3); };
+  // 32 s + 8 vr + 0..7.  The LDS row of key (channel) 8 q + 4 x + j of 32 is 16 x + 4 q + j; K's four units and V's two differ from the
+  // first in an XOR, and the rows of two channels beside each other have one swizzle.
   const bool isv = wave >= 4;
-  const int t8 = tid & 255;
-  const int kt = c4_tile_key(t8), kg = c4_tile_group(t8), vr = c4_tile_r(t8), vc = c4_tile_channel(t8), vm = vc >> 5;
-  const uint32_t from = c4_tile_codes(isv, t8), efrom = c4_tile_exp(isv, t8);
-  const int krow = row_of(kt), vrow[2] = {row_of(vc), row_of(vc + 1)};
+  uint32_t put;
+  {
+    auto row_of = [](int x) { return (x & 96) | (((x >> 2) & 1) << 4) | (((x >> 3) & 3) << 2) | (x & 3); };
+    const int t8 = tid & 255, r = row_of(isv ? c4_tile_channel(t8) : c4_tile_key(t8));
+    put = (uint32_t)(isv ? ATT_K_BYTES + r * ATT_VROW + ((c4_tile_r(t8) ^ att_vswz(r)) << 4)
+                         : r * 256 + (((4 * c4_tile_group(t8)) ^ (r & 15)) << 4));
+  }
   struct Raw {
     u32x4 w, e;
   };
   auto fetch = [&](const uint8_t* p, Raw& r) {
-    r.w = *(const u32x4*)(p + from);
-    if (isv) r.e = *(const u32x4*)(p + efrom);
-    else r.e[0] = p[efrom];
+    const int t8 = (wave & 3) * 64 + att_lane();  // (formed here: the tile body needs the registers)
+    r.w = *(const u32x4*)(p + c4_tile_codes(isv, t8));
+    if (isv) r.e = *(const u32x4*)(p + c4_tile_exp(true, t8));
+    else r.e[0] = p[c4_tile_exp(false, t8)];
   };
-  auto spread = [&](Raw& r, int slot, int key0, bool edge) {
+  auto spread = [&](Raw& r, int key0, bool edge) {  // into the slot that put points at
     if (!isv) {
       const float s = __uint_as_float(r.e[0] << 23);
-      uint8_t* const to = smem + slot + krow * 256;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) *(u32x4*)(to + (((4 * kg + i) ^ (krow & 15)) << 4)) = c4_eight(r.w[i], s);
+      for (int i = 0; i < 4; ++i) *(u32x4*)(smem + (put ^ (uint32_t)(i << 4))) = c4_eight(r.w[i], s);
       return;
     }
     if (edge) {
       // V past the last key takes exponent 0, and so do groups that hold no number (below)
+      const int t8 = (wave & 3) * 64 + att_lane(), vr = c4_tile_r(t8);
       u32x4 bad;
 #pragma unroll
       for (int w = 0; w < 4; ++w) {
@@ -815,16 +819,16 @@ __global__ __launch_bounds__(512) void cache_blocks_kernel(WinArgs a, CacheArgs 
         bad[w] = c4_nan_bytes(r.e[w]) >> 7;
         r.e[w] &= ~(bad[w] * 255u);
       }
-      if ((t8 & 15) == 0) *(u32x4*)(smem + 2 * SLOT + (slot ? 256 : 0) + (vm * 4 + vr) * 16) = bad;
+      if ((t8 & 15) == 0) *(u32x4*)(smem + 2 * SLOT + (put & SLOT ? 256 : 0) + ((t8 >> 6) * 4 + vr) * 16) = bad;
     }
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
       uint32_t lo[2][2], hi[2][2];
 #pragma unroll
       for (int w = 0; w < 2; ++w) c4_four(r.w[2 * s + w], r.e[2 * s + w], lo[w], hi[w]);
-      uint8_t* const to = smem + slot + ATT_K_BYTES;
-      *(u32x4*)(to + vrow[0] * ATT_VROW + (((4 * s + vr) ^ att_vswz(vrow[0])) << 4)) = u32x4{lo[0][0], lo[0][1], lo[1][0], lo[1][1]};
-      *(u32x4*)(to + vrow[1] * ATT_VROW + (((4 * s + vr) ^ att_vswz(vrow[1])) << 4)) = u32x4{hi[0][0], hi[0][1], hi[1][0], hi[1][1]};
+      uint8_t* const to = smem + (put ^ (uint32_t)(s << 6));
+      *(u32x4*)to = u32x4{lo[0][0], lo[0][1], lo[1][0], lo[1][1]};
+      *(u32x4*)(to + ATT_VROW) = u32x4{hi[0][0], hi[0][1], hi[1][0], hi[1][1]};
     }
   };
   auto barrier = [&]() {
@@ -848,18 +852,22 @@ __global__ __launch_bounds__(512) void cache_blocks_kernel(WinArgs a, CacheArgs 
     }
     return idx;
   };
+  // Tiles idx (in LDS), next (its bytes under way) and the one after it, whose page is looked up meanwhile.
   Raw raw;
   int idx = find(i0);
   if (idx < i1) {
     fetch(at, raw);
-    spread(raw, 0, tiles.key<BKV>(idx), idx < tiles.edge);
+    spread(raw, tiles.key<BKV>(idx), idx < tiles.edge);
   }
+  put ^= SLOT;
+  int next = find(idx + 1);
   barrier();
-  while (idx < i1) {
-    const int next = find(idx + 1);
+  // edge tiles in a loop of their own: with both kinds in one the accumulators are copied tile by tile (250 registers, 1.3 times as slow)
+  auto step = [&](auto edge) {
     if (next < i1) fetch(at, raw);
-    const int key0 = tiles.key<BKV>(idx);
-    if (idx < tiles.edge) {
+    const int after = find(next + 1);
+    if constexpr (decltype(edge)::value) {
+      const int key0 = tiles.key<BKV>(idx);
       if (live && key0 <= whi && (key0 + BKV > wlo || key0 < tiles.sink)) {
         mask.key0 = key0;
         att_tile_masked<WinMask<ATT_QB>, QLOG2, 4, true, false>(smem, qf, ko, vo, st, mask, a.scale_log2);
@@ -887,22 +895,29 @@ __global__ __launch_bounds__(512) void cache_blocks_kernel(WinArgs a, CacheArgs 
             lost |= (uint32_t)__shfl_xor((int)lost, 16);
             lost |= (uint32_t)__shfl_xor((int)lost, 32);
 #pragma unroll
-            for (int f = 0; f < D / 16; ++f)
+            for (int f = 0; f < D / 16; ++f) {
+              const float add = lost >> (f >> 1) & 1 ? NAN : 0.0f;  // (onto the sums in place)
 #pragma unroll
-              for (int r = 0; r < 4; ++r) st.o[f][i][r] = lost >> (f >> 1) & 1 ? NAN : st.o[f][i][r];
+              for (int r = 0; r < 4; ++r) st.o[f][i][r] += add;
+            }
           }
         }
       }
-    } else if (live) {
-      att_tile_masked<AttAll, QLOG2, 4, true, false>(smem, qf, ko, vo, st, AttAll{}, a.scale_log2);
+    } else {
+      if (live) att_tile_masked<AttAll, QLOG2, 4, true, false>(smem, qf, ko, vo, st, AttAll{}, a.scale_log2);
     }
-    if (next < i1) spread(raw, slot ^ SLOT, tiles.key<BKV>(next), next < tiles.edge);
+    if (next < i1) spread(raw, tiles.key<BKV>(next), next < tiles.edge);
     ko ^= SLOT;
     vo ^= SLOT;
     slot ^= SLOT;
+    put ^= SLOT;
     idx = next;
+    next = after;
     barrier();
-  }
+  };
+  const int ie = min(i1, tiles.edge);
+  while (idx < ie) step(std::true_type{});
+  while (idx < i1) step(std::false_type{});
 
   // lane: query jq of each block, channels 32 p + 8 g .. + 7
 #pragma unroll
