@@ -42,6 +42,20 @@ __device__ __forceinline__ uint8_t* c4_at(const CacheArgs& c, int b, int h, int 
   return c.pages + c4_block(page, c.blocks, t, slot, c.stride) + (int64_t)h * C4<D>::BYTES;
 }
 
+// The same in two steps, so that the table's entry can be under way while a tile is computed on: the entry of block t, by a vector load (a
+// scalar one would be waited for with every read of LDS), and the places.
+__device__ __forceinline__ int c4_entry(const CacheArgs& c, int b, int t) {
+  int zero;
+  asm("v_mov_b32 %0, 0" : "=v"(zero));
+  return c.table[b * c.ld_table + min((int)c.by_blocks((uint32_t)t), c.table_pages - 1) + zero];
+}
+template <int D>
+__device__ __forceinline__ const uint8_t* c4_of_entry(const CacheArgs& c, int entry, int h, int t, bool& there) {
+  const int page = __builtin_amdgcn_readfirstlane(entry);
+  there = c4_page(page, c.n_pages);
+  return there ? c.pages + c4_block(page, c.blocks, t, (int)c.by_blocks((uint32_t)t), c.stride) + (int64_t)h * C4<D>::BYTES : c.pages;
+}
+
 // ---------------------------------------------------------------- rounding to 4 bits
 // The exponent byte of a group whose largest magnitude is m (255: an infinity or a NaN in it).
 __device__ __forceinline__ int c4_exponent(double m) {
@@ -550,12 +564,6 @@ __global__ __launch_bounds__(256, 3) void cache_rows_kernel(WinArgs a, CacheArgs
   const uint32_t koff = c4_row_k(lane), keoff = c4_row_ke(lane), voff = c4_row_v(lane, 0), veoff = c4_row_ve(lane, 0);
   // Loads that are not needed (no page, past the share) read the pool's first block: as many for every
   // tile, so that the wait for the older ones can count.
-  bool there, next_there;  // whether a page holds the tile
-  auto find = [&](int idx) {
-    const uint8_t* const p = idx < i1 ? c4_at<D>(ca, b, h, tiles.key<BKV>(idx) >> 6) : nullptr;
-    next_there = p != nullptr;
-    return p ? p : ca.pages;
-  };
   C4Raw r;
   auto fetch_k = [&](const uint8_t* p) {
 #pragma unroll
@@ -574,12 +582,20 @@ __global__ __launch_bounds__(256, 3) void cache_rows_kernel(WinArgs a, CacheArgs
 #pragma unroll
   for (int f = 0; f < F; ++f) o[f] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 
-  const uint8_t* at = find(i0 + wave);
-  there = next_there;
-  fetch_k(at);
-  fetch_v(at);
+  // the tile's page, and the entries of the next ones, two tiles ahead
+  auto block_of = [&](int idx) { return tiles.key<BKV>(min(idx, i1 - 1)) >> 6; };
+  bool there = false;
+  const uint8_t* at = nullptr;
+  int entry = 0;
+  if (i0 + wave < i1) {
+    at = c4_of_entry<D>(ca, c4_entry(ca, b, block_of(i0 + wave)), h, block_of(i0 + wave), there);
+    fetch_k(at);
+    entry = c4_entry(ca, b, block_of(i0 + wave + 4));
+    fetch_v(at);
+  }
   for (int idx = i0 + wave; idx < i1; idx += 4) {
-    at = find(idx + 4);
+    bool next_there;
+    at = c4_of_entry<D>(ca, entry, h, block_of(idx + 4), next_there);
     const int key0 = tiles.key<BKV>(idx);
     const bool edge = idx < tiles.edge || !there;
     const float ks[4] = {c4_scale<0>(r.ke), c4_scale<1>(r.ke), c4_scale<2>(r.ke), c4_scale<3>(r.ke)};
@@ -595,6 +611,7 @@ __global__ __launch_bounds__(256, 3) void cache_rows_kernel(WinArgs a, CacheArgs
                                                        kc ? s[i] : f32x4{0.0f, 0.0f, 0.0f, 0.0f}, 0, 0, 0);
     __builtin_amdgcn_sched_barrier(0);
     fetch_k(at);
+    entry = c4_entry(ca, b, block_of(idx + 8));
     __builtin_amdgcn_sched_barrier(0);
     uint32_t lost = 0;  // groups of V in which a key that the row sees holds no number
     if (edge) {
@@ -844,31 +861,26 @@ __global__ __launch_bounds__(512) void cache_blocks_kernel(WinArgs a, CacheArgs 
   st.reset();
   int i0 = 0, i1 = tiles.n;
   if (SPLIT) win_share(tiles.n, sp, a.nsplit, i0, i1);
-  const uint8_t* at = nullptr;
-  auto find = [&](int idx) {  // the next tile that a page holds
-    for (at = nullptr; idx < i1; ++idx) {
-      at = c4_at<D>(ca, b, h, tiles.key<BKV>(idx) >> 6);
-      if (at) break;
-    }
-    return idx;
-  };
-  // Tiles idx (in LDS), next (its bytes under way) and the one after it, whose page is looked up meanwhile.
+  // Tile idx is in LDS, the next one's bytes are under way, and the table's entry of the one after it.  Tiles without a page are passed over.
+  auto block_of = [&](int idx) { return tiles.key<BKV>(min(idx, i1 - 1)) >> 6; };
   Raw raw;
-  int idx = find(i0);
+  int idx = i0, entry = 0;
+  bool there = false;
   if (idx < i1) {
-    fetch(at, raw);
+    fetch(c4_of_entry<D>(ca, c4_entry(ca, b, block_of(idx)), h, block_of(idx), there), raw);
+    entry = c4_entry(ca, b, block_of(idx + 1));
     spread(raw, tiles.key<BKV>(idx), idx < tiles.edge);
   }
   put ^= SLOT;
-  int next = find(idx + 1);
   barrier();
   // edge tiles in a loop of their own: with both kinds in one the accumulators are copied tile by tile (250 registers, 1.3 times as slow)
   auto step = [&](auto edge) {
-    if (next < i1) fetch(at, raw);
-    const int after = find(next + 1);
+    bool next_there;
+    fetch(c4_of_entry<D>(ca, entry, h, block_of(idx + 1), next_there), raw);  // (past the share: this tile again)
+    entry = c4_entry(ca, b, block_of(idx + 2));
     if constexpr (decltype(edge)::value) {
       const int key0 = tiles.key<BKV>(idx);
-      if (live && key0 <= whi && (key0 + BKV > wlo || key0 < tiles.sink)) {
+      if (live && there && key0 <= whi && (key0 + BKV > wlo || key0 < tiles.sink)) {
         mask.key0 = key0;
         att_tile_masked<WinMask<ATT_QB>, QLOG2, 4, true, false>(smem, qf, ko, vo, st, mask, a.scale_log2);
         // rows that see a key whose V holds no number in a group of channels have none there
@@ -904,15 +916,15 @@ __global__ __launch_bounds__(512) void cache_blocks_kernel(WinArgs a, CacheArgs 
         }
       }
     } else {
-      if (live) att_tile_masked<AttAll, QLOG2, 4, true, false>(smem, qf, ko, vo, st, AttAll{}, a.scale_log2);
+      if (live && there) att_tile_masked<AttAll, QLOG2, 4, true, false>(smem, qf, ko, vo, st, AttAll{}, a.scale_log2);
     }
-    if (next < i1) spread(raw, tiles.key<BKV>(next), next < tiles.edge);
+    spread(raw, tiles.key<BKV>(min(idx + 1, i1 - 1)), idx + 1 < tiles.edge);
     ko ^= SLOT;
     vo ^= SLOT;
     slot ^= SLOT;
     put ^= SLOT;
-    idx = next;
-    next = after;
+    ++idx;
+    there = next_there;
     barrier();
   };
   const int ie = min(i1, tiles.edge);
