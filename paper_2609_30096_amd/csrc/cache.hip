@@ -42,18 +42,41 @@ __device__ __forceinline__ uint8_t* c4_at(const CacheArgs& c, int b, int h, int 
   return c.pages + c4_block(page, c.blocks, t, slot, c.stride) + (int64_t)h * C4<D>::BYTES;
 }
 
-// The same in two steps, so that the table's entry can be under way while a tile is computed on: the entry of block t, by a vector load (a
-// scalar one would be waited for with every read of LDS), and the places.
-__device__ __forceinline__ int c4_entry(const CacheArgs& c, int b, int t) {
-  int zero;
-  asm("v_mov_b32 %0, 0" : "=v"(zero));
-  return c.table[b * c.ld_table + min((int)c.by_blocks((uint32_t)t), c.table_pages - 1) + zero];
-}
+// Tiles in their order, the block of 64 places and the table's entry of each from the last one's: tiles seen whole lie one after
+// another but for the step from the first tokens to the window (by division 60 scalar instructions a tile, a fifth of a tile's time).
+struct C4Walk {
+  int idx, t, slot, in;  // the tile's place in the order, its block, the entry, the block in the page
+  template <class Tiles>
+  __device__ __forceinline__ void set(const CacheArgs& c, const Tiles& tiles, int i) {
+    idx = i;
+    t = tiles.template key<C4_BLOCK>(i) >> 6;
+    slot = (int)c.by_blocks((uint32_t)t);
+    in = t - slot * c.blocks;
+  }
+  // the next one, of `end` (the last one again)
+  template <class Tiles>
+  __device__ __forceinline__ void step(const CacheArgs& c, const Tiles& tiles, int end) {
+    if (idx + 1 >= end) return;
+    if (idx < tiles.edge || idx + 1 == tiles.edge + tiles.fs) {
+      set(c, tiles, idx + 1);
+    } else {
+      ++idx, ++t, ++in;
+      if (in == c.blocks) in = 0, ++slot;
+    }
+  }
+  __device__ __forceinline__ int entry(const CacheArgs& c, int b) const {
+    int zero;  // a vector load: a scalar one would be waited for with every read of LDS
+    asm("v_mov_b32 %0, 0" : "=v"(zero));
+    return c.table[b * c.ld_table + slot + zero];
+  }
+};
+
+// The places of block `in` of the page that an entry names; the pool's first where it names none.
 template <int D>
-__device__ __forceinline__ const uint8_t* c4_of_entry(const CacheArgs& c, int entry, int h, int t, bool& there) {
+__device__ __forceinline__ const uint8_t* c4_of_entry(const CacheArgs& c, int entry, int h, int in, bool& there) {
   const int page = __builtin_amdgcn_readfirstlane(entry);
   there = c4_page(page, c.n_pages);
-  return there ? c.pages + c4_block(page, c.blocks, t, (int)c.by_blocks((uint32_t)t), c.stride) + (int64_t)h * C4<D>::BYTES : c.pages;
+  return there ? c.pages + c4_block(page, c.blocks, in, 0, c.stride) + (int64_t)h * C4<D>::BYTES : c.pages;
 }
 
 // ---------------------------------------------------------------- rounding to 4 bits
@@ -583,19 +606,21 @@ __global__ __launch_bounds__(256, 3) void cache_rows_kernel(WinArgs a, CacheArgs
   for (int f = 0; f < F; ++f) o[f] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 
   // the tile's page, and the entries of the next ones, two tiles ahead
-  auto block_of = [&](int idx) { return tiles.key<BKV>(min(idx, i1 - 1)) >> 6; };
   bool there = false;
   const uint8_t* at = nullptr;
+  C4Walk next;
   int entry = 0;
   if (i0 + wave < i1) {
-    at = c4_of_entry<D>(ca, c4_entry(ca, b, block_of(i0 + wave)), h, block_of(i0 + wave), there);
+    next.set(ca, tiles, i0 + wave);
+    at = c4_of_entry<D>(ca, next.entry(ca, b), h, next.in, there);
     fetch_k(at);
-    entry = c4_entry(ca, b, block_of(i0 + wave + 4));
+    next.set(ca, tiles, min(i0 + wave + 4, i1 - 1));
+    entry = next.entry(ca, b);
     fetch_v(at);
   }
   for (int idx = i0 + wave; idx < i1; idx += 4) {
     bool next_there;
-    at = c4_of_entry<D>(ca, entry, h, block_of(idx + 4), next_there);
+    at = c4_of_entry<D>(ca, entry, h, next.in, next_there);
     const int key0 = tiles.key<BKV>(idx);
     const bool edge = idx < tiles.edge || !there;
     const float ks[4] = {c4_scale<0>(r.ke), c4_scale<1>(r.ke), c4_scale<2>(r.ke), c4_scale<3>(r.ke)};
@@ -611,7 +636,8 @@ __global__ __launch_bounds__(256, 3) void cache_rows_kernel(WinArgs a, CacheArgs
                                                        kc ? s[i] : f32x4{0.0f, 0.0f, 0.0f, 0.0f}, 0, 0, 0);
     __builtin_amdgcn_sched_barrier(0);
     fetch_k(at);
-    entry = c4_entry(ca, b, block_of(idx + 8));
+    next.set(ca, tiles, min(idx + 8, i1 - 1));
+    entry = next.entry(ca, b);
     __builtin_amdgcn_sched_barrier(0);
     uint32_t lost = 0;  // groups of V in which a key that the row sees holds no number
     if (edge) {
@@ -813,11 +839,11 @@ __global__ __launch_bounds__(512) void cache_blocks_kernel(WinArgs a, CacheArgs 
   struct Raw {
     u32x4 w, e;
   };
+  const uint32_t from = c4_tile_codes(isv, tid & 255), efrom = c4_tile_exp(isv, tid & 255);
   auto fetch = [&](const uint8_t* p, Raw& r) {
-    const int t8 = (wave & 3) * 64 + att_lane();  // (formed here: the tile body needs the registers)
-    r.w = *(const u32x4*)(p + c4_tile_codes(isv, t8));
-    if (isv) r.e = *(const u32x4*)(p + c4_tile_exp(true, t8));
-    else r.e[0] = p[c4_tile_exp(false, t8)];
+    r.w = *(const u32x4*)(p + from);
+    if (isv) r.e = *(const u32x4*)(p + efrom);
+    else r.e[0] = p[efrom];
   };
   auto spread = [&](Raw& r, int key0, bool edge) {  // into the slot that put points at
     if (!isv) {
@@ -862,13 +888,16 @@ __global__ __launch_bounds__(512) void cache_blocks_kernel(WinArgs a, CacheArgs 
   int i0 = 0, i1 = tiles.n;
   if (SPLIT) win_share(tiles.n, sp, a.nsplit, i0, i1);
   // Tile idx is in LDS, the next one's bytes are under way, and the table's entry of the one after it.  Tiles without a page are passed over.
-  auto block_of = [&](int idx) { return tiles.key<BKV>(min(idx, i1 - 1)) >> 6; };
   Raw raw;
-  int idx = i0, entry = 0;
+  int idx = i0, entry = 0, in1 = 0;  // in1: of the next one, the block in its page
   bool there = false;
+  C4Walk walk = {};                  // the one whose entry is under way
   if (idx < i1) {
-    fetch(c4_of_entry<D>(ca, c4_entry(ca, b, block_of(idx)), h, block_of(idx), there), raw);
-    entry = c4_entry(ca, b, block_of(idx + 1));
+    walk.set(ca, tiles, idx);
+    fetch(c4_of_entry<D>(ca, walk.entry(ca, b), h, walk.in, there), raw);
+    walk.step(ca, tiles, i1);
+    entry = walk.entry(ca, b);
+    in1 = walk.in;
     spread(raw, tiles.key<BKV>(idx), idx < tiles.edge);
   }
   put ^= SLOT;
@@ -876,8 +905,11 @@ __global__ __launch_bounds__(512) void cache_blocks_kernel(WinArgs a, CacheArgs 
   // edge tiles in a loop of their own: with both kinds in one the accumulators are copied tile by tile (250 registers, 1.3 times as slow)
   auto step = [&](auto edge) {
     bool next_there;
-    fetch(c4_of_entry<D>(ca, entry, h, block_of(idx + 1), next_there), raw);  // (past the share: this tile again)
-    entry = c4_entry(ca, b, block_of(idx + 2));
+    fetch(c4_of_entry<D>(ca, entry, h, in1, next_there), raw);  // (past the share: this tile again)
+    const int key1 = walk.t * BKV;
+    walk.step(ca, tiles, i1);
+    entry = walk.entry(ca, b);
+    in1 = walk.in;
     if constexpr (decltype(edge)::value) {
       const int key0 = tiles.key<BKV>(idx);
       if (live && there && key0 <= whi && (key0 + BKV > wlo || key0 < tiles.sink)) {
@@ -918,7 +950,7 @@ __global__ __launch_bounds__(512) void cache_blocks_kernel(WinArgs a, CacheArgs 
     } else {
       if (live && there) att_tile_masked<AttAll, QLOG2, 4, true, false>(smem, qf, ko, vo, st, AttAll{}, a.scale_log2);
     }
-    spread(raw, tiles.key<BKV>(min(idx + 1, i1 - 1)), idx + 1 < tiles.edge);
+    spread(raw, key1, idx + 1 < tiles.edge);
     ko ^= SLOT;
     vo ^= SLOT;
     slot ^= SLOT;
