@@ -440,12 +440,13 @@ __device__ __forceinline__ float c4_scale(uint32_t w) {
 __device__ __forceinline__ u32x4 c4_eight(uint32_t w, float s) {
   return u32x4{c4_pair<0>(w, s), c4_pair<1>(w, s), c4_pair<2>(w, s), c4_pair<3>(w, s)};
 }
-// Two channels (a byte each key) of four keys with exponents e: the channels' four keys, two words each.
-__device__ __forceinline__ void c4_four(uint32_t w, uint32_t e, uint32_t (&lo)[2], uint32_t (&hi)[2]) {
+// Two channels (a byte each key) of four keys with exponents e: the channels' four keys, two words each (the first channel's
+// in lo, or what the selectors of v_perm take).
+__device__ __forceinline__ void c4_four(uint32_t w, uint32_t e, uint32_t (&lo)[2], uint32_t (&hi)[2], uint32_t first = 0x05040100, uint32_t second = 0x07060302) {
   const uint32_t a = c4_pair<0>(w, c4_scale<0>(e)), b = c4_pair<1>(w, c4_scale<1>(e));
   const uint32_t c = c4_pair<2>(w, c4_scale<2>(e)), d = c4_pair<3>(w, c4_scale<3>(e));
-  lo[0] = __builtin_amdgcn_perm(b, a, 0x05040100), hi[0] = __builtin_amdgcn_perm(b, a, 0x07060302);
-  lo[1] = __builtin_amdgcn_perm(d, c, 0x05040100), hi[1] = __builtin_amdgcn_perm(d, c, 0x07060302);
+  lo[0] = __builtin_amdgcn_perm(b, a, first), hi[0] = __builtin_amdgcn_perm(b, a, second);
+  lo[1] = __builtin_amdgcn_perm(d, c, first), hi[1] = __builtin_amdgcn_perm(d, c, second);
 }
 
 // Channels of a row at p: a lane's 8 in bfloat16, 4 and 4 that lie `half` further in float32, so that the lanes of a store cover
@@ -827,13 +828,14 @@ __global__ __launch_bounds__(512) void cache_blocks_kernel(WinArgs a, CacheArgs 
 
   // What this thread brings in: 16 bytes of K, group kg of key kt, or 16 of V, channels vc and vc + 1 of the keys
   // 32 s + 8 vr + 0..7.  The LDS row of key (channel) 8 q + 4 x + j of 32 is 16 x + 4 q + j; K's four units and V's two differ from the
-  // first in an XOR, and the rows of two channels beside each other have one swizzle.
+  // first in an XOR, and the rows of two channels beside each other have one swizzle.  Where j has bit 1 the second channel goes
+  // first: the 16 threads that write together then meet every bank once (in the bytes' own order four times: 676 us, 644 so).
   const bool isv = wave >= 4;
   uint32_t put;
   {
     auto row_of = [](int x) { return (x & 96) | (((x >> 2) & 1) << 4) | (((x >> 3) & 3) << 2) | (x & 3); };
     const int t8 = tid & 255, r = row_of(isv ? c4_tile_channel(t8) : c4_tile_key(t8));
-    put = (uint32_t)(isv ? ATT_K_BYTES + r * ATT_VROW + ((c4_tile_r(t8) ^ att_vswz(r)) << 4)
+    put = (uint32_t)(isv ? ATT_K_BYTES + (r ^ ((t8 >> 1) & 1)) * ATT_VROW + ((c4_tile_r(t8) ^ att_vswz(r)) << 4)
                          : r * 256 + (((4 * c4_tile_group(t8)) ^ (r & 15)) << 4));
   }
   struct Raw {
@@ -862,16 +864,16 @@ __global__ __launch_bounds__(512) void cache_blocks_kernel(WinArgs a, CacheArgs 
         bad[w] = c4_nan_bytes(r.e[w]) >> 7;
         r.e[w] &= ~(bad[w] * 255u);
       }
-      if ((t8 & 15) == 0) *(u32x4*)(smem + 2 * SLOT + (put & SLOT ? 256 : 0) + ((t8 >> 6) * 4 + vr) * 16) = bad;
+      if (c4_tile_j(t8) == 0) *(u32x4*)(smem + 2 * SLOT + (put & SLOT ? 256 : 0) + ((t8 >> 6) * 4 + vr) * 16) = bad;
     }
+    const uint32_t sel = tid & 2 ? 0x07060302u : 0x05040100u;
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
       uint32_t lo[2][2], hi[2][2];
 #pragma unroll
-      for (int w = 0; w < 2; ++w) c4_four(r.w[2 * s + w], r.e[2 * s + w], lo[w], hi[w]);
-      uint8_t* const to = smem + (put ^ (uint32_t)(s << 6));
-      *(u32x4*)to = u32x4{lo[0][0], lo[0][1], lo[1][0], lo[1][1]};
-      *(u32x4*)(to + ATT_VROW) = u32x4{hi[0][0], hi[0][1], hi[1][0], hi[1][1]};
+      for (int w = 0; w < 2; ++w) c4_four(r.w[2 * s + w], r.e[2 * s + w], lo[w], hi[w], sel, sel ^ 0x02020202u);
+      *(u32x4*)(smem + (put ^ (uint32_t)(s << 6))) = u32x4{lo[0][0], lo[0][1], lo[1][0], lo[1][1]};
+      *(u32x4*)(smem + (put ^ (uint32_t)(s << 6) ^ ATT_VROW)) = u32x4{hi[0][0], hi[0][1], hi[1][0], hi[1][1]};
     }
   };
   auto barrier = [&]() {
@@ -996,7 +998,7 @@ __global__ __launch_bounds__(512) void cache_blocks_kernel(WinArgs a, CacheArgs 
 
 // ---------------------------------------------------------------- float32
 // 16 rows a workgroup; a tile of 64 keys is turned into float32 in LDS (rows of K, rows of V^T, 16-byte units at unit ^ (row & 7)), each of
-// the four waves takes 16 of its keys, and the next tile's bytes are under way meanwhile.
+// the four waves takes 16 of its keys, and the next two tiles' bytes are under way meanwhile.
 template <int D, bool VEC, bool SPLIT>
 __global__ __launch_bounds__(256) void cache_f32_kernel(WinArgs a, CacheArgs ca) {
   constexpr int C = D / 16, TK = C4_BLOCK, W = 4, ROWS = 16;
@@ -1058,35 +1060,51 @@ __global__ __launch_bounds__(256) void cache_f32_kernel(WinArgs a, CacheArgs ca)
         *(f32x4*)(smem + HALF + (vc + y) * (TK * 4) + ((unit ^ ((vc + y) & 7)) << 4)) = f32x4{x0[y], x1[y], x2[y], x3[y]};
     }
   };
+  // (a barrier that leaves the loads under way)
+  auto lds_barrier = [&]() {
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt((15 << 0) | (3 << 14) | (7 << 4) | (0 << 8));  // lgkmcnt(0)
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+  };
   WinF32<D> st;
   st.template begin<VEC>(a, seq, tiles, lo1, h, r0 + jq, rows);
-  const uint8_t* at = nullptr;
-  auto find = [&](int idx) {  // the next tile that a page holds
-    for (at = nullptr; idx < i1; ++idx) {
-      at = c4_at<D>(ca, b, h, tiles.key<TK>(idx) >> 6);
-      if (at) break;
-    }
-    return idx;
+  // two tiles' bytes are under way, and the table's entry of the one after them; tiles without a page are passed over
+  Raw raw, raw1;
+  bool there = false, there1 = false;
+  C4Walk walk = {};
+  int entry = 0;
+  auto next = [&](Raw& r, bool& got) {
+    fetch(c4_of_entry<D>(ca, entry, h, walk.in, got), r);
+    walk.step(ca, tiles, i1);
+    entry = walk.entry(ca, b);
   };
-  Raw raw;
-  int idx = find(i0);
-  if (idx < i1) fetch(at, raw);
-  while (idx < i1) {
-    spread(raw);
-    __syncthreads();
-    const int next = find(idx + 1);
-    if (next < i1) fetch(at, raw);
+  if (i0 < i1) {
+    walk.set(ca, tiles, i0);
+    entry = walk.entry(ca, b);
+    next(raw, there);
+    next(raw1, there1);
+  }
+  auto tile = [&](int idx, Raw& r, bool& got) {
+    const bool now = got;
+    spread(r);
+    next(r, got);
+    lds_barrier();
     const int key0 = tiles.key<TK>(idx), k0 = key0 + mine;
     const bool edge = idx < tiles.edge;
-    if (!edge || (k0 <= hi1 && (k0 + 16 > wlo || k0 < tiles.sink))) {
+    if (now && (!edge || (k0 <= hi1 && (k0 + 16 > wlo || k0 < tiles.sink)))) {
       const uint8_t* const kb = smem + (mine + jq) * (D * 4);
       const uint8_t* const vb = smem + HALF + jq * (TK * 4) + ((((mine >> 2) + g) ^ (jq & 7)) << 4);
       st.step([&](int c) { return *(const f32x4*)(kb + (((4 * c + g) ^ (jq & 7)) << 4)); },
               [&](int c) { return *(const f32x4*)(vb + 16 * c * (TK * 4)); }, edge, k0, seq.klen, a.scale_log2);
     }
-    __syncthreads();
-    idx = next;
+    lds_barrier();
+  };
+  for (int idx = i0; idx < i1; idx += 2) {
+    tile(idx, raw, there);
+    if (idx + 1 < i1) tile(idx + 1, raw1, there1);
   }
+  __syncthreads();
   st.template end<VEC, SPLIT>(a, b, h, sp, r0 + jq, rows, (f32x4*)smem, (float*)(smem + SO));
 }
 
@@ -1231,7 +1249,7 @@ static CachePlan cache_plan(int dtype, const track_window& w, int64_t B, int Hk,
   const int64_t blocks = p.nrb * Hk * B;
   int64_t s;
   if (p.form == CachePlan::ROWS) s = cache_rows_split(tiles, blocks, cus);
-  else if (p.form == CachePlan::F32) s = std::min(2 * cus / blocks, tiles / 4);
+  else if (p.form == CachePlan::F32) s = std::min((D == 128 ? 2 : 4) * cus / blocks, tiles / 4);  // as many workgroups as LDS holds
   else s = win_blocks_split(tiles, blocks, rows * Hk * B, cus);
   p.nsplit = (int)std::max<int64_t>(1, std::min<int64_t>(s, 1024));
   return p;

@@ -35,11 +35,15 @@ constexpr uint32_t c4_row_v(int lane, int m) { return (uint32_t)(C4<128>::V + la
 constexpr uint32_t c4_row_ve(int lane, int m) { return (uint32_t)(C4<128>::VE + (lane >> 4) * 16 + 64 * m); }
 
 // Blocks of rows (128 channels): thread t of 256 takes 16 bytes of K and one exponent, another 256 take 16 of V and 16 exponents.
+// V's bytes go to threads in an order that lets 16 of them write to all banks of LDS: 8 bytes j of two r beside each other.
 constexpr int c4_tile_key(int t) { return t >> 2; }            // K: the key, the group
 constexpr int c4_tile_group(int t) { return t & 3; }
-constexpr int c4_tile_channel(int t) { return 32 * (t >> 6) + 2 * (t & 15); }  // V: the two channels' first, r of the keys 32 s + 8 r
-constexpr int c4_tile_r(int t) { return (t >> 4) & 3; }
-constexpr uint32_t c4_tile_codes(bool v, int t) { return (uint32_t)((v ? C4<128>::V : 0) + t * 16); }
+constexpr int c4_tile_j(int t) { return (t & 7) | ((t >> 1) & 8); }            // V: byte j of a group's 16
+constexpr int c4_tile_r(int t) { return ((t >> 3) & 1) | ((t >> 4) & 2); }     // r of the keys 32 s + 8 r
+constexpr int c4_tile_channel(int t) { return 32 * (t >> 6) + 2 * c4_tile_j(t); }  // the two channels' first
+constexpr uint32_t c4_tile_codes(bool v, int t) {
+  return (uint32_t)(v ? C4<128>::V + (t >> 6) * 1024 + c4_tile_r(t) * 256 + c4_tile_j(t) * 16 : t * 16);
+}
 constexpr uint32_t c4_tile_exp(bool v, int t) {
   return (uint32_t)(v ? C4<128>::VE + (t >> 6) * 64 + c4_tile_r(t) * 16 : C4<128>::k_exp(c4_tile_key(t), c4_tile_group(t)));
 }
