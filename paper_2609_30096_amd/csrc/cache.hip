@@ -1000,7 +1000,7 @@ __global__ __launch_bounds__(512) void cache_blocks_kernel(WinArgs a, CacheArgs 
 // 16 rows a workgroup; a tile of 64 keys is turned into float32 in LDS (rows of K, rows of V^T, 16-byte units at unit ^ (row & 7)), each of
 // the four waves takes 16 of its keys, and the next two tiles' bytes are under way meanwhile.
 template <int D, bool VEC, bool SPLIT>
-__global__ __launch_bounds__(256) void cache_f32_kernel(WinArgs a, CacheArgs ca) {
+__global__ __launch_bounds__(256, D == 128 ? 2 : 3) void cache_f32_kernel(WinArgs a, CacheArgs ca) {
   constexpr int C = D / 16, TK = C4_BLOCK, W = 4, ROWS = 16;
   constexpr int HALF = TK * D * 4, NW = D / 32;  // words of codes a thread brings, of K and of V
   constexpr int SO = W * C * 1024, LDS = 2 * HALF > SO + W * 128 ? 2 * HALF : SO + W * 128;
