@@ -50,6 +50,7 @@ struct WinArgs {
   const float* slopes;                // [query heads], or null
   const int32_t *doc_end, *prefix;    // [B][docs], [B][docs + 1], or null
   int docs;
+  bool order;                         // win_place_docs
   float cap_log2, cap_in;             // cap log2(e) (0: none), 2 scale log2(e) / cap
   float* po;          // [nsplit][B][Hk][Lq n][D]: a share's sums
   float2* pml;        // [nsplit][B][Hk][Lq n]: its reference (log2 units) and its denominator
@@ -82,14 +83,16 @@ __device__ __forceinline__ void win_range(const WinArgs& a, const WinSeq& s, int
 
 // The keys [lo, hi] of query i inside its document, those of the document's prefix among them whatever the window's
 // end is; they grow with the position, like the window.  Ends of documents ascend: the last one at or before the
-// position and the first behind it, all in the wave's lanes at once for 64 at most, by halves beyond (a dependent load each).
+// position and the first behind it, all in the wave's lanes at once for 64 at most, by halves beyond (a dependent load each) and
+// where the lanes have sequences of their own (ONE false).
+template <bool ONE = true>
 __device__ __forceinline__ void win_score_range(const WinArgs& a, const WinSeq& s, int i, int& lo, int& hi) {
   win_range(a, s, i, lo, hi);
   if (!a.docs && !a.prefix) return;
   const int p = s.start + i;
   int first = 0, end = INT32_MAX, d = 0;
   const int32_t* const ends = a.doc_end + (int64_t)s.b * a.docs;
-  if (a.docs > 64) {
+  if (!ONE || a.docs > 64) {
     int n = a.docs;  // ends at or before p: d .. d + n
     while (n > 0) {
       const int half = n >> 1;
@@ -288,14 +291,75 @@ __device__ __forceinline__ uint32_t win_keep(int left) { return (uint32_t)((1ull
 // 48 x 32760 131 and 132, 8 of 100003 to 56000 keys 395 and 397, one of 100003 70 and 68).  The last rows of a sequence, which see most keys under a causal
 // mask, start first.
 template <bool LOCAL>
-__device__ __forceinline__ void win_place(const WinArgs& a, int& rb, int& sp, int& h, int& b) {
-  const uint32_t id = LOCAL ? (uint32_t)xcd_remap((int)blockIdx.x, (int)gridDim.x) : blockIdx.x;
+__device__ __forceinline__ void win_place_of(const WinArgs& a, uint32_t id, int& rb, int& sp, int& h, int& b) {
   const uint32_t t = a.by_nrb(id), u = a.by_nsplit(t), v = a.by_inner(u);
   rb = a.nrb - 1 - (int)(id - t * a.nrb);
   sp = (int)(t - u * a.nsplit);
   const int w = (int)(u - v * a.by_inner.d);
   h = LOCAL ? (int)v : w;
   b = LOCAL ? w : (int)v;
+}
+template <bool LOCAL>
+__device__ __forceinline__ void win_place(const WinArgs& a, int& rb, int& sp, int& h, int& b) {
+  win_place_of<LOCAL>(a, LOCAL ? (uint32_t)xcd_remap((int)blockIdx.x, (int)gridDim.x) : blockIdx.x, rb, sp, h, b);
+}
+
+// The same for row blocks of 256 rows inside documents: the workgroups of an XCD take the blocks of their range (up to
+// 256 of them) with the most keys first, by eighths of the most that one has, so that a long one does not start when the others end.
+// 12 heads of 15600 tokens in documents of 3391, 7460 and 4749: 643 us in the rows' order, 544 so (with a cap and a bias 914 and 770).  Each wave counts for itself, four blocks a lane; all get
+// the same numbers, so each block is taken once.
+__device__ __forceinline__ void win_place_docs(const WinArgs& a, int& rb, int& sp, int& h, int& b) {
+  const int q = (int)gridDim.x >> 3, rem = (int)gridDim.x & 7, x = (int)blockIdx.x & 7;
+  const int start = x * q + min(x, rem), n = q + (x < rem);
+  int j = (int)blockIdx.x >> 3, place = j;
+  if (n <= 256) {
+    const int lane = att_lane();
+    int len[4], most = 0;
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+      len[c] = -1;
+      if (64 * c + lane < n) {
+        int r, share, hh, bb, lo, hi, unused;
+        win_place_of<true>(a, (uint32_t)(start + 64 * c + lane), r, share, hh, bb);
+        WinSeq s;
+        s.b = bb;
+        s.qlen = a.q_len ? max(0, min(a.q_len[bb], a.Lq)) : a.Lq;
+        s.klen = a.k_len ? max(0, min(a.k_len[bb], a.Lk)) : a.Lk;
+        s.start = a.q_start ? max(-(int)WIN_MAX, min(a.q_start[bb], (int)WIN_MAX)) : s.klen - s.qlen;
+        s.sink = 0;
+        const int rows = s.qlen * a.n;
+        len[c] = 0;
+        if (r * ATT_BQ < rows) {
+          win_score_range<false>(a, s, (int)a.by_n((uint32_t)(r * ATT_BQ)), lo, unused);
+          win_score_range<false>(a, s, (int)a.by_n((uint32_t)min(r * ATT_BQ + ATT_BQ - 1, rows - 1)), unused, hi);
+          len[c] = max(0, hi - lo + 1);
+        }
+      }
+      most = max(most, len[c]);
+    }
+#pragma unroll
+    for (int o = 32; o >= 1; o >>= 1) most = max(most, __shfl_xor(most, o));
+    const float eighth = 8.0f / (float)(most + 1);
+    int part[4];
+#pragma unroll
+    for (int c = 0; c < 4; ++c) part[c] = len[c] < 0 ? -1 : (int)((float)len[c] * eighth);
+    bool done = false;
+    for (int k = 8; k >= 0 && !done; --k) {  // (8: what rounding may leave at the top)
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        const uint64_t in = __ballot(part[c] == k);
+        const int count = __builtin_popcountll(in);
+        if (!done && j < count) {
+          // the j-th lane of those
+          const int before = __builtin_amdgcn_mbcnt_hi((uint32_t)(in >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)in, 0));
+          place = 64 * c + __builtin_ctzll(__ballot(part[c] == k && before == j));
+          done = true;
+        }
+        if (!done) j -= count;
+      }
+    }
+  }
+  win_place_of<true>(a, (uint32_t)(start + __builtin_amdgcn_readfirstlane(place)), rb, sp, h, b);
 }
 
 // One wave's 16 rows.  step() takes them against 16 keys with v_mfma_f32_16x16x4_f32 (float32

@@ -38,7 +38,8 @@ __global__ __launch_bounds__(512) void window_blocks_kernel(WinArgs a) {
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int jq = lane & 15, g = lane >> 4;
   int rb, sp, h, b;
-  win_place<true>(a, rb, sp, h, b);
+  if (S::ON && a.order) win_place_docs(a, rb, sp, h, b);
+  else win_place<true>(a, rb, sp, h, b);
   const WinSeq seq = win_seq(a, b);
   const int rows = seq.qlen * a.n;
   const int r0 = rb * ATT_BQ;
@@ -965,6 +966,7 @@ static track_status attention_rows(const char* what, int dtype, const track_wind
     // the argument of exp2 in bfloat16 (exp(2 y)), of tanh in float32
     a.cap_in = c->cap > 0.0 ? (float)(dtype == TRACK_DTYPE_BF16 ? 2.0 * log2e * scale / c->cap : scale / c->cap) : 0.0f;
   }
+  a.order = c && c->docs > 0 && p.form == WinPlan::BLOCKS && grid > device_cus() && Lk >= 4096;  // (some 3 us a workgroup)
   ProfScope prof(TRACK_PROF_ATTN_SELF, s);
   const unsigned gr = (unsigned)grid;
 #define TRACK_WIN_F32_OF(DH, C)                                                                             \

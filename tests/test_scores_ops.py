@@ -364,6 +364,58 @@ def test_packed_is_each_alone(dtype):
 
 
 @gpu
+@pytest.mark.parametrize("B,H,Hk,Lq,Lk,docs,right,cap", [
+    (2, 12, 12, 4200, 4200, 3, -1, 0.0),    # workgroups take the documents' blocks longest first: several sequences,
+    (3, 40, 8, 1000, 5000, 7, 0, 30.0),     # shared key heads,
+    (1, 12, 12, 5600, 5700, 70, 0, 0.0),    # more documents than lanes,
+    (8, 12, 12, 5600, 5600, 5, -1, 0.0),    # more blocks an XCD than are put in order
+    (2, 2, 2, 300, 40000, 2, -1, 9.0)])     # shares of the keys
+def test_every_row_of_documents_is_taken(B, H, Hk, Lq, Lk, docs, right, cap):
+    """Queries of zero weigh every key that they see 1 exactly (the cap of 0 is 0), so the log-sum-exp is the log of their number, and
+    V that is 1 in one key in 64 gives an exact count over it: each row once, whatever the order of the workgroups.
+    Errors: the logarithm (2^-23), its factor and the product (2^-24 each); a division and the output's rounding; with a cap
+    5 cap 2^-23 of the logits, of all the same."""
+    import torch
+    say(f"documents {B} {H} {Hk} {Lq} {Lk} {docs}")
+    D, bf = 128, torch.bfloat16
+    q = torch.zeros(B, Lq, H, D, dtype=bf, device="cuda")
+    k = torch.randn(B, Lk, Hk, D, device="cuda", generator=torch.Generator("cuda").manual_seed(3)).to(bf)
+    width = (Lk + 7) // 8 * 8
+    hit = (torch.arange(width, device="cuda")[None, :] - torch.arange(D, device="cuda")[:, None]) % 64 == 0
+    vt = hit.to(bf).expand(B, Hk, D, width).contiguous()
+    rng = np.random.default_rng(docs)
+    ends = np.sort(rng.integers(0, Lk + 1, (B, docs)), axis=1).astype(np.int32)
+    prefix = rng.integers(0, 300, (B, docs + 1)).astype(np.int32)
+    q_len = np.array([Lq - 77 * b for b in range(B)], np.int32)
+    k_len = np.array([Lk - 50 * b for b in range(B)], np.int32)
+    out, lse = torch.full_like(q, 9.0), torch.full((B, H, Lq), 9.0, device="cuda")
+    sc = S(right=right, cap=cap)
+    track.op_attention_scores(sc, q, k, vt, out, lse=lse, workspace=track.attention_scores_workspace(sc, q, k),
+                              **{n: torch.from_numpy(v).cuda() for n, v in
+                                 dict(doc_end=ends, prefix=prefix, q_len=q_len, k_len=k_len).items()})
+    hits = np.concatenate([np.zeros((1, D)), np.cumsum(hit[:, :Lk].cpu().numpy().T, axis=0)])  # of keys before each
+    for b in range(B):
+        lq, lk = int(q_len[b]), int(k_len[b])
+        p = np.arange(lq) + lk - lq
+        bounds = np.concatenate([[0], ends[b].astype(np.int64), [1 << 40]])
+        d = np.searchsorted(ends[b], p, side="right")
+        lo, hi = np.minimum(bounds[d], lk), np.minimum(bounds[d + 1], lk)
+        if right == 0:
+            hi = np.minimum(hi, np.maximum(p + 1, bounds[d] + prefix[b][d]))
+        n = np.maximum(hi - lo, 0)
+        want = (hits[hi] - hits[lo]) / np.maximum(n, 1)[:, None]
+        wlse = np.log(np.maximum(n, 1))
+        got, glse = host(out[b]), host(lse[b])
+        tol = 5 * cap * 2.0 ** -23
+        for h in range(H):
+            _close(got[:lq, h], want, (U[BF16] + 2.0 ** -22 + 2 * tol) * want, f"out {b} {h}")
+            some = n > 0
+            _close(glse[h, :lq][some], wlse[some], 1.01 * 2.0 ** -22 * wlse[some] + tol + 1e-30, f"lse {b} {h}")
+            assert np.all(glse[h, :lq][~some] == -np.inf) and np.all(got[:lq, h][~some] == 0.0)
+        assert np.all(got[lq:] == 9.0) and np.all(glse[:, lq:] == 9.0)
+
+
+@gpu
 @pytest.mark.parametrize("dtype", [BF16, F32])
 @pytest.mark.parametrize("Lq", [1, 90])
 def test_no_keys(dtype, Lq):
