@@ -513,7 +513,7 @@ typedef struct track_cache4 {
   int32_t head_dim;      /* 32, 64 or 128 */
   int32_t table_pages;   /* pages of a sequence; 2^28 tokens at most */
   const int32_t* table;  /* device: page ids, read when a call runs on the stream */
-  int64_t ld_table;      /* entries from sequence to sequence, >= table_pages */
+  int64_t ld_table;      /* entries from sequence to sequence, >= 0 (0: all have the same pages) */
 } track_cache4;
 
 /* Bytes of a page (a multiple of 128), 0 for sizes that are refused. */

@@ -1122,7 +1122,7 @@ static track_status cache_check(const char* what, const track_cache4* c, int64_t
     return fail(TRACK_E_UNSUPPORTED, "%s: pages of %d tokens (multiples of 64 up to 65536), %d heads of %d channels (32, 64, 128)", what,
                 c->page_tokens, c->heads, c->head_dim);
   if (c->n_pages < 1 || c->n_pages > INT32_MAX || c->table_pages < 0 || c->table_pages > WIN_MAX / c->page_tokens ||
-      (B > 1 && c->ld_table < c->table_pages) || c->ld_table < 0)
+      c->ld_table < 0)
     return fail(TRACK_E_SHAPE, "%s: %lld pages, %d of a sequence (2^28 tokens at most), %lld between sequences", what, (long long)c->n_pages,
                 c->table_pages, (long long)c->ld_table);
   if (!c->pages || (c->table_pages && !c->table)) return fail(TRACK_E_INVALID, "%s: null pointer in the cache", what);

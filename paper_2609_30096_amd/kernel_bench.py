@@ -218,6 +218,40 @@ def main():
         seen = [len(set(range(max(0, i - 11), i + 1)) | {0}) for i in range(n - 3, n)]
         window("attn_window_stream", track.Window(left=11, sink=fr, group=fr, scale=ln2), 3 * fr, fr * fr * sum(seen))
     window("attn_window_token", track.Window(scale=ln2), 1, None, 2 * B * L * d * 2)
+    # the same keys and values in the 4-bit cache: in (rotated on the way, out of the fused rows) and back out, then
+    # the three frames and the single tokens on it; and three shots packed in each sequence, with capped logits and a bias
+    # by distance
+    page = 1024
+    each = -(-L // page)
+    table = torch.randperm(B * each, device=dev).to(torch.int32).view(B, each)
+    cache = track.Cache4(H, dh, page, table, n_pages=B * each)
+    first = torch.zeros(B, dtype=torch.int32, device=dev)
+    packed = 2 * M * H * (dh // 2 + dh // 32)
+
+    def append():
+        track.op_cache4_append(cache, heads[:, :, 1], heads[:, :, 2], first, rope=vrope, pos=vpos)
+
+    append()
+    cases["cache4_append"] = (append, None, 2 * M * d * 2 + packed + 3 * 4 * M)
+    cases["cache4_read"] = (lambda: track.op_cache4_read(cache, rq, rk, first), None, 2 * M * d * 2 + packed)
+
+    def cached(name, win, Lq, pairs=None, nbytes=None):
+        q, o = hq[:, L - Lq:], ao.view(B, L, H, dh)[:, L - Lq:]
+        ws = track.attention_cache4_workspace(win, cache, q, L)
+        cases[name] = (lambda: track.op_attention_cache4(win, cache, q, o, Lk=L, workspace=ws),
+                       pairs and 4 * B * H * dh * pairs, nbytes)
+
+    if L % fr == 0:
+        cached("attn_cache4_stream", track.Window(left=11, sink=fr, group=fr, scale=ln2), 3 * fr, fr * fr * sum(seen))
+    cached("attn_cache4_token", track.Window(scale=ln2), 1, None, packed)
+    ends = torch.tensor([[L // 4, L // 2 + L // 8]] * B, dtype=torch.int32, device=dev)
+    shots = [L // 4, L // 2 + L // 8 - L // 4, L - (L // 2 + L // 8)]
+    scores = track.Scores(right=-1, cap=30.0, scale=ln2)
+    slopes = 2.0 ** (-8.0 * (torch.arange(H, device=dev) + 1.0) / H) / fr
+    sws = track.attention_scores_workspace(scores, hq, hk)
+    cases["attn_scores_shots"] = (lambda: track.op_attention_scores(
+        scores, hq, hk, vt, ao.view(B, L, H, dh), slopes=slopes, doc_end=ends, workspace=sws),
+        4 * B * H * dh * sum(n * n for n in shots), None)
     only = set(a.only.split(",")) if a.only else None
     results = []
     for name, (fn, flops, nbytes) in cases.items():

@@ -856,11 +856,19 @@ class Cache4:
         if pages.get_device() != table.get_device():
             raise TypeError(f"pages on {pages.device} beside a table on {table.device}")
         self.heads, self.head_dim, self.page_tokens = heads, head_dim, page_tokens
-        self.pages, self.table = pages, table
+        self._pages, self._table = pages, table  # (their addresses are taken below)
         self.tokens = table.shape[1] * page_tokens  # places of a sequence
         self.c = Cache4C(pages.data_ptr(), pages.shape[0], page_tokens, heads, head_dim, table.shape[1],
-                         table.data_ptr(), max(table.stride(0), table.shape[1]) if table.shape[0] > 1 else table.shape[1])
+                         table.data_ptr(), table.stride(0) if table.shape[0] > 1 else table.shape[1])
         self.layouts = tuple({} for _ in range(5))
+
+    @property
+    def pages(self):
+        return self._pages
+
+    @property
+    def table(self):
+        return self._table
 
     def _rows(self, k, v, start, n, pos, freqs):
         B, L, H, D = k.shape if k.dim() == 4 else (0, 0, 0, 0)

@@ -96,8 +96,7 @@ def _cache_c(**kw):
 BAD_CACHES = [(track.E_UNSUPPORTED, kw) for kw in (dict(page_tokens=0), dict(page_tokens=32), dict(page_tokens=100),
                                                    dict(page_tokens=-64), dict(page_tokens=131072), dict(heads=0),
                                                    dict(heads=(1 << 19) + 1), dict(head_dim=96), dict(head_dim=256))] + \
-    [(track.E_SHAPE, kw) for kw in (dict(n_pages=0), dict(n_pages=1 << 31), dict(table_pages=-1), dict(ld_table=19),
-                                    dict(ld_table=-1), dict(table_pages=(1 << 22) + 1, ld_table=1 << 30),
+    [(track.E_SHAPE, kw) for kw in (dict(n_pages=0), dict(n_pages=1 << 31), dict(table_pages=-1), dict(ld_table=-1), dict(table_pages=(1 << 22) + 1, ld_table=1 << 30),
                                     dict(table_pages=1 << 30, page_tokens=65536, ld_table=1 << 30))] + \
     [(track.E_INVALID, kw) for kw in (dict(pages=0), dict(table=0), dict(pages=P + 64), dict(table=P + 2))]
 
@@ -248,6 +247,10 @@ def test_binding_refusals():
         with pytest.raises((ValueError, TypeError), match=match):
             cache._queries(**dict(dict(q=q, out=out, lse=None, q_len=None, k_len=None, q_start=None, workspace=None), **kw))
     table = cache.table
+    for name in ("pages", "table"):  # their addresses are the cache's
+        with pytest.raises(AttributeError):
+            setattr(cache, name, None)
+    assert track.Cache4(2, 128, 64, table[:1].expand(3, -1), n_pages=4).c.ld_table == 0
     for kw in (dict(table=table.long()), dict(table=table[0]), dict(table=torch.zeros(2, 6, dtype=torch.int32)[:, ::2]),
                dict(n_pages=None), dict(pages=cache.pages[:, 1:]), dict(pages=cache.pages.int()), dict(pages=cache.pages, n_pages=3),
                dict(head_dim=80), dict(page_tokens=100)):
@@ -683,10 +686,14 @@ def test_attention_strides(dtype, Lq):
         track.op_attention_cache4(win, cache, odd(c.tq), out, Lk=Lk, workspace=track.attention_cache4_workspace(win, cache, c.tq, Lk))
         assert np.array_equal(host(out), want)
     c.table[:] = c.table[0]
+    one = track.Cache4(Hk, D, 64, c.cache.table[:1].expand(B, -1), c.cache.pages)  # one row of the table for all
+    shared = torch.zeros_like(c.out)
+    track.op_attention_cache4(win, one, c.tq, shared, Lk=Lk, workspace=track.attention_cache4_workspace(win, one, c.tq, Lk))
     c.cache.table.copy_(torch.from_numpy(c.table))
     c.k[:], c.v[:] = c.k[0], c.v[0]
     got, lse = c.run(win)
     _check(c, win, got, lse)
+    assert np.array_equal(host(shared), got)
 
 
 @gpu
