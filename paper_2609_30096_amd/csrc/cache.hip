@@ -1067,7 +1067,7 @@ __global__ __launch_bounds__(256, D == 128 ? 2 : 3) void cache_f32_kernel(WinArg
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
   };
-  WinF32<D> st;
+  WinF32<D, false, true> st;
   st.template begin<VEC>(a, seq, tiles, lo1, h, r0 + jq, rows);
   // two tiles' bytes are under way, and the table's entry of the one after them; tiles without a page are passed over
   Raw raw, raw1;
@@ -1116,7 +1116,7 @@ int64_t cache4_page_bytes(int heads, int head_dim, int page_tokens) {
   return (int64_t)(page_tokens / C4_BLOCK) * heads * 68 * head_dim;
 }
 
-static track_status cache_check(const char* what, const track_cache4* c, int64_t B, CacheArgs* a) {
+static track_status cache_check(const char* what, const track_cache4* c, CacheArgs* a) {
   if (!c) return fail(TRACK_E_INVALID, "%s: null cache", what);
   if (!cache4_page_bytes(c->heads, c->head_dim, c->page_tokens))
     return fail(TRACK_E_UNSUPPORTED, "%s: pages of %d tokens (multiples of 64 up to 65536), %d heads of %d channels (32, 64, 128)", what,
@@ -1158,7 +1158,7 @@ static track_status cache_rows(const char* what, bool read, int dtype, const tra
                                hipStream_t s) {
   if (dtype != TRACK_DTYPE_F32 && dtype != TRACK_DTYPE_BF16) return fail(TRACK_E_INVALID, "%s: bad dtype %d", what, dtype);
   RowsArgs a = {};
-  const track_status st = cache_check(what, cache, B, &a.c);
+  const track_status st = cache_check(what, cache, &a.c);
   if (st != TRACK_OK) return st;
   const int D = cache->head_dim;
   const int64_t width = (int64_t)cache->heads * D;
@@ -1279,7 +1279,7 @@ track_status attention_cache4(int dtype, const track_window* w, const track_cach
                               const int32_t* q_len, const int32_t* k_len, const int32_t* q_start, void* ws, size_t ws_bytes,
                               hipStream_t s) {
   CacheArgs ca = {};
-  track_status st = cache_check("attention_cache4", cache, B, &ca);
+  track_status st = cache_check("attention_cache4", cache, &ca);
   if (st != TRACK_OK) return st;
   const int Hk = cache->heads, D = cache->head_dim;
   st = win_check("attention_cache4", dtype, w, B, H, Hk, D, Lq, Lk);

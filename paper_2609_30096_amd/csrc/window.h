@@ -366,7 +366,8 @@ __device__ __forceinline__ void win_place_docs(const WinArgs& a, int& rb, int& s
 // products and sums): lane (jq, g) has row jq, kfrag(c) is channels 16 c + 4 g .. + 3 of key jq,
 // vfrag(c) keys 4 g .. + 3 of channel 16 c + jq, and the logits that a lane holds (keys 4 g .. + 3
 // of its row) are the "B" operand of O^T += V^T P^T as they are.
-template <int D, bool SCORED = false>
+// REACH: a V without a number reaches the rows that see its key whatever the weight, also one that fell to zero.
+template <int D, bool SCORED = false, bool REACH = false>
 struct WinF32 {
   static constexpr int C = D / 16;
   f32x4 qf[C], o[C];
@@ -452,7 +453,9 @@ struct WinF32 {
 #pragma unroll 1
           for (int gg = 0; gg < 4; ++gg) {
             const float p = __shfl(x[e], jq + 16 * gg);
-            const uint32_t on = p != 0.0f ? 0xffffffffu : 0u;  // V times 0 where the weight is 0
+            const int key = key0 + 4 * gg + e;
+            const bool weighed = REACH ? !((key > hi) | ((key < lo) & (key >= sink))) : p != 0.0f;
+            const uint32_t on = weighed ? 0xffffffffu : 0u;  // V times 0 where the weight is 0
 #pragma unroll
             for (int c = 0; c < C; ++c)
 #pragma unroll

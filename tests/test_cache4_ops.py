@@ -631,6 +631,33 @@ def test_groups_without_a_number(dtype, Lq, Lk):
 
 @gpu
 @pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("Lq", [1, 4, 100])
+def test_a_weight_that_falls_to_zero(dtype, Lq):
+    """A NaN group of V whose key is seen reaches the rows, though the key's weight is below every float32, in a tile that
+    all rows see whole and in one at the end."""
+    import torch
+    c = Case(dtype, 1, 4, 2, Lq, 230)
+    c.tq = c.tq.abs()
+    rows = np.arange(Lq) + 230 - Lq
+    for x in (70, 229, 230 - Lq):
+        page = c.table[0, x // 64]
+        block = c.pool.raw[page, 0]
+        at = c.pool._at(x % 64)
+        kept = block.copy()
+        block[:, at[0]] = 0xff           # -6 2^4 in every channel: logits below -500
+        block[:, at[2]] = 131
+        block[:, at[3][1]] = 255         # V: channels 32..63
+        c.cache.pages[page] = torch.from_numpy(c.pool.raw[page].reshape(-1).copy()).cuda()
+        got, _ = c.run(W())
+        nan = np.zeros(got.shape, bool)
+        nan[0, rows >= x, :, 32:64] = True
+        assert np.array_equal(np.isnan(got), nan), x
+        block[:] = kept
+        c.cache.pages[page] = torch.from_numpy(c.pool.raw[page].reshape(-1).copy()).cuda()
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [BF16, F32])
 @pytest.mark.parametrize("Lq", [1, 20, 300])
 @pytest.mark.parametrize("scale", [4.0, 12.0])
 def test_large_logits(dtype, Lq, scale):
