@@ -81,16 +81,10 @@ __device__ __forceinline__ const uint8_t* c4_of_entry(const CacheArgs& c, int en
 
 // ---------------------------------------------------------------- rounding to 4 bits
 // The exponent byte of a group whose largest magnitude is m (255: an infinity or a NaN in it).
-__device__ __forceinline__ int c4_exponent(double m) {
-  const uint32_t hi = (uint32_t)(__builtin_bit_cast(uint64_t, m) >> 32);
-  const int x = (int)(hi >> 20) - 1023;                    // m = f 2^x, f in [1, 2)
-  const int e = x - 2 + ((hi & 0xfffff) >= 0xc0000);       // 7 2^(x - 2) = 1.75 2^x
-  return x == 1024 ? 255 : 127 + min(max(e, C4_MIN), C4_MAX);
-}
 __device__ __forceinline__ int c4_exponent(float m) {
   const uint32_t w = __float_as_uint(m);
-  const int x = (int)(w >> 23) - 127;
-  const int e = x - 2 + ((w & 0x7fffff) >= 0x600000);
+  const int x = (int)(w >> 23) - 127;                      // m = f 2^x, f in [1, 2)
+  const int e = x - 2 + ((w & 0x7fffff) >= 0x600000);      // 7 2^(x - 2) = 1.75 2^x
   return x == 128 ? 255 : 127 + min(max(e, C4_MIN), C4_MAX);
 }
 
@@ -100,14 +94,6 @@ __device__ __forceinline__ uint32_t c4_codes(const float (&x)[8], float s) {
   w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[2], x[3], s, 1);
   w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[4], x[5], s, 2);
   return __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[6], x[7], s, 3);
-}
-
-// The code of x at the power of two whose reciprocal is given, ties to the even code (x is finite).
-__device__ __forceinline__ uint32_t c4_code(double x, double inv) {
-  const double y = fabs(x) * inv;  // exact
-  const double f = y < 2.0 ? 2.0 : (y < 4.0 ? 1.0 : 0.5);
-  const double q = rint(y * f) + (y < 2.0 ? 0.0 : (y < 4.0 ? 2.0 : 4.0));
-  return (uint32_t)fmin(q, 7.0) | ((uint32_t)(__builtin_bit_cast(uint64_t, x) >> 60) & 8u);
 }
 
 // The largest of four lanes beside each other.
@@ -208,15 +194,14 @@ __device__ __forceinline__ void c4_settle() {
 
 // Appends.  A workgroup takes 16 tokens of a block, forms their angles once, and its waves walk the heads; a lane has 8 channels of a
 // token, D / 8 lanes a token.  Codes and exponents change places through LDS into the order of the cache, and leave in 16-byte units.
-// A key is what its rotation in float64 rounds to: next to the border of two codes float32 would fall to either (one in some 10^6, a whole
-// step off).  The rotation is float32 all the same: it is off by at most 4e-7 of the pair's length (angle reduced in float64 and
-// rounded once, sine and cosine 2 units, two products and a sum), below D = 2^-20 of the largest value that goes into the lane's group, and where x - D and x + D
-// round to the same code, and the group's largest value to the same exponent, that is the key's.  Elsewhere (one wave's step in a hundred) the wave takes the step
-// again in float64.
+// A key is what its rotation in float64 rounds to: float32 would fall to either side of a border of two codes (one value in some
+// 10^6, a whole step off).  Sines, cosines, products and sum are float64, which this chip's vector units multiply and add at float32's rate; the float32
+// value that the conversion to 4 bits takes is off the sum by its own rounding, which matters only where it meets a border, a number
+// of at most three bits.  There it moves on to the next one on the sum's side.
 template <typename T, int D, int ROT>
 __global__ __launch_bounds__(256) void cache_append_kernel(RowsArgs a) {
   constexpr int LPT = D / 8, TPS = 64 / LPT, STEPS = 16 / TPS, G = D / 32;
-  __shared__ float2 cs[ROT ? 16 * (D / 2) : 1];
+  __shared__ double2 cs[ROT ? 16 * (D / 2) : 1];
   __shared__ __attribute__((aligned(16))) uint32_t kcodes[4][16 * LPT], vcodes[4][16 * LPT];
   __shared__ __attribute__((aligned(16))) uint8_t kexp[4][16 * G], vexp[4][16 * G];  // in the cache's order
   const int lane = threadIdx.x & 63;
@@ -237,12 +222,12 @@ __global__ __launch_bounds__(256) void cache_append_kernel(RowsArgs a) {
   if constexpr (ROT != 0) {
     for (int i = threadIdx.x; i < 16 * (D / 2); i += 256) {
       const int slot = i / (D / 2), p = i % (D / 2);
-      float sn = 0.0f, cn = 1.0f;  // copied channels
+      double sn = 0.0, cn = 1.0;  // copied channels
       if (p < a.pairs && (w.there >> slot & 1)) {
-        sincospif((float)turns_of(slot, p), &sn, &cn);
-        sn *= (float)a.amp, cn *= (float)a.amp;
+        sincospi(turns_of(slot, p), &sn, &cn);
+        sn *= a.amp, cn *= a.amp;
       }
-      cs[i] = float2{cn, sn};
+      cs[i] = double2{cn, sn};
     }
     __syncthreads();
   }
@@ -278,7 +263,6 @@ __global__ __launch_bounds__(256) void cache_append_kernel(RowsArgs a) {
       rk[st].load(kp[st] + 8 * u, a.vec);
       rv[st].load((const T*)a.v + w.b * a.sv + row * a.ldv + (int64_t)h * D + 8 * u, a.vec);
     }
-    uint32_t again = 0;  // steps with a value near a border
 #pragma unroll
     for (int st = 0; st < STEPS; ++st) {
       const int slot = st * TPS + sub;
@@ -308,15 +292,13 @@ __global__ __launch_bounds__(256) void cache_append_kernel(RowsArgs a) {
             z[i] = ldf(kp[st] + (ch < a.pairs ? ch + a.pairs : (ch < 2 * a.pairs ? ch - a.pairs : ch)));
           }
         }
-        float y[8], lo[8], hi[8];
-        const float2* const at = cs + slot * (D / 2);
-        const uint32_t in = c4_quad_max(max(c4_top(x), c4_top(z)));
-        const float off = __uint_as_float(in) * (9.5367431640625e-7f * fabsf((float)a.amp));
-        auto turn = [&](int i, const float2& t, bool low, bool rotated) {
-          y[i] = fmaf(x[i], t.x, z[i] * (low ? -t.y : t.y));
-          y[i] = rotated ? y[i] : x[i];
-          const float d = !rotated || (t.y == 0.0f && t.x == 1.0f) ? 0.0f : off;  // by angle 0 a key stays as it is, ties included
-          lo[i] = y[i] - d, hi[i] = y[i] + d;
+        double r[8];
+        float y[8];
+        const double2* const at = cs + slot * (D / 2);
+        auto turn = [&](int i, const double2& t, bool low, bool rotated) {
+          r[i] = (double)x[i] * t.x + (double)(low ? -z[i] : z[i]) * t.y;
+          y[i] = rotated ? (float)r[i] : x[i];
+          r[i] = rotated ? r[i] : (double)x[i];
         };
         if (ROT == 2 && whole) {
 #pragma unroll
@@ -330,12 +312,17 @@ __global__ __launch_bounds__(256) void cache_append_kernel(RowsArgs a) {
             turn(i, at[min(p, D / 2 - 1)], low, p < a.pairs);
           }
         }
-        const float top = __uint_as_float(c4_quad_max(c4_top(y)));
-        byte = c4_exponent(top + off);
-        const float s = __uint_as_float((uint32_t)byte << 23);
-        word = c4_codes(lo, s);
-        const uint32_t differ = word ^ c4_codes(hi, s);
-        if (__ballot((byte != c4_exponent(fmaxf(top - off, 0.0f)) || byte == 255 || (differ != 0 && in != 0)) && (w.there >> slot & 1))) again |= 1u << st;
+        uint32_t few = ~0u;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) few = min(few, __float_as_uint(y[i]) << 12);
+        if (__ballot(few == 0)) {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            const double d = fabs((double)y[i]), m = fabs(r[i]);
+            y[i] = __uint_as_float(__float_as_uint(y[i]) + (m < d ? ~0u : (m > d ? 1u : 0u)));  // (not a NaN)
+          }
+        }
+        word = c4_round8(y, byte);
       }
       kcodes[wave][slot * LPT + u] = word;
       if ((u & 3) == 0) kexp[wave][kexp_at(u, slot)] = (uint8_t)byte;
@@ -343,48 +330,6 @@ __global__ __launch_bounds__(256) void cache_append_kernel(RowsArgs a) {
       vcodes[wave][slot * LPT + u] = c4_round8(x, byte);
       if ((u & 3) == 0) vexp[wave][16 * (u >> 2) + slot] = (uint8_t)byte;
       if (ROT == 2) __builtin_amdgcn_sched_barrier(0);
-    }
-    if constexpr (ROT != 0) {
-#pragma unroll 1
-      for (; again; again &= again - 1) {
-        const int un = att_lane() % LPT, slot = __builtin_ctz(again) * TPS + att_lane() / LPT;
-        const bool there = w.there >> slot & 1;
-        const T* const p0 = (const T*)a.k + w.b * a.sk + (there ? w.row(slot) : 0) * a.ldk + (int64_t)h * D;
-        C4Unit<T> unit;
-        float x[8];
-        unit.load(p0 + 8 * un, a.vec);
-        unit.get(x);
-        double r[8], sn = 0.0, cn = 1.0, m = 0.0;
-        bool odd = false;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const int ch = 8 * un + i;
-          bool low;
-          const int p = pair_of(un, i, low);
-          if (ROT == 2 || low) {  // (interleaved: the second channel has the first one's)
-            sn = 0.0, cn = 1.0;
-            if (there && p < a.pairs) sincospi(turns_of(slot, p), &sn, &cn);
-            sn *= a.amp, cn *= a.amp;
-          }
-          r[i] = x[i];
-          if (p < a.pairs) {
-            const double z = ROT == 1 ? x[i ^ 1] : ldf(p0 + (low ? ch + a.pairs : ch - a.pairs));
-            r[i] = low ? x[i] * cn - z * sn : z * sn + x[i] * cn;
-          }
-          odd |= !(fabs(r[i]) <= 1.7976931348623157e308);  // an infinity or a NaN
-          m = fmax(m, fabs(r[i]));
-          if (ROT == 2) __builtin_amdgcn_sched_barrier(0);  // eight angles side by side would take 100 registers more
-        }
-        // the largest exponent of the four lanes is that of the largest magnitude
-        const int byte = (int)c4_quad_max((uint32_t)(odd ? 255 : c4_exponent(m)));
-        const double inv = __builtin_bit_cast(double, (uint64_t)(1023 + 127 - byte) << 52);
-        uint32_t word = 0;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) word |= c4_code(r[i], inv) << (4 * i);
-        if (byte == 255) word = 0;
-        kcodes[wave][slot * LPT + un] = word;
-        if ((un & 3) == 0) kexp[wave][kexp_at(un, slot)] = (uint8_t)byte;
-      }
     }
     c4_settle();
     if (lane < D / 2) {
