@@ -192,12 +192,16 @@ __device__ __forceinline__ void c4_settle() {
   __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
 }
 
-// Appends.  A workgroup takes 16 tokens of a block, forms their angles once, and its waves walk the heads; a lane has 8 channels of a
-// token, D / 8 lanes a token.  Codes and exponents change places through LDS into the order of the cache, and leave in 16-byte units.
-// A key is what its rotation in float64 rounds to: float32 would fall to either side of a border of two codes (one value in some
-// 10^6, a whole step off).  Sines, cosines, products and sum are float64, which this chip's vector units multiply and add at float32's rate; the float32
-// value that the conversion to 4 bits takes is off the sum by its own rounding, which matters only where it meets a border, a number
-// of at most three bits.  There it moves on to the next one on the sum's side.
+// Appends.  A workgroup takes 16 tokens of a block, forms their angles once while its first rows are under way, and its waves walk the
+// heads; a lane has 8 channels of a token, D / 8 lanes a token.  Codes and exponents change places through LDS into the order of the
+// cache, and leave in 16-byte units.  A key is what its rotation in float64 rounds to: float32 would fall to either side of a border of two
+// codes (one value in some 10^6, a whole step off).  Sines, cosines, products and sum are float64, which the vector units multiply and
+// add at float32's rate; the float32 value that the conversion to 4 bits takes is off the sum by its own rounding, which matters only where
+// it meets a border, a number of at most three bits.  There it moves on to the next one on the sum's side.  (In float32 with a margin and
+// float64 again where that held a border: 132 us for the three axes below, 184 for halves.)
+// What bounds it: memory, and the conversions, whose time shows beside it.  2 x 32760 tokens of 12 heads: bfloat16 as they are 107 us (4.8
+// TB/s), turned on three axes 115, as halves 124, float32 on three axes 191 (4.8).  Angles in the order of the pairs instead of the lanes':
+// halves 145; rows only after the angles: 117, one head 28 instead of 26.
 template <typename T, int D, int ROT>
 __global__ __launch_bounds__(256) void cache_append_kernel(RowsArgs a) {
   constexpr int LPT = D / 8, TPS = 64 / LPT, STEPS = 16 / TPS, G = D / 32;
@@ -214,20 +218,47 @@ __global__ __launch_bounds__(256) void cache_append_kernel(RowsArgs a) {
   // the lane that has the other channels of this one's pairs (half layout), if they are a unit
   const bool whole = ROT == 2 && (a.pairs & 7) == 0;
   const int other = (8 * u < a.pairs ? a.pairs : (8 * u < 2 * a.pairs ? -a.pairs : 0)) / 8;
-  auto turns_of = [&](int slot, int p) {
-    const int axis = (p >= a.sec0) + (p >= a.sec1);
-    const double t = (double)a.pos[((int64_t)axis * a.B + w.b) * a.L + w.row(slot)] * (a.freqs[p] * 0.15915494309189533577);
-    return 2.0 * (t - rint(t));
+  // a head's rows; the first ones are under way while the angles are formed
+  const T* kp[STEPS];
+  C4Unit<T> rk[STEPS], rv[STEPS];
+  auto fetch = [&](int h) {
+#pragma unroll
+    for (int st = 0; st < STEPS; ++st) {
+      const int slot = st * TPS + sub;
+      const int64_t row = w.there >> slot & 1 ? w.row(slot) : 0;  // (any row of the sequence in a slot without one)
+      kp[st] = (const T*)a.k + w.b * a.sk + row * a.ldk + (int64_t)h * D;
+      rk[st].load(kp[st] + 8 * u, a.vec);
+      rv[st].load((const T*)a.v + w.b * a.sv + row * a.ldv + (int64_t)h * D + 8 * u, a.vec);
+    }
   };
+  const int h0 = part * 4 + wave;
+  if (h0 < a.heads) fetch(h0);
+  // a pair's place among those of a token: the first ones of all lanes beside each other, so that a read meets no bank twice
+  constexpr int PER = ROT == 1 ? 4 : 8;
+  auto angle_at = [](int p) { return (p & (PER - 1)) * (D / 2 / PER) + p / PER; };
   if constexpr (ROT != 0) {
-    for (int i = threadIdx.x; i < 16 * (D / 2); i += 256) {
-      const int slot = i / (D / 2), p = i % (D / 2);
+    // thread: pair p of every (512 / D)-th slot
+    constexpr int N = D / 32;
+    const int p = threadIdx.x % (D / 2), s0 = threadIdx.x / (D / 2);
+    const bool rotated = p < a.pairs;
+    const int axis = (p >= a.sec0) + (p >= a.sec1);
+    const double f = a.freqs[rotated ? p : 0] * 0.15915494309189533577;
+    const int32_t* const pp = a.pos + ((int64_t)(rotated ? axis : 0) * a.B + w.b) * a.L;
+    int at[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int slot = s0 + i * (512 / D);
+      at[i] = pp[w.there >> slot & 1 ? w.row(slot) : 0];
+    }
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
       double sn = 0.0, cn = 1.0;  // copied channels
-      if (p < a.pairs && (w.there >> slot & 1)) {
-        sincospi(turns_of(slot, p), &sn, &cn);
+      if (rotated) {
+        const double t = (double)at[i] * f;
+        sincospi(2.0 * (t - rint(t)), &sn, &cn);
         sn *= a.amp, cn *= a.amp;
       }
-      cs[i] = double2{cn, sn};
+      cs[(s0 + i * (512 / D)) * (D / 2) + angle_at(p)] = double2{cn, sn};
     }
     __syncthreads();
   }
@@ -244,25 +275,15 @@ __global__ __launch_bounds__(256) void cache_append_kernel(RowsArgs a) {
   };
   // the lane's pairs where its unit is all first channels, all second ones or all copied
   const bool low0 = 8 * u < a.pairs;
-  const int first = low0 ? 8 * u : min(8 * u - a.pairs, D / 2 - 8);
+  const int first = min(low0 ? u : u - a.pairs / 8, D / 16 - 1);
   // the exponent's place in the cache's order: K [4 c][G][2 s][2 h], V [G][2 s][8 c]
   auto kexp_at = [&](int un, int slot) {
     const int c = slot & 7;
     return (c & 3) * (4 * G) + 4 * (un >> 2) + 2 * (slot >> 3) + (c >> 2);
   };
   const bool all = w.there == 0xffff;
-  for (int h = part * 4 + wave; h < a.heads; h += 4 * a.hsplit) {
+  for (int h = h0; h < a.heads; h += 4 * a.hsplit) {
     uint8_t* const to = block + (int64_t)h * C4<D>::BYTES;
-    const T* kp[STEPS];
-    C4Unit<T> rk[STEPS], rv[STEPS];
-#pragma unroll
-    for (int st = 0; st < STEPS; ++st) {
-      const int slot = st * TPS + sub;
-      const int64_t row = w.there >> slot & 1 ? w.row(slot) : 0;  // (any row of the sequence in a slot without one)
-      kp[st] = (const T*)a.k + w.b * a.sk + row * a.ldk + (int64_t)h * D;
-      rk[st].load(kp[st] + 8 * u, a.vec);
-      rv[st].load((const T*)a.v + w.b * a.sv + row * a.ldv + (int64_t)h * D + 8 * u, a.vec);
-    }
 #pragma unroll
     for (int st = 0; st < STEPS; ++st) {
       const int slot = st * TPS + sub;
@@ -302,14 +323,14 @@ __global__ __launch_bounds__(256) void cache_append_kernel(RowsArgs a) {
         };
         if (ROT == 2 && whole) {
 #pragma unroll
-          for (int i = 0; i < 8; ++i) turn(i, at[first + i], low0, 8 * u < 2 * a.pairs);
+          for (int i = 0; i < 8; ++i) turn(i, at[first + i * (D / 16)], low0, 8 * u < 2 * a.pairs);
         } else {
           const int un = ROT == 2 ? att_lane() % LPT : u;  // (formed here: eight pairs' places would stay in registers)
 #pragma unroll
           for (int i = 0; i < 8; ++i) {
             bool low;
             const int p = pair_of(un, i, low);
-            turn(i, at[min(p, D / 2 - 1)], low, p < a.pairs);
+            turn(i, at[ROT == 1 ? (i >> 1) * (D / 8) + u : angle_at(min(p, D / 2 - 1))], low, p < a.pairs);
           }
         }
         uint32_t few = ~0u;
@@ -363,6 +384,7 @@ __global__ __launch_bounds__(256) void cache_append_kernel(RowsArgs a) {
       }
     }
     c4_settle();
+    if (h + 4 * a.hsplit < a.heads) fetch(h + 4 * a.hsplit);
   }
 }
 
