@@ -201,7 +201,8 @@ __device__ __forceinline__ void c4_settle() {
 // float64 again where that held a border: 132 us for the three axes below, 184 for halves.)
 // What bounds it: memory, and the conversions, whose time shows beside it.  2 x 32760 tokens of 12 heads: bfloat16 as they are 107 us (4.8
 // TB/s), turned on three axes 115, as halves 124, float32 on three axes 191 (4.8).  Angles in the order of the pairs instead of the lanes':
-// halves 145; rows only after the angles: 117, one head 28 instead of 26.
+// halves 145; rows only after the angles: 117, one head 28 instead of 26.  A token for each of 16 sequences takes 6.2 us, a chain of
+loads and one of sines (8.3 where absent tokens were turned too).
 template <typename T, int D, int ROT>
 __global__ __launch_bounds__(256) void cache_append_kernel(RowsArgs a) {
   constexpr int LPT = D / 8, TPS = 64 / LPT, STEPS = 16 / TPS, G = D / 32;
@@ -253,7 +254,7 @@ __global__ __launch_bounds__(256) void cache_append_kernel(RowsArgs a) {
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       double sn = 0.0, cn = 1.0;  // copied channels
-      if (rotated) {
+      if (rotated && (w.there >> (s0 + i * (512 / D)) & 1)) {
         const double t = (double)at[i] * f;
         sincospi(2.0 * (t - rint(t)), &sn, &cn);
         sn *= a.amp, cn *= a.amp;
@@ -286,6 +287,7 @@ __global__ __launch_bounds__(256) void cache_append_kernel(RowsArgs a) {
     uint8_t* const to = block + (int64_t)h * C4<D>::BYTES;
 #pragma unroll
     for (int st = 0; st < STEPS; ++st) {
+      if (!(w.there >> (st * TPS) & ((1u << TPS) - 1u))) continue;  // (a single token's wave has one such step)
       const int slot = st * TPS + sub;
       float x[8];
       uint32_t word;
