@@ -42,8 +42,9 @@ __device__ __forceinline__ uint8_t* c4_at(const CacheArgs& c, int b, int h, int 
   return c.pages + c4_block(page, c.blocks, t, slot, c.stride) + (int64_t)h * C4<D>::BYTES;
 }
 
-// Tiles in their order, the block of 64 places and the table's entry of each from the last one's: tiles seen whole lie one after
-// another but for the step from the first tokens to the window (by division 60 scalar instructions a tile, a fifth of a tile's time).
+// Tiles in their order, the block of 64 places and the table's entry of each from the last one's: tiles seen whole lie one
+// after another but for the step from the first tokens to the window (by division 60 scalar instructions a tile, a fifth of a
+// tile's time).
 struct C4Walk {
   int idx, t, slot, in;  // the tile's place in the order, its block, the entry, the block in the page
   template <class Tiles>
@@ -88,7 +89,8 @@ __device__ __forceinline__ int c4_exponent(float m) {
   return x == 128 ? 255 : 127 + min(max(e, C4_MIN), C4_MAX);
 }
 
-// Eight channels' codes at scale 2^e, given as its float (exact for float32 values: the conversion rounds once, ties to the even code).
+// Eight channels' codes at scale 2^e, given as its float (exact for float32 values: the conversion rounds once, ties to the
+// even code).
 __device__ __forceinline__ uint32_t c4_codes(const float (&x)[8], float s) {
   uint32_t w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(0, x[0], x[1], s, 0);
   w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[2], x[3], s, 1);
@@ -110,7 +112,8 @@ __device__ __forceinline__ uint32_t c4_top(const float (&x)[8]) {
   return m;
 }
 
-// Four bytes of codes of the lane's 8 channels, and the exponent byte of the group that they and those of the 3 lanes beside it make.
+// Four bytes of codes of the lane's 8 channels, and the exponent byte of the group that they and those of the 3 lanes beside
+// it make.
 __device__ __forceinline__ uint32_t c4_round8(const float (&x)[8], int& byte) {
   byte = c4_exponent(__uint_as_float(c4_quad_max(c4_top(x))));
   const uint32_t w = c4_codes(x, __uint_as_float((uint32_t)byte << 23));
@@ -192,17 +195,18 @@ __device__ __forceinline__ void c4_settle() {
   __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
 }
 
-// Appends.  A workgroup takes 16 tokens of a block, forms their angles once while its first rows are under way, and its waves walk the
-// heads; a lane has 8 channels of a token, D / 8 lanes a token.  Codes and exponents change places through LDS into the order of the
-// cache, and leave in 16-byte units.  A key is what its rotation in float64 rounds to: float32 would fall to either side of a border of two
-// codes (one value in some 10^6, a whole step off).  Sines, cosines, products and sum are float64, which the vector units multiply and
-// add at float32's rate; the float32 value that the conversion to 4 bits takes is off the sum by its own rounding, which matters only where
-// it meets a border, a number of at most three bits.  There it moves on to the next one on the sum's side.  (In float32 with a margin and
-// float64 again where that held a border: 132 us for the three axes below, 184 for halves.)
-// What bounds it: memory, and the conversions, whose time shows beside it.  2 x 32760 tokens of 12 heads: bfloat16 as they are 107 us (4.8
-// TB/s), turned on three axes 115, as halves 124, float32 on three axes 191 (4.8).  Angles in the order of the pairs instead of the lanes':
-// halves 145; rows only after the angles: 117, one head 28 instead of 26.  A token for each of 16 sequences takes 6.2 us, a chain of
-loads and one of sines (8.3 where absent tokens were turned too).
+// Appends.  A workgroup takes 16 tokens of a block, forms their angles once while its first rows are under way, and its waves
+// walk the heads; a lane has 8 channels of a token, D / 8 lanes a token.  Codes and exponents change places through LDS into
+// the order of the cache, and leave in 16-byte units.  A key is what its rotation in float64 rounds to: float32 would fall to
+// either side of a border of two codes (one value in some 10^6, a whole step off).  Sines, cosines, products and sum are
+// float64, which the vector units multiply and add at float32's rate; the float32 value that the conversion to 4 bits takes is
+// off the sum by its own rounding, which matters only where it meets a border, a number of at most three bits.  There it moves
+// on to the next one on the sum's side.  (In float32 with a margin and float64 again where that held a border: 132 us for the
+// three axes below, 184 for halves.) What bounds it: memory, and the conversions, whose time shows beside it.  2 x 32760
+// tokens of 12 heads: bfloat16 as they are 107 us (4.8 TB/s), turned on three axes 115, as halves 124, float32 on three axes
+// 191 (4.8).  Angles in the order of the pairs instead of the lanes': halves 145; rows only after the angles: 117, one head 28
+// instead of 26.  A token for each of 16 sequences takes 6.2 us, a chain of
+// loads and one of sines (8.3 where absent tokens were turned too).
 template <typename T, int D, int ROT>
 __global__ __launch_bounds__(256) void cache_append_kernel(RowsArgs a) {
   constexpr int LPT = D / 8, TPS = 64 / LPT, STEPS = 16 / TPS, G = D / 32;
@@ -418,9 +422,9 @@ __device__ __forceinline__ void c4_four(uint32_t w, uint32_t e, uint32_t (&lo)[2
   lo[1] = __builtin_amdgcn_perm(d, c, first), hi[1] = __builtin_amdgcn_perm(d, c, second);
 }
 
-// Channels of a row at p: a lane's 8 in bfloat16, 4 and 4 that lie `half` further in float32, so that the lanes of a store cover
-// whole lines (65520 tokens of 12 heads: with 8 beside each other 239 us, 211 so).  Codes are 2 bytes each of lo and hi.  Past the caches: 2 x
-// 32760 tokens of 12 heads 114 -> 110 us.
+// Channels of a row at p: a lane's 8 in bfloat16, 4 and 4 that lie `half` further in float32, so that the lanes of a store
+// cover whole lines (65520 tokens of 12 heads: with 8 beside each other 239 us, 211 so).  Codes are 2 bytes each of lo and
+// hi.  Past the caches: 2 x 32760 tokens of 12 heads 114 -> 110 us.
 template <typename T>
 __device__ __forceinline__ void c4_store8(T* p, int half, bool vec, uint32_t lo, uint32_t hi, float s, float s2) {
   if constexpr (sizeof(T) == 2) {
@@ -443,7 +447,9 @@ __device__ __forceinline__ void c4_store8(T* p, int half, bool vec, uint32_t lo,
   }
 }
 
-// Rows out of the cache: the append's shape the other way round.  Places without a page read as zero.
+// Rows out of the cache: the append's shape the other way round.  Places without a page read as zero.  What bounds it: memory,
+// four bytes written (bfloat16) for each one read: 2 x 32760 tokens of 12 heads 110 us among other work, 4.6 TB/s, 80 (6.4)
+// replayed on one cache, whose 107 MB then come out of the Infinity Cache; float32 211 (4.3).
 template <typename T, int D>
 __global__ __launch_bounds__(256) void cache_read_kernel(RowsArgs a) {
   constexpr int LPT = D / 8, TPS = 64 / LPT, STEPS = 16 / TPS, G = D / 32;
@@ -504,17 +510,21 @@ __device__ __forceinline__ uint32_t c4_nan_bytes(uint32_t x) { return ((x & 0x7f
 // Bytes of four keys of which `left` are to keep (any number).
 __device__ __forceinline__ uint32_t c4_keep(int left) { return (uint32_t)((1ull << (8 * min(max(left, 0), 4))) - 1ull); }
 
-// What a lane takes of a 64-key tile: 4 keys' groups of K with their exponents, two channels of each V group for its 16 keys, and these keys'
-// exponents of every group.
+// What a lane takes of a 64-key tile: 4 keys' groups of K with their exponents, two channels of each V group for its 16 keys,
+// and these keys' exponents of every group.
 struct C4Raw {
   u32x4 k[4], v[4], e[4];
   uint32_t ke;
 };
 
-// At most 16 rows a key head (a token of 16 query heads, four tokens of 4).  The four waves of a workgroup take every
-// fourth tile of its share.  The layout makes every operand a lane's own bytes, so a tile goes from memory to
-// registers, 16 bytes a lane and whole lines a load, and there to bfloat16; nothing passes through LDS until the waves' sums meet.
-// The next tile's K takes the place of this one's as soon as its logits are formed, V that of V.
+// At most 16 rows a key head (a token of 16 query heads, four tokens of 4).  The four waves of a workgroup take every fourth
+// tile of its share.  The layout makes every operand a lane's own bytes, so a tile goes from memory to registers, 16 bytes a
+// lane and whole lines a load, and there to bfloat16; nothing passes through LDS until the waves' sums meet. The next tile's K
+// takes the place of this one's as soon as its logits are formed, V that of V. What bounds it: memory (8 sequences of 8 key
+// heads, 100003 to 56000 keys, 680 MB: 112 us and the join 4, 6.1 TB/s; 160 with the table read and the places divided tile by
+// tile), and for short windows the chain of loads (1024 of 8192 keys: 7.8 and 4.0). K's codes and exponents are also what
+// v_mfma_scale_f32_16x16x128_f8f6f4 takes as they lie, with queries split into two 8-bit halves. Its sums are not float32:
+// checked on this chip, they drop what lies some 15 bits below the largest product.  So K is turned into bfloat16.
 template <bool SPLIT>
 __global__ __launch_bounds__(256, 3) void cache_rows_kernel(WinArgs a, CacheArgs ca) {
   constexpr int BKV = C4_BLOCK, D = ATT_D, F = D / 16;
@@ -548,7 +558,8 @@ __global__ __launch_bounds__(256, 3) void cache_rows_kernel(WinArgs a, CacheArgs
   if (tiles.sink == 0 && seq.sink >= lo1) mask.lo[0] = 0;
   // a lane's channels 32 g + 8 step .. + 7, as its bytes of K hold them
   const bf16_t* qp = (const bf16_t*)a.q + b * a.sq + (int64_t)qi * a.ldq + (int64_t)head * D + 32 * g;
-  // (the waves have the same rows; from LDS a tile, and in an order that takes V group by group, 168 registers are enough: three waves a SIMD)
+  // (the waves have the same rows; from LDS a tile, and in an order that takes V group by group, 168 registers are enough:
+  // three waves a SIMD)
   if (wave == 0) {
 #pragma unroll
     for (int kc = 0; kc < D / 32; ++kc) qs[kc][lane] = *(const u32x4*)(qp + kc * 8);
@@ -746,8 +757,12 @@ __global__ __launch_bounds__(256, 3) void cache_rows_kernel(WinArgs a, CacheArgs
 }
 
 // ---------------------------------------------------------------- many rows, bfloat16
-// 256 rows a workgroup, 32 a wave, and the tile body of the plain attention on tiles that the workgroup turns into bfloat16 in LDS
-// (attention_tile.h's layout): half of the threads take K's 16 bytes each, half V's.  The next tile's bytes are under way while one is computed on.
+// 256 rows a workgroup, 32 a wave, and the tile body of the plain attention on tiles that the workgroup turns into bfloat16 in
+// LDS (attention_tile.h's layout): half of the threads take K's 16 bytes each, half V's.  The next tile's bytes are under way
+// while one is computed on. What bounds it: the matrix cores and the conversions in turn.  12 heads, 4680 queries on thirteen
+// frames of 1560 keys, 583 GFLOP: 645 us (549 on bfloat16 keys in window.hip, 26 instructions a thread and 32 KB into LDS a
+// tile fewer); matrix cores busy 49% of the cycles in which a CU has work, 78% of all: 228 workgroups on 256 CUs.  On the way:
+// 864 with scalar table reads and divisions a tile, 676 with V written in the bytes' order.
 template <bool QLOG2, bool SPLIT>
 __global__ __launch_bounds__(512) void cache_blocks_kernel(WinArgs a, CacheArgs ca) {
   constexpr int BKV = ATT_BKV, D = ATT_D, SLOT = ATT_SLOT;
@@ -795,10 +810,11 @@ __global__ __launch_bounds__(512) void cache_blocks_kernel(WinArgs a, CacheArgs 
     for (int kc = 0; kc < D / 32; ++kc) qf[kc][i] = __builtin_bit_cast(bf16x8, *(const u32x4*)(qp + kc * 32));
   }
 
-  // What this thread brings in: 16 bytes of K, group kg of key kt, or 16 of V, channels vc and vc + 1 of the keys
-  // 32 s + 8 vr + 0..7.  The LDS row of key (channel) 8 q + 4 x + j of 32 is 16 x + 4 q + j; K's four units and V's two differ from the
-  // first in an XOR, and the rows of two channels beside each other have one swizzle.  Where j has bit 1 the second channel goes
-  // first: the 16 threads that write together then meet every bank once (in the bytes' own order four times: 676 us, 644 so).
+  // What this thread brings in: 16 bytes of K, group kg of key kt, or 16 of V, channels vc and vc + 1 of the keys 32 s + 8 vr
+  // + 0..7.  The LDS row of key (channel) 8 q + 4 x + j of 32 is 16 x + 4 q + j; K's four units and V's two differ from the
+  // first in an XOR, and the rows of two channels beside each other have one swizzle.  Where j has bit 1 the second channel
+  // goes first: the 16 threads that write together then meet every bank once (in the bytes' own order four times: 676 us, 644
+  // so).
   const bool isv = wave >= 4;
   uint32_t put;
   {
@@ -858,7 +874,8 @@ __global__ __launch_bounds__(512) void cache_blocks_kernel(WinArgs a, CacheArgs 
   st.reset();
   int i0 = 0, i1 = tiles.n;
   if (SPLIT) win_share(tiles.n, sp, a.nsplit, i0, i1);
-  // Tile idx is in LDS, the next one's bytes are under way, and the table's entry of the one after it.  Tiles without a page are passed over.
+  // Tile idx is in LDS, the next one's bytes are under way, and the table's entry of the one after it.  Tiles without a page
+  // are passed over.
   Raw raw;
   int idx = i0, entry = 0, in1 = 0;  // in1: of the next one, the block in its page
   bool there = false;
@@ -873,7 +890,8 @@ __global__ __launch_bounds__(512) void cache_blocks_kernel(WinArgs a, CacheArgs 
   }
   put ^= SLOT;
   barrier();
-  // edge tiles in a loop of their own: with both kinds in one the accumulators are copied tile by tile (250 registers, 1.3 times as slow)
+  // edge tiles in a loop of their own: with both kinds in one the accumulators are copied tile by tile (250 registers, 1.3
+  // times as slow)
   auto step = [&](auto edge) {
     bool next_there;
     fetch(c4_of_entry<D>(ca, entry, h, in1, next_there), raw);  // (past the share: this tile again)
@@ -966,8 +984,10 @@ __global__ __launch_bounds__(512) void cache_blocks_kernel(WinArgs a, CacheArgs 
 }
 
 // ---------------------------------------------------------------- float32
-// 16 rows a workgroup; a tile of 64 keys is turned into float32 in LDS (rows of K, rows of V^T, 16-byte units at unit ^ (row & 7)), each of
-// the four waves takes 16 of its keys, and the next two tiles' bytes are under way meanwhile.
+// 16 rows a workgroup; a tile of 64 keys is turned into float32 in LDS (rows of K, rows of V^T, 16-byte units at unit ^ (row &
+// 7)), each of the four waves takes 16 of its keys, and the next two tiles' bytes are under way meanwhile. What bounds it: a
+// tile's conversion, two barriers, products and softmax in turn, with three workgroups a CU (two at 128 channels): 2 x 8 heads
+// of 64, 301 queries on 1801 keys 38.5 us and the join 4, 43 TFLOP/s (47 with one tile ahead).
 template <int D, bool VEC, bool SPLIT>
 __global__ __launch_bounds__(256, D == 128 ? 2 : 3) void cache_f32_kernel(WinArgs a, CacheArgs ca) {
   constexpr int C = D / 16, TK = C4_BLOCK, W = 4, ROWS = 16;
@@ -1198,11 +1218,12 @@ struct CachePlan {
   int nsplit;
 };
 
-// Shares of the keys for few rows.  None up to 16 tiles, four a wave: the join is a launch more.  Then as many as make the three
-// workgroups a CU that are resident, of four tiles at least, and twice as many for what takes some 100 us, which evens out lengths.
-// Join included, replayed on three caches in turn: 64 key heads of 100003 to 56000 keys 124 us with 8, 122 with 12, 126 with 16, 118 with 24, 117 with
-// 32, 127 with 64; 48 of 32760 51 with 8, 44 with 16, 48 with 24, 45 with 32; 8 of 100003 36 with 32, 29 with 64 and 96; 64 of
-// 16384 32 with 8, 34 with 12, 37 with 24; 512 of 2000 29 with one, 35 with 2; 8 of 16384 17 with 16, 14 with 32, 13 with 64.
+// Shares of the keys for few rows.  None up to 16 tiles, four a wave: the join is a launch more.  Then as many as make the
+// three workgroups a CU that are resident, of four tiles at least, and twice as many for what takes some 100 us, which evens
+// out lengths. Join included, replayed on three caches in turn: 64 key heads of 100003 to 56000 keys 124 us with 8, 122 with
+// 12, 126 with 16, 118 with 24, 117 with 32, 127 with 64; 48 of 32760 51 with 8, 44 with 16, 48 with 24, 45 with 32; 8 of
+// 100003 36 with 32, 29 with 64 and 96; 64 of 16384 32 with 8, 34 with 12, 37 with 24; 512 of 2000 29 with one, 35 with 2; 8
+// of 16384 17 with 16, 14 with 32, 13 with 64.
 static int64_t cache_rows_split(int64_t tiles, int64_t blocks, int64_t cus) {
   if (tiles <= 16) return 1;
   return std::min((blocks * tiles >= 192 * cus ? 6 : 3) * cus / blocks, tiles / 4);

@@ -24,9 +24,9 @@ struct C4 {
   static constexpr int v_exp(int tok, int grp) { return VE + 64 * grp + ((tok >> 3) & 3) * 16 + 8 * (tok >> 5) + (tok & 7); }
 };
 
-// Few rows (128 channels): a lane's 16 bytes of K for 16-key block i of 4, the 4 bytes of these keys' exponents, its 16 bytes of V group m and
-// the 16 exponents of that group.  Lane 16 g + j has key c4_row_key(i, j) and its channels 32 g .. + 31, and of V channels 32 m + 2 j, + 1
-// of the keys 32 s + 8 g + 0..7.
+// Few rows (128 channels): a lane's 16 bytes of K for 16-key block i of 4, the 4 bytes of these keys' exponents, its 16 bytes
+// of V group m and the 16 exponents of that group.  Lane 16 g + j has key c4_row_key(i, j) and its channels 32 g .. + 31, and
+// of V channels 32 m + 2 j, + 1 of the keys 32 s + 8 g + 0..7.
 constexpr int c4_row_key(int i, int j) { return 32 * (i >> 1) + 8 * (j >> 2) + 4 * (i & 1) + (j & 3); }
 constexpr uint32_t c4_row_k(int lane) { return (uint32_t)(c4_row_key(0, lane & 15) * 64 + 16 * (lane >> 4)); }
 constexpr uint32_t c4_row_k_block(int i) { return (uint32_t)(c4_row_key(i, 0) * 64); }

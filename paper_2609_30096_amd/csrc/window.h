@@ -282,14 +282,13 @@ __device__ __forceinline__ f32x4 win_load4(const float* p) {
 // Bits of a pair of keys of which `left` are to keep (any number).
 __device__ __forceinline__ uint32_t win_keep(int left) { return (uint32_t)((1ull << (16 * min(max(left, 0), 2))) - 1ull); }
 
-// Row block, share, key head and sequence of a workgroup.  LOCAL: neighbouring row blocks go to
-// one XCD, whose L2 then serves their common keys (over the XCDs in turn, 12 heads 16384 x 16384
-// under a causal mask took 955 us instead of 824, 2 x 12 heads over a 21-frame video 5.2 ms
-// instead of 4.8), and the sequences follow each other inside a head, so that short ones do
-// not leave one XCD idle (4 sequences of 5000 to 3100 queries: 439 -> 385 us).  Single tokens use
-// a key once and go over the XCDs in turn (8 sequences of 8 key heads, 100003 keys 491 us, 500 the other way;
-// 48 x 32760 131 and 132, 8 of 100003 to 56000 keys 395 and 397, one of 100003 70 and 68).  The last rows of a sequence, which see most keys under a causal
-// mask, start first.
+// Row block, share, key head and sequence of a workgroup.  LOCAL: neighbouring row blocks go to one XCD, whose L2 then serves
+// their common keys (over the XCDs in turn, 12 heads 16384 x 16384 under a causal mask took 955 us instead of 824, 2 x 12
+// heads over a 21-frame video 5.2 ms instead of 4.8), and the sequences follow each other inside a head, so that short ones do
+// not leave one XCD idle (4 sequences of 5000 to 3100 queries: 439 -> 385 us).  Single tokens use a key once and go over the
+// XCDs in turn (8 sequences of 8 key heads, 100003 keys 491 us, 500 the other way; 48 x 32760 131 and 132, 8 of 100003 to
+// 56000 keys 395 and 397, one of 100003 70 and 68).  The last rows of a sequence, which see most keys under a causal mask,
+// start first.
 template <bool LOCAL>
 __device__ __forceinline__ void win_place_of(const WinArgs& a, uint32_t id, int& rb, int& sp, int& h, int& b) {
   const uint32_t t = a.by_nrb(id), u = a.by_nsplit(t), v = a.by_inner(u);
@@ -304,10 +303,10 @@ __device__ __forceinline__ void win_place(const WinArgs& a, int& rb, int& sp, in
   win_place_of<LOCAL>(a, LOCAL ? (uint32_t)xcd_remap((int)blockIdx.x, (int)gridDim.x) : blockIdx.x, rb, sp, h, b);
 }
 
-// The same for row blocks of 256 rows inside documents: the workgroups of an XCD take the blocks of their range (up to
-// 256 of them) with the most keys first, by eighths of the most that one has, so that a long one does not start when the others end.
-// 12 heads of 15600 tokens in documents of 3391, 7460 and 4749: 643 us in the rows' order, 544 so (with a cap and a bias 914 and 770).  Each wave counts for itself, four blocks a lane; all get
-// the same numbers, so each block is taken once.
+// The same for row blocks of 256 rows inside documents: the workgroups of an XCD take the blocks of their range (up to 256 of
+// them) with the most keys first, by eighths of the most that one has, so that a long one does not start when the others end.
+// 12 heads of 15600 tokens in documents of 3391, 7460 and 4749: 643 us in the rows' order, 544 so (with a cap and a bias 914
+// and 770).  Each wave counts for itself, four blocks a lane; all get the same numbers, so each block is taken once.
 __device__ __forceinline__ void win_place_docs(const WinArgs& a, int& rb, int& sp, int& h, int& b) {
   const int q = (int)gridDim.x >> 3, rem = (int)gridDim.x & 7, x = (int)blockIdx.x & 7;
   const int start = x * q + min(x, rem), n = q + (x < rem);
