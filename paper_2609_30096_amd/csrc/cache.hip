@@ -1218,15 +1218,16 @@ struct CachePlan {
   int nsplit;
 };
 
-// Shares of the keys for few rows.  None up to 16 tiles, four a wave: the join is a launch more.  Then as many as make the
-// three workgroups a CU that are resident, of four tiles at least, and twice as many for what takes some 100 us, which evens
+// Shares of the keys for few rows.  None up to 12 tiles, three a wave: the join is a launch more (32 heads of 960 keys 10.6 us
+// with one, 8.9 with 4, of 576 8.7 and 8.7, 128 of 576 9.7 and 10.8).  Then as many as make the three workgroups a CU that are
+// resident, of four tiles or fewer, and twice as many for what takes some 100 us, which evens
 // out lengths. Join included, replayed on three caches in turn: 64 key heads of 100003 to 56000 keys 124 us with 8, 122 with
 // 12, 126 with 16, 118 with 24, 117 with 32, 127 with 64; 48 of 32760 51 with 8, 44 with 16, 48 with 24, 45 with 32; 8 of
 // 100003 36 with 32, 29 with 64 and 96; 64 of 16384 32 with 8, 34 with 12, 37 with 24; 512 of 2000 29 with one, 35 with 2; 8
 // of 16384 17 with 16, 14 with 32, 13 with 64.
 static int64_t cache_rows_split(int64_t tiles, int64_t blocks, int64_t cus) {
-  if (tiles <= 16) return 1;
-  return std::min((blocks * tiles >= 192 * cus ? 6 : 3) * cus / blocks, tiles / 4);
+  if (tiles <= 12) return 1;
+  return std::min((blocks * tiles >= 192 * cus ? 6 : 3) * cus / blocks, (tiles + 3) / 4);
 }
 
 static CachePlan cache_plan(int dtype, const track_window& w, int64_t B, int Hk, int n, int D, int64_t Lq, int64_t Lk) {
