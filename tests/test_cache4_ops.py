@@ -630,6 +630,17 @@ def test_groups_without_a_number(dtype, Lq, Lk):
 
 
 @gpu
+@pytest.mark.parametrize("D,H,Lq,Lk", [(128, 12, 700, 1100), (64, 20, 840, 1090)])
+def test_more_row_blocks_than_places(D, H, Lq, Lk):
+    """Float32 row blocks that fill the chip's places once and a little take shares of the keys."""
+    win = W()
+    c = Case(F32, 1, H, H, Lq, Lk, D=D)
+    assert track.attention_cache4_workspace(win, c.cache, c.tq, Lk) is not None
+    got, lse = c.run(win)
+    _check(c, win, got, lse)
+
+
+@gpu
 @pytest.mark.parametrize("dtype", [BF16, F32])
 @pytest.mark.parametrize("Lq", [1, 4, 100])
 def test_a_weight_that_falls_to_zero(dtype, Lq):
