@@ -404,10 +404,11 @@ template <int SEL>
 __device__ __forceinline__ f32x2 c4_pair_f32(uint32_t w, float s) {
   return __builtin_bit_cast(f32x2, __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, s, SEL));
 }
-// Byte I of w as a float whose exponent it is (255 gives NaN in the conversions).
+// Byte I of w as a float whose exponent it is (255 gives NaN in the conversions).  They look at the exponent alone (checked for all
+// 256 with signs and mantissas of every kind), so the other bytes' bits stay in those: one instruction instead of two.
 template <int I>
 __device__ __forceinline__ float c4_scale(uint32_t w) {
-  return __uint_as_float(((w >> (8 * I)) & 0xffu) << 23);
+  return __uint_as_float(I < 3 ? w << (23 - 8 * I) : w >> 1);
 }
 // Four bytes of codes, 8 channels of one group, as bfloat16.
 __device__ __forceinline__ u32x4 c4_eight(uint32_t w, float s) {
@@ -760,7 +761,7 @@ __global__ __launch_bounds__(256, 3) void cache_rows_kernel(WinArgs a, CacheArgs
 // 256 rows a workgroup, 32 a wave, and the tile body of the plain attention on tiles that the workgroup turns into bfloat16 in
 // LDS (attention_tile.h's layout): half of the threads take K's 16 bytes each, half V's.  The next tile's bytes are under way
 // while one is computed on. What bounds it: the matrix cores and the conversions in turn.  12 heads, 4680 queries on thirteen
-// frames of 1560 keys, 583 GFLOP: 645 us (549 on bfloat16 keys in window.hip, 26 instructions a thread and 32 KB into LDS a
+// frames of 1560 keys, 583 GFLOP: 637 us (549 on bfloat16 keys in window.hip, 26 instructions a thread and 32 KB into LDS a
 // tile fewer); matrix cores busy 49% of the cycles in which a CU has work, 78% of all: 228 workgroups on 256 CUs.  On the way:
 // 864 with scalar table reads and divisions a tile, 676 with V written in the bytes' order.
 template <bool QLOG2, bool SPLIT>
