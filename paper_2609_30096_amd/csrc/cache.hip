@@ -346,7 +346,8 @@ __global__ __launch_bounds__(256) void cache_append_kernel(RowsArgs a) {
 #pragma unroll
           for (int i = 0; i < 8; ++i) {
             const double d = fabs((double)y[i]), m = fabs(r[i]);
-            y[i] = __uint_as_float(__float_as_uint(y[i]) + (m < d ? ~0u : (m > d ? 1u : 0u)));  // (not a NaN)
+            const uint32_t bits = __float_as_uint(y[i]), to = m < d ? ~0u : (m > d ? 1u : 0u);  // (a NaN stays)
+            y[i] = __uint_as_float(bits + (bits << 12 ? 0u : to));  // (others could meet one)
           }
         }
         word = c4_round8(y, byte);

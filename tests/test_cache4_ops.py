@@ -408,6 +408,65 @@ def test_append_special_values(dtype, rotated):
     assert not bad.any(), f"{bad.sum()} bytes, first {np.argwhere(bad)[:3].tolist()}"
 
 
+def _beside_borders(layout):
+    """Float32 keys [1, L, 1, 64] whose rotation lies beside a border of two codes (or, at 7, of two exponents), but rounds to it
+    in float32: the rows, positions, and where."""
+    Ln, D = 192, 64
+    rng = np.random.default_rng(77)
+    pos = rng.integers(0, 500, (1, 1, Ln)).astype(np.int32)  # (angles within 2^-43: the rotations within 2^-40)
+    f = ref.freqs((D // 2,))
+    turn = pos[0, 0][:, None] * f
+    c, s = np.cos(turn), np.sin(turn)
+    first = rng.choice([0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5.0], (Ln, D // 2)) * rng.choice([-1.0, 1.0], (Ln, D // 2))
+    first[:, 0::16] = 6.5            # the groups' largest
+    first[::3, 0::16] = 7.0
+    second = rng.uniform(-1.0, 1.0, first.shape)
+    x, z = (first * c + second * s).astype(np.float32), (-first * s + second * c).astype(np.float32)
+    # the operand with the smaller factor in small steps, to the first sum that float32 rounds to the border
+    fine = np.abs(s) <= np.abs(c)    # z, or x
+    hit = np.zeros(first.shape, bool)
+    for k in range(-400, 401):
+        x1 = np.where(fine, x, x + np.float32(k) * np.spacing(np.abs(x))).astype(np.float32)
+        z1 = np.where(fine, z + np.float32(k) * np.spacing(np.abs(z)), z).astype(np.float32)
+        r = x1.astype(np.float64) * c - z1.astype(np.float64) * s
+        ok = ~hit & (r.astype(np.float32) == first) & (np.abs(r - first) > 2.0 ** -36) & (rng.random(hit.shape) < 0.2)
+        x, z, hit = np.where(ok, x1, x), np.where(ok, z1, z), hit | ok
+    rows = np.empty((1, Ln, 1, D), np.float32)
+    lo, hi = (slice(0, D, 2), slice(1, D, 2)) if layout == "interleaved" else (slice(0, D // 2), slice(D // 2, D))
+    rows[0, :, 0, lo], rows[0, :, 0, hi] = x, z
+    where = np.zeros((Ln, D), bool)
+    where[:, lo] = hit
+    return rows, pos, where
+
+
+@pytest.mark.parametrize("layout", ["interleaved", "half"])
+def test_rows_beside_borders_are_there(layout):
+    rows, pos, where = _beside_borders(layout)
+    r = ref.rope(rows.astype(np.float64), pos, (32,), ref.freqs((32,)), 1.0, layout)
+    once, twice = c4.quantise(r), c4.quantise(r.astype(np.float32).astype(np.float64))
+    assert (once[0][0, :, 0] != twice[0][0, :, 0])[where].sum() > 200, "codes that a rounding to float32 first would change"
+    assert (once[1] != twice[1]).sum() > 8, "exponents"
+
+
+@gpu
+@pytest.mark.parametrize("layout", ["interleaved", "half"])
+def test_keys_beside_borders(layout):
+    import torch
+    rows, pos, _ = _beside_borders(layout)
+    Ln, D = rows.shape[1], rows.shape[3]
+    rope = track.Rope(track.RopeConfig(head_dim=D, rot_dim=D, layout=layout))
+    pool, table = _pool(13, 4, 1, D, 64, 1, 3)
+    cache = _device_cache(pool, table)
+    k = torch.from_numpy(rows).cuda()
+    track.op_cache4_append(cache, k, k, torch.zeros(1, dtype=torch.int32, device="cuda"), rope=rope, pos=torch.from_numpy(pos).cuda())
+    qk = c4.quantise(ref.rope(rows.astype(np.float64), pos, (32,), ref.freqs((32,)), 1.0, layout))
+    qv = c4.quantise(rows.astype(np.float64))
+    for i in range(Ln):
+        pool.put(table[0, i // 64], i % 64, (qk[0][0, i], qk[1][0, i]), (qv[0][0, i], qv[1][0, i]))
+    bad = cache.pages.cpu().numpy().reshape(pool.raw.shape) != pool.raw
+    assert not bad.any(), f"{bad.sum()} bytes, first {np.argwhere(bad)[:3].tolist()}"
+
+
 @gpu
 @pytest.mark.parametrize("dtype", [BF16, F32])
 def test_rows_strides(dtype):
