@@ -468,6 +468,27 @@ def test_keys_beside_borders(layout):
 
 
 @gpu
+def test_values_beside_borders():
+    """Float32 values one and two steps beside every border, at groups of every exponent, as they are."""
+    import torch
+    border = np.array([0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5.0], np.float32)
+    step = np.spacing(border)
+    group = np.concatenate([border + i * step for i in (0, 1, -1, 2, -2)])[:31]
+    tops = [np.float32(x) for x in (6.0, np.nextafter(np.float32(7.0), np.float32(0.0)), 7.0, 4.0)]
+    x = np.stack([np.append(group * (-1) ** (j + np.arange(31)), tops[j % 4]) for j in range(249)])
+    x = (x * 2.0 ** np.arange(-124.0, 125.0)[:, None]).astype(np.float32).reshape(1, 249, 1, 32)
+    pool, table = _pool(15, 6, 1, 32, 64, 1, 4)
+    cache = _device_cache(pool, table)
+    t = torch.from_numpy(x).cuda()
+    track.op_cache4_append(cache, t, -t, torch.zeros(1, dtype=torch.int32, device="cuda"))
+    qk, qv = c4.quantise(x.astype(np.float64)), c4.quantise(-x.astype(np.float64))
+    for i in range(249):
+        pool.put(table[0, i // 64], i % 64, (qk[0][0, i], qk[1][0, i]), (qv[0][0, i], qv[1][0, i]))
+    bad = cache.pages.cpu().numpy().reshape(pool.raw.shape) != pool.raw
+    assert not bad.any(), f"{bad.sum()} bytes, first {np.argwhere(bad)[:3].tolist()}"
+
+
+@gpu
 @pytest.mark.parametrize("dtype", [BF16, F32])
 def test_rows_strides(dtype):
     """Rows of a fused projection, rows at unaligned addresses and sequences in turn: the bytes of contiguous ones, and read back
