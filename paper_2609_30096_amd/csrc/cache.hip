@@ -1107,7 +1107,8 @@ int64_t cache4_page_bytes(int heads, int head_dim, int page_tokens) {
   return (int64_t)(page_tokens / C4_BLOCK) * heads * 68 * head_dim;
 }
 
-static track_status cache_check(const char* what, const track_cache4* c, CacheArgs* a) {
+// empty: a call that does nothing, perhaps of no sequences, whose table has no address.
+static track_status cache_check(const char* what, const track_cache4* c, bool empty, CacheArgs* a) {
   if (!c) return fail(TRACK_E_INVALID, "%s: null cache", what);
   if (!cache4_page_bytes(c->heads, c->head_dim, c->page_tokens))
     return fail(TRACK_E_UNSUPPORTED, "%s: pages of %d tokens (multiples of 64 up to 65536), %d heads of %d channels (32, 64, 128)", what,
@@ -1116,7 +1117,7 @@ static track_status cache_check(const char* what, const track_cache4* c, CacheAr
       c->ld_table < 0)
     return fail(TRACK_E_SHAPE, "%s: %lld pages, %d of a sequence (2^28 tokens at most), %lld between sequences", what, (long long)c->n_pages,
                 c->table_pages, (long long)c->ld_table);
-  if (!c->pages || (c->table_pages && !c->table)) return fail(TRACK_E_INVALID, "%s: null pointer in the cache", what);
+  if (!c->pages || (c->table_pages && !c->table && !empty)) return fail(TRACK_E_INVALID, "%s: null pointer in the cache", what);
   if (((uintptr_t)c->pages & 127) || ((uintptr_t)c->table & 3))
     return fail(TRACK_E_INVALID, "%s: pages need 128-byte alignment, the table 4", what);
   a->pages = (uint8_t*)c->pages;
@@ -1149,7 +1150,7 @@ static track_status cache_rows(const char* what, bool read, int dtype, const tra
                                hipStream_t s) {
   if (dtype != TRACK_DTYPE_F32 && dtype != TRACK_DTYPE_BF16) return fail(TRACK_E_INVALID, "%s: bad dtype %d", what, dtype);
   RowsArgs a = {};
-  const track_status st = cache_check(what, cache, &a.c);
+  const track_status st = cache_check(what, cache, B == 0 || L == 0, &a.c);
   if (st != TRACK_OK) return st;
   const int D = cache->head_dim;
   const int64_t width = (int64_t)cache->heads * D;
@@ -1287,7 +1288,7 @@ track_status attention_cache4(int dtype, const track_window* w, const track_cach
                               const int32_t* q_len, const int32_t* k_len, const int32_t* q_start, void* ws, size_t ws_bytes,
                               hipStream_t s) {
   CacheArgs ca = {};
-  track_status st = cache_check("attention_cache4", cache, &ca);
+  track_status st = cache_check("attention_cache4", cache, B == 0 || Lq == 0, &ca);
   if (st != TRACK_OK) return st;
   const int Hk = cache->heads, D = cache->head_dim;
   st = win_check("attention_cache4", dtype, w, B, H, Hk, D, Lq, Lk);
