@@ -357,6 +357,65 @@ def test_append(case):
     assert not bad.any(), f"{bad.sum()} bytes, first {np.argwhere(bad)[:3].tolist()}"
 
 
+ROTATED = [
+    # dtype, B, L, heads, D, start, sections, layout, scaling, factor
+    (BF16, 2, 70, 2, 128, [3, 60], (64,), "half", "yarn", 8.0),
+    (BF16, 16, 1, 3, 128, list(range(40, 56)), (64,), "half", "yarn", 32.0),
+    (BF16, 1, 40, 3, 128, [100], (20,), "interleaved", "yarn", 4.0),        # channels that are not turned
+    (BF16, 1, 65, 2, 64, [33], (8,), "half", "yarn", 4.0),
+    (BF16, 1, 50, 2, 64, [0], (11,), "half", "yarn", 4.0),                  # pairs that are not whole units
+    (BF16, 1, 65, 2, 128, [0], (32, 16, 16), "half", "none", 1.0),
+    (BF16, 2, 33, 2, 128, [1, 64], (22, 21, 21), "half", "yarn", 8.0),      # axes that end inside a unit
+    (BF16, 1, 40, 5, 32, [30], (4, 2, 2), "half", "linear", 4.0),
+    (BF16, 1, 40, 2, 128, [30], (7, 8), "interleaved", "ntk", 8.0),
+    (F32, 1, 50, 2, 64, [20], (7, 6, 5), "half", "none", 1.0),
+    (F32, 2, 40, 2, 64, [0, 63], (12, 10, 10), "half", "yarn", 8.0),
+    (F32, 1, 70, 1, 128, [64], (64,), "interleaved", "yarn", 16.0),
+    (F32, 1, 40, 2, 128, [10], (30,), "half", "linear", 4.0),
+    (F32, 1, 40, 3, 64, [10], (32,), "interleaved", "ntk", 8.0),
+    (F32, 1, 40, 2, 32, [10], (6, 5, 5), "half", "yarn", 2.0),
+]
+
+
+@gpu
+@pytest.mark.parametrize("case", ROTATED, ids=str)
+def test_append_amplitudes_and_axes(case):
+    """Frequencies of every scaling, amplitudes other than one, and axes in halves: every byte against the definition, which
+    gives other bytes without the amplitude, without the scaling, and with an axis ending a pair early."""
+    import torch
+    dtype, B, Ln, heads, D, start, sections, layout, scaling, factor = case
+    say(f"append {case}")
+    k, v, pos, _ = _rows_inputs((dtype, B, Ln, heads, D, 64, start, None, (), ""), key=17)
+    pos = np.random.default_rng(18).integers(-3000, 3001, (len(sections), B, Ln)).astype(np.int32)
+    rope = track.Rope(track.RopeConfig(head_dim=D, rot_dim=2 * sum(sections), layout=layout, sections=sections, scaling=scaling,
+                                       factor=factor))
+    amp = 1.0 + 0.1 * math.log(factor) if scaling == "yarn" else 1.0
+    assert rope.amplitude == pytest.approx(amp, rel=2.0 ** -23)
+    f = ref.freqs(sections, scaling=scaling, factor=factor)
+    pool, table = _pool(19, B * 4, heads, D, 64, B, 4)
+    cache = _device_cache(pool, table)
+    track.op_cache4_append(cache, dev(k, dtype), dev(v, dtype), torch.tensor(start, dtype=torch.int32, device="cuda"), rope=rope,
+                           pos=torch.from_numpy(pos).cuda())
+
+    def want(sections, f, amp):
+        return c4.quantise(ref.rope(k.astype(np.float64), pos, sections, f, amp, layout))
+
+    qk, qv = want(sections, f, rope.amplitude), c4.quantise(v.astype(np.float64))
+    others = [(sections, ref.freqs(sections), rope.amplitude)] if scaling != "none" else []
+    if amp != 1.0:
+        others.append((sections, f, 1.0))
+    if len(sections) > 1:
+        others.append(((sections[0] - 1, sections[1] + 1, *sections[2:]), f, rope.amplitude))
+    for other in others:
+        assert (want(*other)[0] != qk[0]).any(), other
+    for b in range(B):
+        for i in range(Ln):
+            x = start[b] + i
+            pool.put(table[b, x // 64], x % 64, (qk[0][b, i], qk[1][b, i]), (qv[0][b, i], qv[1][b, i]))
+    bad = cache.pages.cpu().numpy().reshape(pool.raw.shape) != pool.raw
+    assert not bad.any(), f"{bad.sum()} bytes, first {np.argwhere(bad)[:3].tolist()}"
+
+
 @gpu
 @pytest.mark.parametrize("case", ROWS, ids=str)
 def test_read(case):
