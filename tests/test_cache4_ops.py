@@ -826,6 +826,48 @@ def test_a_weight_that_falls_to_zero(dtype, Lq):
 
 
 @gpu
+@pytest.mark.parametrize("dtype,D", KINDS)
+@pytest.mark.parametrize("Lq", [1, 7, 300])
+def test_every_exponent(dtype, D, Lq):
+    """Each query sees its own place only, whose groups have exponents of their own over a hundred octaves: the output is that
+    place's value (its weight over itself: exact in bfloat16, three roundings off in float32), the lse its logit.  A query has
+    channels of one group only, of a size that brings the logit near one."""
+    import torch
+    B, Hk, H, Lk, G = 2, 2, 4, 330, D // 32
+    rng = np.random.default_rng(23)
+    pool, table = _pool(23, B * 6, Hk, D, 64, B, 6)
+    ke, ve = rng.integers(60, 191, (B, Lk, Hk, G)), rng.integers(60, 166, (B, Lk, Hk, G))
+    for b in range(B):
+        for x in range(Lk):
+            at = pool._at(x % 64)
+            block = pool.raw[table[b, x // 64], 0]
+            block[:, at[2]], block[:, at[3]] = ke[b, x], ve[b, x]
+    k, v, _ = pool.places(table, Lk)
+    cache = _device_cache(pool, table)
+    win = W(left=0, right=0)
+    base = normal([23, 2], (B, Lq, H, D), bf16=dtype == BF16)
+    u = U[dtype]
+    for start in range(0, Lk - Lq + 1, Lq if Lq > 1 else 5):
+        rows = np.arange(start, start + Lq)
+        q = np.zeros((B, Lq, H, D), np.float32)
+        for h in range(H):
+            g = (rows + h) % G
+            for i in range(Lq):
+                at = slice(32 * g[i], 32 * g[i] + 32)
+                q[:, i, h, at] = base[:, i, h, at] * 2.0 ** (127.0 - ke[:, rows[i], h // 2, g[i], None])
+        tq = dev(q, dtype)
+        out, lse = torch.empty_like(tq), torch.empty(B, H, Lq, device="cuda")
+        ws = track.attention_cache4_workspace(win, cache, tq, Lk)
+        track.op_attention_cache4(win, cache, tq, out, Lk=Lk, lse=lse, workspace=ws,
+                                  q_start=torch.full((B,), start, dtype=torch.int32, device="cuda"))
+        kk, vv = (np.repeat(t[:, rows], 2, axis=2) for t in (k, v))
+        x, mag = ((a * b).sum(-1).transpose(0, 2, 1) / math.sqrt(D) for a, b in ((q.astype(np.float64), kk), (np.abs(q).astype(np.float64), np.abs(kk))))
+        _close(host(out), vv, (0.0 if dtype == BF16 else 4 * u) * np.abs(vv), f"out {start}")
+        # (D + 2 roundings of the logit, those of exp2, log2 and the weight)
+        _close(host(lse), x, (D + 2) * 2.0 ** -24 * mag + 2.0 ** -20 + 2.0 ** -22 * np.abs(x) + (u if dtype == BF16 else 0.0), f"lse {start}")
+
+
+@gpu
 @pytest.mark.parametrize("dtype", [BF16, F32])
 @pytest.mark.parametrize("Lq", [1, 20, 300])
 @pytest.mark.parametrize("scale", [4.0, 12.0])
