@@ -236,6 +236,23 @@ def test_without_changes_it_is_the_window(dtype, D, Lq, Lk):
 
 
 @gpu
+@pytest.mark.parametrize("dtype,D", [(BF16, 128), (F32, 32), (F32, 64), (F32, 128)])
+@pytest.mark.parametrize("Lq,Lk", [(1, 3000), (9, 700), (400, 900)])
+def test_without_changes_lse_is_the_windows(dtype, D, Lq, Lk):
+    """Both are within _check's tolerance of the same number, so they are within twice that of each other (not the same bits: the
+    changed logits are scaled before the reference is taken off, the window's in one FMA)."""
+    import torch
+    c = Case(dtype, 2, 4, 2, Lq, Lk, D)
+    sc, win = S(left=77, right=1, group=3), track.Window(left=77, right=1, group=3)
+    _, lse = c.run(sc)
+    want, wlse, _, big, _ = ref.attention(c.q, c.k, c.v, 77, 1, 3)
+    k, out, got = c.tk[:, :Lk], torch.empty_like(c.out), torch.empty_like(c.lse)
+    track.op_attention_window(win, c.tq, k, c.tv, out, lse=got, workspace=track.attention_window_workspace(win, c.tq, k))
+    eta = (D + 2) * 2.0 ** -24 * big + 2.0 ** -21 + (Lk + 16) * 2.0 ** -24 + (U[BF16] if dtype == BF16 else 0.0)
+    _close(host(got), lse, 2 * (1.1 * eta + 2.0 ** -22 * np.abs(wlse) + 1e-6), "lse")
+
+
+@gpu
 @pytest.mark.parametrize("dtype", [BF16, F32])
 @pytest.mark.parametrize("Lq,Lk", [(1, 1000), (1, 6000), (9, 700), (400, 900)])
 def test_masked_places(dtype, Lq, Lk):
