@@ -493,7 +493,9 @@ track_status track_op_attention_scores(int32_t dtype, const track_scores* scores
  * which the group's largest magnitude rounds to 6 2^e or less (it is below
  * 7 2^e), so nothing is cut off below 7 2^125.  A group that holds an infinity or
  * a NaN is kept as byte 255, 32 NaNs.  head_dim/2 + head_dim/32 bytes a token's
- * head, for K and for V: 136 at 128 channels, 512 in bfloat16.
+ * head, for K and for V: 136 at 128 channels, 512 in bfloat16.  No append writes the
+ * bytes 0..2, 253 and 254: reads take them as they are, attention takes 253 and 254
+ * as such or as 255.
  *
  * Place x of sequence b lies in page table[b*ld_table + x / page_tokens], at token
  * x % page_tokens.  Sequences may share pages.  Places at or past table_pages *

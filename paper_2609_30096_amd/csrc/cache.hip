@@ -507,8 +507,9 @@ __global__ __launch_bounds__(256) void cache_read_kernel(RowsArgs a) {
 }
 
 // ---------------------------------------------------------------- few rows, bfloat16
-// A byte of 0x80 for each byte of x that is 255.
-__device__ __forceinline__ uint32_t c4_nan_bytes(uint32_t x) { return ((x & 0x7f7f7f7fu) + 0x01010101u) & x & 0x80808080u; }
+// A byte of 0x80 for each byte of x that is 253 or more: 255, and the exponents that no append writes and at which 6 is an
+// infinity in bfloat16.
+__device__ __forceinline__ uint32_t c4_nan_bytes(uint32_t x) { return ((x & 0x7f7f7f7fu) + 0x03030303u) & x & 0x80808080u; }
 // Bytes of four keys of which `left` are to keep (any number).
 __device__ __forceinline__ uint32_t c4_keep(int left) { return (uint32_t)((1ull << (8 * min(max(left, 0), 4))) - 1ull); }
 
@@ -632,8 +633,8 @@ __global__ __launch_bounds__(256, 3) void cache_rows_kernel(WinArgs a, CacheArgs
       for (int i = 0; i < BKV / 16; ++i)
 #pragma unroll
         for (int x = 0; x < 4; ++x) s[i][x] = mk.apply(0, 32 * (i >> 1) + 4 * (i & 1) + x, s[i][x]);
-      // V past the last key, which may be anything, takes exponent 0 (a weight of zero would not remove a NaN), and so do
-      // groups that hold one, whose keys some rows may not see: they are put into the rows that do
+      // V past the last key, which may be anything, takes exponent 0 (a weight of zero would not remove a NaN or an infinity),
+      // and so do groups that may hold one, whose keys some rows may not see: they are put into the rows that do
       const int last = there ? seq.klen - key0 - 8 * g : 0;
       uint32_t any = 0;
 #pragma unroll

@@ -869,6 +869,57 @@ def test_every_exponent(dtype, D, Lq):
 
 @gpu
 @pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("Lq", [1, 4, 100, 300])
+def test_places_that_no_query_sees(dtype, Lq):
+    """Between the first tokens and the window the pages hold what no append has written: any codes and any exponent bytes,
+    whose values pass the largest number too.  No query sees those places, and nothing of them reaches one."""
+    import torch
+    Lk, sink, left = 900, 5, 210
+    c = Case(dtype, 2, 4, 2, Lq, Lk)
+    rng = np.random.default_rng(5)
+    lo = Lk - Lq - left  # the first query's first
+    unseen = np.arange(sink, lo)
+    assert len(unseen) > 300 and lo % 64 and sink % 64  # (in tiles that are seen in part as well)
+    for b in range(2):
+        for x in unseen:
+            at = c.pool._at(x % 64)
+            block = c.pool.raw[c.table[b, x // 64], 0]
+            for i in range(2):
+                block[:, at[i]] = rng.choice([0x77, 0xff, 0x00, 0x61], (2, 64))
+                block[:, at[2 + i]] = rng.choice([0, 2, 127, 252, 253, 254, 255], (2, 4))
+    c.cache.pages.copy_(torch.from_numpy(c.pool.raw.reshape(len(c.pool.raw), -1)))
+    c.k, c.v, c.there = c.pool.places(c.table, Lk)
+    win = W(left=left, sink=sink)
+    got, lse = c.run(win)
+    _check(c, win, got, lse)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("Lq", [1, 4, 100, 300])
+def test_places_that_some_queries_see(dtype, Lq):
+    """Exponent bytes that no append writes, in keys that the later queries see: the earlier ones have what they would have
+    without."""
+    import torch
+    Lk = 500
+    first = Lk - Lq
+    c = Case(dtype, 1, 4, 2, Lq, Lk)
+    odd = sorted({min(x, Lk - 1) for x in (first + max(1, Lq // 3), first + Lq // 2 + 1, Lk - 1)})
+    for i, x in enumerate(odd):
+        at = c.pool._at(x % 64)
+        block = c.pool.raw[c.table[0, x // 64], 0]
+        block[:, at[1]] = 0x77           # 6 in every channel
+        block[:, at[3][i % 4]] = 253 + i % 2
+    c.cache.pages.copy_(torch.from_numpy(c.pool.raw.reshape(len(c.pool.raw), -1)))
+    win = W(left=300)
+    got, lse = c.run(win)
+    clean = first + np.arange(Lq) < odd[0]
+    assert clean.any() == (Lq > 1)
+    _check(c, win, got, lse, rows=clean)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [BF16, F32])
 @pytest.mark.parametrize("Lq", [1, 20, 300])
 @pytest.mark.parametrize("scale", [4.0, 12.0])
 def test_large_logits(dtype, Lq, scale):
