@@ -545,8 +545,8 @@ track_status track_op_cache4_read(int32_t dtype, const track_cache4* cache, int6
  * the places 0 .. k_len[b] - 1 (Lk the most of a sequence, at most table_pages *
  * page_tokens), Hk and head_dim the cache's; all else, window, rows, lengths, types
  * and lse, as there (bfloat16: head_dim 128; float32: 32, 64, 128).  A key or value
- * group that holds no number reaches the rows that see it.  The workspace
- * (256-byte aligned; -1 for what the call refuses) grows with Lk, and one made for the longest
+ * group that holds no number reaches the rows that see it.  The workspace as
+ * there too (256-byte aligned; -1 for what the call refuses): one made for the longest Lk
  * serves calls of fewer keys.  Asynchronous. */
 int64_t track_attention_cache4_workspace_bytes(int32_t dtype, const track_window* window, int32_t B, int32_t H,
                                                int32_t Hk, int32_t head_dim, int64_t Lq, int64_t Lk);

@@ -525,7 +525,10 @@ struct C4Raw {
 // lane and whole lines a load, and there to bfloat16; nothing passes through LDS until the waves' sums meet. The next tile's K
 // takes the place of this one's as soon as its logits are formed, V that of V. What bounds it: memory (8 sequences of 8 key
 // heads, 100003 to 56000 keys, 680 MB: 112 us and the join 4, 6.1 TB/s; 160 with the table read and the places divided tile by
-// tile), and for short windows the chain of loads (1024 of 8192 keys: 7.8 and 4.0). K's codes and exponents are also what
+// tile), and for short windows the chain of loads (1024 of 8192 keys: 7.3 and 4.4).  Loads go past the caches also where
+// sequences share their pages: 32 sequences of 8 key heads on 32760 shared keys take 134 us so and 126 through the caches, after 1
+// GiB written elsewhere 137 and 131, 16 on 8192 27.1 and 27.0, 30.8 and 31.3; on pages of their own 189 and 210, 192 and 275,
+// 33 and 32, 36 and 65.  What the host could know of it, one table row for all, is a part of it only.  K's codes and exponents are also what
 // v_mfma_scale_f32_16x16x128_f8f6f4 takes as they lie, with queries split into two 8-bit halves. Its sums are not float32:
 // checked on this chip, they drop what lies some 15 bits below the largest product.  So K is turned into bfloat16.
 template <bool SPLIT>
@@ -764,7 +767,7 @@ __global__ __launch_bounds__(256, 3) void cache_rows_kernel(WinArgs a, CacheArgs
 // LDS (attention_tile.h's layout): half of the threads take K's 16 bytes each, half V's.  The next tile's bytes are under way
 // while one is computed on. What bounds it: the matrix cores and the conversions in turn.  12 heads, 4680 queries on thirteen
 // frames of 1560 keys, 583 GFLOP: 637 us (549 on bfloat16 keys in window.hip, 26 instructions a thread and 32 KB into LDS a
-// tile fewer); matrix cores busy 49% of the cycles in which a CU has work, 78% of all: 228 workgroups on 256 CUs.  On the way:
+// tile fewer); matrix cores busy 50% of the cycles in which a CU has work, 78% of all: 228 workgroups on 256 CUs.  On the way:
 // 864 with scalar table reads and divisions a tile, 676 with V written in the bytes' order.
 template <bool QLOG2, bool SPLIT>
 __global__ __launch_bounds__(512) void cache_blocks_kernel(WinArgs a, CacheArgs ca) {
@@ -989,8 +992,11 @@ __global__ __launch_bounds__(512) void cache_blocks_kernel(WinArgs a, CacheArgs 
 // ---------------------------------------------------------------- float32
 // 16 rows a workgroup; a tile of 64 keys is turned into float32 in LDS (rows of K, rows of V^T, 16-byte units at unit ^ (row &
 // 7)), each of the four waves takes 16 of its keys, and the next two tiles' bytes are under way meanwhile. What bounds it: a
-// tile's conversion, two barriers, products and softmax in turn, with three workgroups a CU (two at 128 channels): 2 x 8 heads
-// of 64, 301 queries on 1801 keys 38.5 us and the join 4, 43 TFLOP/s (47 with one tile ahead).
+// tile's conversion, two barriers, products and softmax in turn, with as many workgroups a CU as the registers allow (five at 32
+// channels, four at 64, two at 128): 2 x 8 heads of 64, 301 queries on 1801 keys 38.0 us and the join 4.3, a call among others
+// 38.4, 43 TFLOP/s (47 with one tile ahead); 12 heads of 64, 1500 on 4000 keys 74 TFLOP/s, of 128, 2000 on 6000 69, 16 of 32,
+// 1800 on 1800 63.  Single tokens take the same form with most of its 16 rows empty: 8 heads of 128, 8000 keys 21 us, 8 x 40 heads
+// over 8, 32760 keys 248 (1.2 TB/s).
 template <int D, bool VEC, bool SPLIT>
 __global__ __launch_bounds__(256, D == 128 ? 2 : 3) void cache_f32_kernel(WinArgs a, CacheArgs ca) {
   constexpr int C = D / 16, TK = C4_BLOCK, W = 4, ROWS = 16;
@@ -1234,9 +1240,10 @@ static int64_t cache_rows_split(int64_t tiles, int64_t blocks, int64_t cus) {
   return std::min((blocks * tiles >= 192 * cus ? 6 : 3) * cus / blocks, (tiles + 3) / 4);
 }
 
-// Shares for float32 rows: as many workgroups as LDS holds at once; and where the row blocks do not fill the last of their
-// rounds, what fills it better by a tenth, of eight tiles at least (12 heads of 128, 1000 causal rows on 2000 keys, 756 blocks
-// over 512 places: 199 us with one share, 153 with two).  Grows with the tiles.
+// Shares for float32 rows: as many workgroups as the registers allow at once (four a CU at 64 channels, two at 128; at 32, where
+// they allow five, four too); and where the row blocks do not fill the last of their rounds, what fills it better by a tenth, of
+// eight tiles at least (12 heads of 128, 1000 causal rows on 2000 keys, 756 blocks over 512 places: 199 us with one share, 153
+// with two).  Grows with the tiles.
 static int64_t cache_f32_split(int64_t tiles, int64_t blocks, int D, int64_t cus) {
   const int64_t places = (D == 128 ? 2 : 4) * cus;
   auto waste = [&](int64_t s) {  // rounds over those that full ones would take, and the join
