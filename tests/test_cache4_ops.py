@@ -208,13 +208,13 @@ def test_no_sequences(L):
     for dtype in (track.DTYPE_BF16, track.DTYPE_F32):
         assert L.track_op_cache4_append(dtype, none, None, 0, 5, *([P, 512, 2560] * 2), None, None, None, None, 1.0, None) == 0
         assert L.track_op_cache4_read(dtype, none, 0, 5, *([P, 512, 2560] * 2), None, None, None) == 0
-        assert L.track_op_attention_cache4(dtype, W().c(), none, 0, 8, 3, 1280, None, 1024, 3072, None, 1024, 3072, *([None] * 5),
+        assert L.track_op_attention_cache4(dtype, W().c(), none, 0, 8, 2, 1280, None, 1024, 2048, None, 1024, 2048, *([None] * 5),
                                            0, None) == 0
         # one sequence has places, and they are in the table
         assert L.track_op_cache4_append(dtype, none, None, 1, 5, *([P, 512, 2560] * 2), P, None, None, None, 1.0,
                                         None) == track.E_INVALID
         assert L.track_op_cache4_read(dtype, none, 1, 5, *([P, 512, 2560] * 2), P, None, None) == track.E_INVALID
-        assert L.track_op_attention_cache4(dtype, W().c(), none, 1, 8, 3, 1280, P, 1024, 3072, P, 1024, 3072, *([None] * 4), P,
+        assert L.track_op_attention_cache4(dtype, W().c(), none, 1, 8, 2, 1280, P, 1024, 2048, P, 1024, 2048, *([None] * 4), P,
                                            1 << 40, None) == track.E_INVALID
     cache = track.Cache4(4, 128, 64, torch.zeros(0, 20, dtype=torch.int32), n_pages=2)
     assert cache.c.table is None and cache.tokens == 1280
